@@ -247,6 +247,75 @@ int sp_linear_bwd(const float* d_in, const float* d_w, const float* d_dout, int3
 int sp_softmax_ce(const float* d_logits, const int32_t* d_labels, int32_t n_clouds, int32_t m, float* d_loss,
                   float* d_dlogits, void* stream);
 
+/* ---- a transformer over the rows of a sparse tensor -----------------------------------------------------------
+ * Rows in a fixed order (the library numbers voxels in first-occurrence order, so that of a serialised cloud is kept) as
+ * tokens; clouds one after another.  (The paper has no such layers; these are the standard definitions.)  No atomics,
+ * fixed summation order, no host synchronisation; statistics, sums and gradients of parameters are fp32.
+ *
+ * sp_layer_norm_fwd: every row of x [n][c] by itself, biased variance:
+ *   y = gamma * (x - mean) * rstd + beta, rstd = 1/sqrt(var + eps).  d_mean / d_rstd [n] are outputs.
+ * sp_layer_norm_bwd: with g = dy * gamma, xhat = (x - mean) * rstd and means over the row:
+ *   dx = rstd * (g - mean(g) - xhat * mean(g * xhat)), dgamma [c] = sum dy * xhat, dbeta [c] = sum dy over the rows.
+ * Any 1 <= c <= 65536; rows whose width is a multiple of 16 bytes, 16-byte aligned, are read in 16-byte pieces.  dx may be dy. */
+int sp_layer_norm_fwd(const void* d_x, int64_t n, int32_t c, const float* d_gamma, const float* d_beta, float eps, void* d_y,
+                      float* d_mean, float* d_rstd, sp_dtype dt, void* stream);
+int sp_layer_norm_bwd(const void* d_x, const void* d_dy, int64_t n, int32_t c, const float* d_gamma, const float* d_mean,
+                      const float* d_rstd, void* d_dx, float* d_dgamma, float* d_dbeta, sp_dtype dt, void* stream);
+
+/* Attention with a sliding window and a few first rows that stay visible, over packed clouds.
+ * Queries are rows [heads][dim], keys and values rows [kv_heads][dim]; query head h reads key head h / (heads / kv_heads).
+ * Cloud b owns query rows d_q_starts[b] .. d_q_starts[b+1] - 1 and key rows d_k_starts[b] .. d_k_starts[b+1] - 1 (int32
+ * [n_clouds + 1], ascending, in device memory; the two may be one array).  Its a queries are the last of its k positions: query
+ * i stands at position p = i + k - a (negative ones where there are fewer keys), key j at j, and
+ *   i sees j  <=>  0 <= j < k, j <= p + right, and (j >= p - left or j < sinks).
+ * right = 0: causal.  o = softmax over the keys seen of scale * q.k, times v; lse = log of the sum of exponentials (natural), fp32
+ * [n_q][heads].  A query that sees nothing, and a row that belongs to no cloud, has o = 0 and lse = -infinity, and zero gradients.
+ * Keys that a query does not see do not reach its results, whatever they hold (infinities and NaN too).
+ * Starts that are not ascending or out of range give undefined values, but no access outside of the arrays.
+ * Row r, head h, element e of an array lies at [r * ld + h * dim + e] (ld in elements, at least heads * dim or kv_heads * dim): views
+ * of a fused projection are read and written in place.  Arrays that are written overlap no other array.
+ * 1 <= dim <= 128 (SP_ERR_UNSUPPORTED beyond), n_q, n_k <= 2^30, left, right, sinks >= 0.  Rows of whole 16-byte pieces, 16-byte
+ * aligned, are read in such pieces, others element by element.  In bf16 probabilities and their gradients are rounded to bf16
+ * before they are multiplied with rows; scores, sums and accumulators are fp32. */
+typedef struct {
+    int64_t n_q, n_k;          /* rows of q and o; rows of k and v */
+    int32_t n_clouds;
+    int32_t heads, kv_heads, dim;
+    int32_t left, right, sinks;
+    float scale;               /* of the scores, usually 1/sqrt(dim) */
+    sp_dtype dt;               /* storage type of q, k, v, o and their gradients */
+    const int32_t* d_q_starts; /* [n_clouds + 1] */
+    const int32_t* d_k_starts; /* [n_clouds + 1] */
+} sp_window_attn;
+int sp_window_attn_fwd(const sp_window_attn* a, const void* d_q, int64_t ldq, const void* d_k, int64_t ldk, const void* d_v,
+                       int64_t ldv, void* d_o, int64_t ldo, float* d_lse, void* stream);
+/* Gradients of sum(o * dout): d_dq like q, d_dk and d_dv like k and v (summed over the query heads that share them); d_o and d_lse
+ * are the forward pass's results. */
+int sp_window_attn_bwd(const sp_window_attn* a, const void* d_q, int64_t ldq, const void* d_k, int64_t ldk, const void* d_v,
+                       int64_t ldv, const void* d_o, int64_t ldo, const void* d_dout, int64_t lddout, const float* d_lse, void* d_dq,
+                       int64_t lddq, void* d_dk, int64_t lddk, void* d_dv, int64_t lddv, void* stream);
+
+/* The same attention (right = 0) for the next token of each of `batch` sequences, over a cache of `cap` rows a sequence:
+ * caches [batch][cap][kv_heads][dim], q and o [batch][heads][dim], k_new and v_new [batch][kv_heads][dim], all dense.
+ * d_lens int32 [batch]: the tokens before this one, which therefore stands at p = lens[b].  Position j lies in row j for j < sinks,
+ * else in row sinks + (j - sinks) % (cap - sinks): with cap > p nothing is overwritten, else the rows behind the first `sinks`
+ * are a ring.  The call writes k_new and v_new to p's row of the caches, then attends over
+ *   max(p - left, p + 1 - (cap - sinks)) <= j <= p  and  j < min(sinks, p + 1).
+ * lens[b] < 0: no sequence in this slot; o = 0, its caches stay as they are.  cap > sinks >= 0.  lens is not changed. */
+int sp_window_attn_step(const void* d_q, const void* d_k_new, const void* d_v_new, void* d_k_cache, void* d_v_cache,
+                        const int32_t* d_lens, int32_t batch, int32_t cap, int32_t heads, int32_t kv_heads, int32_t dim, int32_t left,
+                        int32_t sinks, float scale, void* d_o, sp_dtype dt, void* stream);
+
+/* Distillation from a teacher's top logits.  d_logits [n][m] of type dt are the student's; the teacher gives, for every row, k
+ * logits d_top [n][k] (fp32) and their columns d_index int32 [n][k].  A column outside [0, m) is no entry (padding); a column may
+ * occur twice.  With temperature T, a = softmax over a row's entries of top / T, and weights w [n] (NULL: 1/n each):
+ *   loss = T^2 * sum over rows of w * sum_j a_j * (log a_j - log softmax(logits / T)[index_j])          -> d_loss [1]
+ *   dlogits[c] = w * T * (softmax(logits / T)[c] - sum of a_j with index_j = c)                         -> d_dlogits [n][m]
+ * A row without entries (or with -infinity in all of them) adds nothing and has a zero gradient.  d_dlogits may be NULL (the loss
+ * alone), or d_logits itself.  1 <= k <= 256, T > 0.  n = 0 gives loss 0. */
+int sp_distill(const void* d_logits, int64_t n, int32_t m, const float* d_top, const int32_t* d_index, int32_t k, float temperature,
+               const float* d_weight, float* d_loss, void* d_dlogits, sp_dtype dt, void* stream);
+
 /* ---- stage-boundary packing of a sparse tensor (Sec. III-B, last paragraph: the coordinate matrix and the
  * feature matrix are what is exchanged between pipeline stages) ---------------------------------------------
  * (C, F) -> one contiguous device buffer that any transport can send as a single message, and back.  Layout,

@@ -532,3 +532,136 @@ def sp_softmax_ce(logits, labels):
     _check(_glue_argtypes().sp_softmax_ce(logits.data_ptr(), labels.data_ptr(), nb, m, loss.data_ptr(), d.data_ptr(),
                                           _stream()))
     return loss, d
+
+
+# ---- a transformer over the rows of a sparse tensor -------------------------------------------------------
+class _WindowAttn(C.Structure):
+    _fields_ = [("n_q", C.c_int64), ("n_k", C.c_int64), ("n_clouds", C.c_int32), ("heads", C.c_int32),
+                ("kv_heads", C.c_int32), ("dim", C.c_int32), ("left", C.c_int32), ("right", C.c_int32),
+                ("sinks", C.c_int32), ("scale", C.c_float), ("dt", C.c_int32), ("d_q_starts", _vp), ("d_k_starts", _vp)]
+
+
+def _token_argtypes():
+    l = lib()
+    if getattr(l, "_token_ready", False):
+        return l
+    f, i4, i8 = C.c_float, C.c_int32, C.c_int64
+    l.sp_layer_norm_fwd.argtypes = [_vp, i8, i4, _vp, _vp, f, _vp, _vp, _vp, i4, _vp]
+    l.sp_layer_norm_bwd.argtypes = [_vp, _vp, i8, i4, _vp, _vp, _vp, _vp, _vp, _vp, i4, _vp]
+    a = C.POINTER(_WindowAttn)
+    l.sp_window_attn_fwd.argtypes = [a] + [_vp, i8] * 4 + [_vp, _vp]
+    l.sp_window_attn_bwd.argtypes = [a] + [_vp, i8] * 5 + [_vp] + [_vp, i8] * 3 + [_vp]
+    l.sp_window_attn_step.argtypes = [_vp] * 6 + [i4] * 7 + [f, _vp, i4, _vp]
+    l.sp_distill.argtypes = [_vp, i8, i4, _vp, _vp, i4, f, _vp, _vp, _vp, i4, _vp]
+    l._token_ready = True
+    return l
+
+
+def _need_shape(t: torch.Tensor, shape, name: str):
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have the shape {tuple(shape)}, not {tuple(t.shape)}")
+
+
+def sp_layer_norm_fwd(x: torch.Tensor, gamma: torch.Tensor, beta: torch.Tensor, eps: float = 1e-5):
+    """x [n][c], gamma / beta fp32 [c].  Returns (y, mean fp32 [n], rstd fp32 [n])."""
+    _need_cuda(x, None, "x"), _need_cuda(gamma, torch.float32, "gamma"), _need_cuda(beta, torch.float32, "beta")
+    n, c = x.shape
+    _need_shape(gamma, (c,), "gamma"), _need_shape(beta, (c,), "beta")
+    y, mean, rstd = torch.empty_like(x), _f32((n,), x.device), _f32((n,), x.device)
+    _check(_token_argtypes().sp_layer_norm_fwd(x.data_ptr(), n, c, gamma.data_ptr(), beta.data_ptr(), eps, y.data_ptr(),
+                                               mean.data_ptr(), rstd.data_ptr(), _dt(x), _stream()))
+    return y, mean, rstd
+
+
+def sp_layer_norm_bwd(x, dy, gamma, mean, rstd):
+    """Returns (dx, dgamma fp32 [c], dbeta fp32 [c])."""
+    _need_cuda(x, None, "x"), _need_cuda(dy, x.dtype, "dy"), _need_cuda(gamma, torch.float32, "gamma")
+    _need_cuda(mean, torch.float32, "mean"), _need_cuda(rstd, torch.float32, "rstd")
+    n, c = x.shape
+    _need_shape(dy, (n, c), "dy"), _need_shape(gamma, (c,), "gamma"), _need_shape(mean, (n,), "mean"), _need_shape(rstd, (n,), "rstd")
+    dx, dgamma, dbeta = torch.empty_like(x), _f32((c,), x.device), _f32((c,), x.device)
+    _check(_token_argtypes().sp_layer_norm_bwd(x.data_ptr(), dy.data_ptr(), n, c, gamma.data_ptr(), mean.data_ptr(), rstd.data_ptr(),
+                                               dx.data_ptr(), dgamma.data_ptr(), dbeta.data_ptr(), _dt(x), _stream()))
+    return dx, dgamma, dbeta
+
+
+def _head_rows(t: torch.Tensor, dtype, name: str):
+    """[rows][heads][dim] whose heads lie one after another in a row; rows may be further apart (a view of a fused projection)."""
+    if not t.is_cuda or t.ndim != 3 or t.dtype != dtype:
+        raise ValueError(f"{name} must be a CUDA tensor [rows][heads][dim] of {dtype}")
+    n, h, d = t.shape
+    if (t.stride(2) != 1 and d > 1) or (t.stride(1) != d and h > 1) or (n > 1 and t.stride(0) < h * d):
+        raise ValueError(f"the heads of a row of {name} must lie one after another, and rows must not overlap")
+    return t.data_ptr(), (t.stride(0) if n > 1 else h * d)
+
+
+def _window(q, k, v, q_starts, k_starts, left, right, sinks, scale):
+    _need_cuda(q_starts, torch.int32, "q_starts"), _need_cuda(k_starts, torch.int32, "k_starts")
+    if q_starts.ndim != 1 or k_starts.shape != q_starts.shape or q_starts.numel() < 1:
+        raise ValueError("q_starts and k_starts must be [clouds + 1]")
+    n_q, heads, dim = q.shape
+    n_k, kv_heads, _ = k.shape
+    _need_shape(k, (n_k, kv_heads, dim), "k"), _need_shape(v, (n_k, kv_heads, dim), "v")
+    return _WindowAttn(n_q, n_k, q_starts.numel() - 1, heads, kv_heads, dim, left, right, sinks,
+                       dim ** -0.5 if scale is None else scale, _dt(q), q_starts.data_ptr(), k_starts.data_ptr())
+
+
+def sp_window_attn_fwd(q, k, v, q_starts, k_starts, left: int, right: int = 0, sinks: int = 0, scale=None):
+    """q [n_q][heads][dim], k and v [n_k][kv_heads][dim] (views of a fused projection too), starts int32 [clouds + 1] (device).
+    scale None: 1/sqrt(dim).  Returns (o [n_q][heads][dim], lse fp32 [n_q][heads])."""
+    rows = [x for t, name in ((q, "q"), (k, "k"), (v, "v")) for x in _head_rows(t, q.dtype, name)]
+    a = _window(q, k, v, q_starts, k_starts, left, right, sinks, scale)
+    o, lse = torch.empty(q.shape, dtype=q.dtype, device=q.device), _f32(q.shape[:2], q.device)
+    _check(_token_argtypes().sp_window_attn_fwd(C.byref(a), *rows, o.data_ptr(), a.heads * a.dim, lse.data_ptr(), _stream()))
+    return o, lse
+
+
+def sp_window_attn_bwd(q, k, v, o, dout, lse, q_starts, k_starts, left: int, right: int = 0, sinks: int = 0, scale=None, out=None):
+    """Gradients of sum(o * dout): (dq, dk, dv), new tensors, or written into the three of `out` (views of one buffer too)."""
+    rows = [x for t, name in ((q, "q"), (k, "k"), (v, "v"), (o, "o"), (dout, "dout")) for x in _head_rows(t, q.dtype, name)]
+    a = _window(q, k, v, q_starts, k_starts, left, right, sinks, scale)
+    _need_cuda(lse, torch.float32, "lse")
+    _need_shape(o, q.shape, "o"), _need_shape(dout, q.shape, "dout"), _need_shape(lse, q.shape[:2], "lse")
+    if out is None:
+        out = tuple(torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
+    for t, like, name in zip(out, (q, k, v), ("dq", "dk", "dv")):
+        _need_shape(t, like.shape, name)
+    grads = [x for t, name in zip(out, ("dq", "dk", "dv")) for x in _head_rows(t, q.dtype, name)]
+    _check(_token_argtypes().sp_window_attn_bwd(C.byref(a), *rows, lse.data_ptr(), *grads, _stream()))
+    return tuple(out)
+
+
+def sp_window_attn_step(q, k_new, v_new, k_cache, v_cache, lens, left: int, sinks: int = 0, scale=None):
+    """One token of each sequence: q [batch][heads][dim], k_new and v_new [batch][kv_heads][dim], caches [batch][cap][kv_heads][dim]
+    (written at the token's row), lens int32 [batch] (tokens before this one; negative: an empty slot).  Returns o."""
+    for t, name in ((q, "q"), (k_new, "k_new"), (v_new, "v_new"), (k_cache, "k_cache"), (v_cache, "v_cache")):
+        _need_cuda(t, q.dtype, name)
+    _need_cuda(lens, torch.int32, "lens")
+    batch, heads, dim = q.shape
+    _, cap, kv_heads, _ = k_cache.shape
+    for t, name in ((k_new, "k_new"), (v_new, "v_new")):
+        _need_shape(t, (batch, kv_heads, dim), name)
+    for t, name in ((k_cache, "k_cache"), (v_cache, "v_cache")):
+        _need_shape(t, (batch, cap, kv_heads, dim), name)
+    _need_shape(lens, (batch,), "lens")
+    o = torch.empty_like(q)
+    _check(_token_argtypes().sp_window_attn_step(q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
+                                                 lens.data_ptr(), batch, cap, heads, kv_heads, dim, left, sinks,
+                                                 dim ** -0.5 if scale is None else scale, o.data_ptr(), _dt(q), _stream()))
+    return o
+
+
+def sp_distill(logits, top, index, temperature: float = 1.0, weight=None, want_grad: bool = True):
+    """logits [n][m]; the teacher's logits top fp32 [n][k] in columns index int32 [n][k] (outside [0, m): no entry); weight fp32 [n]
+    (None: 1/n each).  Returns (loss fp32 [1], dlogits or None)."""
+    _need_cuda(logits, None, "logits"), _need_cuda(top, torch.float32, "top"), _need_cuda(index, torch.int32, "index")
+    n, m = logits.shape
+    k = top.shape[1]
+    _need_shape(top, (n, k), "top"), _need_shape(index, (n, k), "index")
+    if weight is not None:
+        _need_cuda(weight, torch.float32, "weight"), _need_shape(weight, (n,), "weight")
+    loss, d = _f32((1,), logits.device), (torch.empty_like(logits) if want_grad else None)
+    _check(_token_argtypes().sp_distill(logits.data_ptr(), n, m, top.data_ptr(), index.data_ptr(), k, temperature,
+                                        weight.data_ptr() if weight is not None else None, loss.data_ptr(),
+                                        d.data_ptr() if want_grad else None, _dt(logits), _stream()))
+    return loss, d

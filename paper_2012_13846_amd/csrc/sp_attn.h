@@ -1,0 +1,202 @@
+// What the kernels of the windowed attention share: which cloud a row belongs to, which keys a query sees, and one row's results
+// computed by one wavefront, key by key.
+#pragma once
+
+#include "sp_elem.h"
+
+namespace sp {
+
+constexpr int kMaxDim = 128;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+// Row r, head h of an array starts at p + r * ld + h * dim.
+template <typename T>
+struct Rows {
+    T* p;
+    int64_t ld;
+    __device__ __forceinline__ T* at(int64_t r, int h, int dim) const { return p + r * ld + (int64_t)h * dim; }
+};
+
+struct Window {
+    const int32_t *q_starts, *k_starts;
+    int n_q, n_k, clouds;
+    int heads, kv_heads, group, dim;
+    int left, right, sinks;  // at most n_k, n_q and n_k: more changes nothing, and positions +- these fit 32 bits
+    float scale;
+};
+
+template <typename T>
+struct AttnFwd {
+    Window w;
+    Rows<const T> q, k, v;
+    Rows<T> o;
+    float* lse;  // [n_q][heads]
+};
+
+template <typename T>
+struct AttnBwd {
+    Window w;
+    Rows<const T> q, k, v, o, dout;
+    const float* lse;
+    float* delta;  // [n_q][heads]: dout . o
+    Rows<T> dq, dk, dv;
+};
+
+// Clouds 1 .. clouds are the caller's; 0 and clouds + 1 hold the rows before the first and after the last.
+__device__ __forceinline__ int cloud_begin(const int32_t* starts, int clouds, int n, int c) {
+    if (c <= 0) return 0;
+    if (c > clouds + 1) return n;
+    return min(max(starts[c - 1], 0), n);
+}
+// The last cloud with begin / T + number <= t.  Rows cut cloud by cloud into tiles of T: cloud c has the tile numbers from
+// begin(c) / T + c on, which are at least as many as its tiles.  T = 1 leaves the number out: the cloud of row t.
+template <int T>
+__device__ __forceinline__ int cloud_of(const int32_t* starts, int clouds, int n, int t) {
+    int lo = 0, hi = clouds + 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (cloud_begin(starts, clouds, n, mid) / T + (T > 1 ? mid : 0) <= t) lo = mid;
+        else hi = mid - 1;
+    }
+    return lo;
+}
+
+struct Cloud {
+    int q0, a, k0, b;  // first query row, queries, first key row, keys
+    int off;           // query i stands at position i + off
+    __device__ __forceinline__ Cloud(const Window& w, int c) {
+        q0 = cloud_begin(w.q_starts, w.clouds, w.n_q, c);
+        a = max(0, cloud_begin(w.q_starts, w.clouds, w.n_q, c + 1) - q0);
+        k0 = cloud_begin(w.k_starts, w.clouds, w.n_k, c);
+        b = max(0, cloud_begin(w.k_starts, w.clouds, w.n_k, c + 1) - k0);
+        off = b - a;
+        partners = c >= 1 && c <= w.clouds;
+    }
+    bool partners;  // false: these rows belong to no cloud, see nothing and are seen by nobody
+};
+
+// The keys that query i of a cloud sees, in order: t-th of n
+struct Seen {
+    int first, lo, n;
+    __device__ __forceinline__ Seen(const Window& w, const Cloud& c, int i) {
+        const int p = i + c.off;
+        const int hi = c.partners ? min(max(p + w.right + 1, 0), c.b) : 0;
+        lo = min(max(p - w.left, 0), hi);
+        first = min(w.sinks, lo);
+        n = first + hi - lo;
+    }
+    __device__ __forceinline__ int key(int t) const { return t < first ? t : lo + t - first; }
+};
+
+__device__ __forceinline__ float lane_value(float v, int lane) {
+    return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), lane));
+}
+template <typename Op>
+__device__ __forceinline__ float wave_reduce(float v) {
+#pragma unroll
+    for (int s = 32; s > 0; s >>= 1) v = Op::of(v, __shfl_xor(v, s));
+    return v;
+}
+
+// ---- one row by one wavefront: lanes are keys (or queries) for the scores and elements for the products with rows --------------
+// All lanes must come here together.
+
+template <typename T>
+__device__ __forceinline__ float dot(const T* a, const T* b, int dim) {
+    float s = 0.f;
+    for (int e = 0; e < dim; ++e) s = fmaf(elem(a[e]), elem(b[e]), s);
+    return s;
+}
+// acc[e] += value of lane t * row t's elements, for the n rows that at(t) gives
+template <typename T, typename At>
+__device__ __forceinline__ void add_rows(float (&acc)[2], float value, int n, int dim, At at) {
+    const int lane = threadIdx.x & 63;
+    for (int t = 0; t < n; ++t) {
+        const T* row = at(t);
+        const float x = lane_value(value, t);
+        if (lane < dim) acc[0] = fmaf(x, elem(row[lane]), acc[0]);
+        if (lane + 64 < dim) acc[1] = fmaf(x, elem(row[lane + 64]), acc[1]);
+    }
+}
+template <typename T>
+__device__ __forceinline__ void put_row(T* row, const float (&acc)[2], int dim) {
+    const int lane = threadIdx.x & 63;
+    if (lane < dim) row[lane] = to_elem<T>(acc[0]);
+    if (lane + 64 < dim) row[lane + 64] = to_elem<T>(acc[1]);
+}
+
+template <typename T>
+__device__ __forceinline__ void forward_row(const AttnFwd<T>& f, const Cloud& c, int i, int h) {
+    const Window& w = f.w;
+    const int lane = threadIdx.x & 63, kh = h / w.group;
+    const Seen seen(w, c, i);
+    const float c2 = w.scale * kLog2e;
+    const T* q = f.q.at(c.q0 + i, h, w.dim);
+    float m = -INFINITY, l = 0.f, acc[2] = {0.f, 0.f};  // m: the largest score times c2 so far
+    for (int t0 = 0; t0 < seen.n; t0 += 64) {
+        const bool in = t0 + lane < seen.n;
+        const float s = in ? dot(q, f.k.at(c.k0 + seen.key(t0 + lane), kh, w.dim), w.dim) * c2 : -INFINITY;
+        const float top = fmaxf(m, wave_reduce<Max>(s));
+        const float base = top == -INFINITY ? 0.f : top;
+        const float old = __builtin_amdgcn_exp2f(m - base), p = in ? __builtin_amdgcn_exp2f(s - base) : 0.f;
+        l = l * old + wave_reduce<Add>(p);
+        acc[0] *= old;
+        acc[1] *= old;
+        add_rows<T>(acc, p, min(64, seen.n - t0), w.dim, [&](int t) { return f.v.at(c.k0 + seen.key(t0 + t), kh, w.dim); });
+        m = top;
+    }
+    const float inv = seen.n > 0 ? 1.f / l : 0.f;
+    acc[0] *= inv;
+    acc[1] *= inv;
+    put_row(f.o.at(c.q0 + i, h, w.dim), acc, w.dim);
+    if (lane == 0) f.lse[(int64_t)(c.q0 + i) * w.heads + h] = seen.n > 0 ? m * kLn2 + logf(l) : -INFINITY;
+}
+
+template <typename T>
+__device__ __forceinline__ void query_gradient_row(const AttnBwd<T>& g, const Cloud& c, int i, int h) {
+    const Window& w = g.w;
+    const int lane = threadIdx.x & 63, kh = h / w.group;
+    const Seen seen(w, c, i);
+    const int64_t r = c.q0 + i;
+    const float lse = g.lse[r * w.heads + h], delta = g.delta[r * w.heads + h];
+    float acc[2] = {0.f, 0.f};
+    for (int t0 = 0; t0 < seen.n; t0 += 64) {
+        float ds = 0.f;
+        if (t0 + lane < seen.n) {
+            const int64_t j = c.k0 + seen.key(t0 + lane);
+            const float p = __builtin_amdgcn_exp2f((dot(g.q.at(r, h, w.dim), g.k.at(j, kh, w.dim), w.dim) * w.scale - lse) * kLog2e);
+            ds = p * (dot(g.dout.at(r, h, w.dim), g.v.at(j, kh, w.dim), w.dim) - delta) * w.scale;
+        }
+        add_rows<T>(acc, ds, min(64, seen.n - t0), w.dim, [&](int t) { return g.k.at(c.k0 + seen.key(t0 + t), kh, w.dim); });
+    }
+    put_row(g.dq.at(r, h, w.dim), acc, w.dim);
+}
+
+template <typename T>
+__device__ __forceinline__ void key_gradient_row(const AttnBwd<T>& g, const Cloud& c, int j, int kh) {
+    const Window& w = g.w;
+    const int lane = threadIdx.x & 63;
+    // queries at positions j - right .. j + left (all later ones for the first keys)
+    const int end = c.partners ? c.a : 0;
+    const int lo = min(max(j - w.right - c.off, 0), end);
+    const int hi = j < w.sinks ? end : min(max(j + w.left + 1 - c.off, lo), end);
+    float ak[2] = {0.f, 0.f}, av[2] = {0.f, 0.f};
+    const T *k = g.k.at(c.k0 + j, kh, w.dim), *v = g.v.at(c.k0 + j, kh, w.dim);
+    for (int h = kh * w.group; h < (kh + 1) * w.group; ++h)
+        for (int i0 = lo; i0 < hi; i0 += 64) {
+            float p = 0.f, ds = 0.f;
+            if (i0 + lane < hi) {
+                const int64_t r = c.q0 + i0 + lane;
+                p = __builtin_amdgcn_exp2f((dot(g.q.at(r, h, w.dim), k, w.dim) * w.scale - g.lse[r * w.heads + h]) * kLog2e);
+                ds = p * (dot(g.dout.at(r, h, w.dim), v, w.dim) - g.delta[r * w.heads + h]) * w.scale;
+            }
+            const int n = min(64, hi - i0);
+            add_rows<T>(ak, ds, n, w.dim, [&](int t) { return g.q.at(c.q0 + i0 + t, h, w.dim); });
+            add_rows<T>(av, p, n, w.dim, [&](int t) { return g.dout.at(c.q0 + i0 + t, h, w.dim); });
+        }
+    put_row(g.dk.at(c.k0 + j, kh, w.dim), ak, w.dim);
+    put_row(g.dv.at(c.k0 + j, kh, w.dim), av, w.dim);
+}
+
+}  // namespace sp

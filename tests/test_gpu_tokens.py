@@ -1,0 +1,488 @@
+"""Layer norm, windowed attention with its step, and distillation on the GPU against oracle/tokens.py (float64).
+
+Tolerances are bounds of the error, element by element, from half a step of the storage type (u) and of fp32 (2^-24)
+relative to each rounded value, as derived beside each comparison.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import tokens
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16 = torch.float32, torch.bfloat16
+U32 = torch.finfo(F32).eps / 2
+
+
+@pytest.fixture(scope="module")
+def sp():
+    from paper_2012_13846_amd import binding
+    binding.lib()
+    return binding
+
+
+def half_step(dt):
+    return torch.finfo(dt).eps / 2
+
+
+def host(t):
+    return t.detach().double().cpu().numpy()
+
+
+def rows(rng, dt, *shape, scale=1.0, shift=0.0):
+    """Values of the storage type, on the GPU (read back exactly by host)."""
+    return torch.from_numpy((rng.standard_normal(shape) * scale + shift).astype(np.float32)).to(dt).cuda()
+
+
+def within(got, want, bound, what):
+    got, want = host(got), np.asarray(want)
+    assert got.shape == want.shape, what
+    fine = np.isfinite(want)
+    assert np.array_equal(fine, np.isfinite(got)), f"{what}: finite in other places"
+    assert np.array_equal(got[~fine & ~np.isnan(want)], want[~fine & ~np.isnan(want)]), f"{what}: infinities differ"
+    over = np.abs(got[fine] - want[fine]) - np.broadcast_to(bound, want.shape)[fine]
+    assert over.size == 0 or over.max() <= 0, f"{what}: {over.max():.3e} over its bound"
+
+
+# ---- layer normalisation ---------------------------------------------------------------------------------------
+NORM = [(1, 1), (1, 16), (3, 5), (1428, 128), (515, 77), (130, 64), (33, 1000), (257, 1024), (65, 2048), (19, 4096), (5, 8192), (4, 8191),
+        (3, 16384), (2, 16392), (2, 40001), (7, 513), (40, 24), (9, 2056), (6, 4100), (70001, 8)]
+
+
+@pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("n,c", NORM)
+def test_layer_norm(sp, n, c, dt):
+    rng = np.random.default_rng(n * 7 + c)
+    x = rows(rng, dt, n, c, scale=1.5, shift=0.3)
+    dy = rows(rng, dt, n, c)
+    gamma, beta = rows(rng, F32, c, scale=0.2, shift=1.0), rows(rng, F32, c, scale=0.2)
+    eps = 1e-5
+    y, mean, rstd = sp.sp_layer_norm_fwd(x, gamma, beta, eps)
+    X, DY, G, B = host(x), host(dy), host(gamma), host(beta)
+    Y, M, R = tokens.layer_norm_fwd(X, G, B, eps)
+    u = half_step(dt) if dt == BF16 else U32
+    depth = 24 * U32                       # a pairwise sum of up to 2^16 values, 16 of them in a lane, and the steps behind it
+    top = np.abs(X).max(axis=1)
+    within(mean, M, depth * top, "mean")
+    # the variance's relative error: squares and their sum; d = x - m is rounded to half a step of x, which weighs top * rstd
+    rel = depth * (1 + top * R) ** 2
+    within(rstd, R, rel * R, "rstd")
+    xh = np.abs((X - M[:, None]) * R[:, None])
+    slack = (rel[:, None] * (xh + 1) + depth * (top * R)[:, None]) * np.abs(G)
+    within(y, Y, slack + (u + 2 * U32) * (np.abs(Y) + np.abs(B)), "y")
+    # backward from the GPU's own statistics: the formula's inputs are exact then
+    dx, dgamma, dbeta = sp.sp_layer_norm_bwd(x, dy, gamma, mean, rstd)
+    M, R = host(mean), host(rstd)
+    DX, DG, DB = tokens.layer_norm_bwd(X, DY, G, M, R)
+    xh, g = np.abs((X - M[:, None]) * R[:, None]), np.abs(DY * G)
+    wide = R[:, None] * (g + g.mean(1)[:, None] + xh * (g * xh).mean(1)[:, None])
+    within(dx, DX, depth * wide + u * np.abs(DX), "dx")
+    # the rows' sums: up to 2^10 rows one after another in a lane, the lanes' sums in fp64
+    run = (10 + min(n, 1100)) * U32
+    within(dgamma, DG, run * np.abs(DY * xh).sum(0) + U32 * np.abs(DG), "dgamma")
+    within(dbeta, DB, run * np.abs(DY).sum(0) + U32 * np.abs(DB), "dbeta")
+
+
+def test_layer_norm_edges(sp):
+    gamma, beta = torch.ones(48, device="cuda"), torch.zeros(48, device="cuda")
+    empty = torch.empty((0, 48), device="cuda")
+    y, mean, rstd = sp.sp_layer_norm_fwd(empty, gamma, beta)
+    dx, dgamma, dbeta = sp.sp_layer_norm_bwd(empty, empty, gamma, mean, rstd)
+    assert y.shape == (0, 48) and dx.shape == (0, 48) and not dgamma.any() and not dbeta.any()
+    x = torch.randn((6, 48), device="cuda")
+    x[2, 5], x[4, 0] = float("nan"), float("inf")
+    x[5] = 3.25                                               # no spread
+    y, mean, rstd = sp.sp_layer_norm_fwd(x, gamma, beta, 1e-5)
+    assert torch.isfinite(y[[0, 1, 3, 5]]).all() and not torch.isfinite(y[[2, 4]]).any()
+    assert not y[5].any() and float(mean[5]) == 3.25 and abs(float(rstd[5]) - 1e5 ** 0.5) < 1e-3
+    with pytest.raises(ValueError):
+        sp.sp_layer_norm_fwd(x, gamma[:40], beta)
+    with pytest.raises(ValueError):
+        sp.sp_layer_norm_fwd(x[:, ::2], gamma[:24].contiguous(), beta[:24].contiguous())
+    # rows that begin off a 16-byte border are read element by element
+    flat = torch.randn(6 * 48 + 1, device="cuda")
+    a = sp.sp_layer_norm_fwd(flat[1:].view(6, 48), gamma, beta)[0]
+    b = sp.sp_layer_norm_fwd(flat[1:].clone().view(6, 48), gamma, beta)[0]
+    assert float((a - b).abs().max()) <= 32 * U32 * 10      # sums of 48 values in two orders, results below 10
+
+
+# ---- windowed attention ----------------------------------------------------------------------------------------
+# queries and keys of each cloud, heads, kv_heads, dim, left, right, sinks
+ATTN = {
+    "one": ([1], [1], 1, 1, 1, 0, 0, 0),
+    "causal": ([130], [130], 4, 2, 64, 40, 0, 4),
+    "full": ([97], [97], 2, 2, 32, 1000, 1000, 0),
+    "both_sides": ([64, 1, 129, 0, 200], [64, 1, 129, 0, 200], 3, 3, 48, 17, 9, 1),
+    "self_only": ([70], [70], 2, 1, 16, 0, 0, 0),
+    "sinks_far": ([300], [300], 2, 1, 32, 10, 0, 70),
+    "sinks_all": ([90], [90], 1, 1, 8, 3, 2, 500),
+    "prompt": ([33, 5], [290, 140], 8, 2, 128, 100, 0, 3),
+    "last_token": ([1, 1, 1], [257, 64, 1], 6, 1, 80, 64, 0, 2),
+    "more_queries": ([100, 40], [30, 0], 2, 2, 64, 8, 0, 2),
+    "more_queries_right": ([70], [20], 2, 2, 24, 5, 33, 0),
+    "odd_dim": ([75, 66], [75, 66], 5, 5, 33, 30, 4, 2),
+    "narrow": ([40], [40], 4, 4, 3, 9, 0, 1),
+    "wide_odd": ([140], [140], 2, 1, 127, 64, 64, 5),
+    "group5": ([150], [150], 10, 2, 96, 63, 1, 17),
+    "many": ([3] * 50 + [65], [3] * 50 + [65], 2, 2, 16, 2, 2, 1),
+    "long": ([1100], [1100], 1, 1, 64, 500, 0, 4),
+    "negative_scale": ([60], [60], 2, 2, 32, 20, 0, 0),
+}
+
+
+def attn_inputs(case, dt, fused=False, gap=0):
+    a, b, h, kv, d, left, right, sinks = ATTN[case]
+    rng = np.random.default_rng(zlib_of(case))
+    qs, ks = np.concatenate([[0], np.cumsum(a)]) + gap, np.concatenate([[0], np.cumsum(b)]) + gap
+    n_q, n_k = int(qs[-1]) + gap, int(ks[-1]) + gap
+    if fused and a == b:
+        w = rows(rng, dt, n_q, h + 2 * kv, d)
+        q, k, v = w[:, :h], w[:, h:h + kv], w[:, h + kv:]
+    else:
+        q, k, v = rows(rng, dt, n_q, h, d), rows(rng, dt, n_k, kv, d), rows(rng, dt, n_k, kv, d)
+    starts = [torch.tensor(s, dtype=torch.int32, device="cuda") for s in (qs, ks)]
+    scale = (-0.2 if case == "negative_scale" else 1 / math.sqrt(d))
+    return q, k, v, rows(rng, dt, n_q, h, d), starts, (qs, ks), dict(left=left, right=right, sinks=sinks, scale=scale)
+
+
+def zlib_of(text):
+    import zlib
+    return zlib.crc32(text.encode())
+
+
+def attn_errors(dt, q, k, keys, scale):
+    """(u, g): half a step of the type; the relative error of a probability in fp32: the score's (a sum of d products of size
+    |q||k|), its place in the exponent once more, the exponential, and the sum over the keys."""
+    d = q.shape[2]
+    size = abs(scale) * float(np.linalg.norm(host(q), axis=2).max(initial=0)) * float(np.linalg.norm(host(k), axis=2).max(initial=0))
+    return (half_step(dt) if dt == BF16 else U32), ((d + 6) * size + 2 * keys + 2 * d + 16) * U32
+
+
+def check_attention(sp, q, k, v, do, starts, host_starts, shape, dt, what):
+    o, lse = sp.sp_window_attn_fwd(q, k, v, *starts, **shape)
+    most = int(np.diff(host_starts[1]).max(initial=0))
+    u, g = attn_errors(dt, q, k, most, shape["scale"])
+    s = (shape["left"], shape["right"], shape["sinks"], shape["scale"])
+    O, LSE, bound = tokens.window_attn_fwd(host(q), host(k), host(v), *host_starts, *s, u, g)
+    within(lse, LSE, g * (1 + np.where(np.isfinite(LSE), np.abs(LSE), 0)), what + " lse")
+    within(o, O, bound, what + " o")
+    Os = torch.from_numpy(O).to(dt).cuda()                    # backward from the oracle's results
+    lse32 = torch.from_numpy(LSE).to(F32).cuda()
+    grads = sp.sp_window_attn_bwd(q, k, v, Os, do, lse32, *starts, **shape)
+    g += 2 * U32 * float(np.abs(LSE[np.isfinite(LSE)]).max(initial=0))
+    queries = int(np.diff(host_starts[0]).max(initial=0)) * (q.shape[1] // k.shape[1])
+    want, bounds = tokens.window_attn_bwd(host(q), host(k), host(v), host(Os), host(do), host(lse32), *host_starts, *s, u, g + 2 * queries * U32)
+    for got, ref, b, name in zip(grads, want, bounds, ("dq", "dk", "dv")):
+        within(got, ref, b, f"{what} {name}")
+    return o, lse, grads
+
+
+@pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("case", sorted(ATTN))
+def test_window_attention(sp, case, dt):
+    q, k, v, do, starts, hs, shape = attn_inputs(case, dt, fused=True)
+    check_attention(sp, q, k, v, do, starts, hs, shape, dt, case)
+
+
+@pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("case", ["both_sides", "prompt", "sinks_far"])
+def test_rows_outside_of_every_cloud_are_empty(sp, case, dt):
+    q, k, v, do, starts, hs, shape = attn_inputs(case, dt, gap=5)
+    o, lse, (dq, dk, dv) = check_attention(sp, q, k, v, do, starts, hs, shape, dt, case)
+    for t in (o, dq, dk, dv):
+        assert not t[:5].any() and not t[-5:].any()
+    assert torch.isneginf(lse[:5]).all() and torch.isneginf(lse[-5:]).all()
+
+
+@pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
+def test_attention_without_rows_or_clouds(sp, dt):
+    none, some = torch.empty((0, 2, 16), dtype=dt, device="cuda"), torch.ones((7, 2, 16), dtype=dt, device="cuda")
+    zero = torch.zeros(1, dtype=torch.int32, device="cuda")
+    o, lse = sp.sp_window_attn_fwd(some, none, none, zero, zero, left=3)
+    assert not o.any() and torch.isneginf(lse).all()
+    o, lse = sp.sp_window_attn_fwd(none, some, some, zero, zero, left=3)
+    dq, dk, dv = sp.sp_window_attn_bwd(none, some, some, o, none, lse, zero, zero, left=3)
+    assert dq.shape == (0, 2, 16) and not dk.any() and not dv.any()
+
+
+@pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
+def test_starts_that_are_no_starts_stay_inside_of_the_arrays(sp, dt):
+    """The results are undefined; what lies around the arrays is not touched."""
+    n, h, d = 100, 2, 32
+    room = torch.full((3 * n, h, d), 7.0, dtype=dt, device="cuda")
+    q, grad = room[n:2 * n], torch.full((3, 3 * n, h, d), 7.0, dtype=dt, device="cuda")
+    for bad in ([0, 250, 100], [-50, 30, 100], [60, 20, 90], [100, 0, 0], [2 ** 31 - 1, -2 ** 31, 5]):
+        st = torch.tensor(bad, dtype=torch.int32, device="cuda")
+        o, lse = sp.sp_window_attn_fwd(q, q, q, st, st, left=9, right=3, sinks=2)
+        sp.sp_window_attn_bwd(q, q, q, o, q, lse, st, st, left=9, right=3, sinks=2, out=[g[n:2 * n] for g in grad])
+    assert (grad[:, :n] == 7).all() and (grad[:, 2 * n:] == 7).all() and (room == 7).all()
+
+
+@pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("case", ["both_sides", "wide_odd", "prompt"])
+def test_attention_on_strided_and_unaligned_rows(sp, case, dt):
+    """Rows further apart, starting off 16-byte borders; gradients written into one fused buffer."""
+    q, k, v, do, starts, hs, shape = attn_inputs(case, dt)
+    want = check_attention(sp, q, k, v, do, starts, hs, shape, dt, case)
+
+    def spread(t, extra):
+        n, h, d = t.shape
+        buf = torch.full((n * (h * d + extra) + 1,), 9.0, dtype=dt, device="cuda")
+        view = buf[1:].as_strided((n, h, d), (h * d + extra, d, 1))
+        view.copy_(t)
+        return view
+
+    o, lse = sp.sp_window_attn_fwd(spread(q, 3), spread(k, 5), spread(v, 1), *starts, **shape)
+    u, g = attn_errors(dt, q, k, int(np.diff(hs[1]).max()), shape["scale"])
+    s = (shape["left"], shape["right"], shape["sinks"], shape["scale"])
+    O, _, bound = tokens.window_attn_fwd(host(q), host(k), host(v), *hs, *s, u, g)
+    within(o, O, bound, case)
+    outs = [spread(torch.zeros_like(t), e) for t, e in ((q, 2), (k, 4), (v, 0))]
+    got = sp.sp_window_attn_bwd(spread(q, 3), spread(k, 5), spread(v, 1), spread(o, 7), spread(do, 1), lse, *starts, **shape, out=outs)
+    ref, bounds = tokens.window_attn_bwd(host(q), host(k), host(v), host(o), host(do), host(lse), *hs, *s, u,
+                                         g + 2 * U32 * (q.shape[0] * q.shape[1] + float(lse[torch.isfinite(lse)].abs().max())))
+    for t, r, b, name in zip(got, ref, bounds, ("dq", "dk", "dv")):
+        within(t, r, b, f"{case} {name}")
+    assert len(want) == 3
+
+
+@pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("dim", [16, 64, 72, 128])
+def test_what_is_not_seen_does_not_reach_results(sp, dt, dim):
+    """Not-a-numbers, infinities and the type's extremes in rows that some queries see and others, in the same tile, do not."""
+    rng = np.random.default_rng(dim)
+    n, h, kv, left, sinks = 150, 4, 2, 5, 2
+    q, do = rows(rng, dt, n, h, dim), rows(rng, dt, n, h, dim)
+    k, v = rows(rng, dt, n, kv, dim), rows(rng, dt, n, kv, dim)
+    starts = torch.tensor([0, 70, n], dtype=torch.int32, device="cuda")
+    shape = dict(left=left, right=0, sinks=sinks)
+    o, lse = sp.sp_window_attn_fwd(q, k, v, starts, starts, **shape)
+    dq, dk, dv = sp.sp_window_attn_bwd(q, k, v, o, do, lse, starts, starts, **shape)
+    k2, v2, q2, do2 = k.clone(), v.clone(), q.clone(), do.clone()
+    bad = [20, 100]                                           # seen by queries 20..25 and 100..105
+    v2[20, 0], v2[100] = float("inf"), float("nan")
+    k2[100, 1] = float("nan")
+    clean = torch.ones(n, dtype=torch.bool, device="cuda")
+    for j in bad:
+        clean[j:j + left + 1] = False
+    o2, lse2 = sp.sp_window_attn_fwd(q, k2, v2, starts, starts, **shape)
+    assert torch.equal(o2[clean], o[clean]) and torch.equal(lse2[clean], lse[clean])
+    assert not torch.isfinite(o2[100:106]).any() and not torch.isfinite(o2[20:26, :2]).any() and torch.equal(o2[20:26, 2:], o[20:26, 2:])
+    dq2, dk2, dv2 = sp.sp_window_attn_bwd(q, k2, v2, o2, do, lse2, starts, starts, **shape)
+    assert torch.equal(dq2[clean], dq[clean])
+    # a query's bad values reach the keys that it sees and no other
+    q2[120], do2[120, 0] = float("nan"), float("inf")
+    o3, lse3 = sp.sp_window_attn_fwd(q2, k, v, starts, starts, **shape)
+    dq3, dk3, dv3 = sp.sp_window_attn_bwd(q2, k, v, o3, do2, lse3, starts, starts, **shape)
+    far = torch.ones(n, dtype=torch.bool, device="cuda")
+    far[115:121], far[70:72] = False, False                   # its window and its cloud's first rows
+    assert torch.equal(dk3[far], dk[far]) and torch.equal(dv3[far], dv[far]) and torch.equal(dq3[:120], dq[:120])
+    assert not torch.isfinite(dv3[115:121]).any()
+
+
+@pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
+def test_scores_of_extreme_size(sp, dt):
+    """One key far above the others takes all of the weight; scores far below zero leave finite results."""
+    n, d = 130, 64
+    rng = np.random.default_rng(2)
+    q, k, v = rows(rng, dt, n, 1, d), rows(rng, dt, n, 1, d), rows(rng, dt, n, 1, d)
+    q[:, 0, 0], k[:, 0, 0] = 1000.0, -1000.0
+    k[40, 0, 0] = 1000.0
+    starts = torch.tensor([0, n], dtype=torch.int32, device="cuda")
+    o, lse = sp.sp_window_attn_fwd(q, k, v, starts, starts, left=n, right=n)
+    assert torch.equal(o, v[40:41].expand(n, 1, d)) and torch.isfinite(lse).all()
+    o, lse = sp.sp_window_attn_fwd(q, k, v, starts, starts, left=10, right=0)
+    assert torch.isfinite(o).all() and torch.isfinite(lse).all()
+
+
+def test_attention_gradients_against_differences(sp):
+    q, k, v, do, starts, hs, shape = attn_inputs("both_sides", F32)
+    o, lse = sp.sp_window_attn_fwd(q, k, v, *starts, **shape)
+    grads = sp.sp_window_attn_bwd(q, k, v, o, do, lse, *starts, **shape)
+    rng = np.random.default_rng(9)
+    step = 2.0 ** -5
+    for t, g in zip((q, k, v), grads):
+        way = torch.from_numpy(rng.standard_normal(t.shape).astype(np.float32)).cuda()
+        way /= way.norm()
+        ends = []
+        for sign in (1, -1):
+            parts = [x + sign * step * way if x is t else x for x in (q, k, v)]
+            ends.append(float((sp.sp_window_attn_fwd(*parts, *starts, **shape)[0].double() * do.double()).sum()))
+        slope, want = (ends[0] - ends[1]) / (2 * step), float((g.double() * way.double()).sum())
+        # central differences leave step^2 / 6 of the third derivative (of the size of the gradient), fp32 sums of 40000 values
+        # below 2^-24 * their size over 2 * step
+        size = float(g.double().norm())
+        noise = U32 * 16 * float((o.double() * do.double()).norm()) / step
+        assert abs(slope - want) <= step ** 2 * size + noise
+
+
+# ---- one token -------------------------------------------------------------------------------------------------
+STEP = {
+    "first_tokens": dict(lens=[0, 1, 2, 3, -1, 5], cap=8, heads=2, kv=1, dim=32, left=3, sinks=1),
+    "no_wrap": dict(lens=[63, 64, 200, 0, 255], cap=256, heads=8, kv=2, dim=128, left=100, sinks=4),
+    "ring": dict(lens=[5000, 77, 76, 75, 20, -5, 1000003], cap=76, heads=4, kv=4, dim=64, left=71, sinks=4),
+    "ring_of_one": dict(lens=[9, 0, 1, 4], cap=5, heads=4, kv=2, dim=16, left=8, sinks=4),
+    "window_past_ring": dict(lens=[100, 30], cap=40, heads=3, kv=1, dim=48, left=1000, sinks=0),
+    "odd": dict(lens=[12, 130, 64], cap=131, heads=5, kv=5, dim=33, left=70, sinks=3),
+    "group7": dict(lens=[700, 699], cap=701, heads=14, kv=2, dim=80, left=600, sinks=17),
+    "long": dict(lens=[4999, 123], cap=5000, heads=16, kv=1, dim=128, left=4500, sinks=5),
+    "narrow": dict(lens=[40, 41], cap=64, heads=2, kv=2, dim=1, left=20, sinks=2),
+    "wide_group": dict(lens=[333], cap=400, heads=40, kv=2, dim=64, left=399, sinks=0),
+    "only_itself": dict(lens=[50, 0], cap=60, heads=2, kv=1, dim=64, left=0, sinks=0),
+}
+
+
+@pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("case", sorted(STEP))
+def test_attention_step(sp, case, dt):
+    s = STEP[case]
+    rng = np.random.default_rng(zlib_of(case))
+    n, h, kv, d, cap, sinks = len(s["lens"]), s["heads"], s["kv"], s["dim"], s["cap"], s["sinks"]
+    q, kn, vn = rows(rng, dt, n, h, d), rows(rng, dt, n, kv, d), rows(rng, dt, n, kv, d)
+    kc, vc = rows(rng, dt, n, cap, kv, d), rows(rng, dt, n, cap, kv, d)
+    for b, p in enumerate(s["lens"]):                          # rows that hold no token yet hold anything
+        if p < cap:
+            kc[b, max(p, 0):], vc[b, max(p, 0):] = float("nan"), float("inf")
+    K, V = host(kc), host(vc)
+    u, g = attn_errors(dt, q, torch.cat([kc.nan_to_num(0).flatten(0, 1), kn]), cap, 1 / math.sqrt(d))
+    want, bound = tokens.window_attn_step(host(q), host(kn), host(vn), K, V, s["lens"], s["left"], sinks, 1 / math.sqrt(d), u, g)
+    o = sp.sp_window_attn_step(q, kn, vn, kc, vc, torch.tensor(s["lens"], dtype=torch.int32, device="cuda"), s["left"], sinks)
+    assert np.array_equal(host(kc), K, equal_nan=True) and np.array_equal(host(vc), V, equal_nan=True)
+    within(o, want, bound, case)
+
+
+def test_steps_follow_the_prompt(sp):
+    """Prompt through the packed form, then token by token through the ring: the results of the whole sequence at once."""
+    dt, n, prompt, h, kv, d, left, sinks, cap = BF16, 90, 37, 4, 2, 64, 20, 3, 24
+    rng = np.random.default_rng(4)
+    q, k, v = rows(rng, dt, n, h, d), rows(rng, dt, n, kv, d), rows(rng, dt, n, kv, d)
+    u, g = attn_errors(dt, q, k, n, 1 / math.sqrt(d))
+    want, _, bound = tokens.window_attn_fwd(host(q), host(k), host(v), [0, n], [0, n], left, 0, sinks, 1 / math.sqrt(d), u, g)
+    kc, vc = torch.zeros((1, cap, kv, d), dtype=dt, device="cuda"), torch.zeros((1, cap, kv, d), dtype=dt, device="cuda")
+    for j in range(prompt):
+        at = tokens.step_slot(j, sinks, cap)
+        kc[0, at], vc[0, at] = k[j], v[j]
+    for t in range(prompt, n):
+        o = sp.sp_window_attn_step(q[t:t + 1], k[t:t + 1], v[t:t + 1], kc, vc, torch.tensor([t], dtype=torch.int32, device="cuda"), left, sinks)
+        within(o[0], want[t], bound[t], f"token {t}")
+
+
+# ---- distillation ----------------------------------------------------------------------------------------------
+DISTILL = [(1, 1, 1, 1.0), (5, 3, 2, 2.0), (700, 40, 5, 2.0), (33, 41, 41, 4.0), (9, 1000, 100, 1.0), (3, 4097, 256, 0.5), (4, 32000, 32, 1.0),
+           (2, 65536, 64, 3.0), (2, 65544, 7, 1.0), (2, 131072, 64, 1.0), (1, 140000, 10, 1.0), (3, 16001, 16, 1.0), (2, 20003, 33, 2.0),
+           (20, 128, 128, 1.0), (50, 30, 256, 1.0), (5, 2050, 20, 1.0), (1030, 64, 3, 1.0)]
+
+
+@pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("n,m,k,temp", DISTILL)
+def test_distillation(sp, n, m, k, temp, dt):
+    rng = np.random.default_rng(n + m + k)
+    z, top = rows(rng, dt, n, m, scale=2.0), rows(rng, F32, n, k, scale=2.0, shift=1.0)
+    index = np.stack([rng.permutation(m)[:k] if k <= m else rng.integers(0, m, k) for _ in range(n)]).astype(np.int32)
+    index[rng.random((n, k)) < 0.1] = -1
+    if n > 2:
+        index[1], index[2, -1] = m + 3, index[2, 0]            # a row without entries; one column twice
+        top[0, 0] = float("-inf")
+    weight = torch.from_numpy(rng.random(n).astype(np.float32)).cuda() if n % 2 else None
+    loss, dz = sp.sp_distill(z, top, torch.from_numpy(index).cuda(), temp, weight)
+    W = None if weight is None else host(weight)
+    want, DZ = tokens.distill(host(z), host(top), index, temp, W)
+    u = half_step(dt) if dt == BF16 else U32
+    Z = host(z)
+    # exponents of size |z - max| / T and sums of m (pairwise: 16 pieces of 8 in a lane, then a tree): relative error of p and a
+    rel = (4 * np.ptp(Z, axis=1) / temp + 4 * float(np.ptp(host(top)[np.isfinite(host(top))])) / temp + 160 + k) * U32
+    w = (np.full(n, 1 / n) if W is None else W) * temp
+    s = Z / temp
+    p = np.exp(s - s.max(1, keepdims=True))
+    p /= p.sum(1, keepdims=True)
+    share = np.abs(DZ / np.where(w > 0, w, 1)[:, None] - p) + p
+    within(dz, DZ, (rel * w)[:, None] * share + u * np.abs(DZ), "dz")
+    # every term a (log a - z/T + lse), a sums to 1
+    size = np.abs(s).max(1) + np.log(m) + np.abs(host(top)[np.isfinite(host(top))]).max() / temp + np.log(k) + 1
+    within(loss, [want], (w * temp * (rel + 6 * U32) * size).sum() + U32 * abs(want), "loss")
+    alone, none = sp.sp_distill(z, top, torch.from_numpy(index).cuda(), temp, weight, want_grad=False)
+    assert none is None and torch.equal(alone, loss)
+
+
+def test_distillation_edges(sp):
+    z = torch.randn((5, 40), device="cuda")
+    top, index = torch.zeros((5, 2), device="cuda"), torch.tensor([[1, 2]] * 5, dtype=torch.int32, device="cuda")
+    z[0, 7] = float("-inf")                                    # a masked class
+    z[1, 2] = float("-inf")                                    # a masked class that the teacher wants
+    z[2] = float("nan")
+    z[3] = -3.4e38                                             # all classes at the type's lowest value
+    top[4] = float("-inf")
+    loss, dz = sp.sp_distill(z, top, index)
+    assert not torch.isfinite(loss).any()
+    assert float(dz[0, 7]) == 0 and float(dz[1, 2]) == pytest.approx(-0.5 / 5, rel=1e-6) and torch.isnan(dz[2]).all() and not dz[4].any()
+    assert float(dz[3, 0]) == pytest.approx(1 / 40 / 5, rel=1e-6) and float(dz[3, 1]) == pytest.approx((1 / 40 - 0.5) / 5, rel=1e-6)
+    loss, dz = sp.sp_distill(z[:0], top[:0], index[:0])
+    assert float(loss) == 0 and dz.shape == (0, 40)
+    with pytest.raises(sp.SpError):
+        sp.sp_distill(z, top, index, temperature=0.0)
+    with pytest.raises(ValueError):
+        sp.sp_distill(z, top, index[:4])
+
+
+# ---- streams, graphs, repeatability ----------------------------------------------------------------------------
+def token_step(sp, s):
+    y, mean, rstd = sp.sp_layer_norm_fwd(s["x"], s["gamma"], s["beta"])
+    w = y.view(-1, 6, 32)
+    o, lse = sp.sp_window_attn_fwd(w[:, :4], w[:, 4:5], w[:, 5:], s["starts"], s["starts"], left=30, right=3, sinks=2)
+    loss, dz = sp.sp_distill(o.view(-1, 128), s["top"], s["index"], 2.0)
+    dw = torch.empty_like(y).view(-1, 6, 32)
+    sp.sp_window_attn_bwd(w[:, :4], w[:, 4:5], w[:, 5:], o, dz.view(-1, 4, 32), lse, s["starts"], s["starts"], left=30, right=3, sinks=2,
+                          out=(dw[:, :4], dw[:, 4:5], dw[:, 5:]))
+    dx, dgamma, dbeta = sp.sp_layer_norm_bwd(s["x"], dw.view(-1, 192), s["gamma"], mean, rstd)
+    return [loss, dx, dgamma, dbeta, o, lse]
+
+
+def token_state(seed, dt):
+    rng = np.random.default_rng(seed)
+    n = 611
+    return {"x": rows(rng, dt, n, 192), "gamma": rows(rng, F32, 192, scale=0.1, shift=1), "beta": rows(rng, F32, 192, scale=0.1),
+            "starts": torch.tensor([0, 100, 400, n], dtype=torch.int32, device="cuda"), "top": rows(rng, F32, n, 6),
+            "index": torch.from_numpy(rng.integers(-1, 128, (n, 6)).astype(np.int32)).cuda()}
+
+
+@pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
+def test_results_repeat_and_streams_do_not_matter(sp, dt):
+    s = token_state(1, dt)
+    want = token_step(sp, s)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        with torch.cuda.stream(side):
+            got = token_step(sp, s)
+        again = token_step(sp, s)
+        torch.cuda.synchronize()
+        for a, b, c in zip(want, got, again):
+            assert torch.equal(a, b) and torch.equal(a, c)
+
+
+@pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
+def test_captured_steps_replay(sp, dt):
+    s = token_state(2, dt)
+    token_step(sp, s)                                          # the library's pool holds the workspaces then
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        token_step(sp, s)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        out = token_step(sp, s)
+    for seed in (3, 4, 5):
+        fresh = token_state(seed, dt)
+        for name, t in fresh.items():
+            s[name].copy_(t)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(out, token_step(sp, fresh)):
+            assert torch.equal(a, b)
+        torch.cuda.synchronize()
