@@ -49,18 +49,23 @@ __device__ __forceinline__ int cloud_begin(const int32_t* starts, int clouds, in
     if (c > clouds + 1) return n;
     return min(max(starts[c - 1], 0), n);
 }
-// The last cloud with begin / T + number <= t.  Rows cut cloud by cloud into tiles of T: cloud c has the tile numbers from
-// begin(c) / T + c on, which are at least as many as its tiles.  T = 1 leaves the number out: the cloud of row t.
-template <int T>
-__device__ __forceinline__ int cloud_of(const int32_t* starts, int clouds, int n, int t) {
+// Rows cut cloud by cloud into tiles of `tile`, each row of the array standing for `per` rows of the cut: cloud c has the tile
+// numbers from begin(c) * per / tile + c on, which are at least as many as its tiles.
+__device__ __forceinline__ int64_t first_tile(const int32_t* starts, int clouds, int n, int c, int per, int tile) {
+    return (int64_t)cloud_begin(starts, clouds, n, c) * per / tile + c;
+}
+// The last cloud whose first tile is <= t: a wavefront looks at 64 clouds at a time.  All lanes must come here together.
+__device__ __forceinline__ int cloud_of_tile(const int32_t* starts, int clouds, int n, int64_t t, int per, int tile) {
     int lo = 0, hi = clouds + 1;
     while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (cloud_begin(starts, clouds, n, mid) / T + (T > 1 ? mid : 0) <= t) lo = mid;
-        else hi = mid - 1;
+        const int step = (hi - lo + 63) / 64, c = lo + ((int)(threadIdx.x & 63) + 1) * step;
+        const bool behind = c <= hi && first_tile(starts, clouds, n, c, per, tile) <= t;
+        lo += step * __popcll(__ballot(behind));
+        hi = min(hi, lo + step - 1);
     }
-    return lo;
+    return __builtin_amdgcn_readfirstlane(lo);
 }
+inline int64_t tile_numbers(int64_t n, int clouds, int per, int tile) { return n * per / tile + clouds + 2; }
 
 struct Cloud {
     int q0, a, k0, b;  // first query row, queries, first key row, keys

@@ -1,76 +1,635 @@
 // Attention with a sliding window and a few first rows that stay visible, over packed clouds: forward pass and gradients.
 #include <algorithm>
 
-#include "sp_attn.h"
+#include "sp_attn_tile.h"
 
 namespace sp {
 namespace {
 
 constexpr int kThreads = 256;
 
+// ---- forward -------------------------------------------------------------------------------------------------------
+// A workgroup has 128 rows of one key head: a row is a query and one of the `group` query heads that share the key head, so that keys
+// and values in LDS serve all of them and a tile of few queries sees few keys.  A wavefront has 32 of these rows, and goes over the
+// keys that any row of the workgroup sees, 64 (bf16) or 32 (fp32) at a time.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void attn_fwd_rows_kernel(AttnFwd<T> f) {
-    const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int64_t row = at / f.w.heads;
-    if (row >= f.w.n_q) return;
-    const Cloud c(f.w, cloud_of<1>(f.w.q_starts, f.w.clouds, f.w.n_q, (int)row));
-    forward_row(f, c, (int)row - c.q0, (int)(at % f.w.heads));
+constexpr int kKeys = sizeof(T) == 2 ? 64 : 32;
+constexpr int kRows = 128;  // a workgroup's
+constexpr int kWaveRows = 32;
+
+// What a workgroup's rows see: the slots of its tiles are the first keys, then a stretch.
+struct Reach {
+    int first, lo, n;
+    __device__ __forceinline__ Reach(const Window& w, const Cloud& c, int p_min, int p_max) {
+        const int hi = c.partners ? min(max(p_max + w.right + 1, 0), c.b) : 0;
+        lo = min(max(p_min - w.left, 0), hi);
+        first = min(w.sinks, lo);
+        n = first + hi - lo;
+    }
+    __device__ __forceinline__ int key(int slot) const { return slot + (slot < first ? 0 : lo - first); }
+    // whether rows at positions p_min .. p_max see all (none) of the `count` keys from `slot` on
+    __device__ __forceinline__ bool all(const Window& w, int slot, int count, int p_min, int p_max) const {
+        const int k = key(slot);
+        return slot >= first && slot + count <= n && k >= p_max - w.left && k + count - 1 <= p_min + w.right;
+    }
+    __device__ __forceinline__ bool none(const Window& w, int slot, int count, int p_min, int p_max) const {
+        const int k = key(slot);
+        return slot >= n || (k >= w.sinks && (k > p_max + w.right || k + count - 1 < p_min - w.left));
+    }
+};
+__device__ __forceinline__ bool sees(const Window& w, int p, int key) {
+    return (key <= p + w.right) & ((key >= p - w.left) | (key < w.sinks));
+}
+constexpr int kNowhere = -(1 << 30);  // the position of a row that is none: sees nothing
+
+__device__ __forceinline__ float exponent_scale(const Window& w) {
+    // exp2 of score * this; not quite zero for a scale of zero, so that a hidden key's -infinity stays one.  The scale's sign is the
+    // operand's: rows are negated when they are loaded.
+    return fmaxf(fabsf(w.scale) * kLog2e, 1e-30f);
 }
 
-// delta = dout . o of every query and head: a wavefront a row and head
+// A workgroup's tile of rows
+struct RowTile {
+    int kh, cloud;
+    int64_t r0;
+    __device__ __forceinline__ RowTile(const Window& w, int tiles) {
+        const int64_t item = item_of_block(blockIdx.x, gridDim.x), t = item % tiles;
+        kh = (int)(item / tiles);
+        cloud = cloud_of_tile(w.q_starts, w.clouds, w.n_q, t, w.group, kRows);
+        r0 = (t - first_tile(w.q_starts, w.clouds, w.n_q, cloud, w.group, kRows)) * kRows;
+    }
+};
+
+// A lane's row of a workgroup's tile, its wavefront's positions and what the workgroup sees
+struct WaveRows {
+    Reach reach;
+    int64_t w0;        // the wavefront's first row
+    bool there, whole; // this lane's row exists; all of the wavefront's do
+    int query, head, p;
+    int p_min, p_max;  // of the wavefront; one that has no row sees nothing
+    __device__ __forceinline__ WaveRows(const Window& w, const Cloud& c, int64_t r0, int64_t rows)
+        : reach(w, c, (int)(r0 / w.group) + c.off, (int)((min(r0 + kRows, rows) - 1) / w.group) + c.off) {
+        w0 = r0 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * kWaveRows;
+        const int64_t row = w0 + (threadIdx.x & 31);
+        there = row < rows;
+        whole = w0 + kWaveRows <= rows;
+        query = (int)(row / w.group);
+        head = (int)(row % w.group);
+        p = there ? query + c.off : kNowhere;
+        p_min = w0 < rows ? (int)(w0 / w.group) + c.off : kNowhere;
+        p_max = w0 < rows ? (int)((min(w0 + kWaveRows, rows) - 1) / w.group) + c.off : kNowhere;
+    }
+};
+
+template <typename T, int NT, bool VEC>
+__global__ __launch_bounds__(kThreads, 2) void attn_fwd_kernel(AttnFwd<T> f, int tiles) {
+    using Tl = Tile<T, NT>;
+    constexpr int kN = kKeys<T>, kB = kN / 32, kTileBytes = kN * Tl::kRowBytes;
+    __shared__ __attribute__((aligned(1024))) char lds[4 * kTileBytes];  // keys and values, two of each
+    __shared__ int marks[kN];
+    const Window& w = f.w;
+    const RowTile rt(w, tiles);
+    const Cloud c(w, rt.cloud);
+    const int64_t rows = (int64_t)c.a * w.group;
+    if (rt.r0 >= rows) return;
+    const WaveRows wr(w, c, rt.r0, rows);
+    const Reach& reach = wr.reach;
+    const int lane = threadIdx.x & 63, kh = rt.kh, h = kh * w.group + wr.head;
+    if (reach.n < 2 * kN || w.dim % 32) clear_lds<kThreads>(lds, 4 * kTileBytes);
+    const auto pl = Tl::place();
+    typename Tl::Frag q[Tl::kSteps];
+    Tl::template load_row<VEC>(q, f.q.at(c.q0 + wr.query, h, w.dim), w.dim, wr.there, w.scale < 0.f);
+    const float c2 = exponent_scale(w);
+    auto load = [&](int slot, int buf) {
+        load_tile<T, NT, VEC, kThreads>(lds + buf * 2 * kTileBytes, kN, w.dim,
+                                        [&](int r) { return slot + r < reach.n ? f.k.at(c.k0 + reach.key(slot + r), kh, w.dim) : nullptr; });
+        load_tile<T, NT, VEC, kThreads>(lds + (buf * 2 + 1) * kTileBytes, kN, w.dim,
+                                        [&](int r) { return slot + r < reach.n ? f.v.at(c.k0 + reach.key(slot + r), kh, w.dim) : nullptr; });
+    };
+
+    f32x16 acc[NT];
+    float m, l;                 // the row's largest score so far; this lane's half of the sum of exponentials
+    bool finite, again = false; // again: sums that were not finite, a second time without what rows do not see
+    bool met = false;           // ... and whether this row sees something that is not finite
+    const bool none = reach.n == 0 || wr.p + w.right < 0;  // the row sees nothing (else the last of its keys is seen at least)
+    for (;; again = true) {
+#pragma unroll
+        for (int d = 0; d < NT; ++d) acc[d] = f32x16{};
+        m = -INFINITY;
+        l = 0.f;
+        if (reach.n > 0) load(0, 0);
+        for (int slot = 0, buf = 0; slot < reach.n; slot += kN, buf ^= 1) {
+            char *keys = lds + buf * 2 * kTileBytes, *values = keys + kTileBytes;
+            wait_tiles();
+            if (slot + kN < reach.n) load(slot + kN, buf ^ 1);
+            if (again) clean_tiles<T, NT, kN, kThreads>(keys, values, marks);
+            if (reach.none(w, slot, kN, wr.p_min, wr.p_max)) continue;
+            f32x16 s[kB] = {};
+#pragma unroll
+            for (int st = 0; st < Tl::kSteps; ++st)
+#pragma unroll
+                for (int b = 0; b < kB; ++b) s[b] = Tl::mma(Tl::direct(keys, pl, b, st), q[st], s[b]);
+            if (again || !wr.whole || !reach.all(w, slot, kN, wr.p_min, wr.p_max)) {
+#pragma unroll
+                for (int b = 0; b < kB; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int r = b * 32 + 8 * (i / 4) + 4 * (lane >> 5) + i % 4;
+                        const bool seen = (slot + r < reach.n) & sees(w, wr.p, reach.key(slot + r));
+                        s[b][i] = seen ? s[b][i] : -INFINITY;
+                        if (again) met |= seen & (marks[r] != 0);
+                    }
+            }
+            float top = m;
+#pragma unroll
+            for (int b = 0; b < kB; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
+            top = halves<Max>(top);
+            if (__any(top > m)) {
+                const float old = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - top) * c2);
+                l *= old;
+#pragma unroll
+                for (int d = 0; d < NT; ++d) acc[d] *= old;
+                m = top;
+            }
+            const float m2 = m == -INFINITY ? 0.f : m * c2;
+            // one operation less than the difference first; m2's rounding, which stands in the exponents and in lse, is below 2^-17 then
+            if (__all(fabsf(m2) < 64.f)) {
+#pragma unroll
+                for (int b = 0; b < kB; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], c2, -m2));
+            } else {
+                const float top0 = m == -INFINITY ? 0.f : m;
+#pragma unroll
+                for (int b = 0; b < kB; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[b][i] = __builtin_amdgcn_exp2f((s[b][i] - top0) * c2);
+            }
+#pragma unroll
+            for (int b = 0; b < kB; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) l += s[b][i];
+#pragma unroll
+            for (int b = 0; b < kB; ++b)
+#pragma unroll
+                for (int st = 0; st < Tl::kTSteps; ++st) {
+                    const auto pr = Tl::operand(s[b], st);
+#pragma unroll
+                    for (int d = 0; d < NT; ++d) acc[d] = Tl::mma(Tl::turned(values, pl, b, st, d), pr, acc[d]);
+                }
+        }
+        l = halves<Add>(l);
+        const float inv = none ? 0.f : 1.f / l;
+        float check = 0.f;
+#pragma unroll
+        for (int d = 0; d < NT; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) check = fmaf(acc[d][i] *= inv, 0.f, check);
+        finite = halves<Add>(check) == 0.f;
+        if (again || !__syncthreads_or(wr.there && !finite)) break;
+    }
+    const uint64_t seen_by = __ballot(wr.there && met);
+    const uint32_t by_row = (uint32_t)seen_by | (uint32_t)(seen_by >> 32);  // rows that see what is not finite: key by key
+    if (wr.there && !(by_row >> (lane & 31) & 1)) {
+        put_column<T, NT, VEC>(f.o.at(c.q0 + wr.query, h, w.dim), acc, w.dim);
+        if (lane < 32)
+            f.lse[(int64_t)(c.q0 + wr.query) * w.heads + h] = none ? -INFINITY : (m * c2 + __builtin_amdgcn_logf(l)) * kLn2;
+    }
+    for (uint32_t bad = by_row; bad; bad &= bad - 1) {
+        const int64_t r = wr.w0 + __builtin_ctz(bad);
+        forward_row(f, c, (int)(r / w.group), kh * w.group + (int)(r % w.group));
+    }
+}
+
+// ---- gradients -----------------------------------------------------------------------------------------------------
+// Two kernels compute the scores again, each for what it can sum without atomics: dq by rows like the forward pass (and delta = dout . o
+// on the way), dk and dv by keys.  The second goes over the rows of all query heads that share the key head, so their sum needs no
+// second step.
+
+template <typename T, int NT, bool VEC>
+__global__ __launch_bounds__(kThreads, sizeof(T) * NT < 16 ? 2 : 1) void attn_dq_kernel(AttnBwd<T> g, int tiles) {
+    using Tl = Tile<T, NT>;
+    constexpr int kN = kKeys<T>, kB = kN / 32, kTileBytes = kN * Tl::kRowBytes;
+    __shared__ __attribute__((aligned(1024))) char lds[4 * kTileBytes];
+    __shared__ int marks[kN];
+    const Window& w = g.w;
+    const RowTile rt(w, tiles);
+    const Cloud c(w, rt.cloud);
+    const int64_t rows = (int64_t)c.a * w.group;
+    if (rt.r0 >= rows) return;
+    const WaveRows wr(w, c, rt.r0, rows);
+    const int lane = threadIdx.x & 63, kh = rt.kh, h = kh * w.group + wr.head;
+    if (wr.reach.n < 2 * kN || w.dim % 32) clear_lds<kThreads>(lds, 4 * kTileBytes);
+    const auto pl = Tl::place();
+    typename Tl::Frag q[Tl::kSteps], dout[Tl::kSteps];
+    Tl::template load_row<VEC>(q, g.q.at(c.q0 + wr.query, h, w.dim), w.dim, wr.there, w.scale < 0.f);
+    Tl::template load_row<VEC>(dout, g.dout.at(c.q0 + wr.query, h, w.dim), w.dim, wr.there, false);
+    float delta = 0.f;
+    {
+        typename Tl::Frag o[Tl::kSteps];
+        Tl::template load_row<VEC>(o, g.o.at(c.q0 + wr.query, h, w.dim), w.dim, wr.there, false);
+#pragma unroll
+        for (int st = 0; st < Tl::kSteps; ++st)
+#pragma unroll
+            for (int i = 0; i < Tl::kPer; ++i) delta = fmaf((float)o[st][i], (float)dout[st][i], delta);
+        delta = halves<Add>(delta);
+    }
+    const int64_t stat = (int64_t)(c.q0 + wr.query) * w.heads + h;
+    if (wr.there && lane < 32) g.delta[stat] = delta;
+    const float l2 = wr.there ? g.lse[stat] * kLog2e : 0.f, c2 = exponent_scale(w);
+    auto load = [&](int slot, int buf) {
+        load_tile<T, NT, VEC, kThreads>(lds + buf * 2 * kTileBytes, kN, w.dim, [&](int r) {
+            return slot + r < wr.reach.n ? g.k.at(c.k0 + wr.reach.key(slot + r), kh, w.dim) : nullptr;
+        });
+        load_tile<T, NT, VEC, kThreads>(lds + (buf * 2 + 1) * kTileBytes, kN, w.dim, [&](int r) {
+            return slot + r < wr.reach.n ? g.v.at(c.k0 + wr.reach.key(slot + r), kh, w.dim) : nullptr;
+        });
+    };
+    f32x16 acc[NT];
+    bool again = false, met = false;  // as in the forward pass
+    for (;; again = true) {
+#pragma unroll
+        for (int d = 0; d < NT; ++d) acc[d] = f32x16{};
+        if (wr.reach.n > 0) load(0, 0);
+        for (int slot = 0, buf = 0; slot < wr.reach.n; slot += kN, buf ^= 1) {
+            char *keys = lds + buf * 2 * kTileBytes, *values = keys + kTileBytes;
+            wait_tiles();
+            if (slot + kN < wr.reach.n) load(slot + kN, buf ^ 1);
+            if (again) clean_tiles<T, NT, kN, kThreads>(keys, values, marks);
+            if (wr.reach.none(w, slot, kN, wr.p_min, wr.p_max)) continue;
+            const bool all = !again && wr.whole && wr.reach.all(w, slot, kN, wr.p_min, wr.p_max);
+#pragma unroll
+            for (int b = 0; b < kB; ++b) {
+                f32x16 s = {}, dp = {};
+#pragma unroll
+                for (int st = 0; st < Tl::kSteps; ++st) {
+                    s = Tl::mma(Tl::direct(keys, pl, b, st), q[st], s);
+                    dp = Tl::mma(Tl::direct(values, pl, b, st), dout[st], dp);
+                }
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c2, -l2)) * (dp[i] - delta);
+                if (!all)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int r = b * 32 + 8 * (i / 4) + 4 * (lane >> 5) + i % 4;
+                        const bool seen = (slot + r < wr.reach.n) & sees(w, wr.p, wr.reach.key(slot + r));
+                        s[i] = seen ? s[i] : 0.f;
+                        if (again) met |= seen & (marks[r] != 0);
+                    }
+#pragma unroll
+                for (int st = 0; st < Tl::kTSteps; ++st) {
+                    const auto ds = Tl::operand(s, st);
+#pragma unroll
+                    for (int d = 0; d < NT; ++d) acc[d] = Tl::mma(Tl::turned(keys, pl, b, st, d), ds, acc[d]);
+                }
+            }
+        }
+        float check = 0.f;
+#pragma unroll
+        for (int d = 0; d < NT; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) check = fmaf(acc[d][i] *= w.scale, 0.f, check);
+        const bool finite = halves<Add>(check) == 0.f;
+        if (again || !__syncthreads_or(wr.there && !finite)) break;
+    }
+    const uint64_t seen_by = __ballot(wr.there && met);
+    const uint32_t by_row = (uint32_t)seen_by | (uint32_t)(seen_by >> 32);
+    if (wr.there && !(by_row >> (lane & 31) & 1)) put_column<T, NT, VEC>(g.dq.at(c.q0 + wr.query, h, w.dim), acc, w.dim);
+    __threadfence_block();  // delta, which other lanes read
+    for (uint32_t bad = by_row; bad; bad &= bad - 1) {
+        const int64_t r = wr.w0 + __builtin_ctz(bad);
+        query_gradient_row(g, c, (int)(r / w.group), kh * w.group + (int)(r % w.group));
+    }
+}
+
+// The first keys of a cloud are seen by all later queries: a tile with them would take many times the others' time.  With few of them
+// (at most kSplitSinks) the keys' kernel leaves their pairs beyond the window out and its sums in fp32 (`first`); attn_far_kernel adds
+// up those pairs, `chunk` rows to a wavefront (`far`), and attn_join_kernel adds both, the chunks in order.
+constexpr int kSplitSinks = 128;
+struct Split {
+    int sinks, chunk;  // 0: not split
+    float *first, *far;  // [cloud or chunk][kv_heads][sinks][dk, dv][dim]
+};
+__device__ __forceinline__ int64_t split_at(const Window& w, const Split& sp, int64_t part, int kh, int key) {
+    return (((part * w.kv_heads + kh) * sp.sinks + key) * 2) * w.dim;
+}
+// the first row that sees a key of the 32 from `key` on beyond its window
+__device__ __forceinline__ int64_t far_begin(const Window& w, const Cloud& c, int key) {
+    return (int64_t)max(w.left + key + 1 - c.off, 0) * w.group;
+}
+
+// Keys' gradients from 32 rows after another: what both kernels share
+template <typename T, int NT>
+struct KeyGrads {
+    using Tl = Tile<T, NT>;
+    typename Tl::Frag k[Tl::kSteps], v[Tl::kSteps];
+    f32x16 dk[NT], dv[NT];
+    // rows 32 b .. of the tiles q and dout; stats: the rows' lse * log2(e), delta and position
+    template <typename Hidden>
+    __device__ __forceinline__ void add(const char* q, const char* dout, const float* l2, const float* delta, const typename Tl::Place& pl,
+                                        int b, float c2, bool all, Hidden hidden) {
+        const int half = 4 * ((threadIdx.x & 63) >> 5);
+        f32x16 s = {}, dp = {};
+#pragma unroll
+        for (int st = 0; st < Tl::kSteps; ++st) {
+            s = Tl::mma(Tl::direct(q, pl, b, st), k[st], s);
+            dp = Tl::mma(Tl::direct(dout, pl, b, st), v[st], dp);
+        }
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const f32x4 l = *reinterpret_cast<const f32x4*>(l2 + b * 32 + 8 * g + half), de = *reinterpret_cast<const f32x4*>(delta + b * 32 + 8 * g + half);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float p = __builtin_amdgcn_exp2f(fmaf(s[4 * g + i], c2, -l[i])), ds = p * (dp[4 * g + i] - de[i]);
+                if (!all) {
+                    const bool away = hidden(b * 32 + 8 * g + half + i);
+                    p = away ? 0.f : p;
+                    ds = away ? 0.f : ds;
+                }
+                s[4 * g + i] = p;
+                dp[4 * g + i] = ds;
+            }
+        }
+#pragma unroll
+        for (int st = 0; st < Tl::kTSteps; ++st) {
+            const auto p = Tl::operand(s, st), ds = Tl::operand(dp, st);
+#pragma unroll
+            for (int d = 0; d < NT; ++d) {
+                dv[d] = Tl::mma(Tl::turned(dout, pl, b, st, d), p, dv[d]);
+                dk[d] = Tl::mma(Tl::turned(q, pl, b, st, d), ds, dk[d]);
+            }
+        }
+    }
+};
+
+// A row's statistics on their way from memory to LDS
+struct RowStat {
+    float l2, delta;
+    int p;
+};
 template <typename T>
-__global__ __launch_bounds__(kThreads) void attn_delta_kernel(AttnBwd<T> g) {
-    const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int64_t row = at / g.w.heads;
-    if (row >= g.w.n_q) return;
-    const int h = (int)(at % g.w.heads), lane = threadIdx.x & 63;
-    const T *o = g.o.at(row, h, g.w.dim), *d = g.dout.at(row, h, g.w.dim);
-    float s = 0.f;
-    for (int e = lane; e < g.w.dim; e += 64) s += elem(o[e]) * elem(d[e]);
-    s = wave_reduce<Add>(s);
-    if (lane == 0) g.delta[at] = s;
+__device__ __forceinline__ RowStat row_stat(const AttnBwd<T>& g, const Cloud& c, int kh, int64_t row, int64_t end) {
+    RowStat r{0.f, 0.f, kNowhere};
+    if (row < end) {
+        const int i = (int)(row / g.w.group);
+        const int64_t at = (int64_t)(c.q0 + i) * g.w.heads + kh * g.w.group + (int)(row % g.w.group);
+        r = {g.lse[at] * kLog2e, g.delta[at], i + c.off};
+    }
+    return r;
+}
+template <typename T>
+__device__ __forceinline__ const T* head_row(const Rows<const T>& t, const Window& w, const Cloud& c, int kh, int64_t row) {
+    return t.at(c.q0 + row / w.group, kh * w.group + (int)(row % w.group), w.dim);
+}
+
+template <typename T, int NT, bool VEC>
+__global__ __launch_bounds__(kThreads, 1) void attn_dkv_kernel(AttnBwd<T> g, Split split, int tiles) {
+    using Tl = Tile<T, NT>;
+    constexpr int kN = kKeys<T>, kB = kN / 32, kTileBytes = kN * Tl::kRowBytes;
+    __shared__ __attribute__((aligned(1024))) char lds[4 * kTileBytes];
+    __shared__ __attribute__((aligned(16))) float l2[2][kN], delta[2][kN];
+    __shared__ int pos[2][kN], marks[kN];
+    const Window& w = g.w;
+    const int64_t item = item_of_block(blockIdx.x, gridDim.x), t = item % tiles;
+    const int kh = (int)(item / tiles), cn = cloud_of_tile(w.k_starts, w.clouds, w.n_k, t, 1, kRows);
+    const Cloud c(w, cn);
+    const int64_t j0 = (t - first_tile(w.k_starts, w.clouds, w.n_k, cn, 1, kRows)) * kRows;
+    if (j0 >= c.b) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int jw = (int)j0 + wave * kWaveRows, j = jw + (lane & 31);
+    const bool there = j < c.b, split_here = split.sinks > 0;
+    const int sinks = split_here ? 0 : w.sinks;
+    // the rows that see a key of the workgroup's
+    const int a = c.partners ? c.a : 0;
+    const int64_t begin = (int64_t)min(max((int)j0 - w.right - c.off, 0), a) * w.group;
+    const int64_t end = j0 < sinks ? (int64_t)a * w.group : max(begin, (int64_t)min(max(min((int)j0 + kRows, c.b) + w.left - c.off, 0), a) * w.group);
+    if (end - begin < 2 * kN || w.dim % 32) clear_lds<kThreads>(lds, 4 * kTileBytes);
+    const auto pl = Tl::place();
+    KeyGrads<T, NT> kg{};
+    Tl::template load_row<VEC>(kg.k, g.k.at(c.k0 + j, kh, w.dim), w.dim, there, w.scale < 0.f);
+    Tl::template load_row<VEC>(kg.v, g.v.at(c.k0 + j, kh, w.dim), w.dim, there, false);
+    const float c2 = exponent_scale(w);
+    auto load = [&](int64_t row, int buf) {
+        load_tile<T, NT, VEC, kThreads>(lds + buf * 2 * kTileBytes, kN, w.dim,
+                                        [&](int r) { return row + r < end ? head_row(g.q, w, c, kh, row + r) : nullptr; });
+        load_tile<T, NT, VEC, kThreads>(lds + (buf * 2 + 1) * kTileBytes, kN, w.dim,
+                                        [&](int r) { return row + r < end ? head_row(g.dout, w, c, kh, row + r) : nullptr; });
+    };
+    auto put_stat = [&](const RowStat& r, int buf) {
+        if (threadIdx.x < kN) {
+            l2[buf][threadIdx.x] = r.l2;
+            delta[buf][threadIdx.x] = r.delta;
+            pos[buf][threadIdx.x] = r.p;
+        }
+    };
+    bool again = false, met = false;  // as in the forward pass: whether a row that sees this key is not finite
+    for (;; again = true) {
+#pragma unroll
+        for (int d = 0; d < NT; ++d) kg.dk[d] = kg.dv[d] = f32x16{};
+        if (begin < end) {
+            load(begin, 0);
+            put_stat(row_stat(g, c, kh, threadIdx.x < kN ? begin + threadIdx.x : end, end), 0);
+        }
+        int buf = 0;
+        for (int64_t row = begin; row < end; row += kN, buf ^= 1) {
+            char *q = lds + buf * 2 * kTileBytes, *dout = q + kTileBytes;
+            wait_tiles();
+            RowStat next{};
+            if (row + kN < end) {
+                load(row + kN, buf ^ 1);
+                next = row_stat(g, c, kh, threadIdx.x < kN ? row + kN + threadIdx.x : end, end);
+            }
+            if (again) clean_tiles<T, NT, kN, kThreads>(q, dout, marks);
+            const int p_min = (int)(row / w.group) + c.off, p_max = (int)((min(row + kN, end) - 1) / w.group) + c.off;
+            const bool none = jw >= c.b || jw > p_max + w.right || (jw + kWaveRows - 1 < p_min - w.left && jw >= sinks);
+            const bool all = !again && row + kN <= end && jw + kWaveRows - 1 <= p_min + w.right && jw >= p_max - w.left;
+            if (!none)
+#pragma unroll
+                for (int b = 0; b < kB; ++b)
+                    kg.add(q, dout, l2[buf], delta[buf], pl, b, c2, all, [&](int r) {
+                        const int p = pos[buf][r];
+                        const bool seen = (j <= p + w.right) & ((j >= p - w.left) | (j < sinks));
+                        if (again) met |= seen & (marks[r] != 0);
+                        return !seen;
+                    });
+            if (row + kN < end) put_stat(next, buf ^ 1);
+        }
+        float check = 0.f;
+#pragma unroll
+        for (int d = 0; d < NT; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) check = fmaf(kg.dk[d][i] *= w.scale, 0.f, fmaf(kg.dv[d][i], 0.f, check));
+        const bool finite = halves<Add>(check) == 0.f;
+        if (again || !__syncthreads_or(there && !finite)) break;
+    }
+    const bool part = split_here && j < split.sinks && c.partners;
+    const uint64_t seen_by = __ballot(there && !part && met);
+    const uint32_t by_row = (uint32_t)seen_by | (uint32_t)(seen_by >> 32);
+    if (there && part) {
+        float* to = split.first + split_at(w, split, cn - 1, kh, j);
+        // a value that is not finite sends attn_join_kernel over the rows one by one
+        if (met) kg.dk[0][0] = NAN;
+        put_column<float, NT, false>(to, kg.dk, w.dim);
+        put_column<float, NT, false>(to + w.dim, kg.dv, w.dim);
+    } else if (there && !(by_row >> (lane & 31) & 1)) {
+        put_column<T, NT, VEC>(g.dk.at(c.k0 + j, kh, w.dim), kg.dk, w.dim);
+        put_column<T, NT, VEC>(g.dv.at(c.k0 + j, kh, w.dim), kg.dv, w.dim);
+    }
+    for (uint32_t bad = by_row; bad; bad &= bad - 1) key_gradient_row(g, c, jw + __builtin_ctz(bad), kh);
+}
+
+template <typename T, int NT, bool VEC>
+__global__ __launch_bounds__(64, 1) void attn_far_kernel(AttnBwd<T> g, Split split, int tiles) {
+    using Tl = Tile<T, NT>;
+    constexpr int kTileBytes = 32 * Tl::kRowBytes;
+    __shared__ __attribute__((aligned(1024))) char lds[4 * kTileBytes];
+    __shared__ __attribute__((aligned(16))) float l2[2][32], delta[2][32];
+    __shared__ int pos[2][32];
+    const Window& w = g.w;
+    const int64_t item = item_of_block(blockIdx.x, gridDim.x), t = item % tiles;
+    const int groups = (split.sinks + 31) / 32, key0 = (int)(item / tiles) % groups * 32, kh = (int)(item / tiles) / groups;
+    const int cn = cloud_of_tile(w.q_starts, w.clouds, w.n_q, t, w.group, split.chunk);
+    const Cloud c(w, cn);
+    const int64_t r0 = (t - first_tile(w.q_starts, w.clouds, w.n_q, cn, w.group, split.chunk)) * split.chunk;
+    const int64_t begin = max(r0, far_begin(w, c, key0)), end = min(r0 + split.chunk, (int64_t)c.a * w.group);
+    if (!c.partners || begin >= end || key0 >= c.b) return;
+    const int lane = threadIdx.x, j = key0 + (lane & 31);
+    const bool there = j < min(split.sinks, c.b);
+    if (end - begin < 64 || w.dim % 32) clear_lds<64>(lds, 4 * kTileBytes);
+    const auto pl = Tl::place();
+    KeyGrads<T, NT> kg{};
+    Tl::template load_row<VEC>(kg.k, g.k.at(c.k0 + j, kh, w.dim), w.dim, there, w.scale < 0.f);
+    Tl::template load_row<VEC>(kg.v, g.v.at(c.k0 + j, kh, w.dim), w.dim, there, false);
+    const float c2 = exponent_scale(w);
+    auto load = [&](int64_t row, int buf) {
+        load_tile<T, NT, VEC, 64>(lds + buf * 2 * kTileBytes, 32, w.dim,
+                                  [&](int r) { return row + r < end ? head_row(g.q, w, c, kh, row + r) : nullptr; });
+        load_tile<T, NT, VEC, 64>(lds + (buf * 2 + 1) * kTileBytes, 32, w.dim,
+                                  [&](int r) { return row + r < end ? head_row(g.dout, w, c, kh, row + r) : nullptr; });
+    };
+    auto put_stat = [&](const RowStat& r, int buf) {
+        if (lane < 32) {
+            l2[buf][lane] = r.l2;
+            delta[buf][lane] = r.delta;
+            pos[buf][lane] = r.p;
+        }
+    };
+    load(begin, 0);
+    put_stat(row_stat(g, c, kh, lane < 32 ? begin + lane : end, end), 0);
+    int buf = 0;
+    for (int64_t row = begin; row < end; row += 32, buf ^= 1) {
+        wait_tiles();
+        RowStat next{};
+        if (row + 32 < end) {
+            load(row + 32, buf ^ 1);
+            next = row_stat(g, c, kh, lane < 32 ? row + 32 + lane : end, end);
+        }
+        const char* q = lds + buf * 2 * kTileBytes;
+        const bool all = row + 32 <= end && key0 + 31 < (int)(row / w.group) + c.off - w.left;
+        kg.add(q, q + kTileBytes, l2[buf], delta[buf], pl, 0, c2, all, [&](int r) { return j >= pos[buf][r] - w.left; });
+        if (row + 32 < end) put_stat(next, buf ^ 1);
+    }
+    if (there) {
+#pragma unroll
+        for (int d = 0; d < NT; ++d) kg.dk[d] *= w.scale;
+        float* to = split.far + split_at(w, split, t, kh, j);
+        put_column<float, NT, false>(to, kg.dk, w.dim);
+        put_column<float, NT, false>(to + w.dim, kg.dv, w.dim);
+    }
+}
+
+// a wavefront a cloud, key head and one of the first keys
+template <typename T>
+__global__ __launch_bounds__(64) void attn_join_kernel(AttnBwd<T> g, Split split) {
+    const Window& w = g.w;
+    const int cn = (int)blockIdx.x + 1, kh = blockIdx.y, j = blockIdx.z, lane = threadIdx.x;
+    const Cloud c(w, cn);
+    if (j >= c.b) return;
+    const int64_t t0 = first_tile(w.q_starts, w.clouds, w.n_q, cn, w.group, split.chunk), rows = (int64_t)c.a * w.group;
+    const int64_t far0 = far_begin(w, c, j / 32 * 32);
+    // chunks with a row behind far0 were written
+    const int64_t u0 = min(far0, rows) / split.chunk, u1 = far0 < rows ? (rows + split.chunk - 1) / split.chunk : u0;
+    float sum[2][2] = {}, check = 0.f;
+    for (int q = 0; q < 2; ++q)
+        for (int e = 0; e < 2; ++e)
+            if (lane + 64 * e < w.dim) {
+                const int at = q * w.dim + lane + 64 * e;
+                float s = split.first[split_at(w, split, cn - 1, kh, j) + at];
+#pragma unroll 8
+                for (int64_t u = u0; u < u1; ++u) s += split.far[split_at(w, split, t0 + u, kh, j) + at];
+                sum[q][e] = s;
+                check = fmaf(s, 0.f, check);
+            }
+    if (__any(check != 0.f)) {
+        key_gradient_row(g, c, j, kh);
+        return;
+    }
+    put_row(g.dk.at(c.k0 + j, kh, w.dim), sum[0], w.dim);
+    put_row(g.dv.at(c.k0 + j, kh, w.dim), sum[1], w.dim);
+}
+
+template <typename T, int NT, bool VEC>
+int forward_sized(const AttnFwd<T>& f, hipStream_t s) {
+    const int64_t tiles = tile_numbers(f.w.n_q, f.w.clouds, f.w.group, kRows);
+    if (tiles * f.w.kv_heads > INT32_MAX) return fail(SP_ERR_UNSUPPORTED, "more than 2^31 tiles of rows");
+    hipLaunchKernelGGL((attn_fwd_kernel<T, NT, VEC>), dim3((unsigned)(tiles * f.w.kv_heads)), dim3(kThreads), 0, s, f, (int)tiles);
+    SP_HIP(hipGetLastError());
+    return SP_OK;
 }
 
 template <typename T>
-__global__ __launch_bounds__(kThreads) void attn_dq_rows_kernel(AttnBwd<T> g) {
-    const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int64_t row = at / g.w.heads;
-    if (row >= g.w.n_q) return;
-    const Cloud c(g.w, cloud_of<1>(g.w.q_starts, g.w.clouds, g.w.n_q, (int)row));
-    query_gradient_row(g, c, (int)row - c.q0, (int)(at % g.w.heads));
-}
-
-template <typename T>
-__global__ __launch_bounds__(kThreads) void attn_dkv_rows_kernel(AttnBwd<T> g) {
-    const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int64_t row = at / g.w.kv_heads;
-    if (row >= g.w.n_k) return;
-    const Cloud c(g.w, cloud_of<1>(g.w.k_starts, g.w.clouds, g.w.n_k, (int)row));
-    key_gradient_row(g, c, (int)row - c.k0, (int)(at % g.w.kv_heads));
-}
-
-unsigned row_blocks(int64_t rows, int heads) { return (unsigned)((rows * heads + 3) / 4); }
+bool in_pieces(const Rows<T>& r) { return r.ld * (int64_t)sizeof(T) % 16 == 0 && aligned16(r.p); }
 
 template <typename T>
 int forward(const AttnFwd<T>& f, hipStream_t s) {
     if (f.w.n_q == 0) return SP_OK;
-    hipLaunchKernelGGL(attn_fwd_rows_kernel<T>, dim3(row_blocks(f.w.n_q, f.w.heads)), dim3(kThreads), 0, s, f);
+    const bool vec = f.w.dim * sizeof(T) % 16 == 0 && in_pieces(f.q) && in_pieces(f.k) && in_pieces(f.v) && in_pieces(f.o);
+    const int nt = (f.w.dim + 31) / 32;
+    if (vec) return nt == 1 ? forward_sized<T, 1, true>(f, s) : nt == 2 ? forward_sized<T, 2, true>(f, s) : nt == 3 ? forward_sized<T, 3, true>(f, s) : forward_sized<T, 4, true>(f, s);
+    return nt == 1 ? forward_sized<T, 1, false>(f, s) : nt == 2 ? forward_sized<T, 2, false>(f, s) : nt == 3 ? forward_sized<T, 3, false>(f, s) : forward_sized<T, 4, false>(f, s);
+}
+
+template <typename T, int NT, bool VEC>
+int backward_sized(AttnBwd<T> g, hipStream_t s) {
+    const Window& w = g.w;
+    const int64_t q_tiles = tile_numbers(w.n_q, w.clouds, w.group, kRows), k_tiles = tile_numbers(w.n_k, w.clouds, 1, kRows);
+    if (std::max(q_tiles, k_tiles) * w.kv_heads > INT32_MAX) return fail(SP_ERR_UNSUPPORTED, "more than 2^31 tiles of rows");
+    Buf delta = dev_alloc((size_t)w.n_q * w.heads * 4, s), parts;
+    if (!delta) return SP_ERR_ALLOC;
+    g.delta = ptr<float>(delta);
+    Split split{0, 1024, nullptr, nullptr};
+    const int groups = (w.sinks + 31) / 32;
+    int64_t chunks = 0;
+    if (w.sinks > 0 && w.sinks <= kSplitSinks && w.n_q > 0 && w.clouds > 0 && w.n_k - w.left > 2048) {
+        chunks = tile_numbers(w.n_q, w.clouds, w.group, split.chunk);
+        const size_t each = (size_t)w.kv_heads * w.sinks * 2 * w.dim;
+        parts = dev_alloc((chunks + w.clouds) * each * 4, s);
+        if (!parts) return SP_ERR_ALLOC;
+        split.sinks = w.sinks;
+        split.first = ptr<float>(parts);
+        split.far = split.first + w.clouds * each;
+    }
+    if (w.n_q > 0)
+        hipLaunchKernelGGL((attn_dq_kernel<T, NT, VEC>), dim3((unsigned)(q_tiles * w.kv_heads)), dim3(kThreads), 0, s, g, (int)q_tiles);
+    if (w.n_k > 0)
+        hipLaunchKernelGGL((attn_dkv_kernel<T, NT, VEC>), dim3((unsigned)(k_tiles * w.kv_heads)), dim3(kThreads), 0, s, g, split, (int)k_tiles);
+    if (split.sinks) {
+        hipLaunchKernelGGL((attn_far_kernel<T, NT, VEC>), dim3((unsigned)(chunks * w.kv_heads * groups)), dim3(64), 0, s, g, split, (int)chunks);
+        hipLaunchKernelGGL(attn_join_kernel<T>, dim3(w.clouds, w.kv_heads, split.sinks), dim3(64), 0, s, g, split);
+    }
     SP_HIP(hipGetLastError());
     return SP_OK;
 }
 
 template <typename T>
-int backward(AttnBwd<T> g, hipStream_t s) {
-    Buf delta = dev_alloc((size_t)g.w.n_q * g.w.heads * 4, s);
-    if (!delta) return SP_ERR_ALLOC;
-    g.delta = ptr<float>(delta);
-    if (g.w.n_q > 0) {
-        hipLaunchKernelGGL(attn_delta_kernel<T>, dim3(row_blocks(g.w.n_q, g.w.heads)), dim3(kThreads), 0, s, g);
-        hipLaunchKernelGGL(attn_dq_rows_kernel<T>, dim3(row_blocks(g.w.n_q, g.w.heads)), dim3(kThreads), 0, s, g);
-    }
-    if (g.w.n_k > 0) hipLaunchKernelGGL(attn_dkv_rows_kernel<T>, dim3(row_blocks(g.w.n_k, g.w.kv_heads)), dim3(kThreads), 0, s, g);
-    SP_HIP(hipGetLastError());
-    return SP_OK;
+int backward(const AttnBwd<T>& g, hipStream_t s) {
+    const bool vec = g.w.dim * sizeof(T) % 16 == 0 && in_pieces(g.q) && in_pieces(g.k) && in_pieces(g.v) && in_pieces(g.o) && in_pieces(g.dout) &&
+                     in_pieces(g.dq) && in_pieces(g.dk) && in_pieces(g.dv);
+    const int nt = (g.w.dim + 31) / 32;
+    if (vec) return nt == 1 ? backward_sized<T, 1, true>(g, s) : nt == 2 ? backward_sized<T, 2, true>(g, s) : nt == 3 ? backward_sized<T, 3, true>(g, s) : backward_sized<T, 4, true>(g, s);
+    return nt == 1 ? backward_sized<T, 1, false>(g, s) : nt == 2 ? backward_sized<T, 2, false>(g, s) : nt == 3 ? backward_sized<T, 3, false>(g, s) : backward_sized<T, 4, false>(g, s);
 }
 
 int check(const sp_window_attn* a, Window* w) {
@@ -81,8 +640,8 @@ int check(const sp_window_attn* a, Window* w) {
     if (a->dim < 1) return fail(SP_ERR_INVALID_ARG, "bad head width");
     if (a->left < 0 || a->right < 0 || a->sinks < 0) return fail(SP_ERR_INVALID_ARG, "left, right and sinks must not be negative");
     if (!(a->scale > -3.0e38f && a->scale < 3.0e38f)) return fail(SP_ERR_INVALID_ARG, "the scale must be finite");
-    if (a->dim > kMaxDim || a->heads > 65535 || a->n_q > 1 << 30 || a->n_k > 1 << 30)
-        return fail(SP_ERR_UNSUPPORTED, "head widths above %d, more than 65535 heads or more than 2^30 rows", kMaxDim);
+    if (a->dim > kMaxDim || a->heads > 65535 || a->n_q > 1 << 29 || a->n_k > 1 << 29)
+        return fail(SP_ERR_UNSUPPORTED, "head widths above %d, more than 65535 heads or more than 2^29 rows", kMaxDim);
     if (!a->d_q_starts || !a->d_k_starts) return fail(SP_ERR_INVALID_ARG, "the starts are NULL");
     w->q_starts = a->d_q_starts;
     w->k_starts = a->d_k_starts;

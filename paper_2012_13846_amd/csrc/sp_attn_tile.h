@@ -1,0 +1,229 @@
+// Tiles of rows in LDS and their products on the matrix cores, for the windowed attention's kernels.
+//
+// All products are 32 x 32 blocks (v_mfma_f32_32x32x16_bf16, v_mfma_f32_32x32x2_f32).  A block's accumulators hold, in lane l, column
+// l % 32 and rows 8 g + 4 (l / 32) + i (g, i < 4).  Scores are computed so that a lane holds 16 keys of one query (or 16 queries of one
+// key), and the second product contracts over just these: any order of the contraction is right as long as both operands have it, so a
+// lane's accumulators are, rounded, its second operand, and no value moves between lanes.
+//   rows of a tile as they lie ("direct", the first operand of scores): lane l reads 16 bytes of row l % 32, piece 2 s + l / 32 in step s;
+//   rows of a tile transposed (the first operand of the second product): element l % 32 of rows 8 g + 4 (l / 32) + i; bf16: a 64-bit
+//   transposing LDS read gives a lane 4 rows of its column.
+// A tile's row is C pieces of 16 bytes (a power of two); piece p of row r lies at p ^ swizzle(r), so that 16 rows' same piece, and four
+// consecutive rows' same 64 bytes, fall on different banks.
+#pragma once
+
+#include <type_traits>
+
+#include "sp_attn.h"
+
+namespace sp {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+#define SP_LDS __attribute__((address_space(3)))
+
+constexpr int pieces_of(int bytes) { return bytes <= 64 ? 4 : bytes <= 128 ? 8 : bytes <= 256 ? 16 : 32; }
+
+template <int C>
+__device__ __forceinline__ int swizzle(int row) {
+    if constexpr (C >= 16) return ((row & 3) << 2) | ((row >> 2) & 3);
+    else if constexpr (C == 8) return (((row >> 1) & 1) << 2) | ((row >> 2) & 3);
+    else return (row >> 2) & 3;
+}
+
+// NT: head width in 32s, rounded up.  What is beyond `dim` is zero in LDS and registers.
+template <typename T, int NT>
+struct Tile {
+    static constexpr bool kBf16 = sizeof(T) == 2;
+    static constexpr int kC = pieces_of(NT * 32 * (int)sizeof(T));  // pieces a row of LDS
+    static constexpr int kRowBytes = kC * 16;
+    static constexpr int kPer = 16 / (int)sizeof(T);                // elements a piece
+    static constexpr int kSteps = NT * 32 / (2 * kPer);             // pairs of pieces in a head
+    static constexpr int kTSteps = kBf16 ? 2 : 4;                   // steps of a contraction over 32 rows
+    using Raw = Piece<T, kPer>;
+    using Frag = typename std::conditional<kBf16, bf16x8, f32x4>::type;
+
+    static __device__ __forceinline__ f32x16 mma(const Frag& a, const Frag& b, f32x16 acc) {
+        if constexpr (kBf16) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, acc, 0, 0, 0);
+        else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a[i], b[i], acc, 0, 0, 0);
+            return acc;
+        }
+    }
+
+    // A lane's place in a tile: `direct` for step 0 of rows l % 32, `turned[j]` for element l % 32 and the rows of its half
+    struct Place {
+        int direct, turned[kBf16 ? 2 : 1];
+    };
+    static __device__ __forceinline__ Place place() {
+        const int l = threadIdx.x & 63, h = l >> 5;
+        Place p;
+        p.direct = (l & 31) * kRowBytes + ((h ^ swizzle<kC>(l & 31)) << 4);
+        if constexpr (kBf16) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int row = 8 * j + 4 * h + ((l & 15) >> 2), piece = ((l & 16) >> 3) + ((l & 3) >> 1);
+                p.turned[j] = row * kRowBytes + ((piece ^ swizzle<kC>(row)) << 4) + ((l & 1) << 3);
+            }
+        } else {
+            p.turned[0] = 4 * h * kRowBytes + ((((l & 31) >> 2) ^ swizzle<kC>(4 * h)) << 4) + ((l & 3) << 2);
+        }
+        return p;
+    }
+    // step s of rows 32 blk + l % 32
+    static __device__ __forceinline__ Frag direct(const char* tile, const Place& p, int blk, int s) {
+        return __builtin_bit_cast(Frag, *reinterpret_cast<const uint4*>(tile + (p.direct ^ (2 * s << 4)) + blk * 32 * kRowBytes));
+    }
+    // step s of the contraction over rows 32 blk .., element 32 dt + l % 32
+    static __device__ __forceinline__ Frag turned(const char* tile, const Place& p, int blk, int s, int dt) {
+        if constexpr (kBf16) {
+            const char* at = tile + (blk * 32 + 16 * s) * kRowBytes;
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((SP_LDS s16x4*)(at + (p.turned[0] ^ (dt << 6))));
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((SP_LDS s16x4*)(at + (p.turned[1] ^ (dt << 6))));
+            return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        } else {
+            f32x4 v;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                // swizzle(8 s + 4 h + i) without h's part, which `turned` holds
+                const int row = 8 * s + i, x = (dt << 3) ^ swizzle<kC>(row);
+                v[i] = *reinterpret_cast<const float*>(tile + (blk * 32 + row) * kRowBytes + (p.turned[0] ^ (x << 4)));
+            }
+            return v;
+        }
+    }
+    // accumulators of 32 rows as the second operand of step s of a contraction over them
+    static __device__ __forceinline__ Frag operand(const f32x16& v, int s) {
+        Frag r;
+#pragma unroll
+        for (int i = 0; i < (kBf16 ? 8 : 4); ++i) {
+            if constexpr (kBf16) r[i] = (__bf16)v[8 * s + i];
+            else r[i] = v[4 * s + i];
+        }
+        return r;
+    }
+    // a lane's pieces of one row in global memory, as operands: piece 2 s + l / 32 in step s
+    template <bool VEC>
+    static __device__ __forceinline__ void load_row(Frag (&f)[kSteps], const T* row, int dim, bool there, bool negate) {
+        const int h = (threadIdx.x & 63) >> 5;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            const int at = (2 * s + h) * kPer;
+            Frag v = {};
+            if constexpr (VEC) {
+                if (there && at < dim) v = __builtin_bit_cast(Frag, *reinterpret_cast<const uint4*>(row + at));
+            } else {
+                Piece<T, kPer> e{};
+                if (there)
+                    for (int i = 0; i < kPer; ++i)
+                        if (at + i < dim) e.e[i] = row[at + i];
+                v = __builtin_bit_cast(Frag, e);
+            }
+            if (negate)
+#pragma unroll
+                for (int i = 0; i < kPer; ++i) v[i] = -v[i];
+            f[s] = v;
+        }
+    }
+};
+
+// `rows` rows into LDS at `tile`: row r from where at(r) says (nullptr: it stays as it is).  16-byte pieces go past the registers (a
+// wavefront writes 1024 consecutive bytes an instruction) and are there after wait_tiles(); others are read element by element.
+template <typename T, int NT, bool VEC, int THREADS, typename At>
+__device__ __forceinline__ void load_tile(char* tile, int rows, int dim, At at) {
+    using Tl = Tile<T, NT>;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll
+    for (int base = 0; base < rows * Tl::kC; base += THREADS) {
+        const int p = base + threadIdx.x, row = p / Tl::kC, piece = (p % Tl::kC) ^ swizzle<Tl::kC>(row);
+        const T* from = piece * Tl::kPer < dim ? at(row) : nullptr;
+        if constexpr (VEC) {
+            if (from)
+                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t*)(from + piece * Tl::kPer),
+                                                 (SP_LDS uint32_t*)(tile + (base + wave * 64) * 16), 16, 0, 0);
+        } else if (from) {
+            Piece<T, Tl::kPer> e{};
+            for (int i = 0; i < Tl::kPer; ++i)
+                if (piece * Tl::kPer + i < dim) e.e[i] = from[piece * Tl::kPer + i];
+            *reinterpret_cast<uint4*>(tile + p * 16) = __builtin_bit_cast(uint4, e);
+        }
+    }
+}
+__device__ __forceinline__ void wait_tiles() {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+}
+template <int THREADS>
+__device__ __forceinline__ void clear_lds(char* p, int bytes) {
+    for (int i = threadIdx.x * 16; i < bytes; i += THREADS * 16) *reinterpret_cast<uint4*>(p + i) = uint4{0, 0, 0, 0};
+    __syncthreads();
+}
+
+// Infinities and not-a-numbers of a tile become zero, and their rows are marked: for the second run of a workgroup whose results are
+// not finite (0 * infinity), which takes what a row does not see out of its sums.
+template <typename T, int NT, int THREADS>
+__device__ __forceinline__ void clean_tile(char* tile, int rows, int* marks) {
+    using Tl = Tile<T, NT>;
+    for (int p = threadIdx.x; p < rows * Tl::kC; p += THREADS) {
+        auto e = __builtin_bit_cast(typename Tl::Raw, *reinterpret_cast<const uint4*>(tile + p * 16));
+        bool bad = false;
+#pragma unroll
+        for (int i = 0; i < Tl::kPer; ++i)
+            if (!(fabsf(elem(e.e[i])) < INFINITY)) {
+                bad = true;
+                e.e[i] = 0;
+            }
+        if (bad) {
+            *reinterpret_cast<uint4*>(tile + p * 16) = __builtin_bit_cast(uint4, e);
+            marks[p / Tl::kC] = 1;
+        }
+    }
+}
+template <typename T, int NT, int ROWS, int THREADS>
+__device__ __forceinline__ void clean_tiles(char* a, char* b, int* marks) {
+    if (threadIdx.x < ROWS) marks[threadIdx.x] = 0;
+    __syncthreads();
+    clean_tile<T, NT, THREADS>(a, ROWS, marks);
+    clean_tile<T, NT, THREADS>(b, ROWS, marks);
+    __syncthreads();
+}
+
+// the two halves of a wavefront combined, in both
+template <typename Op>
+__device__ __forceinline__ float halves(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return Op::of(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+// Accumulators whose column is a row of the result: elements 32 d + 8 g + 4 (l / 32) + i, four at a time
+template <typename T, int NT, bool VEC>
+__device__ __forceinline__ void put_column(T* row, const f32x16 (&acc)[NT], int dim) {
+    const int h = (threadIdx.x & 63) >> 5;
+#pragma unroll
+    for (int d = 0; d < NT; ++d)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int at = d * 32 + 8 * g + 4 * h;
+            if constexpr (VEC) {
+                struct alignas(4 * sizeof(T)) Four { T e[4]; } v;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v.e[i] = to_elem<T>(acc[d][4 * g + i]);
+                if (at < dim) *reinterpret_cast<Four*>(row + at) = v;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (at + i < dim) row[at + i] = to_elem<T>(acc[d][4 * g + i]);
+            }
+        }
+}
+
+// Workgroups go to the 8 XCDs by turns: neighbouring items, which read the same rows, to one XCD.
+__device__ __forceinline__ int64_t item_of_block(int64_t block, int64_t items) {
+    const int64_t each = items / 8, extra = items % 8, x = block % 8;
+    return x * each + (x < extra ? x : extra) + block / 8;
+}
+
+}  // namespace sp

@@ -129,6 +129,9 @@ ATTN = {
     "group5": ([150], [150], 10, 2, 96, 63, 1, 17),
     "many": ([3] * 50 + [65], [3] * 50 + [65], 2, 2, 16, 2, 2, 1),
     "long": ([1100], [1100], 1, 1, 64, 500, 0, 4),
+    "far_first_keys": ([2300, 40, 0, 700], [2300, 40, 0, 700], 4, 2, 32, 20, 0, 5),
+    "far_first_keys_odd": ([1500, 900], [1500, 900], 5, 1, 33, 3, 1, 70),
+    "far_first_keys_prompt": ([600, 50], [1900, 400], 2, 2, 128, 64, 0, 33),
     "negative_scale": ([60], [60], 2, 2, 32, 20, 0, 0),
 }
 
