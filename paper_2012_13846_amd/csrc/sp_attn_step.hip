@@ -1,5 +1,7 @@
 // One new token of each sequence: its key and value go to the ring cache, and it attends over the window and the first tokens.
-#include "sp_attn.h"
+#include <algorithm>
+
+#include "sp_attn_tile.h"
 
 namespace sp {
 namespace {
@@ -15,53 +17,199 @@ struct StepArgs {
     float scale;
 };
 
-// A wavefront a sequence and query head.  The new token's rows are read from k_new and v_new: another wavefront may be writing them
-// to the cache.
-template <typename T>
-__global__ __launch_bounds__(kThreads) void attn_step_rows_kernel(StepArgs<T> a) {
-    const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int lane = threadIdx.x & 63;
-    if (at >= (int64_t)a.batch * a.heads) return;
-    const int b = (int)(at / a.heads), h = (int)(at % a.heads), kh = h / a.group, p = a.lens[b], ring = a.cap - a.sinks;
+constexpr int kHeads = 32;  // query heads of a workgroup: the columns of a product
+constexpr int kKeys = 32;   // of a wavefront's tile
+
+// The keys a token at position p sees, in order: t-th of n; and the cache's row of a position
+struct StepSeen {
+    int p, first, lo, n, sinks, ring;
+    template <typename T>
+    __device__ __forceinline__ StepSeen(const StepArgs<T>& a, int b) : p(a.lens[b]), sinks(a.sinks), ring(a.cap - a.sinks) {
+        lo = max(max(p - a.left, p - ring + 1), 0);
+        first = min(sinks, lo);
+        n = p < 0 ? 0 : first + p + 1 - lo;
+    }
+    __device__ __forceinline__ int key(int t) const { return t + (t < first ? 0 : lo - first); }
+    __device__ __forceinline__ int row(int j) const { return j < sinks ? j : sinks + (j - sinks) % ring; }
+};
+
+// fp32 heads above 64 have room for one tile of keys and values a wavefront
+template <typename T, int NT>
+constexpr int kStepBufs = Tile<T, NT>::kRowBytes > 256 ? 1 : 2;
+
+// Reads a sequence's window once and does little else: bound by memory.  A workgroup has up to 32 query heads of one key head and a
+// part of the sequence's keys; its four wavefronts take tiles of 32 keys by turns, each through LDS of its own (two tiles of keys
+// and values, the next on its way while one is used), with no barrier until their sums are joined.  The new token's rows are read
+// from k_new and v_new: another workgroup may be writing them to the cache.
+template <typename T, int NT, bool VEC>
+__global__ __launch_bounds__(kThreads, 1) void attn_step_kernel(StepArgs<T> a, int parts, float* __restrict__ partial) {
+    using Tl = Tile<T, NT>;
+    constexpr int kTileBytes = kKeys * Tl::kRowBytes, kBufs = kStepBufs<T, NT>;
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int part = blockIdx.x, columns = (a.group + kHeads - 1) / kHeads, kh = blockIdx.y / columns, h0 = blockIdx.y % columns * kHeads, b = blockIdx.z;
+    const int here = min(kHeads, a.group - h0);
+    const StepSeen seen(a, b);
     const int64_t fresh = ((int64_t)b * a.kv_heads + kh) * a.dim, slot_step = (int64_t)a.kv_heads * a.dim;
     const int64_t cache = (int64_t)b * a.cap * slot_step + (int64_t)kh * a.dim;
-    auto slot = [&](int j) { return j < a.sinks ? j : a.sinks + (j - a.sinks) % ring; };
-    T* o = a.o + at * a.dim;
-    float m = -INFINITY, l = 0.f, acc[2] = {0.f, 0.f};
-    if (p >= 0) {
-        if (h % a.group == 0)
-            for (int e = lane; e < a.dim; e += 64) {
-                a.k_cache[cache + slot(p) * slot_step + e] = a.k_new[fresh + e];
-                a.v_cache[cache + slot(p) * slot_step + e] = a.v_new[fresh + e];
-            }
-        const int lo = max(max(p - a.left, p - ring + 1), 0), first = min(a.sinks, lo), n = first + p + 1 - lo;
-        auto row = [&](const T* all, const T* now, int t) {
-            const int j = t < first ? t : lo + t - first;
-            return j == p ? now + fresh : all + cache + slot(j) * slot_step;
-        };
-        const float c2 = a.scale * kLog2e;
-        for (int t0 = 0; t0 < n; t0 += 64) {
-            const bool in = t0 + lane < n;
-            const float s = in ? dot(a.q + at * a.dim, row(a.k_cache, a.k_new, t0 + lane), a.dim) * c2 : -INFINITY;
-            const float top = fmaxf(m, wave_reduce<Max>(s)), base = top == -INFINITY ? 0.f : top;
-            const float old = __builtin_amdgcn_exp2f(m - base), e = in ? __builtin_amdgcn_exp2f(s - base) : 0.f;
-            l = l * old + wave_reduce<Add>(e);
-            acc[0] *= old;
-            acc[1] *= old;
-            add_rows<T>(acc, e, min(64, n - t0), a.dim, [&](int t) { return row(a.v_cache, a.v_new, t0 + t); });
-            m = top;
+    if (part == 0 && h0 == 0 && seen.p >= 0)
+        for (int e = threadIdx.x; e < a.dim; e += kThreads) {
+            a.k_cache[cache + seen.row(seen.p) * slot_step + e] = a.k_new[fresh + e];
+            a.v_cache[cache + seen.row(seen.p) * slot_step + e] = a.v_new[fresh + e];
         }
-        acc[0] /= l;
-        acc[1] /= l;
+    const int each = ((seen.n + parts - 1) / parts + kKeys - 1) / kKeys * kKeys, begin = min(part * each, seen.n), end = min(begin + each, seen.n);
+    char* mine = lds + wave * 2 * kBufs * kTileBytes;
+    const auto pl = Tl::place();
+    typename Tl::Frag q[Tl::kSteps];
+    const int column = lane & 31;
+    Tl::template load_row<VEC>(q, a.q + ((int64_t)b * a.heads + kh * a.group + h0 + column) * a.dim, a.dim, column < here, a.scale < 0.f);
+    const float c2 = fmaxf(fabsf(a.scale) * kLog2e, 1e-30f);  // as in the packed form
+    auto clear = [&](char* p, int bytes) {
+        for (int i = lane * 16; i < bytes; i += 64 * 16) *reinterpret_cast<uint4*>(p + i) = uint4{0, 0, 0, 0};
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    };
+    if (a.dim % 32) clear(mine, 2 * kBufs * kTileBytes);
+    auto load = [&](int t, int buf) {
+        char* keys = mine + buf * 2 * kTileBytes;
+        if (t + kKeys > end) clear(keys, 2 * kTileBytes);
+        auto row = [&](const T* all, const T* now, int r) -> const T* {
+            if (t + r >= end) return nullptr;
+            const int j = seen.key(t + r);
+            return j == seen.p ? now + fresh : all + cache + seen.row(j) * slot_step;
+        };
+        load_tile<T, NT, VEC, 64>(keys, kKeys, a.dim, [&](int r) { return row(a.k_cache, a.k_new, r); });
+        load_tile<T, NT, VEC, 64>(keys + kTileBytes, kKeys, a.dim, [&](int r) { return row(a.v_cache, a.v_new, r); });
+    };
+    f32x16 acc[NT] = {};
+    float m = -INFINITY, l = 0.f;
+    int t = begin + wave * kKeys, buf = 0;
+    if (t < end) load(t, 0);
+    for (; t < end; t += 4 * kKeys, buf ^= kBufs - 1) {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        if (kBufs == 2 && t + 4 * kKeys < end) load(t + 4 * kKeys, buf ^ 1);
+        const char *keys = mine + buf * 2 * kTileBytes, *values = keys + kTileBytes;
+        f32x16 s = {};
+#pragma unroll
+        for (int st = 0; st < Tl::kSteps; ++st) s = Tl::mma(Tl::direct(keys, pl, 0, st), q[st], s);
+        if (t + kKeys > end)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = t + 8 * (i / 4) + 4 * (lane >> 5) + i % 4 < end ? s[i] : -INFINITY;
+        float top = m;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, s[i]);
+        top = halves<Max>(top);
+        const float base = top == -INFINITY ? 0.f : top, old = __builtin_amdgcn_exp2f((m - base) * c2);
+        l *= old;
+#pragma unroll
+        for (int d = 0; d < NT; ++d) acc[d] *= old;
+        m = top;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            s[i] = __builtin_amdgcn_exp2f((s[i] - base) * c2);
+            l += s[i];
+        }
+#pragma unroll
+        for (int st = 0; st < Tl::kTSteps; ++st) {
+            const auto pr = Tl::operand(s, st);
+#pragma unroll
+            for (int d = 0; d < NT; ++d) acc[d] = Tl::mma(Tl::turned(values, pl, 0, st, d), pr, acc[d]);
+        }
+        if (kBufs == 1 && t + 4 * kKeys < end) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            load(t + 4 * kKeys, 0);
+        }
     }
-    put_row(o, acc, a.dim);
+    l = halves<Add>(l);
+    // [wavefront][column][NT * 32 sums, maximum, sum of exponentials]
+    constexpr int kRow = NT * 32 + 2;
+    float* sums = reinterpret_cast<float*>(lds);
+    __syncthreads();
+    if (column < here) {
+        float* to = sums + (wave * kHeads + column) * kRow;
+        put_column<float, NT, false>(to, acc, NT * 32);
+        if (lane < 32) {
+            to[NT * 32] = m;
+            to[NT * 32 + 1] = l;
+        }
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < here * a.dim; i += kThreads) {
+        const int col = i / a.dim, e = i % a.dim;
+        const float* from = sums + col * kRow;
+        float top = -INFINITY, v = 0.f, total = 0.f;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) top = fmaxf(top, from[k * kHeads * kRow + NT * 32]);
+        const float base = top == -INFINITY ? 0.f : top;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float* f = from + k * kHeads * kRow;
+            const float x = __builtin_amdgcn_exp2f((f[NT * 32] - base) * c2);
+            v = fmaf(f[e], x, v);
+            total = fmaf(f[NT * 32 + 1], x, total);
+        }
+        const int64_t out = (int64_t)b * a.heads + kh * a.group + h0 + col;
+        if (parts == 1) {
+            a.o[out * a.dim + e] = to_elem<T>(seen.n > 0 ? v / total : 0.f);
+        } else {
+            float* to = partial + (out * parts + part) * (a.dim + 2);
+            to[e] = v;
+            if (e == 0) {
+                to[a.dim] = top;
+                to[a.dim + 1] = total;
+            }
+        }
+    }
+}
+
+// the parts of a sequence and head, in order
+template <typename T>
+__global__ __launch_bounds__(128) void attn_step_join_kernel(StepArgs<T> a, int parts, const float* __restrict__ partial) {
+    const int64_t out = (int64_t)blockIdx.y * a.heads + blockIdx.x;
+    const float *from = partial + out * parts * (a.dim + 2), c2 = fmaxf(fabsf(a.scale) * kLog2e, 1e-30f);
+    const int e = threadIdx.x, lane = e & 63;
+    float top = -INFINITY;
+    for (int k = lane; k < parts; k += 64) top = fmaxf(top, from[k * (a.dim + 2) + a.dim]);
+    top = wave_reduce<Max>(top);
+    if (e >= a.dim) return;
+    const float base = top == -INFINITY ? 0.f : top;
+    float v = 0.f, total = 0.f;
+#pragma unroll 8
+    for (int k = 0; k < parts; ++k) {
+        const float* f = from + k * (a.dim + 2);
+        const float x = __builtin_amdgcn_exp2f((f[a.dim] - base) * c2);
+        v = fmaf(f[e], x, v);
+        total = fmaf(f[a.dim + 1], x, total);
+    }
+    a.o[out * a.dim + e] = to_elem<T>(a.lens[blockIdx.y] >= 0 ? v / total : 0.f);
+}
+
+template <typename T, int NT, bool VEC>
+int step_sized(const StepArgs<T>& a, hipStream_t s) {
+    using Tl = Tile<T, NT>;
+    const int columns = (a.group + kHeads - 1) / kHeads;
+    const int64_t items = (int64_t)a.batch * a.kv_heads * columns, most = std::min<int64_t>(a.cap, (int64_t)a.left + 1 + a.sinks);
+    // enough workgroups to fill the chip several times, of at least one tile for each wavefront
+    const int parts = (int)std::max<int64_t>(1, std::min<int64_t>((1024 + items - 1) / items, (most + 4 * kKeys - 1) / (4 * kKeys)));
+    Buf partial;
+    if (parts > 1) {
+        partial = dev_alloc((size_t)a.batch * a.heads * parts * (a.dim + 2) * 4, s);
+        if (!partial) return SP_ERR_ALLOC;
+    }
+    auto kernel = attn_step_kernel<T, NT, VEC>;
+    const size_t lds = std::max<size_t>((size_t)8 * kStepBufs<T, NT> * kKeys * Tl::kRowBytes, (size_t)4 * kHeads * (NT * 32 + 2) * 4);
+    if (lds > 64 * 1024) SP_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+    hipLaunchKernelGGL(kernel, dim3(parts, a.kv_heads * columns, a.batch), dim3(kThreads), lds, s, a, parts, ptr<float>(partial));
+    if (parts > 1) hipLaunchKernelGGL(attn_step_join_kernel<T>, dim3(a.heads, a.batch), dim3(128), 0, s, a, parts, ptr<float>(partial));
+    SP_HIP(hipGetLastError());
+    return SP_OK;
 }
 
 template <typename T>
 int step(const StepArgs<T>& a, hipStream_t s) {
-    hipLaunchKernelGGL(attn_step_rows_kernel<T>, dim3((unsigned)(((int64_t)a.batch * a.heads + 3) / 4)), dim3(kThreads), 0, s, a);
-    SP_HIP(hipGetLastError());
-    return SP_OK;
+    const bool vec = a.dim * sizeof(T) % 16 == 0 && aligned16(a.q) && aligned16(a.k_new) && aligned16(a.v_new) && aligned16(a.k_cache) && aligned16(a.v_cache);
+    const int nt = (a.dim + 31) / 32;
+    if (vec) return nt == 1 ? step_sized<T, 1, true>(a, s) : nt == 2 ? step_sized<T, 2, true>(a, s) : nt == 3 ? step_sized<T, 3, true>(a, s) : step_sized<T, 4, true>(a, s);
+    return nt == 1 ? step_sized<T, 1, false>(a, s) : nt == 2 ? step_sized<T, 2, false>(a, s) : nt == 3 ? step_sized<T, 3, false>(a, s) : step_sized<T, 4, false>(a, s);
 }
 
 }  // namespace

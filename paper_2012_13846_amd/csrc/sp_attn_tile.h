@@ -132,13 +132,14 @@ struct Tile {
 
 // `rows` rows into LDS at `tile`: row r from where at(r) says (nullptr: it stays as it is).  16-byte pieces go past the registers (a
 // wavefront writes 1024 consecutive bytes an instruction) and are there after wait_tiles(); others are read element by element.
+// THREADS: of the workgroup, or 64 for a wavefront that loads a tile of its own.
 template <typename T, int NT, bool VEC, int THREADS, typename At>
 __device__ __forceinline__ void load_tile(char* tile, int rows, int dim, At at) {
     using Tl = Tile<T, NT>;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int thread = threadIdx.x % THREADS, wave = __builtin_amdgcn_readfirstlane(thread >> 6);
 #pragma unroll
     for (int base = 0; base < rows * Tl::kC; base += THREADS) {
-        const int p = base + threadIdx.x, row = p / Tl::kC, piece = (p % Tl::kC) ^ swizzle<Tl::kC>(row);
+        const int p = base + thread, row = p / Tl::kC, piece = (p % Tl::kC) ^ swizzle<Tl::kC>(row);
         const T* from = piece * Tl::kPer < dim ? at(row) : nullptr;
         if constexpr (VEC) {
             if (from)
