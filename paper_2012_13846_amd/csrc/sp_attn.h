@@ -97,13 +97,6 @@ struct Seen {
 __device__ __forceinline__ float lane_value(float v, int lane) {
     return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), lane));
 }
-template <typename Op>
-__device__ __forceinline__ float wave_reduce(float v) {
-#pragma unroll
-    for (int s = 32; s > 0; s >>= 1) v = Op::of(v, __shfl_xor(v, s));
-    return v;
-}
-
 // ---- one row by one wavefront: lanes are keys (or queries) for the scores and elements for the products with rows --------------
 // All lanes must come here together.
 
@@ -142,10 +135,10 @@ __device__ __forceinline__ void forward_row(const AttnFwd<T>& f, const Cloud& c,
     for (int t0 = 0; t0 < seen.n; t0 += 64) {
         const bool in = t0 + lane < seen.n;
         const float s = in ? dot(q, f.k.at(c.k0 + seen.key(t0 + lane), kh, w.dim), w.dim) * c2 : -INFINITY;
-        const float top = fmaxf(m, wave_reduce<Max>(s));
+        const float top = fmaxf(m, lanes_reduce<64, Max>(s));
         const float base = top == -INFINITY ? 0.f : top;
         const float old = __builtin_amdgcn_exp2f(m - base), p = in ? __builtin_amdgcn_exp2f(s - base) : 0.f;
-        l = l * old + wave_reduce<Add>(p);
+        l = l * old + lanes_reduce<64, Add>(p);
         acc[0] *= old;
         acc[1] *= old;
         add_rows<T>(acc, p, min(64, seen.n - t0), w.dim, [&](int t) { return f.v.at(c.k0 + seen.key(t0 + t), kh, w.dim); });

@@ -11,11 +11,12 @@ constexpr int kThreads = 256;
 // ---- forward -------------------------------------------------------------------------------------------------------
 // A workgroup has 128 rows of one key head: a row is a query and one of the `group` query heads that share the key head, so that keys
 // and values in LDS serve all of them and a tile of few queries sees few keys.  A wavefront has 32 of these rows, and goes over the
-// keys that any row of the workgroup sees, 64 (bf16) or 32 (fp32) at a time.
+// keys that any row of the workgroup sees, 64 (bf16) or 32 (fp32) at a time; the next keys are on their way to LDS meanwhile.
 template <typename T>
 constexpr int kKeys = sizeof(T) == 2 ? 64 : 32;
 constexpr int kRows = 128;  // a workgroup's
 constexpr int kWaveRows = 32;
+constexpr int kNowhere = -(1 << 30);  // the position of a row that is none: sees nothing
 
 // What a workgroup's rows see: the slots of its tiles are the first keys, then a stretch.
 struct Reach {
@@ -30,17 +31,35 @@ struct Reach {
     // whether rows at positions p_min .. p_max see all (none) of the `count` keys from `slot` on
     __device__ __forceinline__ bool all(const Window& w, int slot, int count, int p_min, int p_max) const {
         const int k = key(slot);
-        return slot >= first && slot + count <= n && k >= p_max - w.left && k + count - 1 <= p_min + w.right;
+        return (slot >= first) & (slot + count <= n) & (k >= p_max - w.left) & (k + count - 1 <= p_min + w.right);
     }
     __device__ __forceinline__ bool none(const Window& w, int slot, int count, int p_min, int p_max) const {
         const int k = key(slot);
-        return slot >= n || (k >= w.sinks && (k > p_max + w.right || k + count - 1 < p_min - w.left));
+        return (k >= w.sinks) & ((k > p_max + w.right) | (k + count - 1 < p_min - w.left));
     }
 };
-__device__ __forceinline__ bool sees(const Window& w, int p, int key) {
-    return (key <= p + w.right) & ((key >= p - w.left) | (key < w.sinks));
-}
-constexpr int kNowhere = -(1 << 30);  // the position of a row that is none: sees nothing
+
+// Whether a lane's row sees the keys of a tile, by the key's number in the tile
+struct SeenInTile {
+    const Window& w;
+    const Reach& reach;
+    int slot, p, low;
+    uint32_t width;
+    bool plain;  // keys one after another, none of the first: one range
+    __device__ __forceinline__ SeenInTile(const Window& w_, const Reach& reach_, int slot_, int p_) : w(w_), reach(reach_), slot(slot_), p(p_) {
+        const int k = reach.key(slot);
+        plain = (slot >= reach.first) & (k >= w.sinks);
+        low = p - w.left - k;
+        const int high = min(p + w.right - k, reach.n - slot - 1);
+        width = high >= low ? (uint32_t)(high - low) + 1 : 0;
+        low += 4 * ((int)(threadIdx.x & 63) >> 5) * -1;  // of the lane's half: element i of group g is key 8 g + i then
+    }
+    __device__ __forceinline__ bool operator()(int r) const { return (uint32_t)(r - low) < width; }
+    __device__ __forceinline__ bool slow(int r) const {
+        const int at = slot + r + 4 * ((int)(threadIdx.x & 63) >> 5), k = reach.key(at);
+        return (at < reach.n) & (k <= p + w.right) & ((k >= p - w.left) | (k < w.sinks));
+    }
+};
 
 __device__ __forceinline__ float exponent_scale(const Window& w) {
     // exp2 of score * this; not quite zero for a scale of zero, so that a hidden key's -infinity stays one.  The scale's sign is the
@@ -53,24 +72,25 @@ struct RowTile {
     int kh, cloud;
     int64_t r0;
     __device__ __forceinline__ RowTile(const Window& w, int tiles) {
-        const int64_t item = item_of_block(blockIdx.x, gridDim.x), t = item % tiles;
-        kh = (int)(item / tiles);
+        const uint32_t item = item_of_block(blockIdx.x, gridDim.x), t = item % (uint32_t)tiles;
+        kh = (int)(item / (uint32_t)tiles);
         cloud = cloud_of_tile(w.q_starts, w.clouds, w.n_q, t, w.group, kRows);
         r0 = (t - first_tile(w.q_starts, w.clouds, w.n_q, cloud, w.group, kRows)) * kRows;
     }
 };
 
-// A lane's row of a workgroup's tile, its wavefront's positions and what the workgroup sees
+// A lane's row of a workgroup's tile, its wavefront's positions and what the workgroup sees.  (Rows of a cloud are counted from its
+// first; a cloud has at most 2^31 of them.)
 struct WaveRows {
-    Reach reach;
-    int64_t w0;        // the wavefront's first row
+    uint32_t w0;       // the wavefront's first row
     bool there, whole; // this lane's row exists; all of the wavefront's do
     int query, head, p;
     int p_min, p_max;  // of the wavefront; one that has no row sees nothing
-    __device__ __forceinline__ WaveRows(const Window& w, const Cloud& c, int64_t r0, int64_t rows)
+    Reach reach;
+    __device__ __forceinline__ WaveRows(const Window& w, const Cloud& c, uint32_t r0, uint32_t rows)
         : reach(w, c, (int)(r0 / w.group) + c.off, (int)((min(r0 + kRows, rows) - 1) / w.group) + c.off) {
         w0 = r0 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * kWaveRows;
-        const int64_t row = w0 + (threadIdx.x & 31);
+        const uint32_t row = w0 + (threadIdx.x & 31);
         there = row < rows;
         whole = w0 + kWaveRows <= rows;
         query = (int)(row / w.group);
@@ -78,6 +98,45 @@ struct WaveRows {
         p = there ? query + c.off : kNowhere;
         p_min = w0 < rows ? (int)(w0 / w.group) + c.off : kNowhere;
         p_max = w0 < rows ? (int)((min(w0 + kWaveRows, rows) - 1) / w.group) + c.off : kNowhere;
+    }
+};
+
+// The keys and values of a workgroup's slots, kN at a time, into LDS
+template <typename T, int NT, bool VEC>
+struct KeyTiles {
+    static constexpr int kN = kKeys<T>, kTileBytes = kN * Tile<T, NT>::kRowBytes;
+    const Window& w;
+    const Reach& reach;
+    const T *k, *v;  // the cloud's first rows of this key head
+    uint32_t ldk, ldv;  // bytes between rows
+    int64_t ldk_elements, ldv_elements;
+    TileLoads<T, NT, kN, kThreads> lk, lv;
+    __device__ __forceinline__ KeyTiles(const Window& w_, const Reach& reach_, const Rows<const T>& k_, const Rows<const T>& v_, const Cloud& c, int kh)
+        : w(w_), reach(reach_), k(k_.at(c.k0, kh, w_.dim)), v(v_.at(c.k0, kh, w_.dim)), ldk((uint32_t)(k_.ld * sizeof(T))),
+          ldv((uint32_t)(v_.ld * sizeof(T))), ldk_elements(k_.ld), ldv_elements(v_.ld) {
+        if constexpr (VEC) {
+            lk.place(w.dim, [&](int r) { return r * ldk; });
+            lv.place(w.dim, [&](int r) { return r * ldv; });
+        }
+    }
+    __device__ __forceinline__ void one(char* tile, const TileLoads<T, NT, kN, kThreads>& l, const T* p, uint32_t ld, int64_t ld_elements, int slot) const {
+        const uint32_t row = w.dim * (uint32_t)sizeof(T);
+        if constexpr (VEC) {
+            const uint32_t at = lds_address(tile);
+            if (slot >= reach.first) {
+                l.load(at, memory_of(p + reach.key(slot) * ld_elements, (min(kN, reach.n - slot) - 1) * ld + row));
+            } else {
+                const int split = min(kN, reach.first - slot), rest = min(kN, reach.n - slot) - split;
+                l.load_two(at, memory_of(p + slot * ld_elements, (split - 1) * ld + row), split,
+                           memory_of(p + reach.lo * ld_elements, rest > 0 ? (rest - 1) * ld + row : 0), split * ld);
+            }
+        } else {
+            load_elements<T, NT, kN, kThreads>(tile, w.dim, [&](int r) { return slot + r < reach.n ? p + reach.key(slot + r) * ld_elements : nullptr; });
+        }
+    }
+    __device__ __forceinline__ void load(char* lds, int slot, int buf) const {
+        one(lds + buf * 2 * kTileBytes, lk, k, ldk, ldk_elements, slot);
+        one(lds + (buf * 2 + 1) * kTileBytes, lv, v, ldv, ldv_elements, slot);
     }
 };
 
@@ -92,53 +151,55 @@ __global__ __launch_bounds__(kThreads, 2) void attn_fwd_kernel(AttnFwd<T> f, int
     const Cloud c(w, rt.cloud);
     const int64_t rows = (int64_t)c.a * w.group;
     if (rt.r0 >= rows) return;
-    const WaveRows wr(w, c, rt.r0, rows);
+    const WaveRows wr(w, c, (uint32_t)rt.r0, (uint32_t)rows);
     const Reach& reach = wr.reach;
     const int lane = threadIdx.x & 63, kh = rt.kh, h = kh * w.group + wr.head;
-    if (reach.n < 2 * kN || w.dim % 32) clear_lds<kThreads>(lds, 4 * kTileBytes);
     const auto pl = Tl::place();
+    const KeyTiles<T, NT, VEC> kt(w, reach, f.k, f.v, c, kh);
+    if (reach.n > 0) kt.load(lds, 0, 0);
     typename Tl::Frag q[Tl::kSteps];
     Tl::template load_row<VEC>(q, f.q.at(c.q0 + wr.query, h, w.dim), w.dim, wr.there, w.scale < 0.f);
     const float c2 = exponent_scale(w);
-    auto load = [&](int slot, int buf) {
-        load_tile<T, NT, VEC, kThreads>(lds + buf * 2 * kTileBytes, kN, w.dim,
-                                        [&](int r) { return slot + r < reach.n ? f.k.at(c.k0 + reach.key(slot + r), kh, w.dim) : nullptr; });
-        load_tile<T, NT, VEC, kThreads>(lds + (buf * 2 + 1) * kTileBytes, kN, w.dim,
-                                        [&](int r) { return slot + r < reach.n ? f.v.at(c.k0 + reach.key(slot + r), kh, w.dim) : nullptr; });
-    };
+    const bool none = reach.n == 0 || wr.p + w.right < 0;  // the row sees nothing (else the last of its keys is seen at least)
 
     f32x16 acc[NT];
-    float m, l;                 // the row's largest score so far; this lane's half of the sum of exponentials
-    bool finite, again = false; // again: sums that were not finite, a second time without what rows do not see
-    bool met = false;           // ... and whether this row sees something that is not finite
-    const bool none = reach.n == 0 || wr.p + w.right < 0;  // the row sees nothing (else the last of its keys is seen at least)
-    for (;; again = true) {
+    float m, l;        // at most 8 powers of two below the row's largest score so far; this lane's half of the sum of exponentials
+    bool met = false;  // this row sees something that is not finite
+    // again: sums that were not finite, a second time without what rows do not see
+    auto pass = [&](auto again) {
 #pragma unroll
         for (int d = 0; d < NT; ++d) acc[d] = f32x16{};
         m = -INFINITY;
         l = 0.f;
-        if (reach.n > 0) load(0, 0);
         for (int slot = 0, buf = 0; slot < reach.n; slot += kN, buf ^= 1) {
             char *keys = lds + buf * 2 * kTileBytes, *values = keys + kTileBytes;
             wait_tiles();
-            if (slot + kN < reach.n) load(slot + kN, buf ^ 1);
-            if (again) clean_tiles<T, NT, kN, kThreads>(keys, values, marks);
+            if (slot + kN < reach.n) kt.load(lds, slot + kN, buf ^ 1);
+            if constexpr (again) clean_tiles<T, NT, kN, kThreads>(keys, values, marks);
             if (reach.none(w, slot, kN, wr.p_min, wr.p_max)) continue;
             f32x16 s[kB] = {};
 #pragma unroll
             for (int st = 0; st < Tl::kSteps; ++st)
 #pragma unroll
                 for (int b = 0; b < kB; ++b) s[b] = Tl::mma(Tl::direct(keys, pl, b, st), q[st], s[b]);
-            if (again || !wr.whole || !reach.all(w, slot, kN, wr.p_min, wr.p_max)) {
+            if (again || !(wr.whole & reach.all(w, slot, kN, wr.p_min, wr.p_max))) {
+                const SeenInTile seen(w, reach, slot, wr.p);
+                if (!again && seen.plain) {
 #pragma unroll
-                for (int b = 0; b < kB; ++b)
+                    for (int b = 0; b < kB; ++b)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int r = b * 32 + 8 * (i / 4) + 4 * (lane >> 5) + i % 4;
-                        const bool seen = (slot + r < reach.n) & sees(w, wr.p, reach.key(slot + r));
-                        s[b][i] = seen ? s[b][i] : -INFINITY;
-                        if (again) met |= seen & (marks[r] != 0);
-                    }
+                        for (int i = 0; i < 16; ++i) s[b][i] = seen(b * 32 + 8 * (i / 4) + i % 4) ? s[b][i] : -INFINITY;
+                } else {
+#pragma unroll
+                    for (int b = 0; b < kB; ++b)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const int r = b * 32 + 8 * (i / 4) + i % 4;
+                            const bool sees = seen.slow(r);
+                            s[b][i] = sees ? s[b][i] : -INFINITY;
+                            if constexpr (again) met |= sees & (marks[r + 4 * (lane >> 5)] != 0);
+                        }
+                }
             }
             float top = m;
 #pragma unroll
@@ -146,7 +207,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_fwd_kernel(AttnFwd<T> f, int
 #pragma unroll
                 for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
             top = halves<Max>(top);
-            if (__any(top > m)) {
+            if (__any((top - m) * c2 > 8.f)) {
                 const float old = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - top) * c2);
                 l *= old;
 #pragma unroll
@@ -161,16 +222,18 @@ __global__ __launch_bounds__(kThreads, 2) void attn_fwd_kernel(AttnFwd<T> f, int
 #pragma unroll
                     for (int i = 0; i < 16; ++i) s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], c2, -m2));
             } else {
-                const float top0 = m == -INFINITY ? 0.f : m;
+                const float from = m == -INFINITY ? 0.f : m;
 #pragma unroll
                 for (int b = 0; b < kB; ++b)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) s[b][i] = __builtin_amdgcn_exp2f((s[b][i] - top0) * c2);
+                    for (int i = 0; i < 16; ++i) s[b][i] = __builtin_amdgcn_exp2f((s[b][i] - from) * c2);
             }
+            float sum[4] = {};
 #pragma unroll
             for (int b = 0; b < kB; ++b)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) l += s[b][i];
+                for (int i = 0; i < 16; ++i) sum[i % 4] += s[b][i];
+            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
 #pragma unroll
             for (int b = 0; b < kB; ++b)
 #pragma unroll
@@ -187,8 +250,11 @@ __global__ __launch_bounds__(kThreads, 2) void attn_fwd_kernel(AttnFwd<T> f, int
         for (int d = 0; d < NT; ++d)
 #pragma unroll
             for (int i = 0; i < 16; ++i) check = fmaf(acc[d][i] *= inv, 0.f, check);
-        finite = halves<Add>(check) == 0.f;
-        if (again || !__syncthreads_or(wr.there && !finite)) break;
+        return __syncthreads_or(wr.there & (halves<Add>(check) != 0.f));
+    };
+    if (pass(std::false_type{})) {
+        kt.load(lds, 0, 0);
+        pass(std::true_type{});
     }
     const uint64_t seen_by = __ballot(wr.there && met);
     const uint32_t by_row = (uint32_t)seen_by | (uint32_t)(seen_by >> 32);  // rows that see what is not finite: key by key
@@ -198,7 +264,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_fwd_kernel(AttnFwd<T> f, int
             f.lse[(int64_t)(c.q0 + wr.query) * w.heads + h] = none ? -INFINITY : (m * c2 + __builtin_amdgcn_logf(l)) * kLn2;
     }
     for (uint32_t bad = by_row; bad; bad &= bad - 1) {
-        const int64_t r = wr.w0 + __builtin_ctz(bad);
+        const uint32_t r = wr.w0 + __builtin_ctz(bad);
         forward_row(f, c, (int)(r / w.group), kh * w.group + (int)(r % w.group));
     }
 }
@@ -219,10 +285,12 @@ __global__ __launch_bounds__(kThreads, sizeof(T) * NT < 16 ? 2 : 1) void attn_dq
     const Cloud c(w, rt.cloud);
     const int64_t rows = (int64_t)c.a * w.group;
     if (rt.r0 >= rows) return;
-    const WaveRows wr(w, c, rt.r0, rows);
+    const WaveRows wr(w, c, (uint32_t)rt.r0, (uint32_t)rows);
+    const Reach& reach = wr.reach;
     const int lane = threadIdx.x & 63, kh = rt.kh, h = kh * w.group + wr.head;
-    if (wr.reach.n < 2 * kN || w.dim % 32) clear_lds<kThreads>(lds, 4 * kTileBytes);
     const auto pl = Tl::place();
+    const KeyTiles<T, NT, VEC> kt(w, reach, g.k, g.v, c, kh);
+    if (reach.n > 0) kt.load(lds, 0, 0);
     typename Tl::Frag q[Tl::kSteps], dout[Tl::kSteps];
     Tl::template load_row<VEC>(q, g.q.at(c.q0 + wr.query, h, w.dim), w.dim, wr.there, w.scale < 0.f);
     Tl::template load_row<VEC>(dout, g.dout.at(c.q0 + wr.query, h, w.dim), w.dim, wr.there, false);
@@ -239,27 +307,19 @@ __global__ __launch_bounds__(kThreads, sizeof(T) * NT < 16 ? 2 : 1) void attn_dq
     const int64_t stat = (int64_t)(c.q0 + wr.query) * w.heads + h;
     if (wr.there && lane < 32) g.delta[stat] = delta;
     const float l2 = wr.there ? g.lse[stat] * kLog2e : 0.f, c2 = exponent_scale(w);
-    auto load = [&](int slot, int buf) {
-        load_tile<T, NT, VEC, kThreads>(lds + buf * 2 * kTileBytes, kN, w.dim, [&](int r) {
-            return slot + r < wr.reach.n ? g.k.at(c.k0 + wr.reach.key(slot + r), kh, w.dim) : nullptr;
-        });
-        load_tile<T, NT, VEC, kThreads>(lds + (buf * 2 + 1) * kTileBytes, kN, w.dim, [&](int r) {
-            return slot + r < wr.reach.n ? g.v.at(c.k0 + wr.reach.key(slot + r), kh, w.dim) : nullptr;
-        });
-    };
     f32x16 acc[NT];
-    bool again = false, met = false;  // as in the forward pass
-    for (;; again = true) {
+    bool met = false;
+    auto pass = [&](auto again) {  // as in the forward pass
 #pragma unroll
         for (int d = 0; d < NT; ++d) acc[d] = f32x16{};
-        if (wr.reach.n > 0) load(0, 0);
-        for (int slot = 0, buf = 0; slot < wr.reach.n; slot += kN, buf ^= 1) {
+        for (int slot = 0, buf = 0; slot < reach.n; slot += kN, buf ^= 1) {
             char *keys = lds + buf * 2 * kTileBytes, *values = keys + kTileBytes;
             wait_tiles();
-            if (slot + kN < wr.reach.n) load(slot + kN, buf ^ 1);
-            if (again) clean_tiles<T, NT, kN, kThreads>(keys, values, marks);
-            if (wr.reach.none(w, slot, kN, wr.p_min, wr.p_max)) continue;
-            const bool all = !again && wr.whole && wr.reach.all(w, slot, kN, wr.p_min, wr.p_max);
+            if (slot + kN < reach.n) kt.load(lds, slot + kN, buf ^ 1);
+            if constexpr (again) clean_tiles<T, NT, kN, kThreads>(keys, values, marks);
+            if (reach.none(w, slot, kN, wr.p_min, wr.p_max)) continue;
+            const bool all = !again && (wr.whole & reach.all(w, slot, kN, wr.p_min, wr.p_max));
+            const SeenInTile seen(w, reach, slot, wr.p);
 #pragma unroll
             for (int b = 0; b < kB; ++b) {
                 f32x16 s = {}, dp = {};
@@ -270,14 +330,20 @@ __global__ __launch_bounds__(kThreads, sizeof(T) * NT < 16 ? 2 : 1) void attn_dq
                 }
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c2, -l2)) * (dp[i] - delta);
-                if (!all)
+                if (!all) {
+                    if (!again && seen.plain) {
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int r = b * 32 + 8 * (i / 4) + 4 * (lane >> 5) + i % 4;
-                        const bool seen = (slot + r < wr.reach.n) & sees(w, wr.p, wr.reach.key(slot + r));
-                        s[i] = seen ? s[i] : 0.f;
-                        if (again) met |= seen & (marks[r] != 0);
+                        for (int i = 0; i < 16; ++i) s[i] = seen(b * 32 + 8 * (i / 4) + i % 4) ? s[i] : 0.f;
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const int r = b * 32 + 8 * (i / 4) + i % 4;
+                            const bool sees = seen.slow(r);
+                            s[i] = sees ? s[i] : 0.f;
+                            if constexpr (again) met |= sees & (marks[r + 4 * (lane >> 5)] != 0);
+                        }
                     }
+                }
 #pragma unroll
                 for (int st = 0; st < Tl::kTSteps; ++st) {
                     const auto ds = Tl::operand(s, st);
@@ -291,15 +357,18 @@ __global__ __launch_bounds__(kThreads, sizeof(T) * NT < 16 ? 2 : 1) void attn_dq
         for (int d = 0; d < NT; ++d)
 #pragma unroll
             for (int i = 0; i < 16; ++i) check = fmaf(acc[d][i] *= w.scale, 0.f, check);
-        const bool finite = halves<Add>(check) == 0.f;
-        if (again || !__syncthreads_or(wr.there && !finite)) break;
+        return __syncthreads_or(wr.there & (halves<Add>(check) != 0.f));
+    };
+    if (pass(std::false_type{})) {
+        kt.load(lds, 0, 0);
+        pass(std::true_type{});
     }
     const uint64_t seen_by = __ballot(wr.there && met);
     const uint32_t by_row = (uint32_t)seen_by | (uint32_t)(seen_by >> 32);
     if (wr.there && !(by_row >> (lane & 31) & 1)) put_column<T, NT, VEC>(g.dq.at(c.q0 + wr.query, h, w.dim), acc, w.dim);
     __threadfence_block();  // delta, which other lanes read
     for (uint32_t bad = by_row; bad; bad &= bad - 1) {
-        const int64_t r = wr.w0 + __builtin_ctz(bad);
+        const uint32_t r = wr.w0 + __builtin_ctz(bad);
         query_gradient_row(g, c, (int)(r / w.group), kh * w.group + (int)(r % w.group));
     }
 }
@@ -309,7 +378,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) * NT < 16 ? 2 : 1) void attn_dq
 // up those pairs, `chunk` rows to a wavefront (`far`), and attn_join_kernel adds both, the chunks in order.
 constexpr int kSplitSinks = 128;
 struct Split {
-    int sinks, chunk;  // 0: not split
+    int sinks, chunk;    // 0: not split; a multiple of `group`
     float *first, *far;  // [cloud or chunk][kv_heads][sinks][dk, dv][dim]
 };
 __device__ __forceinline__ int64_t split_at(const Window& w, const Split& sp, int64_t part, int kh, int key) {
@@ -320,38 +389,109 @@ __device__ __forceinline__ int64_t far_begin(const Window& w, const Cloud& c, in
     return (int64_t)max(w.left + key + 1 - c.off, 0) * w.group;
 }
 
-// Keys' gradients from 32 rows after another: what both kernels share
-template <typename T, int NT>
+// The rows (queries and dout) that a workgroup of the keys' kernels goes over, `step` of at most N at a time: whole queries, so that a
+// row's place in its tile does not change, unless a query's heads are more than N.
+template <typename T, int NT, bool VEC, int N, int THREADS>
+struct QueryTiles {
+    using Tl = Tile<T, NT>;
+    static constexpr int kTileBytes = N * Tl::kRowBytes;
+    const AttnBwd<T>& g;
+    const Cloud& c;
+    int kh, step;
+    int64_t end;  // the rows' end, a multiple of `group`
+    TileLoads<T, NT, N, THREADS> lq, ld;
+    __device__ __forceinline__ QueryTiles(const AttnBwd<T>& g_, const Cloud& c_, int kh_, int64_t end_) : g(g_), c(c_), kh(kh_), end(end_) {
+        const int group = g.w.group, row = g.w.dim * (int)sizeof(T);
+        step = group <= N ? N / group * group : N;
+        if constexpr (VEC) {
+            const uint32_t ldq = (uint32_t)(g.q.ld * sizeof(T)), ldd = (uint32_t)(g.dout.ld * sizeof(T));
+            lq.place(g.w.dim, [&](int r) { return r < step ? r / group * ldq + r % group * row : kOutside; });
+            ld.place(g.w.dim, [&](int r) { return r < step ? r / group * ldd + r % group * row : kOutside; });
+        }
+    }
+    __device__ __forceinline__ void one(char* tile, const TileLoads<T, NT, N, THREADS>& l, const Rows<const T>& t, int64_t row) const {
+        const int group = g.w.group;
+        if constexpr (VEC) {
+            const int64_t i = row / group, left = min((int64_t)step, end - row) / group;  // queries
+            l.load(lds_address(tile), memory_of(t.at(c.q0 + i, kh * group, g.w.dim),
+                                                (uint32_t)((left - 1) * t.ld + group * g.w.dim) * (uint32_t)sizeof(T)));
+        } else {
+            load_elements<T, NT, N, THREADS>(tile, g.w.dim, [&](int r) {
+                return r < step && row + r < end ? t.at(c.q0 + (row + r) / group, kh * group + (int)((row + r) % group), g.w.dim) : nullptr;
+            });
+        }
+    }
+    __device__ __forceinline__ void load(char* tiles, int64_t row) const {
+        one(tiles, lq, g.q, row);
+        one(tiles + kTileBytes, ld, g.dout, row);
+    }
+};
+
+// A row's statistics on their way from memory to LDS
+struct RowStat {
+    float l2, delta;
+    int p;
+};
+template <typename T>
+__device__ __forceinline__ RowStat row_stat(const AttnBwd<T>& g, const Cloud& c, int kh, int64_t row, bool there) {
+    RowStat r{0.f, 0.f, kNowhere};
+    if (there) {
+        const int i = (int)((uint32_t)row / (uint32_t)g.w.group);
+        const int64_t at = (int64_t)(c.q0 + i) * g.w.heads + kh * g.w.group + (int)((uint32_t)row % (uint32_t)g.w.group);
+        r = {g.lse[at] * kLog2e, g.delta[at], i + c.off};
+    }
+    return r;
+}
+template <int N>
+struct RowStats {
+    __attribute__((aligned(16))) float l2[N], delta[N];
+    __attribute__((aligned(16))) int p[N];
+    __device__ __forceinline__ void put(const RowStat& r, int at) {
+        l2[at] = r.l2;
+        delta[at] = r.delta;
+        p[at] = r.p;
+    }
+};
+
+// Keys' gradients from 32 rows after another.  VLDS: the values are read from LDS when they are needed, for heads so wide that
+// registers for both would leave a SIMD one wavefront.
+template <typename T, int NT, bool VLDS>
 struct KeyGrads {
     using Tl = Tile<T, NT>;
-    typename Tl::Frag k[Tl::kSteps], v[Tl::kSteps];
+    typename Tl::Frag k[Tl::kSteps], v[VLDS ? 1 : Tl::kSteps];
+    const char* v_tile;  // this wavefront's 32 rows
     f32x16 dk[NT], dv[NT];
-    // rows 32 b .. of the tiles q and dout; stats: the rows' lse * log2(e), delta and position
-    template <typename Hidden>
-    __device__ __forceinline__ void add(const char* q, const char* dout, const float* l2, const float* delta, const typename Tl::Place& pl,
-                                        int b, float c2, bool all, Hidden hidden) {
-        const int half = 4 * ((threadIdx.x & 63) >> 5);
+    // rows 32 b .. of the tiles q and dout
+    template <int N, typename Seen>
+    __device__ __forceinline__ void add(const char* q, const char* dout, const RowStats<N>& stats, const typename Tl::Place& pl, int b, float c2,
+                                        bool all, Seen seen) {
+        const int half = b * 32 + 4 * ((threadIdx.x & 63) >> 5);
         f32x16 s = {}, dp = {};
 #pragma unroll
         for (int st = 0; st < Tl::kSteps; ++st) {
             s = Tl::mma(Tl::direct(q, pl, b, st), k[st], s);
-            dp = Tl::mma(Tl::direct(dout, pl, b, st), v[st], dp);
+            dp = Tl::mma(Tl::direct(dout, pl, b, st), VLDS ? Tl::direct(v_tile, pl, 0, st) : v[VLDS ? 0 : st], dp);
         }
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-            const f32x4 l = *reinterpret_cast<const f32x4*>(l2 + b * 32 + 8 * g + half), de = *reinterpret_cast<const f32x4*>(delta + b * 32 + 8 * g + half);
+            const f32x4 l = *reinterpret_cast<const f32x4*>(stats.l2 + half + 8 * g), de = *reinterpret_cast<const f32x4*>(stats.delta + half + 8 * g);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                float p = __builtin_amdgcn_exp2f(fmaf(s[4 * g + i], c2, -l[i])), ds = p * (dp[4 * g + i] - de[i]);
-                if (!all) {
-                    const bool away = hidden(b * 32 + 8 * g + half + i);
-                    p = away ? 0.f : p;
-                    ds = away ? 0.f : ds;
-                }
-                s[4 * g + i] = p;
-                dp[4 * g + i] = ds;
+                s[4 * g + i] = __builtin_amdgcn_exp2f(fmaf(s[4 * g + i], c2, -l[i]));
+                dp[4 * g + i] = s[4 * g + i] * (dp[4 * g + i] - de[i]);
             }
         }
+        if (!all)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int4 p = *reinterpret_cast<const int4*>(stats.p + half + 8 * g);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const bool sees = seen(i == 0 ? p.x : i == 1 ? p.y : i == 2 ? p.z : p.w, half + 8 * g + i);
+                    s[4 * g + i] = sees ? s[4 * g + i] : 0.f;
+                    dp[4 * g + i] = sees ? dp[4 * g + i] : 0.f;
+                }
+            }
 #pragma unroll
         for (int st = 0; st < Tl::kTSteps; ++st) {
             const auto p = Tl::operand(s, st), ds = Tl::operand(dp, st);
@@ -364,113 +504,114 @@ struct KeyGrads {
     }
 };
 
-// A row's statistics on their way from memory to LDS
-struct RowStat {
-    float l2, delta;
-    int p;
-};
-template <typename T>
-__device__ __forceinline__ RowStat row_stat(const AttnBwd<T>& g, const Cloud& c, int kh, int64_t row, int64_t end) {
-    RowStat r{0.f, 0.f, kNowhere};
-    if (row < end) {
-        const int i = (int)(row / g.w.group);
-        const int64_t at = (int64_t)(c.q0 + i) * g.w.heads + kh * g.w.group + (int)(row % g.w.group);
-        r = {g.lse[at] * kLog2e, g.delta[at], i + c.off};
-    }
-    return r;
-}
-template <typename T>
-__device__ __forceinline__ const T* head_row(const Rows<const T>& t, const Window& w, const Cloud& c, int kh, int64_t row) {
-    return t.at(c.q0 + row / w.group, kh * w.group + (int)(row % w.group), w.dim);
-}
+template <typename T, int NT>
+constexpr bool kValuesInLds = sizeof(T) == 2 && NT >= 3;
+template <typename T, int NT>
+constexpr int kStepRows = sizeof(T) == 2 && !kValuesInLds<T, NT> ? 64 : 32;
 
 template <typename T, int NT, bool VEC>
-__global__ __launch_bounds__(kThreads, 1) void attn_dkv_kernel(AttnBwd<T> g, Split split, int tiles) {
+__global__ __launch_bounds__(kThreads, sizeof(T) * NT <= 8 ? 2 : 1) void attn_dkv_kernel(AttnBwd<T> g, Split split, int tiles) {
     using Tl = Tile<T, NT>;
-    constexpr int kN = kKeys<T>, kB = kN / 32, kTileBytes = kN * Tl::kRowBytes;
+    constexpr bool kVLds = kValuesInLds<T, NT>;
+    constexpr int kN = kStepRows<T, NT>, kB = kN / 32, kTileBytes = kN * Tl::kRowBytes;
     __shared__ __attribute__((aligned(1024))) char lds[4 * kTileBytes];
-    __shared__ __attribute__((aligned(16))) float l2[2][kN], delta[2][kN];
-    __shared__ int pos[2][kN], marks[kN];
+    __shared__ __attribute__((aligned(1024))) char values[kVLds ? kRows * Tl::kRowBytes : 16];
+    __shared__ RowStats<kN> stats[2];
+    __shared__ int marks[kN];
     const Window& w = g.w;
-    const int64_t item = item_of_block(blockIdx.x, gridDim.x), t = item % tiles;
-    const int kh = (int)(item / tiles), cn = cloud_of_tile(w.k_starts, w.clouds, w.n_k, t, 1, kRows);
+    const uint32_t item = item_of_block(blockIdx.x, gridDim.x), t = item % (uint32_t)tiles;
+    const int kh = (int)(item / (uint32_t)tiles), cn = cloud_of_tile(w.k_starts, w.clouds, w.n_k, t, 1, kRows);
     const Cloud c(w, cn);
-    const int64_t j0 = (t - first_tile(w.k_starts, w.clouds, w.n_k, cn, 1, kRows)) * kRows;
-    if (j0 >= c.b) return;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int jw = (int)j0 + wave * kWaveRows, j = jw + (lane & 31);
+    const int64_t tile0 = (t - first_tile(w.k_starts, w.clouds, w.n_k, cn, 1, kRows)) * kRows;
+    if (tile0 >= c.b) return;
+    const int j0 = (int)tile0, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int jw = j0 + wave * kWaveRows, j = jw + (lane & 31);
     const bool there = j < c.b, split_here = split.sinks > 0;
     const int sinks = split_here ? 0 : w.sinks;
     // the rows that see a key of the workgroup's
     const int a = c.partners ? c.a : 0;
-    const int64_t begin = (int64_t)min(max((int)j0 - w.right - c.off, 0), a) * w.group;
-    const int64_t end = j0 < sinks ? (int64_t)a * w.group : max(begin, (int64_t)min(max(min((int)j0 + kRows, c.b) + w.left - c.off, 0), a) * w.group);
-    if (end - begin < 2 * kN || w.dim % 32) clear_lds<kThreads>(lds, 4 * kTileBytes);
+    const int i0 = min(max(j0 - w.right - c.off, 0), a), i1 = j0 < sinks ? a : max(i0, min(max(min(j0 + kRows, c.b) + w.left - c.off, 0), a));
+    const int64_t begin = (int64_t)i0 * w.group, end = (int64_t)i1 * w.group;
     const auto pl = Tl::place();
-    KeyGrads<T, NT> kg{};
-    Tl::template load_row<VEC>(kg.k, g.k.at(c.k0 + j, kh, w.dim), w.dim, there, w.scale < 0.f);
-    Tl::template load_row<VEC>(kg.v, g.v.at(c.k0 + j, kh, w.dim), w.dim, there, false);
+    const QueryTiles<T, NT, VEC, kN, kThreads> qt(g, c, kh, end);
+    KeyGrads<T, NT, kVLds> kg;
     const float c2 = exponent_scale(w);
-    auto load = [&](int64_t row, int buf) {
-        load_tile<T, NT, VEC, kThreads>(lds + buf * 2 * kTileBytes, kN, w.dim,
-                                        [&](int r) { return row + r < end ? head_row(g.q, w, c, kh, row + r) : nullptr; });
-        load_tile<T, NT, VEC, kThreads>(lds + (buf * 2 + 1) * kTileBytes, kN, w.dim,
-                                        [&](int r) { return row + r < end ? head_row(g.dout, w, c, kh, row + r) : nullptr; });
+    bool met = false;
+    auto stat_of = [&](int64_t row) {
+        return row_stat(g, c, kh, row + threadIdx.x, (int)threadIdx.x < qt.step && row + threadIdx.x < end);
     };
-    auto put_stat = [&](const RowStat& r, int buf) {
-        if (threadIdx.x < kN) {
-            l2[buf][threadIdx.x] = r.l2;
-            delta[buf][threadIdx.x] = r.delta;
-            pos[buf][threadIdx.x] = r.p;
+    auto start = [&] {
+        if (begin < end) {
+            qt.load(lds, begin);
+            const RowStat r = stat_of(begin);
+            if (threadIdx.x < kN) stats[0].put(r, threadIdx.x);
         }
     };
-    bool again = false, met = false;  // as in the forward pass: whether a row that sees this key is not finite
-    for (;; again = true) {
+    start();
+    Tl::template load_row<VEC>(kg.k, g.k.at(c.k0 + j, kh, w.dim), w.dim, there, w.scale < 0.f);
+    if constexpr (kVLds) {
+        const T* v = g.v.at(c.k0 + j0, kh, w.dim);
+        const int64_t ldv = g.v.ld;
+        if constexpr (VEC) {
+            TileLoads<T, NT, kRows, kThreads> lv;
+            lv.place(w.dim, [&](int r) { return r * (uint32_t)(ldv * sizeof(T)); });
+            lv.load(lds_address(values), memory_of(v, (uint32_t)((min(kRows, c.b - j0) - 1) * ldv + w.dim) * (uint32_t)sizeof(T)));
+        } else {
+            load_elements<T, NT, kRows, kThreads>(values, w.dim, [&](int r) { return j0 + r < c.b ? v + r * ldv : nullptr; });
+        }
+        kg.v_tile = values + wave * kWaveRows * Tl::kRowBytes;
+        if (begin >= end) wait_tiles();  // no workgroup ends with a load on its way
+    } else {
+        Tl::template load_row<VEC>(kg.v, g.v.at(c.k0 + j, kh, w.dim), w.dim, there, false);
+    }
+    // j - right <= p <= j + left, for the first keys all p behind
+    const int low = j - w.right;
+    const uint32_t width = j < sinks ? 0x7fffffffu : (uint32_t)(w.left + w.right);
+    auto pass = [&](auto again) {
 #pragma unroll
         for (int d = 0; d < NT; ++d) kg.dk[d] = kg.dv[d] = f32x16{};
-        if (begin < end) {
-            load(begin, 0);
-            put_stat(row_stat(g, c, kh, threadIdx.x < kN ? begin + threadIdx.x : end, end), 0);
-        }
         int buf = 0;
-        for (int64_t row = begin; row < end; row += kN, buf ^= 1) {
+        for (int64_t row = begin; row < end; row += qt.step, buf ^= 1) {
             char *q = lds + buf * 2 * kTileBytes, *dout = q + kTileBytes;
             wait_tiles();
             RowStat next{};
-            if (row + kN < end) {
-                load(row + kN, buf ^ 1);
-                next = row_stat(g, c, kh, threadIdx.x < kN ? row + kN + threadIdx.x : end, end);
+            const bool more = row + qt.step < end;
+            if (more) {
+                qt.load(lds + (buf ^ 1) * 2 * kTileBytes, row + qt.step);
+                next = stat_of(row + qt.step);
             }
-            if (again) clean_tiles<T, NT, kN, kThreads>(q, dout, marks);
-            const int p_min = (int)(row / w.group) + c.off, p_max = (int)((min(row + kN, end) - 1) / w.group) + c.off;
-            const bool none = jw >= c.b || jw > p_max + w.right || (jw + kWaveRows - 1 < p_min - w.left && jw >= sinks);
-            const bool all = !again && row + kN <= end && jw + kWaveRows - 1 <= p_min + w.right && jw >= p_max - w.left;
+            if constexpr (again) clean_tiles<T, NT, kN, kThreads>(q, dout, marks);
+            const int p_min = (int)((uint32_t)row / (uint32_t)w.group) + c.off;
+            const int p_max = (int)((uint32_t)(min(row + qt.step, end) - 1) / (uint32_t)w.group) + c.off;
+            const bool none = (jw >= c.b) | (jw > p_max + w.right) | ((jw + kWaveRows - 1 < p_min - w.left) & (jw >= sinks));
+            const bool all = !again && ((row + kN <= end) & (qt.step == kN) & (jw + kWaveRows - 1 <= p_min + w.right) & (jw >= p_max - w.left));
             if (!none)
 #pragma unroll
                 for (int b = 0; b < kB; ++b)
-                    kg.add(q, dout, l2[buf], delta[buf], pl, b, c2, all, [&](int r) {
-                        const int p = pos[buf][r];
-                        const bool seen = (j <= p + w.right) & ((j >= p - w.left) | (j < sinks));
-                        if (again) met |= seen & (marks[r] != 0);
-                        return !seen;
+                    kg.add(q, dout, stats[buf], pl, b, c2, all, [&](int p, int r) {
+                        const bool seen = (uint32_t)(p - low) <= width;
+                        if constexpr (again) met |= seen & (marks[r] != 0);
+                        return seen;
                     });
-            if (row + kN < end) put_stat(next, buf ^ 1);
+            if (more && threadIdx.x < kN) stats[buf ^ 1].put(next, threadIdx.x);
         }
         float check = 0.f;
 #pragma unroll
         for (int d = 0; d < NT; ++d)
 #pragma unroll
             for (int i = 0; i < 16; ++i) check = fmaf(kg.dk[d][i] *= w.scale, 0.f, fmaf(kg.dv[d][i], 0.f, check));
-        const bool finite = halves<Add>(check) == 0.f;
-        if (again || !__syncthreads_or(there && !finite)) break;
+        return __syncthreads_or(there & (halves<Add>(check) != 0.f));
+    };
+    if (pass(std::false_type{})) {
+        start();
+        pass(std::true_type{});
     }
     const bool part = split_here && j < split.sinks && c.partners;
     const uint64_t seen_by = __ballot(there && !part && met);
     const uint32_t by_row = (uint32_t)seen_by | (uint32_t)(seen_by >> 32);
     if (there && part) {
         float* to = split.first + split_at(w, split, cn - 1, kh, j);
-        // a value that is not finite sends attn_join_kernel over the rows one by one
-        if (met) kg.dk[0][0] = NAN;
+        if (met) kg.dk[0][0] = NAN;  // sends attn_join_kernel over the rows one by one
         put_column<float, NT, false>(to, kg.dk, w.dim);
         put_column<float, NT, false>(to + w.dim, kg.dv, w.dim);
     } else if (there && !(by_row >> (lane & 31) & 1)) {
@@ -485,11 +626,10 @@ __global__ __launch_bounds__(64, 1) void attn_far_kernel(AttnBwd<T> g, Split spl
     using Tl = Tile<T, NT>;
     constexpr int kTileBytes = 32 * Tl::kRowBytes;
     __shared__ __attribute__((aligned(1024))) char lds[4 * kTileBytes];
-    __shared__ __attribute__((aligned(16))) float l2[2][32], delta[2][32];
-    __shared__ int pos[2][32];
+    __shared__ RowStats<32> stats[2];
     const Window& w = g.w;
-    const int64_t item = item_of_block(blockIdx.x, gridDim.x), t = item % tiles;
-    const int groups = (split.sinks + 31) / 32, key0 = (int)(item / tiles) % groups * 32, kh = (int)(item / tiles) / groups;
+    const uint32_t item = item_of_block(blockIdx.x, gridDim.x), t = item % (uint32_t)tiles;
+    const int groups = (split.sinks + 31) / 32, key0 = (int)(item / (uint32_t)tiles) % groups * 32, kh = (int)(item / (uint32_t)tiles) / groups;
     const int cn = cloud_of_tile(w.q_starts, w.clouds, w.n_q, t, w.group, split.chunk);
     const Cloud c(w, cn);
     const int64_t r0 = (t - first_tile(w.q_starts, w.clouds, w.n_q, cn, w.group, split.chunk)) * split.chunk;
@@ -497,39 +637,33 @@ __global__ __launch_bounds__(64, 1) void attn_far_kernel(AttnBwd<T> g, Split spl
     if (!c.partners || begin >= end || key0 >= c.b) return;
     const int lane = threadIdx.x, j = key0 + (lane & 31);
     const bool there = j < min(split.sinks, c.b);
-    if (end - begin < 64 || w.dim % 32) clear_lds<64>(lds, 4 * kTileBytes);
     const auto pl = Tl::place();
-    KeyGrads<T, NT> kg{};
+    const QueryTiles<T, NT, VEC, 32, 64> qt(g, c, kh, end);
+    KeyGrads<T, NT, false> kg;
+    auto stat_of = [&](int64_t row) { return row_stat(g, c, kh, row + lane, lane < qt.step && row + lane < end); };
+    qt.load(lds, begin);
+    {
+        const RowStat r = stat_of(begin);
+        if (lane < 32) stats[0].put(r, lane);
+    }
     Tl::template load_row<VEC>(kg.k, g.k.at(c.k0 + j, kh, w.dim), w.dim, there, w.scale < 0.f);
     Tl::template load_row<VEC>(kg.v, g.v.at(c.k0 + j, kh, w.dim), w.dim, there, false);
     const float c2 = exponent_scale(w);
-    auto load = [&](int64_t row, int buf) {
-        load_tile<T, NT, VEC, 64>(lds + buf * 2 * kTileBytes, 32, w.dim,
-                                  [&](int r) { return row + r < end ? head_row(g.q, w, c, kh, row + r) : nullptr; });
-        load_tile<T, NT, VEC, 64>(lds + (buf * 2 + 1) * kTileBytes, 32, w.dim,
-                                  [&](int r) { return row + r < end ? head_row(g.dout, w, c, kh, row + r) : nullptr; });
-    };
-    auto put_stat = [&](const RowStat& r, int buf) {
-        if (lane < 32) {
-            l2[buf][lane] = r.l2;
-            delta[buf][lane] = r.delta;
-            pos[buf][lane] = r.p;
-        }
-    };
-    load(begin, 0);
-    put_stat(row_stat(g, c, kh, lane < 32 ? begin + lane : end, end), 0);
+#pragma unroll
+    for (int d = 0; d < NT; ++d) kg.dk[d] = kg.dv[d] = f32x16{};
     int buf = 0;
-    for (int64_t row = begin; row < end; row += 32, buf ^= 1) {
-        wait_tiles();
+    for (int64_t row = begin; row < end; row += qt.step, buf ^= 1) {
+        wait_own_tiles();
         RowStat next{};
-        if (row + 32 < end) {
-            load(row + 32, buf ^ 1);
-            next = row_stat(g, c, kh, lane < 32 ? row + 32 + lane : end, end);
+        const bool more = row + qt.step < end;
+        if (more) {
+            qt.load(lds + (buf ^ 1) * 2 * kTileBytes, row + qt.step);
+            next = stat_of(row + qt.step);
         }
         const char* q = lds + buf * 2 * kTileBytes;
-        const bool all = row + 32 <= end && key0 + 31 < (int)(row / w.group) + c.off - w.left;
-        kg.add(q, q + kTileBytes, l2[buf], delta[buf], pl, 0, c2, all, [&](int r) { return j >= pos[buf][r] - w.left; });
-        if (row + 32 < end) put_stat(next, buf ^ 1);
+        const bool all = (row + 32 <= end) & (qt.step == 32) & (key0 + 31 < (int)((uint32_t)row / (uint32_t)w.group) + c.off - w.left);
+        kg.add(q, q + kTileBytes, stats[buf], pl, 0, c2, all, [&](int p, int) { return j < p - w.left; });
+        if (more && lane < 32) stats[buf ^ 1].put(next, lane);
     }
     if (there) {
 #pragma unroll
@@ -580,7 +714,7 @@ int forward_sized(const AttnFwd<T>& f, hipStream_t s) {
 }
 
 template <typename T>
-bool in_pieces(const Rows<T>& r) { return r.ld * (int64_t)sizeof(T) % 16 == 0 && aligned16(r.p); }
+bool in_pieces(const Rows<T>& r) { return r.ld * (int64_t)sizeof(T) % 16 == 0 && r.ld * (int64_t)sizeof(T) <= kMostRowBytes && aligned16(r.p); }
 
 template <typename T>
 int forward(const AttnFwd<T>& f, hipStream_t s) {
@@ -599,7 +733,7 @@ int backward_sized(AttnBwd<T> g, hipStream_t s) {
     Buf delta = dev_alloc((size_t)w.n_q * w.heads * 4, s), parts;
     if (!delta) return SP_ERR_ALLOC;
     g.delta = ptr<float>(delta);
-    Split split{0, 1024, nullptr, nullptr};
+    Split split{0, (1024 + w.group - 1) / w.group * w.group, nullptr, nullptr};
     const int groups = (w.sinks + 31) / 32;
     int64_t chunks = 0;
     if (w.sinks > 0 && w.sinks <= kSplitSinks && w.n_q > 0 && w.clouds > 0 && w.n_k - w.left > 2048) {
@@ -626,7 +760,7 @@ int backward_sized(AttnBwd<T> g, hipStream_t s) {
 template <typename T>
 int backward(const AttnBwd<T>& g, hipStream_t s) {
     const bool vec = g.w.dim * sizeof(T) % 16 == 0 && in_pieces(g.q) && in_pieces(g.k) && in_pieces(g.v) && in_pieces(g.o) && in_pieces(g.dout) &&
-                     in_pieces(g.dq) && in_pieces(g.dk) && in_pieces(g.dv);
+                     in_pieces(g.dq) && in_pieces(g.dk) && in_pieces(g.dv) && g.w.group <= 32;
     const int nt = (g.w.dim + 31) / 32;
     if (vec) return nt == 1 ? backward_sized<T, 1, true>(g, s) : nt == 2 ? backward_sized<T, 2, true>(g, s) : nt == 3 ? backward_sized<T, 3, true>(g, s) : backward_sized<T, 4, true>(g, s);
     return nt == 1 ? backward_sized<T, 1, false>(g, s) : nt == 2 ? backward_sized<T, 2, false>(g, s) : nt == 3 ? backward_sized<T, 3, false>(g, s) : backward_sized<T, 4, false>(g, s);
@@ -642,6 +776,7 @@ int check(const sp_window_attn* a, Window* w) {
     if (!(a->scale > -3.0e38f && a->scale < 3.0e38f)) return fail(SP_ERR_INVALID_ARG, "the scale must be finite");
     if (a->dim > kMaxDim || a->heads > 65535 || a->n_q > 1 << 29 || a->n_k > 1 << 29)
         return fail(SP_ERR_UNSUPPORTED, "head widths above %d, more than 65535 heads or more than 2^29 rows", kMaxDim);
+    if (a->n_q * (a->heads / a->kv_heads) > INT32_MAX) return fail(SP_ERR_UNSUPPORTED, "more than 2^31 rows and heads that share a key head");
     if (!a->d_q_starts || !a->d_k_starts) return fail(SP_ERR_INVALID_ARG, "the starts are NULL");
     w->q_starts = a->d_q_starts;
     w->k_starts = a->d_k_starts;

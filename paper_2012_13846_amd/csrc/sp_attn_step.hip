@@ -22,15 +22,21 @@ constexpr int kKeys = 32;   // of a wavefront's tile
 
 // The keys a token at position p sees, in order: t-th of n; and the cache's row of a position
 struct StepSeen {
-    int p, first, lo, n, sinks, ring;
+    int p, first, lo, n, sinks, ring, from, at;  // position `from`, the first behind the first keys, lies in row sinks + at
     template <typename T>
     __device__ __forceinline__ StepSeen(const StepArgs<T>& a, int b) : p(a.lens[b]), sinks(a.sinks), ring(a.cap - a.sinks) {
         lo = max(max(p - a.left, p - ring + 1), 0);
         first = min(sinks, lo);
         n = p < 0 ? 0 : first + p + 1 - lo;
+        from = max(lo, sinks);
+        at = (from - sinks) % ring;
     }
     __device__ __forceinline__ int key(int t) const { return t + (t < first ? 0 : lo - first); }
-    __device__ __forceinline__ int row(int j) const { return j < sinks ? j : sinks + (j - sinks) % ring; }
+    // of a key that is seen: fewer than `ring` behind `from`
+    __device__ __forceinline__ int row(int j) const {
+        const int r = at + (j - from);
+        return j < sinks ? j : sinks + (r < ring ? r : r - ring);
+    }
 };
 
 // fp32 heads above 64 have room for one tile of keys and values a wavefront
@@ -64,28 +70,45 @@ __global__ __launch_bounds__(kThreads, 1) void attn_step_kernel(StepArgs<T> a, i
     const int column = lane & 31;
     Tl::template load_row<VEC>(q, a.q + ((int64_t)b * a.heads + kh * a.group + h0 + column) * a.dim, a.dim, column < here, a.scale < 0.f);
     const float c2 = fmaxf(fabsf(a.scale) * kLog2e, 1e-30f);  // as in the packed form
-    auto clear = [&](char* p, int bytes) {
-        for (int i = lane * 16; i < bytes; i += 64 * 16) *reinterpret_cast<uint4*>(p + i) = uint4{0, 0, 0, 0};
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    };
-    if (a.dim % 32) clear(mine, 2 * kBufs * kTileBytes);
+    // rows of the cache by 32 bits from the sequence's first (step() sees to it); the new token's from another place
+    const uint32_t row_bytes = (uint32_t)(slot_step * sizeof(T)), head_bytes = a.dim * (uint32_t)sizeof(T);
     auto load = [&](int t, int buf) {
-        char* keys = mine + buf * 2 * kTileBytes;
-        if (t + kKeys > end) clear(keys, 2 * kTileBytes);
-        auto row = [&](const T* all, const T* now, int r) -> const T* {
-            if (t + r >= end) return nullptr;
-            const int j = seen.key(t + r);
-            return j == seen.p ? now + fresh : all + cache + seen.row(j) * slot_step;
-        };
-        load_tile<T, NT, VEC, 64>(keys, kKeys, a.dim, [&](int r) { return row(a.k_cache, a.k_new, r); });
-        load_tile<T, NT, VEC, 64>(keys + kTileBytes, kKeys, a.dim, [&](int r) { return row(a.v_cache, a.v_new, r); });
+        char *keys = mine + buf * 2 * kTileBytes, *values = keys + kTileBytes;
+        if constexpr (VEC) {
+            using Ld = TileLoads<T, NT, kKeys, 64>;
+            const uint32_t bytes = (uint32_t)(a.cap - 1) * row_bytes + head_bytes;
+            const u32x4 k_ring = memory_of(a.k_cache + cache, bytes), v_ring = memory_of(a.v_cache + cache, bytes);
+            const u32x4 k_token = memory_of(a.k_new + fresh, head_bytes), v_token = memory_of(a.v_new + fresh, head_bytes);
+#pragma unroll
+            for (int k = 0; k < Ld::kLoads; ++k) {
+                const int at = t + Ld::row(k), j = seen.key(at), piece = Ld::piece(k);
+                const uint32_t k_at = Ld::lds_of(lds_address(keys), k), v_at = Ld::lds_of(lds_address(values), k);
+                const bool in = (at < end) & (piece * Tl::kPer < a.dim);
+                if (j == seen.p) {
+                    memory_to_lds(k_token, in ? piece * 16 : kOutside, k_at);
+                    memory_to_lds(v_token, in ? piece * 16 : kOutside, v_at);
+                } else {
+                    const uint32_t off = in ? seen.row(j) * row_bytes + piece * 16 : 0xffffff00u;
+                    memory_to_lds(k_ring, off, k_at);
+                    memory_to_lds(v_ring, off, v_at);
+                }
+            }
+        } else {
+            auto from = [&](const T* all, const T* now, int r) -> const T* {
+                if (t + r >= end) return nullptr;
+                const int j = seen.key(t + r);
+                return j == seen.p ? now + fresh : all + cache + seen.row(j) * slot_step;
+            };
+            load_elements<T, NT, kKeys, 64>(keys, a.dim, [&](int r) { return from(a.k_cache, a.k_new, r); });
+            load_elements<T, NT, kKeys, 64>(values, a.dim, [&](int r) { return from(a.v_cache, a.v_new, r); });
+        }
     };
     f32x16 acc[NT] = {};
     float m = -INFINITY, l = 0.f;
     int t = begin + wave * kKeys, buf = 0;
     if (t < end) load(t, 0);
     for (; t < end; t += 4 * kKeys, buf ^= kBufs - 1) {
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        wait_own_tiles();
         if (kBufs == 2 && t + 4 * kKeys < end) load(t + 4 * kKeys, buf ^ 1);
         const char *keys = mine + buf * 2 * kTileBytes, *values = keys + kTileBytes;
         f32x16 s = {};
@@ -169,7 +192,7 @@ __global__ __launch_bounds__(128) void attn_step_join_kernel(StepArgs<T> a, int 
     const int e = threadIdx.x, lane = e & 63;
     float top = -INFINITY;
     for (int k = lane; k < parts; k += 64) top = fmaxf(top, from[k * (a.dim + 2) + a.dim]);
-    top = wave_reduce<Max>(top);
+    top = lanes_reduce<64, Max>(top);
     if (e >= a.dim) return;
     const float base = top == -INFINITY ? 0.f : top;
     float v = 0.f, total = 0.f;
@@ -206,7 +229,7 @@ int step_sized(const StepArgs<T>& a, hipStream_t s) {
 
 template <typename T>
 int step(const StepArgs<T>& a, hipStream_t s) {
-    const bool vec = a.dim * sizeof(T) % 16 == 0 && aligned16(a.q) && aligned16(a.k_new) && aligned16(a.v_new) && aligned16(a.k_cache) && aligned16(a.v_cache);
+    const bool vec = a.dim * sizeof(T) % 16 == 0 && (int64_t)a.cap * a.kv_heads * a.dim * (int64_t)sizeof(T) < 0xf0000000ll && aligned16(a.q) && aligned16(a.k_new) && aligned16(a.v_new) && aligned16(a.k_cache) && aligned16(a.v_cache);
     const int nt = (a.dim + 31) / 32;
     if (vec) return nt == 1 ? step_sized<T, 1, true>(a, s) : nt == 2 ? step_sized<T, 2, true>(a, s) : nt == 3 ? step_sized<T, 3, true>(a, s) : step_sized<T, 4, true>(a, s);
     return nt == 1 ? step_sized<T, 1, false>(a, s) : nt == 2 ? step_sized<T, 2, false>(a, s) : nt == 3 ? step_sized<T, 3, false>(a, s) : step_sized<T, 4, false>(a, s);

@@ -130,38 +130,83 @@ struct Tile {
     }
 };
 
-// `rows` rows into LDS at `tile`: row r from where at(r) says (nullptr: it stays as it is).  16-byte pieces go past the registers (a
-// wavefront writes 1024 consecutive bytes an instruction) and are there after wait_tiles(); others are read element by element.
-// THREADS: of the workgroup, or 64 for a wavefront that loads a tile of its own.
-template <typename T, int NT, bool VEC, int THREADS, typename At>
-__device__ __forceinline__ void load_tile(char* tile, int rows, int dim, At at) {
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+constexpr uint32_t kOutside = 0x80000000u;  // behind every tile's bytes: the load writes zeros
+// The last row of a tile's bytes must lie below kOutside, for which rows are at most this far apart
+constexpr int64_t kMostRowBytes = 1 << 24;
+
+// Memory as far as `bytes` behind `base` (scalars), for loads that check their offset against it
+__device__ __forceinline__ u32x4 memory_of(const void* base, uint32_t bytes) {
+    const uint64_t at = (uint64_t)base;
+    return u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)at), (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(at >> 32) & 0xffffu),
+                 (uint32_t)__builtin_amdgcn_readfirstlane(bytes), 0x00020000u};
+}
+// 16 bytes a lane from memory to LDS, past the registers; lane l writes at `lds` + 16 l (a scalar).  There after wait_tiles().
+__device__ __forceinline__ void memory_to_lds(u32x4 memory, uint32_t offset, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(memory) : "memory");
+}
+__device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(SP_LDS const char*)p; }
+
+// What a thread loads of a tile of ROWS rows: piece p = thread, thread + THREADS, ... of its ROWS * kC, which lies at byte 16 p of the
+// tile.  THREADS: of the workgroup, or 64 for a wavefront with a tile of its own.
+template <typename T, int NT, int ROWS, int THREADS>
+struct TileLoads {
     using Tl = Tile<T, NT>;
-    const int thread = threadIdx.x % THREADS, wave = __builtin_amdgcn_readfirstlane(thread >> 6);
+    static constexpr int kLoads = (ROWS * Tl::kC + THREADS - 1) / THREADS;
+    uint32_t off[kLoads];
+    static __device__ __forceinline__ int at(int k) { return k * THREADS + (int)(threadIdx.x % THREADS); }
+    static __device__ __forceinline__ int row(int k) { return at(k) / Tl::kC; }
+    static __device__ __forceinline__ int piece(int k) { return (at(k) % Tl::kC) ^ swizzle<Tl::kC>(row(k)); }
+    // row r of the tile lies `row_at(r)` bytes behind the tile's memory
+    template <typename RowAt>
+    __device__ __forceinline__ void place(int dim, RowAt row_at) {
 #pragma unroll
-    for (int base = 0; base < rows * Tl::kC; base += THREADS) {
-        const int p = base + thread, row = p / Tl::kC, piece = (p % Tl::kC) ^ swizzle<Tl::kC>(row);
-        const T* from = piece * Tl::kPer < dim ? at(row) : nullptr;
-        if constexpr (VEC) {
-            if (from)
-                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t*)(from + piece * Tl::kPer),
-                                                 (SP_LDS uint32_t*)(tile + (base + wave * 64) * 16), 16, 0, 0);
-        } else if (from) {
-            Piece<T, Tl::kPer> e{};
+        for (int k = 0; k < kLoads; ++k) off[k] = piece(k) * Tl::kPer < dim ? row_at(row(k)) + piece(k) * 16 : kOutside;
+    }
+    static __device__ __forceinline__ uint32_t lds_of(uint32_t tile, int k) {
+        return tile + k * THREADS * 16 + __builtin_amdgcn_readfirstlane((threadIdx.x % THREADS) >> 6) * 1024;
+    }
+    static __device__ __forceinline__ bool mine(int k) { return ROWS * Tl::kC % THREADS == 0 || at(k) < ROWS * Tl::kC; }
+    __device__ __forceinline__ void load(uint32_t tile, u32x4 memory) const {
+#pragma unroll
+        for (int k = 0; k < kLoads; ++k)
+            if (mine(k)) memory_to_lds(memory, off[k], lds_of(tile, k));
+    }
+    // the first `split` rows from one place, the others from another, as if it began `back` bytes earlier
+    __device__ __forceinline__ void load_two(uint32_t tile, u32x4 one, int split, u32x4 two, uint32_t back) const {
+#pragma unroll
+        for (int k = 0; k < kLoads; ++k)
+            if (mine(k)) {
+                if (row(k) < split) memory_to_lds(one, off[k], lds_of(tile, k));
+                else memory_to_lds(two, off[k] - back, lds_of(tile, k));
+            }
+    }
+};
+
+// Rows that are no 16-byte pieces, element by element: row r of the tile from where at(r) says, zeros for nullptr.
+template <typename T, int NT, int ROWS, int THREADS, typename At>
+__device__ __forceinline__ void load_elements(char* tile, int dim, At at) {
+    using Tl = Tile<T, NT>;
+    using Ld = TileLoads<T, NT, ROWS, THREADS>;
+#pragma unroll 1
+    for (int k = 0; k < Ld::kLoads; ++k) {
+        if (!Ld::mine(k)) continue;
+        const int e0 = Ld::piece(k) * Tl::kPer;
+        const T* from = e0 < dim ? at(Ld::row(k)) : nullptr;
+        Piece<T, Tl::kPer> e{};
+        if (from)
             for (int i = 0; i < Tl::kPer; ++i)
-                if (piece * Tl::kPer + i < dim) e.e[i] = from[piece * Tl::kPer + i];
-            *reinterpret_cast<uint4*>(tile + p * 16) = __builtin_bit_cast(uint4, e);
-        }
+                if (e0 + i < dim) e.e[i] = from[e0 + i];
+        *reinterpret_cast<uint4*>(tile + Ld::at(k) * 16) = __builtin_bit_cast(uint4, e);
     }
 }
+// All of a workgroup's loads into LDS are there, for every thread
 __device__ __forceinline__ void wait_tiles() {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     __syncthreads();
 }
-template <int THREADS>
-__device__ __forceinline__ void clear_lds(char* p, int bytes) {
-    for (int i = threadIdx.x * 16; i < bytes; i += THREADS * 16) *reinterpret_cast<uint4*>(p + i) = uint4{0, 0, 0, 0};
-    __syncthreads();
-}
+// A wavefront's loads into LDS of its own
+__device__ __forceinline__ void wait_own_tiles() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
 
 // Infinities and not-a-numbers of a tile become zero, and their rows are marked: for the second run of a workgroup whose results are
 // not finite (0 * infinity), which takes what a row does not see out of its sums.
@@ -222,9 +267,9 @@ __device__ __forceinline__ void put_column(T* row, const f32x16 (&acc)[NT], int 
 }
 
 // Workgroups go to the 8 XCDs by turns: neighbouring items, which read the same rows, to one XCD.
-__device__ __forceinline__ int64_t item_of_block(int64_t block, int64_t items) {
-    const int64_t each = items / 8, extra = items % 8, x = block % 8;
-    return x * each + (x < extra ? x : extra) + block / 8;
+__device__ __forceinline__ uint32_t item_of_block(uint32_t block, uint32_t items) {
+    const uint32_t each = items / 8, extra = items % 8, x = block % 8;
+    return x * each + min(x, extra) + block / 8;
 }
 
 }  // namespace sp

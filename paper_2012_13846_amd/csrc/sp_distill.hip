@@ -34,70 +34,99 @@ struct DistillArgs {
     hipStream_t s;
 };
 
-// What the lanes of a row know of its teacher: entries in LDS (a: softmax, then the gradient's share; col: column or -1)
+// A row's entries in LDS (a: softmax; col: column or -1, up to a multiple of 4), made by the first kLead of the row's lanes, all of
+// them in one wavefront, while the others read the row.
 struct Entries {
     float *a, *log_a, *zj;
     int32_t* col;
-    __device__ __forceinline__ Entries(float* p, int k) : a(p), log_a(p + k), zj(p + 2 * k), col(reinterpret_cast<int32_t*>(p + 3 * k)) {}
+    int k;
+    static constexpr int kWords = 4;
+    __device__ __forceinline__ Entries(float* p, int k_) : k(k_) {
+        const int pitch = (k + 3) & ~3;
+        a = p;
+        log_a = p + pitch;
+        zj = p + 2 * pitch;
+        col = reinterpret_cast<int32_t*>(p + 3 * pitch);
+    }
 };
+template <int LANES>
+constexpr int kLead = LANES < 64 ? LANES : 64;
 
-// a_j = softmax(top / T) over the row's entries, in LDS; whether there are any.  The row's lanes call it together.
-template <typename T, int LANES>
-__device__ __forceinline__ bool teacher(const Entries& e, const T* z, int64_t row, int m, const float* top, const int32_t* index, int k,
-                                        float inv_t, int l, float* room, int* turn) {
-    float mx[1] = {-INFINITY}, s[1] = {0.f};
-    for (int j = l; j < k; j += LANES) {
-        const int col = index[row * k + j];
-        const bool in = col >= 0 && col < m;
-        const float t = in ? top[row * k + j] : -INFINITY;
+__device__ __forceinline__ float exp2_of(float v) { return __builtin_amdgcn_exp2f(v); }
+__device__ __forceinline__ float log_of(float v) { return __builtin_amdgcn_logf(v) * 0.6931471805599453f; }
+
+// a_j = softmax(top / T) over the row's entries; whether there are any.  By the leading lanes.
+template <typename T, int L>
+__device__ __forceinline__ bool teacher(const Entries& e, const T* z, int64_t row, int m, const float* top, const int32_t* index, float inv_t,
+                                        int l) {
+    float mx = -INFINITY, s = 0.f;
+    for (int j = l; j < e.k; j += L) {
+        const int col = index[row * e.k + j];
+        const bool in = (unsigned)col < (unsigned)m;
+        const float t = in ? top[row * e.k + j] : -INFINITY;
         e.col[j] = in ? col : -1;
         e.log_a[j] = t;
         e.zj[j] = in ? elem(z[col]) : 0.f;
-        mx[0] = fmaxf(mx[0], t);
+        mx = fmaxf(mx, t);
     }
-    reduce_lanes<LANES, Max>(mx, room, turn);
-    for (int j = l; j < k; j += LANES) {
-        const float t = (e.log_a[j] - mx[0]) * inv_t;
+    if (l < (-e.k & 3)) {
+        e.col[e.k + l] = -1;
+        e.a[e.k + l] = 0.f;
+    }
+    mx = lanes_reduce<L, Max>(mx);
+    for (int j = l; j < e.k; j += L) {
+        const float t = (e.log_a[j] - mx) * inv_t;
+        const float a = e.col[j] < 0 || t == -INFINITY ? 0.f : exp2_of(t * kLog2e);
         e.log_a[j] = t;
-        e.a[j] = e.col[j] < 0 || t == -INFINITY ? 0.f : expf(t);
-        s[0] += e.a[j];
+        e.a[j] = a;
+        s += a;
     }
-    reduce_lanes<LANES, Add>(s, room, turn);
-    const float log_s = logf(s[0]);
-    for (int j = l; j < k; j += LANES) {
-        e.a[j] /= s[0];
+    s = lanes_reduce<L, Add>(s);
+    const float log_s = log_of(s), inv = 1.f / s;
+    for (int j = l; j < e.k; j += L) {
+        e.a[j] *= inv;
         e.log_a[j] -= log_s;
     }
-    return mx[0] != -INFINITY;
+    return mx != -INFINITY;
 }
 
-// sum over j of a_j (log a_j - (z_j - max) / T)
-template <int LANES>
-__device__ __forceinline__ float teacher_loss(const Entries& e, int k, float mx, float inv_t, int l, float* room, int* turn) {
-    float part[1] = {0.f};
-    for (int j = l; j < k; j += LANES) {
+// sum over j of a_j (log a_j - (z_j - max) / T), by the leading lanes
+template <int L>
+__device__ __forceinline__ float teacher_loss(const Entries& e, float mx, float inv_t, int l) {
+    float part = 0.f;
+    for (int j = l; j < e.k; j += L) {
         const float a = e.a[j];
-        if (a != 0.f) part[0] += a * (e.log_a[j] - (e.zj[j] - mx) * inv_t);
+        if (a != 0.f) part += a * (e.log_a[j] - (e.zj[j] - mx) * inv_t);
     }
-    reduce_lanes<LANES, Add>(part, room, turn);
-    return part[0];
+    return lanes_reduce<L, Add>(part);
 }
 
-// dz at the teacher's columns: scale * (p - the shares of all entries of the column)
-template <typename T, int LANES>
-__device__ __forceinline__ void teacher_columns(const Entries& e, T* dz, int k, float c2, float mx, float inv_sum, float scale, int l) {
-    for (int j = l; j < k; j += LANES) {
+// dz at the teacher's columns: scale * (p - the shares of all entries of the column), by the leading lanes
+template <typename T, int L>
+__device__ __forceinline__ void teacher_columns(const Entries& e, T* dz, float c2, float mx, float inv_sum, float scale, int l) {
+    for (int j = l; j < e.k; j += L) {
         const int col = e.col[j];
         if (col < 0) continue;
         float a = 0.f;
-        bool first = true;
-        for (int i = 0; i < k; ++i)
-            if (e.col[i] == col) {
-                first &= i >= j;
-                a += e.a[i];
-            }
-        if (first) dz[col] = to_elem<T>(scale * (__builtin_amdgcn_exp2f((e.zj[j] - mx) * c2) * inv_sum - a));
+        int first = j;
+        for (int i = 0; i < e.k; i += 4) {
+            const int4 c = *reinterpret_cast<const int4*>(e.col + i);
+            const float4 v = *reinterpret_cast<const float4*>(e.a + i);
+            a += c.x == col ? v.x : 0.f;
+            a += c.y == col ? v.y : 0.f;
+            a += c.z == col ? v.z : 0.f;
+            a += c.w == col ? v.w : 0.f;
+            first = min(first, c.x == col ? i : c.y == col ? i + 1 : c.z == col ? i + 2 : c.w == col ? i + 3 : j);
+        }
+        if (first == j) dz[col] = to_elem<T>(scale * (exp2_of((e.zj[j] - mx) * c2) * inv_sum - a));
     }
+}
+
+// The lanes of a row meet: LDS and memory that one wrote is there for the others
+template <int LANES>
+__device__ __forceinline__ void meet() {
+    if constexpr (LANES > 64) __syncthreads();
+    else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 }
 
 // R pieces of V logits a lane
@@ -106,13 +135,14 @@ __global__ __launch_bounds__(kBlock<LANES>) void distill_kernel(const T* z, int6
                                                                 const int32_t* __restrict__ index, int k, float inv_t, float tt,
                                                                 const float* __restrict__ weight, float each,
                                                                 double* __restrict__ partial, T* dz) {
-    constexpr int kGroups = kBlock<LANES> / LANES;
-    extern __shared__ float lds[];
+    constexpr int kGroups = kBlock<LANES> / LANES, L = kLead<LANES>;
+    extern __shared__ __attribute__((aligned(16))) float lds[];
     __shared__ float room[kReduceRoom<LANES>];
     __shared__ double losses[kGroups];
+    __shared__ int any[kGroups];
     int turn = 0;
     const int g = threadIdx.x / LANES, l = threadIdx.x % LANES;
-    const Entries e(lds + g * 4 * k, k);
+    const Entries e(lds + g * Entries::kWords * ((k + 3) & ~3), k);
     const float c2 = kLog2e * inv_t;
     double loss = 0.0;
     for (int64_t row = (int64_t)blockIdx.x * kGroups + g; row < n; row += (int64_t)gridDim.x * kGroups) {
@@ -123,7 +153,11 @@ __global__ __launch_bounds__(kBlock<LANES>) void distill_kernel(const T* z, int6
             const int col = (r * LANES + l) * V;
             if (col < m) v[r] = load_piece<T, V>(zr + col);
         }
-        const bool some = teacher<T, LANES>(e, zr, row, m, top, index, k, inv_t, l, room, &turn);
+        bool some = true;
+        if (l < L) {
+            some = teacher<T, L>(e, zr, row, m, top, index, inv_t, l);
+            if (LANES > 64 && l == 0) any[g] = some;
+        }
         float mx[1] = {-INFINITY}, sum[1] = {0.f};
 #pragma unroll
         for (int r = 0; r < R; ++r)
@@ -131,15 +165,14 @@ __global__ __launch_bounds__(kBlock<LANES>) void distill_kernel(const T* z, int6
 #pragma unroll
                 for (int i = 0; i < V; ++i) mx[0] = fmaxf(mx[0], elem(v[r].e[i]));
         reduce_lanes<LANES, Max>(mx, room, &turn);
+        if (LANES > 64) some = any[g];
 #pragma unroll
         for (int r = 0; r < R; ++r)
             if ((r * LANES + l) * V < m)
 #pragma unroll
-                for (int i = 0; i < V; ++i) sum[0] += __builtin_amdgcn_exp2f((elem(v[r].e[i]) - mx[0]) * c2);
+                for (int i = 0; i < V; ++i) sum[0] += exp2_of((elem(v[r].e[i]) - mx[0]) * c2);
         reduce_lanes<LANES, Add>(sum, room, &turn);
         const float w = weight ? weight[row] : each, inv_sum = 1.f / sum[0], scale = w * tt * inv_t;
-        const float part = teacher_loss<LANES>(e, k, mx[0], inv_t, l, room, &turn);
-        if (l == 0 && some) loss += (double)w * (double)tt * ((double)part + (double)logf(sum[0]));
         if (dz) {
 #pragma unroll
             for (int r = 0; r < R; ++r) {
@@ -147,15 +180,17 @@ __global__ __launch_bounds__(kBlock<LANES>) void distill_kernel(const T* z, int6
                 Piece<T, V> o;
 #pragma unroll
                 for (int i = 0; i < V; ++i)
-                    o.e[i] = to_elem<T>(some ? scale * (__builtin_amdgcn_exp2f((elem(v[r].e[i]) - mx[0]) * c2) * inv_sum) : 0.f);
+                    o.e[i] = to_elem<T>(some ? scale * (exp2_of((elem(v[r].e[i]) - mx[0]) * c2) * inv_sum) : 0.f);
                 if (col < m) store_piece<T, V>(dz + row * m + col, o);
             }
-            if constexpr (LANES > 64) __syncthreads();  // the row is written before its columns of the teacher are written again
-            else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            if (some) teacher_columns<T, LANES>(e, dz + row * m, k, c2, mx[0], inv_sum, scale, l);
         }
-        if constexpr (LANES > 64) __syncthreads();  // the next row's entries overwrite these
-        else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        meet<LANES>();  // the row is written before its columns of the teacher are written again
+        if (l < L) {
+            const float part = teacher_loss<L>(e, mx[0], inv_t, l);
+            if (l == 0 && some) loss += (double)w * (double)tt * ((double)part + (double)log_of(sum[0]));
+            if (dz && some) teacher_columns<T, L>(e, dz + row * m, c2, mx[0], inv_sum, scale, l);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the leading lanes alone use the entries
     }
     if (l == 0) losses[g] = loss;
     __syncthreads();
@@ -166,51 +201,97 @@ __global__ __launch_bounds__(kBlock<LANES>) void distill_kernel(const T* z, int6
     }
 }
 
-// Rows that do not fit the registers of a workgroup
-constexpr int kWide = 1024;
+// Rows that would leave a CU one workgroup if they stayed in registers: read twice, the second time from the chip's last cache, with a
+// running maximum and sum the first time.
+constexpr int kWide = 512;
 template <typename T, int V>
-__global__ __launch_bounds__(kWide) void distill_wide_kernel(const T* z, int64_t n, int m, const float* __restrict__ top,
-                                                             const int32_t* __restrict__ index, int k, float inv_t, float tt,
-                                                             const float* __restrict__ weight, float each, double* __restrict__ partial,
-                                                             T* dz) {
-    extern __shared__ float lds[];
-    __shared__ float room[kReduceRoom<kWide>];
-    int turn = 0;
+__global__ __launch_bounds__(kWide, 4) void distill_wide_kernel(const T* z, int64_t n, int m, const float* __restrict__ top,
+                                                                const int32_t* __restrict__ index, int k, float inv_t, float tt,
+                                                                const float* __restrict__ weight, float each,
+                                                                double* __restrict__ partial, T* dz) {
+    constexpr int kAhead = V == 1 ? 8 : 4;  // pieces asked for at a time
+    extern __shared__ __attribute__((aligned(16))) float lds[];
+    __shared__ float room[2][2 * kWide / 64];
+    __shared__ int any;
     const int l = threadIdx.x;
     const Entries e(lds, k);
     const float c2 = kLog2e * inv_t;
     double loss = 0.0;
-    for (int64_t row = blockIdx.x; row < n; row += gridDim.x) {
+    int turn = 0;
+    for (int64_t row = blockIdx.x; row < n; row += gridDim.x, turn ^= 1) {
         const T* zr = z + row * m;
-        const bool some = teacher<T, kWide>(e, zr, row, m, top, index, k, inv_t, l, room, &turn);
-        float mx[1] = {-INFINITY}, sum[1] = {0.f};
-        for (int64_t col = l * V; col < m; col += kWide * V) {
-            const Piece<T, V> v = load_piece<T, V>(zr + col);
-#pragma unroll
-            for (int i = 0; i < V; ++i) mx[0] = fmaxf(mx[0], elem(v.e[i]));
+        bool some = true;
+        if (l < 64) {
+            some = teacher<T, 64>(e, zr, row, m, top, index, inv_t, l);
+            if (l == 0) any = some;
         }
-        reduce_lanes<kWide, Max>(mx, room, &turn);
-        for (int64_t col = l * V; col < m; col += kWide * V) {
-            const Piece<T, V> v = load_piece<T, V>(zr + col);
+        float mx = -INFINITY, sum = 0.f;
+        for (int64_t c0 = (int64_t)l * V; c0 < m; c0 += (int64_t)kWide * V * kAhead) {
+            Piece<T, V> v[kAhead];
 #pragma unroll
-            for (int i = 0; i < V; ++i) sum[0] += __builtin_amdgcn_exp2f((elem(v.e[i]) - mx[0]) * c2);
+            for (int r = 0; r < kAhead; ++r) {
+                const int64_t col = c0 + (int64_t)r * kWide * V;
+                if (col < m) v[r] = load_piece<T, V>(zr + col);
+            }
+            float t = mx;
+#pragma unroll
+            for (int r = 0; r < kAhead; ++r)
+                if (c0 + (int64_t)r * kWide * V < m)
+#pragma unroll
+                    for (int i = 0; i < V; ++i) t = fmaxf(t, elem(v[r].e[i]));
+            const float base = t == -INFINITY ? 0.f : t;
+            sum *= exp2_of((mx - base) * c2);
+            mx = t;
+#pragma unroll
+            for (int r = 0; r < kAhead; ++r)
+                if (c0 + (int64_t)r * kWide * V < m)
+#pragma unroll
+                    for (int i = 0; i < V; ++i) sum += exp2_of((elem(v[r].e[i]) - base) * c2);
         }
-        reduce_lanes<kWide, Add>(sum, room, &turn);
-        const float w = weight ? weight[row] : each, inv_sum = 1.f / sum[0], scale = w * tt * inv_t;
-        const float part = teacher_loss<kWide>(e, k, mx[0], inv_t, l, room, &turn);
-        if (l == 0 && some) loss += (double)w * (double)tt * ((double)part + (double)logf(sum[0]));
-        if (dz) {
-            for (int64_t col = l * V; col < m; col += kWide * V) {
-                Piece<T, V> v = load_piece<T, V>(zr + col);
-#pragma unroll
-                for (int i = 0; i < V; ++i)
-                    v.e[i] = to_elem<T>(some ? scale * (__builtin_amdgcn_exp2f((elem(v.e[i]) - mx[0]) * c2) * inv_sum) : 0.f);
-                store_piece<T, V>(dz + row * m + col, v);
+        // the lanes' maxima and sums joined
+        {
+            const float top_w = lanes_reduce<64, Max>(mx), base = top_w == -INFINITY ? 0.f : top_w;
+            const float sum_w = lanes_reduce<64, Add>(sum * exp2_of((mx - base) * c2));
+            if ((l & 63) == 0) {
+                room[turn][l >> 6] = top_w;
+                room[turn][kWide / 64 + (l >> 6)] = sum_w;
             }
             __syncthreads();
-            if (some) teacher_columns<T, kWide>(e, dz + row * m, k, c2, mx[0], inv_sum, scale, l);
+            float all = -INFINITY, s = 0.f;
+#pragma unroll
+            for (int i = 0; i < kWide / 64; ++i) all = fmaxf(all, room[turn][i]);
+            const float from = all == -INFINITY ? 0.f : all;
+#pragma unroll
+            for (int i = 0; i < kWide / 64; ++i) s += room[turn][kWide / 64 + i] * exp2_of((room[turn][i] - from) * c2);
+            mx = all;
+            sum = all == -INFINITY ? NAN : s;  // nothing but -infinity: there is no softmax
+        }
+        some = any;
+        const float w = weight ? weight[row] : each, inv_sum = 1.f / sum, scale = w * tt * inv_t, p_scale = scale * inv_sum;
+        if (dz) {
+            for (int64_t c0 = (int64_t)l * V; c0 < m; c0 += (int64_t)kWide * V * kAhead) {
+                Piece<T, V> v[kAhead];
+#pragma unroll
+                for (int r = 0; r < kAhead; ++r) {
+                    const int64_t col = c0 + (int64_t)r * kWide * V;
+                    if (col < m) v[r] = load_piece<T, V>(zr + col);
+                }
+#pragma unroll
+                for (int r = 0; r < kAhead; ++r) {
+                    const int64_t col = c0 + (int64_t)r * kWide * V;
+#pragma unroll
+                    for (int i = 0; i < V; ++i) v[r].e[i] = to_elem<T>(some ? p_scale * exp2_of((elem(v[r].e[i]) - mx) * c2) : 0.f);
+                    if (col < m) store_piece<T, V>(dz + row * m + col, v[r]);
+                }
+            }
         }
         __syncthreads();
+        if (l < 64) {
+            const float part = teacher_loss<64>(e, mx, inv_t, l);
+            if (l == 0 && some) loss += (double)w * (double)tt * ((double)part + (double)log_of(sum));
+            if (dz && some) teacher_columns<T, 64>(e, dz + row * m, c2, mx, inv_sum, scale, l);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
     if (l == 0) partial[blockIdx.x] = loss;
 }
@@ -241,7 +322,7 @@ int launch(const DistillArgs& a) {
     if (!partial) return SP_ERR_ALLOC;
     const float inv_t = 1.f / a.temperature, tt = a.temperature * a.temperature, each = 1.f / (float)a.n;
     auto kernel = distill_kernel<T, V, LANES, R>;
-    hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kBlock<LANES>), (size_t)kGroups * 4 * a.k * 4, a.s, static_cast<const T*>(a.z), a.n, a.m,
+    hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kBlock<LANES>), (size_t)kGroups * Entries::kWords * ((a.k + 3) & ~3) * 4, a.s, static_cast<const T*>(a.z), a.n, a.m,
                        a.top, a.index, a.k, inv_t, tt, a.weight, each, ptr<double>(partial), static_cast<T*>(a.dz));
     return finish(a, ptr<double>(partial), blocks);
 }
@@ -253,7 +334,7 @@ int launch_wide(const DistillArgs& a) {
     if (!partial) return SP_ERR_ALLOC;
     const float inv_t = 1.f / a.temperature, tt = a.temperature * a.temperature, each = 1.f / (float)a.n;
     auto kernel = distill_wide_kernel<T, V>;
-    hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kWide), (size_t)4 * a.k * 4, a.s, static_cast<const T*>(a.z), a.n, a.m, a.top, a.index, a.k,
+    hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kWide), (size_t)Entries::kWords * ((a.k + 3) & ~3) * 4, a.s, static_cast<const T*>(a.z), a.n, a.m, a.top, a.index, a.k,
                        inv_t, tt, a.weight, each, ptr<double>(partial), static_cast<T*>(a.dz));
     return finish(a, ptr<double>(partial), blocks);
 }
@@ -268,8 +349,6 @@ int sized(const DistillArgs& a) {
     if (pieces <= 256) return launch<T, V, 64, 4>(a);
     if (pieces <= 1024) return launch<T, V, 256, 4>(a);
     if (pieces <= 4096) return launch<T, V, 256, 16>(a);
-    if (pieces <= 8192) return launch<T, V, 1024, 8>(a);
-    if (pieces <= 16384) return launch<T, V, 1024, 16>(a);
     return launch_wide<T, V>(a);
 }
 

@@ -46,6 +46,29 @@ struct Max {
     static constexpr float none = -INFINITY;
 };
 
+// A value from another lane of the same 4, 8 or 16, without LDS.  All of them must be active.
+template <int CTRL>
+__device__ __forceinline__ float from_lane(float v) {
+    return __uint_as_float(__builtin_amdgcn_update_dpp(0u, __float_as_uint(v), CTRL, 0xf, 0xf, true));
+}
+// v reduced over LANES (4 to 64) neighbouring lanes, in all of them
+template <int LANES, typename Op>
+__device__ __forceinline__ float lanes_reduce(float v) {
+    v = Op::of(v, from_lane<0xB1>(v));                        // the neighbour (quad_perm 1 0 3 2)
+    v = Op::of(v, from_lane<0x4E>(v));                        // the other pair (2 3 0 1)
+    if constexpr (LANES >= 8) v = Op::of(v, from_lane<0x141>(v));   // the other half of 8 (mirrored)
+    if constexpr (LANES >= 16) v = Op::of(v, from_lane<0x140>(v));  // of 16
+    if constexpr (LANES >= 32) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = Op::of(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    }
+    if constexpr (LANES >= 64) {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = Op::of(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    }
+    return v;
+}
+
 // N <= 2 values reduced over LANES threads that share a row: neighbouring lanes of a wavefront, or a whole workgroup of LANES
 // threads (then `room` has kReduceRoom<LANES> floats, used in halves by turns, so that one barrier a call is enough).  Every lane
 // gets the results, in an order of operations that does not change.
@@ -55,9 +78,7 @@ template <int LANES, typename Op, int N>
 __device__ __forceinline__ void reduce_lanes(float (&v)[N], float* room, int* turn) {
     static_assert(N <= 2, "room for two values a wavefront");
 #pragma unroll
-    for (int s = (LANES < 64 ? LANES : 64) / 2; s > 0; s >>= 1)
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = Op::of(v[i], __shfl_xor(v[i], s));
+    for (int i = 0; i < N; ++i) v[i] = lanes_reduce<(LANES < 64 ? LANES : 64), Op>(v[i]);
     if constexpr (LANES > 64) {
         constexpr int kWaves = LANES / 64;
         float* r = room + *turn * 2 * kWaves;
