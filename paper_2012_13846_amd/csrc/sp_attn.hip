@@ -39,26 +39,26 @@ struct Reach {
     }
 };
 
-// Whether a lane's row sees the keys of a tile, by the key's number in the tile
+// Whether a lane's row sees the keys of a tile, by the key's number in the tile (8 g + i: the lane's half is in the borders): a range,
+// and the first `head` of them where the tile has first keys (`heads`).  First keys before a gap are seen by every row of the workgroup:
+// the window of its first row begins behind them.  Without a gap a slot is its key, and its border is the range's upper one too.
 struct SeenInTile {
-    const Window& w;
-    const Reach& reach;
-    int slot, p, low;
+    int low, head;
     uint32_t width;
-    bool plain;  // keys one after another, none of the first: one range
-    __device__ __forceinline__ SeenInTile(const Window& w_, const Reach& reach_, int slot_, int p_) : w(w_), reach(reach_), slot(slot_), p(p_) {
-        const int k = reach.key(slot);
-        plain = (slot >= reach.first) & (k >= w.sinks);
-        low = p - w.left - k;
+    bool heads;
+    __device__ __forceinline__ SeenInTile(const Window& w, const Reach& reach, int slot, int p) {
+        const int half = 4 * ((int)(threadIdx.x & 63) >> 5), k = slot + reach.lo - reach.first;
         const int high = min(p + w.right - k, reach.n - slot - 1);
+        low = p - w.left - k;
         width = high >= low ? (uint32_t)(high - low) + 1 : 0;
-        low += 4 * ((int)(threadIdx.x & 63) >> 5) * -1;  // of the lane's half: element i of group g is key 8 g + i then
+        const bool gap = reach.lo >= w.sinks;
+        head = gap ? reach.first - slot : min(w.sinks - slot, high + 1);
+        heads = (gap ? reach.first : w.sinks) > slot;
+        low -= half;
+        head -= half;
     }
-    __device__ __forceinline__ bool operator()(int r) const { return (uint32_t)(r - low) < width; }
-    __device__ __forceinline__ bool slow(int r) const {
-        const int at = slot + r + 4 * ((int)(threadIdx.x & 63) >> 5), k = reach.key(at);
-        return (at < reach.n) & (k <= p + w.right) & ((k >= p - w.left) | (k < w.sinks));
-    }
+    __device__ __forceinline__ bool in_range(int r) const { return (uint32_t)(r - low) < width; }
+    __device__ __forceinline__ bool sees(int r) const { return in_range(r) | (r < head); }
 };
 
 __device__ __forceinline__ float exponent_scale(const Window& w) {
@@ -141,7 +141,7 @@ struct KeyTiles {
 };
 
 template <typename T, int NT, bool VEC>
-__global__ __launch_bounds__(kThreads, 2) void attn_fwd_kernel(AttnFwd<T> f, int tiles) {
+__global__ __launch_bounds__(kThreads, NT <= 2 ? 3 : 2) void attn_fwd_kernel(AttnFwd<T> f, int tiles) {
     using Tl = Tile<T, NT>;
     constexpr int kN = kKeys<T>, kB = kN / 32, kTileBytes = kN * Tl::kRowBytes;
     __shared__ __attribute__((aligned(1024))) char lds[4 * kTileBytes];  // keys and values, two of each
@@ -184,18 +184,18 @@ __global__ __launch_bounds__(kThreads, 2) void attn_fwd_kernel(AttnFwd<T> f, int
                 for (int b = 0; b < kB; ++b) s[b] = Tl::mma(Tl::direct(keys, pl, b, st), q[st], s[b]);
             if (again || !(wr.whole & reach.all(w, slot, kN, wr.p_min, wr.p_max))) {
                 const SeenInTile seen(w, reach, slot, wr.p);
-                if (!again && seen.plain) {
+                if (!again && !seen.heads) {
 #pragma unroll
                     for (int b = 0; b < kB; ++b)
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) s[b][i] = seen(b * 32 + 8 * (i / 4) + i % 4) ? s[b][i] : -INFINITY;
+                        for (int i = 0; i < 16; ++i) s[b][i] = seen.in_range(b * 32 + 8 * (i / 4) + i % 4) ? s[b][i] : -INFINITY;
                 } else {
 #pragma unroll
                     for (int b = 0; b < kB; ++b)
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
                             const int r = b * 32 + 8 * (i / 4) + i % 4;
-                            const bool sees = seen.slow(r);
+                            const bool sees = seen.sees(r);
                             s[b][i] = sees ? s[b][i] : -INFINITY;
                             if constexpr (again) met |= sees & (marks[r + 4 * (lane >> 5)] != 0);
                         }
@@ -275,7 +275,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_fwd_kernel(AttnFwd<T> f, int
 // second step.
 
 template <typename T, int NT, bool VEC>
-__global__ __launch_bounds__(kThreads, sizeof(T) * NT < 16 ? 2 : 1) void attn_dq_kernel(AttnBwd<T> g, int tiles) {
+__global__ __launch_bounds__(kThreads, NT == 1 ? 4 : sizeof(T) * NT == 4 ? 3 : sizeof(T) * NT < 16 ? 2 : 1) void attn_dq_kernel(AttnBwd<T> g, int tiles) {
     using Tl = Tile<T, NT>;
     constexpr int kN = kKeys<T>, kB = kN / 32, kTileBytes = kN * Tl::kRowBytes;
     __shared__ __attribute__((aligned(1024))) char lds[4 * kTileBytes];
@@ -331,14 +331,14 @@ __global__ __launch_bounds__(kThreads, sizeof(T) * NT < 16 ? 2 : 1) void attn_dq
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c2, -l2)) * (dp[i] - delta);
                 if (!all) {
-                    if (!again && seen.plain) {
+                    if (!again && !seen.heads) {
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) s[i] = seen(b * 32 + 8 * (i / 4) + i % 4) ? s[i] : 0.f;
+                        for (int i = 0; i < 16; ++i) s[i] = seen.in_range(b * 32 + 8 * (i / 4) + i % 4) ? s[i] : 0.f;
                     } else {
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
                             const int r = b * 32 + 8 * (i / 4) + i % 4;
-                            const bool sees = seen.slow(r);
+                            const bool sees = seen.sees(r);
                             s[i] = sees ? s[i] : 0.f;
                             if constexpr (again) met |= sees & (marks[r + 4 * (lane >> 5)] != 0);
                         }
@@ -444,11 +444,11 @@ __device__ __forceinline__ RowStat row_stat(const AttnBwd<T>& g, const Cloud& c,
 }
 template <int N>
 struct RowStats {
-    __attribute__((aligned(16))) float l2[N], delta[N];
+    __attribute__((aligned(16))) float l2[N], minus_delta[N];
     __attribute__((aligned(16))) int p[N];
     __device__ __forceinline__ void put(const RowStat& r, int at) {
         l2[at] = r.l2;
-        delta[at] = r.delta;
+        minus_delta[at] = -r.delta;
         p[at] = r.p;
     }
 };
@@ -466,7 +466,13 @@ struct KeyGrads {
     __device__ __forceinline__ void add(const char* q, const char* dout, const RowStats<N>& stats, const typename Tl::Place& pl, int b, float c2,
                                         bool all, Seen seen) {
         const int half = b * 32 + 4 * ((threadIdx.x & 63) >> 5);
-        f32x16 s = {}, dp = {};
+        f32x16 s = {}, dp;  // dp begins at -delta
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const f32x4 de = *reinterpret_cast<const f32x4*>(stats.minus_delta + half + 8 * g);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) dp[4 * g + i] = de[i];
+        }
 #pragma unroll
         for (int st = 0; st < Tl::kSteps; ++st) {
             s = Tl::mma(Tl::direct(q, pl, b, st), k[st], s);
@@ -474,11 +480,11 @@ struct KeyGrads {
         }
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-            const f32x4 l = *reinterpret_cast<const f32x4*>(stats.l2 + half + 8 * g), de = *reinterpret_cast<const f32x4*>(stats.delta + half + 8 * g);
+            const f32x4 l = *reinterpret_cast<const f32x4*>(stats.l2 + half + 8 * g);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 s[4 * g + i] = __builtin_amdgcn_exp2f(fmaf(s[4 * g + i], c2, -l[i]));
-                dp[4 * g + i] = s[4 * g + i] * (dp[4 * g + i] - de[i]);
+                dp[4 * g + i] *= s[4 * g + i];
             }
         }
         if (!all)
@@ -507,10 +513,10 @@ struct KeyGrads {
 template <typename T, int NT>
 constexpr bool kValuesInLds = sizeof(T) == 2 && NT >= 3;
 template <typename T, int NT>
-constexpr int kStepRows = sizeof(T) == 2 && !kValuesInLds<T, NT> ? 64 : 32;
+constexpr int kStepRows = sizeof(T) == 2 && NT <= 2 ? 64 : 32;
 
 template <typename T, int NT, bool VEC>
-__global__ __launch_bounds__(kThreads, sizeof(T) * NT <= 8 ? 2 : 1) void attn_dkv_kernel(AttnBwd<T> g, Split split, int tiles) {
+__global__ __launch_bounds__(kThreads, NT == 1 ? (sizeof(T) == 2 ? 4 : 3) : sizeof(T) * NT == 4 ? 3 : sizeof(T) * NT <= 8 ? 2 : 1) void attn_dkv_kernel(AttnBwd<T> g, Split split, int tiles) {
     using Tl = Tile<T, NT>;
     constexpr bool kVLds = kValuesInLds<T, NT>;
     constexpr int kN = kStepRows<T, NT>, kB = kN / 32, kTileBytes = kN * Tl::kRowBytes;
@@ -586,7 +592,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) * NT <= 8 ? 2 : 1) void attn_dk
             const bool none = (jw >= c.b) | (jw > p_max + w.right) | ((jw + kWaveRows - 1 < p_min - w.left) & (jw >= sinks));
             const bool all = !again && ((row + kN <= end) & (qt.step == kN) & (jw + kWaveRows - 1 <= p_min + w.right) & (jw >= p_max - w.left));
             if (!none)
-#pragma unroll
+#pragma unroll 1
                 for (int b = 0; b < kB; ++b)
                     kg.add(q, dout, stats[buf], pl, b, c2, all, [&](int p, int r) {
                         const bool seen = (uint32_t)(p - low) <= width;
@@ -674,25 +680,37 @@ __global__ __launch_bounds__(64, 1) void attn_far_kernel(AttnBwd<T> g, Split spl
     }
 }
 
-// a wavefront a cloud, key head and one of the first keys
+// a workgroup a cloud, key head and one of the first keys: every wavefront a quarter of the chunks
 template <typename T>
-__global__ __launch_bounds__(64) void attn_join_kernel(AttnBwd<T> g, Split split) {
+__global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnBwd<T> g, Split split) {
+    __shared__ float sums[4][2 * kMaxDim];
     const Window& w = g.w;
-    const int cn = (int)blockIdx.x + 1, kh = blockIdx.y, j = blockIdx.z, lane = threadIdx.x;
+    const int cn = (int)blockIdx.x + 1, kh = blockIdx.y, j = blockIdx.z, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const Cloud c(w, cn);
     if (j >= c.b) return;
     const int64_t t0 = first_tile(w.q_starts, w.clouds, w.n_q, cn, w.group, split.chunk), rows = (int64_t)c.a * w.group;
     const int64_t far0 = far_begin(w, c, j / 32 * 32);
     // chunks with a row behind far0 were written
     const int64_t u0 = min(far0, rows) / split.chunk, u1 = far0 < rows ? (rows + split.chunk - 1) / split.chunk : u0;
+    const int64_t quarter = (u1 - u0 + 3) / 4, v0 = min(u0 + wave * quarter, u1), v1 = min(v0 + quarter, u1);
+    const float* far = split.far + split_at(w, split, t0, kh, j);
+    const int64_t step = split_at(w, split, 1, 0, 0);
+    for (int at = lane; at < 2 * w.dim; at += 64) {
+        float s = 0.f;
+#pragma unroll 16
+        for (int64_t u = v0; u < v1; ++u) s += far[u * step + at];
+        sums[wave][at] = s;
+    }
+    __syncthreads();
+    if (wave) return;
+    const float* first = split.first + split_at(w, split, cn - 1, kh, j);
     float sum[2][2] = {}, check = 0.f;
     for (int q = 0; q < 2; ++q)
         for (int e = 0; e < 2; ++e)
             if (lane + 64 * e < w.dim) {
                 const int at = q * w.dim + lane + 64 * e;
-                float s = split.first[split_at(w, split, cn - 1, kh, j) + at];
-#pragma unroll 8
-                for (int64_t u = u0; u < u1; ++u) s += split.far[split_at(w, split, t0 + u, kh, j) + at];
+                float s = first[at];
+                for (int k = 0; k < 4; ++k) s += sums[k][at];
                 sum[q][e] = s;
                 check = fmaf(s, 0.f, check);
             }
@@ -733,7 +751,9 @@ int backward_sized(AttnBwd<T> g, hipStream_t s) {
     Buf delta = dev_alloc((size_t)w.n_q * w.heads * 4, s), parts;
     if (!delta) return SP_ERR_ALLOC;
     g.delta = ptr<float>(delta);
-    Split split{0, (1024 + w.group - 1) / w.group * w.group, nullptr, nullptr};
+    // rows a wavefront: what it writes is an eighth of what it reads at most
+    const int chunk = std::max(512, 8 * (w.sinks <= kSplitSinks ? w.sinks : 0));
+    Split split{0, (chunk + w.group - 1) / w.group * w.group, nullptr, nullptr};
     const int groups = (w.sinks + 31) / 32;
     int64_t chunks = 0;
     if (w.sinks > 0 && w.sinks <= kSplitSinks && w.n_q > 0 && w.clouds > 0 && w.n_k - w.left > 2048) {
@@ -751,7 +771,7 @@ int backward_sized(AttnBwd<T> g, hipStream_t s) {
         hipLaunchKernelGGL((attn_dkv_kernel<T, NT, VEC>), dim3((unsigned)(k_tiles * w.kv_heads)), dim3(kThreads), 0, s, g, split, (int)k_tiles);
     if (split.sinks) {
         hipLaunchKernelGGL((attn_far_kernel<T, NT, VEC>), dim3((unsigned)(chunks * w.kv_heads * groups)), dim3(64), 0, s, g, split, (int)chunks);
-        hipLaunchKernelGGL(attn_join_kernel<T>, dim3(w.clouds, w.kv_heads, split.sinks), dim3(64), 0, s, g, split);
+        hipLaunchKernelGGL(attn_join_kernel<T>, dim3(w.clouds, w.kv_heads, split.sinks), dim3(kThreads), 0, s, g, split);
     }
     SP_HIP(hipGetLastError());
     return SP_OK;

@@ -344,7 +344,7 @@ int launch_wide(const DistillArgs& a) {
 template <typename T, int V>
 int sized(const DistillArgs& a) {
     const int pieces = (a.m + V - 1) / V;
-    if (pieces <= 16 && a.k <= 64) return launch<T, V, 16, 1>(a);
+    if (pieces <= 16 && a.k <= 32) return launch<T, V, 8, 2>(a);
     if (pieces <= 64 && a.k <= 64) return launch<T, V, 16, 4>(a);
     if (pieces <= 256) return launch<T, V, 64, 4>(a);
     if (pieces <= 1024) return launch<T, V, 256, 4>(a);
