@@ -558,7 +558,7 @@ def _token_argtypes():
 
 
 def _need_shape(t: torch.Tensor, shape, name: str):
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{name} must have the shape {tuple(shape)}, not {tuple(t.shape)}")
 
 
@@ -589,10 +589,10 @@ def _head_rows(t: torch.Tensor, dtype, name: str):
     """[rows][heads][dim] whose heads lie one after another in a row; rows may be further apart (a view of a fused projection)."""
     if not t.is_cuda or t.ndim != 3 or t.dtype != dtype:
         raise ValueError(f"{name} must be a CUDA tensor [rows][heads][dim] of {dtype}")
-    n, h, d = t.shape
-    if (t.stride(2) != 1 and d > 1) or (t.stride(1) != d and h > 1) or (n > 1 and t.stride(0) < h * d):
+    (n, h, d), (sn, sh, sd) = t.shape, t.stride()
+    if (sd != 1 and d > 1) or (sh != d and h > 1) or (n > 1 and sn < h * d):
         raise ValueError(f"the heads of a row of {name} must lie one after another, and rows must not overlap")
-    return t.data_ptr(), (t.stride(0) if n > 1 else h * d)
+    return t.data_ptr(), (sn if n > 1 else h * d)
 
 
 def _window(q, k, v, q_starts, k_starts, left, right, sinks, scale):

@@ -43,6 +43,9 @@ struct AttnBwd {
     Rows<T> dq, dk, dv;
 };
 
+template <typename T>
+int attn_backward(const AttnBwd<T>& g, hipStream_t s);  // sp_attn_bwd.hip
+
 // Clouds 1 .. clouds are the caller's; 0 and clouds + 1 hold the rows before the first and after the last.
 __device__ __forceinline__ int cloud_begin(const int32_t* starts, int clouds, int n, int c) {
     if (c <= 0) return 0;

@@ -1,161 +1,27 @@
-// Attention with a sliding window and a few first rows that stay visible, over packed clouds: forward pass and gradients.
+// Attention with a sliding window and a few first rows that stay visible, over packed clouds: the forward pass (sp_attn_bwd.hip: the gradients).
 #include <algorithm>
 
-#include "sp_attn_tile.h"
+#include "sp_attn_rows.h"
 
 namespace sp {
 namespace {
 
-constexpr int kThreads = 256;
-
-// ---- forward -------------------------------------------------------------------------------------------------------
-// A workgroup has 128 rows of one key head: a row is a query and one of the `group` query heads that share the key head, so that keys
-// and values in LDS serve all of them and a tile of few queries sees few keys.  A wavefront has 32 of these rows, and goes over the
-// keys that any row of the workgroup sees, 64 (bf16) or 32 (fp32) at a time; the next keys are on their way to LDS meanwhile.
-template <typename T>
-constexpr int kKeys = sizeof(T) == 2 ? 64 : 32;
-constexpr int kRows = 128;  // a workgroup's
-constexpr int kWaveRows = 32;
-constexpr int kNowhere = -(1 << 30);  // the position of a row that is none: sees nothing
-
-// What a workgroup's rows see: the slots of its tiles are the first keys, then a stretch.
-struct Reach {
-    int first, lo, n;
-    __device__ __forceinline__ Reach(const Window& w, const Cloud& c, int p_min, int p_max) {
-        const int hi = c.partners ? min(max(p_max + w.right + 1, 0), c.b) : 0;
-        lo = min(max(p_min - w.left, 0), hi);
-        first = min(w.sinks, lo);
-        n = first + hi - lo;
-    }
-    __device__ __forceinline__ int key(int slot) const { return slot + (slot < first ? 0 : lo - first); }
-    // whether rows at positions p_min .. p_max see all (none) of the `count` keys from `slot` on
-    __device__ __forceinline__ bool all(const Window& w, int slot, int count, int p_min, int p_max) const {
-        const int k = key(slot);
-        return (slot >= first) & (slot + count <= n) & (k >= p_max - w.left) & (k + count - 1 <= p_min + w.right);
-    }
-    __device__ __forceinline__ bool none(const Window& w, int slot, int count, int p_min, int p_max) const {
-        const int k = key(slot);
-        return (k >= w.sinks) & ((k > p_max + w.right) | (k + count - 1 < p_min - w.left));
-    }
-};
-
-// Whether a lane's row sees the keys of a tile, by the key's number in the tile (8 g + i: the lane's half is in the borders): a range,
-// and the first `head` of them where the tile has first keys (`heads`).  First keys before a gap are seen by every row of the workgroup:
-// the window of its first row begins behind them.  Without a gap a slot is its key, and its border is the range's upper one too.
-struct SeenInTile {
-    int low, head;
-    uint32_t width;
-    bool heads;
-    __device__ __forceinline__ SeenInTile(const Window& w, const Reach& reach, int slot, int p) {
-        const int half = 4 * ((int)(threadIdx.x & 63) >> 5), k = slot + reach.lo - reach.first;
-        const int high = min(p + w.right - k, reach.n - slot - 1);
-        low = p - w.left - k;
-        width = high >= low ? (uint32_t)(high - low) + 1 : 0;
-        const bool gap = reach.lo >= w.sinks;
-        head = gap ? reach.first - slot : min(w.sinks - slot, high + 1);
-        heads = (gap ? reach.first : w.sinks) > slot;
-        low -= half;
-        head -= half;
-    }
-    __device__ __forceinline__ bool in_range(int r) const { return (uint32_t)(r - low) < width; }
-    __device__ __forceinline__ bool sees(int r) const { return in_range(r) | (r < head); }
-};
-
-__device__ __forceinline__ float exponent_scale(const Window& w) {
-    // exp2 of score * this; not quite zero for a scale of zero, so that a hidden key's -infinity stays one.  The scale's sign is the
-    // operand's: rows are negated when they are loaded.
-    return fmaxf(fabsf(w.scale) * kLog2e, 1e-30f);
-}
-
-// A workgroup's tile of rows
-struct RowTile {
-    int kh, cloud;
-    int64_t r0;
-    __device__ __forceinline__ RowTile(const Window& w, int tiles) {
-        const uint32_t item = item_of_block(blockIdx.x, gridDim.x), t = item % (uint32_t)tiles;
-        kh = (int)(item / (uint32_t)tiles);
-        cloud = cloud_of_tile(w.q_starts, w.clouds, w.n_q, t, w.group, kRows);
-        r0 = (t - first_tile(w.q_starts, w.clouds, w.n_q, cloud, w.group, kRows)) * kRows;
-    }
-};
-
-// A lane's row of a workgroup's tile, its wavefront's positions and what the workgroup sees.  (Rows of a cloud are counted from its
-// first; a cloud has at most 2^31 of them.)
-struct WaveRows {
-    uint32_t w0;       // the wavefront's first row
-    bool there, whole; // this lane's row exists; all of the wavefront's do
-    int query, head, p;
-    int p_min, p_max;  // of the wavefront; one that has no row sees nothing
-    Reach reach;
-    __device__ __forceinline__ WaveRows(const Window& w, const Cloud& c, uint32_t r0, uint32_t rows)
-        : reach(w, c, (int)(r0 / w.group) + c.off, (int)((min(r0 + kRows, rows) - 1) / w.group) + c.off) {
-        w0 = r0 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * kWaveRows;
-        const uint32_t row = w0 + (threadIdx.x & 31);
-        there = row < rows;
-        whole = w0 + kWaveRows <= rows;
-        query = (int)(row / w.group);
-        head = (int)(row % w.group);
-        p = there ? query + c.off : kNowhere;
-        p_min = w0 < rows ? (int)(w0 / w.group) + c.off : kNowhere;
-        p_max = w0 < rows ? (int)((min(w0 + kWaveRows, rows) - 1) / w.group) + c.off : kNowhere;
-    }
-};
-
-// The keys and values of a workgroup's slots, kN at a time, into LDS
-template <typename T, int NT, bool VEC>
-struct KeyTiles {
-    static constexpr int kN = kKeys<T>, kTileBytes = kN * Tile<T, NT>::kRowBytes;
-    const Window& w;
-    const Reach& reach;
-    const T *k, *v;  // the cloud's first rows of this key head
-    uint32_t ldk, ldv;  // bytes between rows
-    int64_t ldk_elements, ldv_elements;
-    TileLoads<T, NT, kN, kThreads> lk, lv;
-    __device__ __forceinline__ KeyTiles(const Window& w_, const Reach& reach_, const Rows<const T>& k_, const Rows<const T>& v_, const Cloud& c, int kh)
-        : w(w_), reach(reach_), k(k_.at(c.k0, kh, w_.dim)), v(v_.at(c.k0, kh, w_.dim)), ldk((uint32_t)(k_.ld * sizeof(T))),
-          ldv((uint32_t)(v_.ld * sizeof(T))), ldk_elements(k_.ld), ldv_elements(v_.ld) {
-        if constexpr (VEC) {
-            lk.place(w.dim, [&](int r) { return r * ldk; });
-            lv.place(w.dim, [&](int r) { return r * ldv; });
-        }
-    }
-    __device__ __forceinline__ void one(char* tile, const TileLoads<T, NT, kN, kThreads>& l, const T* p, uint32_t ld, int64_t ld_elements, int slot) const {
-        const uint32_t row = w.dim * (uint32_t)sizeof(T);
-        if constexpr (VEC) {
-            const uint32_t at = lds_address(tile);
-            if (slot >= reach.first) {
-                l.load(at, memory_of(p + reach.key(slot) * ld_elements, (min(kN, reach.n - slot) - 1) * ld + row));
-            } else {
-                const int split = min(kN, reach.first - slot), rest = min(kN, reach.n - slot) - split;
-                l.load_two(at, memory_of(p + slot * ld_elements, (split - 1) * ld + row), split,
-                           memory_of(p + reach.lo * ld_elements, rest > 0 ? (rest - 1) * ld + row : 0), split * ld);
-            }
-        } else {
-            load_elements<T, NT, kN, kThreads>(tile, w.dim, [&](int r) { return slot + r < reach.n ? p + reach.key(slot + r) * ld_elements : nullptr; });
-        }
-    }
-    __device__ __forceinline__ void load(char* lds, int slot, int buf) const {
-        one(lds + buf * 2 * kTileBytes, lk, k, ldk, ldk_elements, slot);
-        one(lds + (buf * 2 + 1) * kTileBytes, lv, v, ldv, ldv_elements, slot);
-    }
-};
-
-template <typename T, int NT, bool VEC>
-__global__ __launch_bounds__(kThreads, NT <= 2 ? 3 : 2) void attn_fwd_kernel(AttnFwd<T> f, int tiles) {
+template <typename T, int NT, bool VEC, int W>
+__global__ __launch_bounds__(64 * W, NT <= 2 ? 3 : 2) void attn_fwd_kernel(AttnFwd<T> f, int tiles) {
     using Tl = Tile<T, NT>;
-    constexpr int kN = kKeys<T>, kB = kN / 32, kTileBytes = kN * Tl::kRowBytes;
+    constexpr int kN = kKeys<T, W>, kB = kN / 32, kTileBytes = kN * Tl::kRowBytes;
     __shared__ __attribute__((aligned(1024))) char lds[4 * kTileBytes];  // keys and values, two of each
     __shared__ int marks[kN];
     const Window& w = f.w;
-    const RowTile rt(w, tiles);
+    const RowTile<W> rt(w, tiles);
     const Cloud c(w, rt.cloud);
     const int64_t rows = (int64_t)c.a * w.group;
     if (rt.r0 >= rows) return;
-    const WaveRows wr(w, c, (uint32_t)rt.r0, (uint32_t)rows);
+    const WaveRows<W> wr(w, c, (uint32_t)rt.r0, (uint32_t)rows);
     const Reach& reach = wr.reach;
     const int lane = threadIdx.x & 63, kh = rt.kh, h = kh * w.group + wr.head;
     const auto pl = Tl::place();
-    const KeyTiles<T, NT, VEC> kt(w, reach, f.k, f.v, c, kh);
+    const KeyTiles<T, NT, VEC, W> kt(w, reach, f.k, f.v, c, kh);
     if (reach.n > 0) kt.load(lds, 0, 0);
     typename Tl::Frag q[Tl::kSteps];
     Tl::template load_row<VEC>(q, f.q.at(c.q0 + wr.query, h, w.dim), w.dim, wr.there, w.scale < 0.f);
@@ -175,7 +41,7 @@ __global__ __launch_bounds__(kThreads, NT <= 2 ? 3 : 2) void attn_fwd_kernel(Att
             char *keys = lds + buf * 2 * kTileBytes, *values = keys + kTileBytes;
             wait_tiles();
             if (slot + kN < reach.n) kt.load(lds, slot + kN, buf ^ 1);
-            if constexpr (again) clean_tiles<T, NT, kN, kThreads>(keys, values, marks);
+            if constexpr (again) clean_tiles<T, NT, kN, 64 * W>(keys, values, marks);
             if (reach.none(w, slot, kN, wr.p_min, wr.p_max)) continue;
             f32x16 s[kB] = {};
 #pragma unroll
@@ -269,521 +135,28 @@ __global__ __launch_bounds__(kThreads, NT <= 2 ? 3 : 2) void attn_fwd_kernel(Att
     }
 }
 
-// ---- gradients -----------------------------------------------------------------------------------------------------
-// Two kernels compute the scores again, each for what it can sum without atomics: dq by rows like the forward pass (and delta = dout . o
-// on the way), dk and dv by keys.  The second goes over the rows of all query heads that share the key head, so their sum needs no
-// second step.
-
-template <typename T, int NT, bool VEC>
-__global__ __launch_bounds__(kThreads, NT == 1 ? 4 : sizeof(T) * NT == 4 ? 3 : sizeof(T) * NT < 16 ? 2 : 1) void attn_dq_kernel(AttnBwd<T> g, int tiles) {
-    using Tl = Tile<T, NT>;
-    constexpr int kN = kKeys<T>, kB = kN / 32, kTileBytes = kN * Tl::kRowBytes;
-    __shared__ __attribute__((aligned(1024))) char lds[4 * kTileBytes];
-    __shared__ int marks[kN];
-    const Window& w = g.w;
-    const RowTile rt(w, tiles);
-    const Cloud c(w, rt.cloud);
-    const int64_t rows = (int64_t)c.a * w.group;
-    if (rt.r0 >= rows) return;
-    const WaveRows wr(w, c, (uint32_t)rt.r0, (uint32_t)rows);
-    const Reach& reach = wr.reach;
-    const int lane = threadIdx.x & 63, kh = rt.kh, h = kh * w.group + wr.head;
-    const auto pl = Tl::place();
-    const KeyTiles<T, NT, VEC> kt(w, reach, g.k, g.v, c, kh);
-    if (reach.n > 0) kt.load(lds, 0, 0);
-    typename Tl::Frag q[Tl::kSteps], dout[Tl::kSteps];
-    Tl::template load_row<VEC>(q, g.q.at(c.q0 + wr.query, h, w.dim), w.dim, wr.there, w.scale < 0.f);
-    Tl::template load_row<VEC>(dout, g.dout.at(c.q0 + wr.query, h, w.dim), w.dim, wr.there, false);
-    float delta = 0.f;
-    {
-        typename Tl::Frag o[Tl::kSteps];
-        Tl::template load_row<VEC>(o, g.o.at(c.q0 + wr.query, h, w.dim), w.dim, wr.there, false);
-#pragma unroll
-        for (int st = 0; st < Tl::kSteps; ++st)
-#pragma unroll
-            for (int i = 0; i < Tl::kPer; ++i) delta = fmaf((float)o[st][i], (float)dout[st][i], delta);
-        delta = halves<Add>(delta);
-    }
-    const int64_t stat = (int64_t)(c.q0 + wr.query) * w.heads + h;
-    if (wr.there && lane < 32) g.delta[stat] = delta;
-    const float l2 = wr.there ? g.lse[stat] * kLog2e : 0.f, c2 = exponent_scale(w);
-    f32x16 acc[NT];
-    bool met = false;
-    auto pass = [&](auto again) {  // as in the forward pass
-#pragma unroll
-        for (int d = 0; d < NT; ++d) acc[d] = f32x16{};
-        for (int slot = 0, buf = 0; slot < reach.n; slot += kN, buf ^= 1) {
-            char *keys = lds + buf * 2 * kTileBytes, *values = keys + kTileBytes;
-            wait_tiles();
-            if (slot + kN < reach.n) kt.load(lds, slot + kN, buf ^ 1);
-            if constexpr (again) clean_tiles<T, NT, kN, kThreads>(keys, values, marks);
-            if (reach.none(w, slot, kN, wr.p_min, wr.p_max)) continue;
-            const bool all = !again && (wr.whole & reach.all(w, slot, kN, wr.p_min, wr.p_max));
-            const SeenInTile seen(w, reach, slot, wr.p);
-#pragma unroll
-            for (int b = 0; b < kB; ++b) {
-                f32x16 s = {}, dp = {};
-#pragma unroll
-                for (int st = 0; st < Tl::kSteps; ++st) {
-                    s = Tl::mma(Tl::direct(keys, pl, b, st), q[st], s);
-                    dp = Tl::mma(Tl::direct(values, pl, b, st), dout[st], dp);
-                }
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c2, -l2)) * (dp[i] - delta);
-                if (!all) {
-                    if (!again && !seen.heads) {
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) s[i] = seen.in_range(b * 32 + 8 * (i / 4) + i % 4) ? s[i] : 0.f;
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const int r = b * 32 + 8 * (i / 4) + i % 4;
-                            const bool sees = seen.sees(r);
-                            s[i] = sees ? s[i] : 0.f;
-                            if constexpr (again) met |= sees & (marks[r + 4 * (lane >> 5)] != 0);
-                        }
-                    }
-                }
-#pragma unroll
-                for (int st = 0; st < Tl::kTSteps; ++st) {
-                    const auto ds = Tl::operand(s, st);
-#pragma unroll
-                    for (int d = 0; d < NT; ++d) acc[d] = Tl::mma(Tl::turned(keys, pl, b, st, d), ds, acc[d]);
-                }
-            }
-        }
-        float check = 0.f;
-#pragma unroll
-        for (int d = 0; d < NT; ++d)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) check = fmaf(acc[d][i] *= w.scale, 0.f, check);
-        return __syncthreads_or(wr.there & (halves<Add>(check) != 0.f));
-    };
-    if (pass(std::false_type{})) {
-        kt.load(lds, 0, 0);
-        pass(std::true_type{});
-    }
-    const uint64_t seen_by = __ballot(wr.there && met);
-    const uint32_t by_row = (uint32_t)seen_by | (uint32_t)(seen_by >> 32);
-    if (wr.there && !(by_row >> (lane & 31) & 1)) put_column<T, NT, VEC>(g.dq.at(c.q0 + wr.query, h, w.dim), acc, w.dim);
-    __threadfence_block();  // delta, which other lanes read
-    for (uint32_t bad = by_row; bad; bad &= bad - 1) {
-        const uint32_t r = wr.w0 + __builtin_ctz(bad);
-        query_gradient_row(g, c, (int)(r / w.group), kh * w.group + (int)(r % w.group));
-    }
-}
-
-// The first keys of a cloud are seen by all later queries: a tile with them would take many times the others' time.  With few of them
-// (at most kSplitSinks) the keys' kernel leaves their pairs beyond the window out and its sums in fp32 (`first`); attn_far_kernel adds
-// up those pairs, `chunk` rows to a wavefront (`far`), and attn_join_kernel adds both, the chunks in order.
-constexpr int kSplitSinks = 128;
-struct Split {
-    int sinks, chunk;    // 0: not split; a multiple of `group`
-    float *first, *far;  // [cloud or chunk][kv_heads][sinks][dk, dv][dim]
-};
-__device__ __forceinline__ int64_t split_at(const Window& w, const Split& sp, int64_t part, int kh, int key) {
-    return (((part * w.kv_heads + kh) * sp.sinks + key) * 2) * w.dim;
-}
-// the first row that sees a key of the 32 from `key` on beyond its window
-__device__ __forceinline__ int64_t far_begin(const Window& w, const Cloud& c, int key) {
-    return (int64_t)max(w.left + key + 1 - c.off, 0) * w.group;
-}
-
-// The rows (queries and dout) that a workgroup of the keys' kernels goes over, `step` of at most N at a time: whole queries, so that a
-// row's place in its tile does not change, unless a query's heads are more than N.
-template <typename T, int NT, bool VEC, int N, int THREADS>
-struct QueryTiles {
-    using Tl = Tile<T, NT>;
-    static constexpr int kTileBytes = N * Tl::kRowBytes;
-    const AttnBwd<T>& g;
-    const Cloud& c;
-    int kh, step;
-    int64_t end;  // the rows' end, a multiple of `group`
-    TileLoads<T, NT, N, THREADS> lq, ld;
-    __device__ __forceinline__ QueryTiles(const AttnBwd<T>& g_, const Cloud& c_, int kh_, int64_t end_) : g(g_), c(c_), kh(kh_), end(end_) {
-        const int group = g.w.group, row = g.w.dim * (int)sizeof(T);
-        step = group <= N ? N / group * group : N;
-        if constexpr (VEC) {
-            const uint32_t ldq = (uint32_t)(g.q.ld * sizeof(T)), ldd = (uint32_t)(g.dout.ld * sizeof(T));
-            lq.place(g.w.dim, [&](int r) { return r < step ? r / group * ldq + r % group * row : kOutside; });
-            ld.place(g.w.dim, [&](int r) { return r < step ? r / group * ldd + r % group * row : kOutside; });
-        }
-    }
-    __device__ __forceinline__ void one(char* tile, const TileLoads<T, NT, N, THREADS>& l, const Rows<const T>& t, int64_t row) const {
-        const int group = g.w.group;
-        if constexpr (VEC) {
-            const int64_t i = row / group, left = min((int64_t)step, end - row) / group;  // queries
-            l.load(lds_address(tile), memory_of(t.at(c.q0 + i, kh * group, g.w.dim),
-                                                (uint32_t)((left - 1) * t.ld + group * g.w.dim) * (uint32_t)sizeof(T)));
-        } else {
-            load_elements<T, NT, N, THREADS>(tile, g.w.dim, [&](int r) {
-                return r < step && row + r < end ? t.at(c.q0 + (row + r) / group, kh * group + (int)((row + r) % group), g.w.dim) : nullptr;
-            });
-        }
-    }
-    __device__ __forceinline__ void load(char* tiles, int64_t row) const {
-        one(tiles, lq, g.q, row);
-        one(tiles + kTileBytes, ld, g.dout, row);
-    }
-};
-
-// A row's statistics on their way from memory to LDS
-struct RowStat {
-    float l2, delta;
-    int p;
-};
-template <typename T>
-__device__ __forceinline__ RowStat row_stat(const AttnBwd<T>& g, const Cloud& c, int kh, int64_t row, bool there) {
-    RowStat r{0.f, 0.f, kNowhere};
-    if (there) {
-        const int i = (int)((uint32_t)row / (uint32_t)g.w.group);
-        const int64_t at = (int64_t)(c.q0 + i) * g.w.heads + kh * g.w.group + (int)((uint32_t)row % (uint32_t)g.w.group);
-        r = {g.lse[at] * kLog2e, g.delta[at], i + c.off};
-    }
-    return r;
-}
-template <int N>
-struct RowStats {
-    __attribute__((aligned(16))) float l2[N], minus_delta[N];
-    __attribute__((aligned(16))) int p[N];
-    __device__ __forceinline__ void put(const RowStat& r, int at) {
-        l2[at] = r.l2;
-        minus_delta[at] = -r.delta;
-        p[at] = r.p;
-    }
-};
-
-// Keys' gradients from 32 rows after another.  VLDS: the values are read from LDS when they are needed, for heads so wide that
-// registers for both would leave a SIMD one wavefront.
-template <typename T, int NT, bool VLDS>
-struct KeyGrads {
-    using Tl = Tile<T, NT>;
-    typename Tl::Frag k[Tl::kSteps], v[VLDS ? 1 : Tl::kSteps];
-    const char* v_tile;  // this wavefront's 32 rows
-    f32x16 dk[NT], dv[NT];
-    // rows 32 b .. of the tiles q and dout
-    template <int N, typename Seen>
-    __device__ __forceinline__ void add(const char* q, const char* dout, const RowStats<N>& stats, const typename Tl::Place& pl, int b, float c2,
-                                        bool all, Seen seen) {
-        const int half = b * 32 + 4 * ((threadIdx.x & 63) >> 5);
-        f32x16 s = {}, dp;  // dp begins at -delta
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const f32x4 de = *reinterpret_cast<const f32x4*>(stats.minus_delta + half + 8 * g);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) dp[4 * g + i] = de[i];
-        }
-#pragma unroll
-        for (int st = 0; st < Tl::kSteps; ++st) {
-            s = Tl::mma(Tl::direct(q, pl, b, st), k[st], s);
-            dp = Tl::mma(Tl::direct(dout, pl, b, st), VLDS ? Tl::direct(v_tile, pl, 0, st) : v[VLDS ? 0 : st], dp);
-        }
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const f32x4 l = *reinterpret_cast<const f32x4*>(stats.l2 + half + 8 * g);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                s[4 * g + i] = __builtin_amdgcn_exp2f(fmaf(s[4 * g + i], c2, -l[i]));
-                dp[4 * g + i] *= s[4 * g + i];
-            }
-        }
-        if (!all)
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int4 p = *reinterpret_cast<const int4*>(stats.p + half + 8 * g);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const bool sees = seen(i == 0 ? p.x : i == 1 ? p.y : i == 2 ? p.z : p.w, half + 8 * g + i);
-                    s[4 * g + i] = sees ? s[4 * g + i] : 0.f;
-                    dp[4 * g + i] = sees ? dp[4 * g + i] : 0.f;
-                }
-            }
-#pragma unroll
-        for (int st = 0; st < Tl::kTSteps; ++st) {
-            const auto p = Tl::operand(s, st), ds = Tl::operand(dp, st);
-#pragma unroll
-            for (int d = 0; d < NT; ++d) {
-                dv[d] = Tl::mma(Tl::turned(dout, pl, b, st, d), p, dv[d]);
-                dk[d] = Tl::mma(Tl::turned(q, pl, b, st, d), ds, dk[d]);
-            }
-        }
-    }
-};
-
-template <typename T, int NT>
-constexpr bool kValuesInLds = sizeof(T) == 2 && NT >= 3;
-template <typename T, int NT>
-constexpr int kStepRows = sizeof(T) == 2 && NT <= 2 ? 64 : 32;
-
-template <typename T, int NT, bool VEC>
-__global__ __launch_bounds__(kThreads, NT == 1 ? (sizeof(T) == 2 ? 4 : 3) : sizeof(T) * NT == 4 ? 3 : sizeof(T) * NT <= 8 ? 2 : 1) void attn_dkv_kernel(AttnBwd<T> g, Split split, int tiles) {
-    using Tl = Tile<T, NT>;
-    constexpr bool kVLds = kValuesInLds<T, NT>;
-    constexpr int kN = kStepRows<T, NT>, kB = kN / 32, kTileBytes = kN * Tl::kRowBytes;
-    __shared__ __attribute__((aligned(1024))) char lds[4 * kTileBytes];
-    __shared__ __attribute__((aligned(1024))) char values[kVLds ? kRows * Tl::kRowBytes : 16];
-    __shared__ RowStats<kN> stats[2];
-    __shared__ int marks[kN];
-    const Window& w = g.w;
-    const uint32_t item = item_of_block(blockIdx.x, gridDim.x), t = item % (uint32_t)tiles;
-    const int kh = (int)(item / (uint32_t)tiles), cn = cloud_of_tile(w.k_starts, w.clouds, w.n_k, t, 1, kRows);
-    const Cloud c(w, cn);
-    const int64_t tile0 = (t - first_tile(w.k_starts, w.clouds, w.n_k, cn, 1, kRows)) * kRows;
-    if (tile0 >= c.b) return;
-    const int j0 = (int)tile0, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int jw = j0 + wave * kWaveRows, j = jw + (lane & 31);
-    const bool there = j < c.b, split_here = split.sinks > 0;
-    const int sinks = split_here ? 0 : w.sinks;
-    // the rows that see a key of the workgroup's
-    const int a = c.partners ? c.a : 0;
-    const int i0 = min(max(j0 - w.right - c.off, 0), a), i1 = j0 < sinks ? a : max(i0, min(max(min(j0 + kRows, c.b) + w.left - c.off, 0), a));
-    const int64_t begin = (int64_t)i0 * w.group, end = (int64_t)i1 * w.group;
-    const auto pl = Tl::place();
-    const QueryTiles<T, NT, VEC, kN, kThreads> qt(g, c, kh, end);
-    KeyGrads<T, NT, kVLds> kg;
-    const float c2 = exponent_scale(w);
-    bool met = false;
-    auto stat_of = [&](int64_t row) {
-        return row_stat(g, c, kh, row + threadIdx.x, (int)threadIdx.x < qt.step && row + threadIdx.x < end);
-    };
-    auto start = [&] {
-        if (begin < end) {
-            qt.load(lds, begin);
-            const RowStat r = stat_of(begin);
-            if (threadIdx.x < kN) stats[0].put(r, threadIdx.x);
-        }
-    };
-    start();
-    Tl::template load_row<VEC>(kg.k, g.k.at(c.k0 + j, kh, w.dim), w.dim, there, w.scale < 0.f);
-    if constexpr (kVLds) {
-        const T* v = g.v.at(c.k0 + j0, kh, w.dim);
-        const int64_t ldv = g.v.ld;
-        if constexpr (VEC) {
-            TileLoads<T, NT, kRows, kThreads> lv;
-            lv.place(w.dim, [&](int r) { return r * (uint32_t)(ldv * sizeof(T)); });
-            lv.load(lds_address(values), memory_of(v, (uint32_t)((min(kRows, c.b - j0) - 1) * ldv + w.dim) * (uint32_t)sizeof(T)));
-        } else {
-            load_elements<T, NT, kRows, kThreads>(values, w.dim, [&](int r) { return j0 + r < c.b ? v + r * ldv : nullptr; });
-        }
-        kg.v_tile = values + wave * kWaveRows * Tl::kRowBytes;
-        if (begin >= end) wait_tiles();  // no workgroup ends with a load on its way
-    } else {
-        Tl::template load_row<VEC>(kg.v, g.v.at(c.k0 + j, kh, w.dim), w.dim, there, false);
-    }
-    // j - right <= p <= j + left, for the first keys all p behind
-    const int low = j - w.right;
-    const uint32_t width = j < sinks ? 0x7fffffffu : (uint32_t)(w.left + w.right);
-    auto pass = [&](auto again) {
-#pragma unroll
-        for (int d = 0; d < NT; ++d) kg.dk[d] = kg.dv[d] = f32x16{};
-        int buf = 0;
-        for (int64_t row = begin; row < end; row += qt.step, buf ^= 1) {
-            char *q = lds + buf * 2 * kTileBytes, *dout = q + kTileBytes;
-            wait_tiles();
-            RowStat next{};
-            const bool more = row + qt.step < end;
-            if (more) {
-                qt.load(lds + (buf ^ 1) * 2 * kTileBytes, row + qt.step);
-                next = stat_of(row + qt.step);
-            }
-            if constexpr (again) clean_tiles<T, NT, kN, kThreads>(q, dout, marks);
-            const int p_min = (int)((uint32_t)row / (uint32_t)w.group) + c.off;
-            const int p_max = (int)((uint32_t)(min(row + qt.step, end) - 1) / (uint32_t)w.group) + c.off;
-            const bool none = (jw >= c.b) | (jw > p_max + w.right) | ((jw + kWaveRows - 1 < p_min - w.left) & (jw >= sinks));
-            const bool all = !again && ((row + kN <= end) & (qt.step == kN) & (jw + kWaveRows - 1 <= p_min + w.right) & (jw >= p_max - w.left));
-            if (!none)
-#pragma unroll 1
-                for (int b = 0; b < kB; ++b)
-                    kg.add(q, dout, stats[buf], pl, b, c2, all, [&](int p, int r) {
-                        const bool seen = (uint32_t)(p - low) <= width;
-                        if constexpr (again) met |= seen & (marks[r] != 0);
-                        return seen;
-                    });
-            if (more && threadIdx.x < kN) stats[buf ^ 1].put(next, threadIdx.x);
-        }
-        float check = 0.f;
-#pragma unroll
-        for (int d = 0; d < NT; ++d)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) check = fmaf(kg.dk[d][i] *= w.scale, 0.f, fmaf(kg.dv[d][i], 0.f, check));
-        return __syncthreads_or(there & (halves<Add>(check) != 0.f));
-    };
-    if (pass(std::false_type{})) {
-        start();
-        pass(std::true_type{});
-    }
-    const bool part = split_here && j < split.sinks && c.partners;
-    const uint64_t seen_by = __ballot(there && !part && met);
-    const uint32_t by_row = (uint32_t)seen_by | (uint32_t)(seen_by >> 32);
-    if (there && part) {
-        float* to = split.first + split_at(w, split, cn - 1, kh, j);
-        if (met) kg.dk[0][0] = NAN;  // sends attn_join_kernel over the rows one by one
-        put_column<float, NT, false>(to, kg.dk, w.dim);
-        put_column<float, NT, false>(to + w.dim, kg.dv, w.dim);
-    } else if (there && !(by_row >> (lane & 31) & 1)) {
-        put_column<T, NT, VEC>(g.dk.at(c.k0 + j, kh, w.dim), kg.dk, w.dim);
-        put_column<T, NT, VEC>(g.dv.at(c.k0 + j, kh, w.dim), kg.dv, w.dim);
-    }
-    for (uint32_t bad = by_row; bad; bad &= bad - 1) key_gradient_row(g, c, jw + __builtin_ctz(bad), kh);
-}
-
-template <typename T, int NT, bool VEC>
-__global__ __launch_bounds__(64, 1) void attn_far_kernel(AttnBwd<T> g, Split split, int tiles) {
-    using Tl = Tile<T, NT>;
-    constexpr int kTileBytes = 32 * Tl::kRowBytes;
-    __shared__ __attribute__((aligned(1024))) char lds[4 * kTileBytes];
-    __shared__ RowStats<32> stats[2];
-    const Window& w = g.w;
-    const uint32_t item = item_of_block(blockIdx.x, gridDim.x), t = item % (uint32_t)tiles;
-    const int groups = (split.sinks + 31) / 32, key0 = (int)(item / (uint32_t)tiles) % groups * 32, kh = (int)(item / (uint32_t)tiles) / groups;
-    const int cn = cloud_of_tile(w.q_starts, w.clouds, w.n_q, t, w.group, split.chunk);
-    const Cloud c(w, cn);
-    const int64_t r0 = (t - first_tile(w.q_starts, w.clouds, w.n_q, cn, w.group, split.chunk)) * split.chunk;
-    const int64_t begin = max(r0, far_begin(w, c, key0)), end = min(r0 + split.chunk, (int64_t)c.a * w.group);
-    if (!c.partners || begin >= end || key0 >= c.b) return;
-    const int lane = threadIdx.x, j = key0 + (lane & 31);
-    const bool there = j < min(split.sinks, c.b);
-    const auto pl = Tl::place();
-    const QueryTiles<T, NT, VEC, 32, 64> qt(g, c, kh, end);
-    KeyGrads<T, NT, false> kg;
-    auto stat_of = [&](int64_t row) { return row_stat(g, c, kh, row + lane, lane < qt.step && row + lane < end); };
-    qt.load(lds, begin);
-    {
-        const RowStat r = stat_of(begin);
-        if (lane < 32) stats[0].put(r, lane);
-    }
-    Tl::template load_row<VEC>(kg.k, g.k.at(c.k0 + j, kh, w.dim), w.dim, there, w.scale < 0.f);
-    Tl::template load_row<VEC>(kg.v, g.v.at(c.k0 + j, kh, w.dim), w.dim, there, false);
-    const float c2 = exponent_scale(w);
-#pragma unroll
-    for (int d = 0; d < NT; ++d) kg.dk[d] = kg.dv[d] = f32x16{};
-    int buf = 0;
-    for (int64_t row = begin; row < end; row += qt.step, buf ^= 1) {
-        wait_own_tiles();
-        RowStat next{};
-        const bool more = row + qt.step < end;
-        if (more) {
-            qt.load(lds + (buf ^ 1) * 2 * kTileBytes, row + qt.step);
-            next = stat_of(row + qt.step);
-        }
-        const char* q = lds + buf * 2 * kTileBytes;
-        const bool all = (row + 32 <= end) & (qt.step == 32) & (key0 + 31 < (int)((uint32_t)row / (uint32_t)w.group) + c.off - w.left);
-        kg.add(q, q + kTileBytes, stats[buf], pl, 0, c2, all, [&](int p, int) { return j < p - w.left; });
-        if (more && lane < 32) stats[buf ^ 1].put(next, lane);
-    }
-    if (there) {
-#pragma unroll
-        for (int d = 0; d < NT; ++d) kg.dk[d] *= w.scale;
-        float* to = split.far + split_at(w, split, t, kh, j);
-        put_column<float, NT, false>(to, kg.dk, w.dim);
-        put_column<float, NT, false>(to + w.dim, kg.dv, w.dim);
-    }
-}
-
-// a workgroup a cloud, key head and one of the first keys: every wavefront a quarter of the chunks
-template <typename T>
-__global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnBwd<T> g, Split split) {
-    __shared__ float sums[4][2 * kMaxDim];
-    const Window& w = g.w;
-    const int cn = (int)blockIdx.x + 1, kh = blockIdx.y, j = blockIdx.z, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const Cloud c(w, cn);
-    if (j >= c.b) return;
-    const int64_t t0 = first_tile(w.q_starts, w.clouds, w.n_q, cn, w.group, split.chunk), rows = (int64_t)c.a * w.group;
-    const int64_t far0 = far_begin(w, c, j / 32 * 32);
-    // chunks with a row behind far0 were written
-    const int64_t u0 = min(far0, rows) / split.chunk, u1 = far0 < rows ? (rows + split.chunk - 1) / split.chunk : u0;
-    const int64_t quarter = (u1 - u0 + 3) / 4, v0 = min(u0 + wave * quarter, u1), v1 = min(v0 + quarter, u1);
-    const float* far = split.far + split_at(w, split, t0, kh, j);
-    const int64_t step = split_at(w, split, 1, 0, 0);
-    for (int at = lane; at < 2 * w.dim; at += 64) {
-        float s = 0.f;
-#pragma unroll 16
-        for (int64_t u = v0; u < v1; ++u) s += far[u * step + at];
-        sums[wave][at] = s;
-    }
-    __syncthreads();
-    if (wave) return;
-    const float* first = split.first + split_at(w, split, cn - 1, kh, j);
-    float sum[2][2] = {}, check = 0.f;
-    for (int q = 0; q < 2; ++q)
-        for (int e = 0; e < 2; ++e)
-            if (lane + 64 * e < w.dim) {
-                const int at = q * w.dim + lane + 64 * e;
-                float s = first[at];
-                for (int k = 0; k < 4; ++k) s += sums[k][at];
-                sum[q][e] = s;
-                check = fmaf(s, 0.f, check);
-            }
-    if (__any(check != 0.f)) {
-        key_gradient_row(g, c, j, kh);
-        return;
-    }
-    put_row(g.dk.at(c.k0 + j, kh, w.dim), sum[0], w.dim);
-    put_row(g.dv.at(c.k0 + j, kh, w.dim), sum[1], w.dim);
-}
-
-template <typename T, int NT, bool VEC>
+template <typename T, int NT, bool VEC, int W>
 int forward_sized(const AttnFwd<T>& f, hipStream_t s) {
-    const int64_t tiles = tile_numbers(f.w.n_q, f.w.clouds, f.w.group, kRows);
+    const int64_t tiles = tile_numbers(f.w.n_q, f.w.clouds, f.w.group, W * kWaveRows);
     if (tiles * f.w.kv_heads > INT32_MAX) return fail(SP_ERR_UNSUPPORTED, "more than 2^31 tiles of rows");
-    hipLaunchKernelGGL((attn_fwd_kernel<T, NT, VEC>), dim3((unsigned)(tiles * f.w.kv_heads)), dim3(kThreads), 0, s, f, (int)tiles);
+    hipLaunchKernelGGL((attn_fwd_kernel<T, NT, VEC, W>), dim3((unsigned)(tiles * f.w.kv_heads)), dim3(64 * W), 0, s, f, (int)tiles);
     SP_HIP(hipGetLastError());
     return SP_OK;
 }
 
-template <typename T>
-bool in_pieces(const Rows<T>& r) { return r.ld * (int64_t)sizeof(T) % 16 == 0 && r.ld * (int64_t)sizeof(T) <= kMostRowBytes && aligned16(r.p); }
+template <typename T, bool VEC, int W>
+int forward_wide(const AttnFwd<T>& f, hipStream_t s) {
+    const int nt = (f.w.dim + 31) / 32;
+    return nt == 1 ? forward_sized<T, 1, VEC, W>(f, s) : nt == 2 ? forward_sized<T, 2, VEC, W>(f, s) : nt == 3 ? forward_sized<T, 3, VEC, W>(f, s) : forward_sized<T, 4, VEC, W>(f, s);
+}
 
 template <typename T>
 int forward(const AttnFwd<T>& f, hipStream_t s) {
     if (f.w.n_q == 0) return SP_OK;
     const bool vec = f.w.dim * sizeof(T) % 16 == 0 && in_pieces(f.q) && in_pieces(f.k) && in_pieces(f.v) && in_pieces(f.o);
-    const int nt = (f.w.dim + 31) / 32;
-    if (vec) return nt == 1 ? forward_sized<T, 1, true>(f, s) : nt == 2 ? forward_sized<T, 2, true>(f, s) : nt == 3 ? forward_sized<T, 3, true>(f, s) : forward_sized<T, 4, true>(f, s);
-    return nt == 1 ? forward_sized<T, 1, false>(f, s) : nt == 2 ? forward_sized<T, 2, false>(f, s) : nt == 3 ? forward_sized<T, 3, false>(f, s) : forward_sized<T, 4, false>(f, s);
-}
-
-template <typename T, int NT, bool VEC>
-int backward_sized(AttnBwd<T> g, hipStream_t s) {
-    const Window& w = g.w;
-    const int64_t q_tiles = tile_numbers(w.n_q, w.clouds, w.group, kRows), k_tiles = tile_numbers(w.n_k, w.clouds, 1, kRows);
-    if (std::max(q_tiles, k_tiles) * w.kv_heads > INT32_MAX) return fail(SP_ERR_UNSUPPORTED, "more than 2^31 tiles of rows");
-    Buf delta = dev_alloc((size_t)w.n_q * w.heads * 4, s), parts;
-    if (!delta) return SP_ERR_ALLOC;
-    g.delta = ptr<float>(delta);
-    // rows a wavefront: what it writes is an eighth of what it reads at most
-    const int chunk = std::max(512, 8 * (w.sinks <= kSplitSinks ? w.sinks : 0));
-    Split split{0, (chunk + w.group - 1) / w.group * w.group, nullptr, nullptr};
-    const int groups = (w.sinks + 31) / 32;
-    int64_t chunks = 0;
-    if (w.sinks > 0 && w.sinks <= kSplitSinks && w.n_q > 0 && w.clouds > 0 && w.n_k - w.left > 2048) {
-        chunks = tile_numbers(w.n_q, w.clouds, w.group, split.chunk);
-        const size_t each = (size_t)w.kv_heads * w.sinks * 2 * w.dim;
-        parts = dev_alloc((chunks + w.clouds) * each * 4, s);
-        if (!parts) return SP_ERR_ALLOC;
-        split.sinks = w.sinks;
-        split.first = ptr<float>(parts);
-        split.far = split.first + w.clouds * each;
-    }
-    if (w.n_q > 0)
-        hipLaunchKernelGGL((attn_dq_kernel<T, NT, VEC>), dim3((unsigned)(q_tiles * w.kv_heads)), dim3(kThreads), 0, s, g, (int)q_tiles);
-    if (w.n_k > 0)
-        hipLaunchKernelGGL((attn_dkv_kernel<T, NT, VEC>), dim3((unsigned)(k_tiles * w.kv_heads)), dim3(kThreads), 0, s, g, split, (int)k_tiles);
-    if (split.sinks) {
-        hipLaunchKernelGGL((attn_far_kernel<T, NT, VEC>), dim3((unsigned)(chunks * w.kv_heads * groups)), dim3(64), 0, s, g, split, (int)chunks);
-        hipLaunchKernelGGL(attn_join_kernel<T>, dim3(w.clouds, w.kv_heads, split.sinks), dim3(kThreads), 0, s, g, split);
-    }
-    SP_HIP(hipGetLastError());
-    return SP_OK;
-}
-
-template <typename T>
-int backward(const AttnBwd<T>& g, hipStream_t s) {
-    const bool vec = g.w.dim * sizeof(T) % 16 == 0 && in_pieces(g.q) && in_pieces(g.k) && in_pieces(g.v) && in_pieces(g.o) && in_pieces(g.dout) &&
-                     in_pieces(g.dq) && in_pieces(g.dk) && in_pieces(g.dv) && g.w.group <= 32;
-    const int nt = (g.w.dim + 31) / 32;
-    if (vec) return nt == 1 ? backward_sized<T, 1, true>(g, s) : nt == 2 ? backward_sized<T, 2, true>(g, s) : nt == 3 ? backward_sized<T, 3, true>(g, s) : backward_sized<T, 4, true>(g, s);
-    return nt == 1 ? backward_sized<T, 1, false>(g, s) : nt == 2 ? backward_sized<T, 2, false>(g, s) : nt == 3 ? backward_sized<T, 3, false>(g, s) : backward_sized<T, 4, false>(g, s);
+    if (few_tiles(tile_numbers(f.w.n_q, f.w.clouds, f.w.group, 4 * kWaveRows), f.w.kv_heads))
+        return vec ? forward_wide<T, true, 1>(f, s) : forward_wide<T, false, 1>(f, s);
+    return vec ? forward_wide<T, true, 4>(f, s) : forward_wide<T, false, 4>(f, s);
 }
 
 int check(const sp_window_attn* a, Window* w) {
@@ -864,9 +237,9 @@ int sp_window_attn_bwd(const sp_window_attn* a, const void* d_q, int64_t ldq, co
     SP_TRY(check_rows(arrays, 9, w.dim));
     hipStream_t s = (hipStream_t)stream;
     if (a->dt == SP_F32)
-        return backward<float>({w, in<float>(d_q, ldq), in<float>(d_k, ldk), in<float>(d_v, ldv), in<float>(d_o, ldo), in<float>(d_dout, lddout),
+        return attn_backward<float>({w, in<float>(d_q, ldq), in<float>(d_k, ldk), in<float>(d_v, ldv), in<float>(d_o, ldo), in<float>(d_dout, lddout),
                                 d_lse, nullptr, out<float>(d_dq, lddq), out<float>(d_dk, lddk), out<float>(d_dv, lddv)}, s);
-    return backward<bf16_t>({w, in<bf16_t>(d_q, ldq), in<bf16_t>(d_k, ldk), in<bf16_t>(d_v, ldv), in<bf16_t>(d_o, ldo),
+    return attn_backward<bf16_t>({w, in<bf16_t>(d_q, ldq), in<bf16_t>(d_k, ldk), in<bf16_t>(d_v, ldv), in<bf16_t>(d_o, ldo),
                              in<bf16_t>(d_dout, lddout), d_lse, nullptr, out<bf16_t>(d_dq, lddq), out<bf16_t>(d_dk, lddk),
                              out<bf16_t>(d_dv, lddv)}, s);
 }

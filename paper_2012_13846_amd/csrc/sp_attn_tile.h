@@ -130,7 +130,6 @@ struct Tile {
     }
 };
 
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr uint32_t kOutside = 0x80000000u;  // behind every tile's bytes: the load writes zeros
 // The last row of a tile's bytes must lie below kOutside, for which rows are at most this far apart
 constexpr int64_t kMostRowBytes = 1 << 24;

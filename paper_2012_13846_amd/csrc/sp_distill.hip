@@ -1,10 +1,10 @@
 // The loss against a teacher's top logits and its gradient, in one pass over the student's logits.
 //
 // Memory bound: n * m logits read, as many gradients written; the teacher's k entries a row are little beside them.  A row stays as it
-// was read, in the registers of the LANES threads that share it (16 lanes to a workgroup of 1024, at most 16 pieces of 16 bytes a
-// thread: 65536 fp32 or 131072 bf16 logits), between the maximum, the sum of exponentials and the gradient, so it is read once; longer
-// rows, and rows that are no whole pieces beyond 16384 elements, are read once more for each.  exp((z - max) / T) is exp2((z - max) *
-// c2) with c2 = log2(e) / T: the difference first, so that rows of the type's lowest value (masked classes) stay what they are.
+// was read, in the registers of the LANES threads that share it (8 lanes to a workgroup of 256, at most 8 pieces of 16 bytes or
+// elements a thread), between the maximum, the sum of exponentials and the gradient, so it is read once; longer rows are read a
+// second time.  exp((z - max) / T) is exp2((z - max) * c2) with c2 = log2(e) / T: the difference first, so that rows of the type's
+// lowest value (masked classes) stay what they are.
 // The teacher's columns are written after the row by the lane that holds the column's first entry; two entries of one column are
 // added by that lane, in the order of the entries, so there are no atomics.
 #include <algorithm>
@@ -201,15 +201,16 @@ __global__ __launch_bounds__(kBlock<LANES>) void distill_kernel(const T* z, int6
     }
 }
 
-// Rows that would leave a CU one workgroup if they stayed in registers: read twice, the second time from the chip's last cache, with a
-// running maximum and sum the first time.
+// Longer rows (16 pieces a thread leave a SIMD two wavefronts: 32768 bf16 logits in registers 270 us, here 194): read twice, the second time from the chip's last cache, with a
+// running maximum and sum the first time.  The gradient's stores do not stay in that cache, which leaves it to the rows: 550 -> 502 us
+// on 4096 x 131072 in bf16 (4.3 TB/s of logits and gradient).  512 threads: 256 take 557 us, 1024 516.
 constexpr int kWide = 512;
 template <typename T, int V>
 __global__ __launch_bounds__(kWide, 4) void distill_wide_kernel(const T* z, int64_t n, int m, const float* __restrict__ top,
                                                                 const int32_t* __restrict__ index, int k, float inv_t, float tt,
                                                                 const float* __restrict__ weight, float each,
                                                                 double* __restrict__ partial, T* dz) {
-    constexpr int kAhead = V == 1 ? 8 : 4;  // pieces asked for at a time
+    constexpr int kAhead = sizeof(T) * V == 16 && V == 8 ? 4 : 8;  // pieces asked for at a time: 8 of bf16 spill
     extern __shared__ __attribute__((aligned(16))) float lds[];
     __shared__ float room[2][2 * kWide / 64];
     __shared__ int any;
@@ -281,7 +282,7 @@ __global__ __launch_bounds__(kWide, 4) void distill_wide_kernel(const T* z, int6
                     const int64_t col = c0 + (int64_t)r * kWide * V;
 #pragma unroll
                     for (int i = 0; i < V; ++i) v[r].e[i] = to_elem<T>(some ? p_scale * exp2_of((elem(v[r].e[i]) - mx) * c2) : 0.f);
-                    if (col < m) store_piece<T, V>(dz + row * m + col, v[r]);
+                    if (col < m) store_piece_past<T, V>(dz + row * m + col, v[r]);
                 }
             }
         }
@@ -339,8 +340,8 @@ int launch_wide(const DistillArgs& a) {
     return finish(a, ptr<double>(partial), blocks);
 }
 
-// The fewest lanes that hold a row in at most 4 pieces (up to a wavefront), then at most 16; with many entries no fewer than a
-// wavefront, which go over the pairs of entries (16 rows a workgroup would also need 16 times the LDS for them).
+// The fewest lanes that hold a row; with many entries no fewer than a wavefront, which go over the pairs of entries (more rows a
+// workgroup would also need more LDS for them).
 template <typename T, int V>
 int sized(const DistillArgs& a) {
     const int pieces = (a.m + V - 1) / V;
@@ -348,7 +349,7 @@ int sized(const DistillArgs& a) {
     if (pieces <= 64 && a.k <= 64) return launch<T, V, 16, 4>(a);
     if (pieces <= 256) return launch<T, V, 64, 4>(a);
     if (pieces <= 1024) return launch<T, V, 256, 4>(a);
-    if (pieces <= 4096) return launch<T, V, 256, 16>(a);
+    if (pieces <= 2048) return launch<T, V, 256, 8>(a);
     return launch_wide<T, V>(a);
 }
 

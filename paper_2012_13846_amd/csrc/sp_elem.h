@@ -37,6 +37,14 @@ __device__ __forceinline__ void store_piece(T* p, const Piece<T, V>& r) {
     else *reinterpret_cast<uint4*>(p) = __builtin_bit_cast(uint4, r);
 }
 
+// for what is not read again soon: leaves the chip's last cache to others
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+template <typename T, int V>
+__device__ __forceinline__ void store_piece_past(T* p, const Piece<T, V>& r) {
+    if constexpr (V == 1) __builtin_nontemporal_store(r.e[0], p);
+    else __builtin_nontemporal_store(__builtin_bit_cast(u32x4, r), reinterpret_cast<u32x4*>(p));
+}
+
 struct Add {
     static __device__ __forceinline__ float of(float a, float b) { return a + b; }
     static constexpr float none = 0.f;
