@@ -132,12 +132,14 @@ ATTN = {
     "far_first_keys": ([2300, 40, 0, 700], [2300, 40, 0, 700], 4, 2, 32, 20, 0, 5),
     "far_first_keys_odd": ([1500, 900], [1500, 900], 5, 1, 33, 3, 1, 70),
     "far_first_keys_prompt": ([600, 50], [1900, 400], 2, 2, 128, 64, 0, 33),
+    "far_first_keys_heads": ([900], [900], 2, 1, 64, 40, 0, 4),
     "negative_scale": ([60], [60], 2, 2, 32, 20, 0, 0),
 }
 
 
-def attn_inputs(case, dt, fused=False, gap=0):
+def attn_inputs(case, dt, fused=False, gap=0, times=1):
     a, b, h, kv, d, left, right, sinks = ATTN[case]
+    h, kv = h * times, kv * times
     rng = np.random.default_rng(zlib_of(case))
     qs, ks = np.concatenate([[0], np.cumsum(a)]) + gap, np.concatenate([[0], np.cumsum(b)]) + gap
     n_q, n_k = int(qs[-1]) + gap, int(ks[-1]) + gap
@@ -187,6 +189,17 @@ def check_attention(sp, q, k, v, do, starts, host_starts, shape, dt, what):
 @pytest.mark.parametrize("case", sorted(ATTN))
 def test_window_attention(sp, case, dt):
     q, k, v, do, starts, hs, shape = attn_inputs(case, dt, fused=True)
+    check_attention(sp, q, k, v, do, starts, hs, shape, dt, case)
+
+
+@pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("case", ["causal", "both_sides", "sinks_far", "prompt", "more_queries", "more_queries_right", "odd_dim", "wide_odd", "group5",
+                                  "many", "negative_scale", "far_first_keys_heads"])
+def test_window_attention_of_many_heads(sp, case, dt):
+    """Enough heads that the chip is full: workgroups of four wavefronts instead of one."""
+    a, b, h, kv = ATTN[case][:4]
+    tiles = min(sum(a) * (h // kv), sum(b)) // 128 + len(a) + 2
+    q, k, v, do, starts, hs, shape = attn_inputs(case, dt, fused=True, times=256 // (tiles * kv) + 1)
     check_attention(sp, q, k, v, do, starts, hs, shape, dt, case)
 
 
@@ -253,11 +266,11 @@ def test_attention_on_strided_and_unaligned_rows(sp, case, dt):
 
 
 @pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
-@pytest.mark.parametrize("dim", [16, 64, 72, 128])
-def test_what_is_not_seen_does_not_reach_results(sp, dt, dim):
+@pytest.mark.parametrize("dim,kv", [(16, 2), (64, 2), (72, 2), (128, 2), (16, 50), (48, 50), (64, 50), (96, 50), (128, 50)])
+def test_what_is_not_seen_does_not_reach_results(sp, dt, dim, kv):
     """Not-a-numbers, infinities and the type's extremes in rows that some queries see and others, in the same tile, do not."""
     rng = np.random.default_rng(dim)
-    n, h, kv, left, sinks = 150, 4, 2, 5, 2
+    n, h, left, sinks = 150, 2 * kv, 5, 2                     # 50 key heads: workgroups of four wavefronts
     q, do = rows(rng, dt, n, h, dim), rows(rng, dt, n, h, dim)
     k, v = rows(rng, dt, n, kv, dim), rows(rng, dt, n, kv, dim)
     starts = torch.tensor([0, 70, n], dtype=torch.int32, device="cuda")
