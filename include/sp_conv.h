@@ -290,7 +290,7 @@ typedef struct {
 int sp_window_attn_fwd(const sp_window_attn* a, const void* d_q, int64_t ldq, const void* d_k, int64_t ldk, const void* d_v,
                        int64_t ldv, void* d_o, int64_t ldo, float* d_lse, void* stream);
 /* Gradients of sum(o * dout): d_dq like q, d_dk and d_dv like k and v (summed over the query heads that share them); d_o and d_lse
- * are the forward pass's results. */
+ * are the forward pass's results (dout . o is taken from o, or in bf16 for rows of few keys from the sums that o was rounded from). */
 int sp_window_attn_bwd(const sp_window_attn* a, const void* d_q, int64_t ldq, const void* d_k, int64_t ldk, const void* d_v,
                        int64_t ldv, const void* d_o, int64_t ldo, const void* d_dout, int64_t lddout, const float* d_lse, void* d_dq,
                        int64_t lddq, void* d_dk, int64_t lddk, void* d_dv, int64_t lddv, void* stream);

@@ -103,7 +103,11 @@ def window_attn_bwd(q, k, v, o, do, lse, q_starts, k_starts, left, right, sinks,
             delta = (D * o[qs, h]).sum(axis=1)[:, None]
             ds = np.where(seen, p * (D @ V.T - delta), 0.0)
             wide = np.where(seen, p * (np.abs(D) @ np.abs(V).T + np.abs(D * o[qs, h]).sum(axis=1)[:, None]), 0.0)
-        e_ds = u * np.abs(ds) + g * wide
+        # delta's own error: that of the rounded o that it may be taken from (window_attn_fwd's bound)
+        with np.errstate(invalid="ignore"):
+            mag = _times(p, np.abs(V), seen)
+            e_delta = u * (np.abs(D) * (np.abs(o[qs, h]) + mag)).sum(axis=1)[:, None]
+            e_ds = u * np.abs(ds) + g * wide + np.where(seen, p * e_delta, 0.0)
         out[0][qs, h] += scale * _times(ds, K, seen)
         out[1][ks, kh] += scale * _times(ds.T, Q, seen.T)
         out[2][ks, kh] += _times(p.T, D, seen.T)

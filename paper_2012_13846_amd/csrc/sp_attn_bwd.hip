@@ -12,6 +12,12 @@ constexpr int kThreads = 256;  // of a workgroup that joins
 // on the way), dk and dv by keys.  The second goes over the rows of all query heads that share the key head, so their sum needs no
 // second step.
 
+// delta = dout . o = sum of p (dout . v).  From o it has the error of o's rounding, half a step, which stands in every dS of the row and
+// does not average out where few keys share it: dq and dk are 0.0027 off in bf16 with 5 to 16 keys a row and 0.0037 with two (relative
+// norms; the results' own rounding is 0.0017, that of dS 0.0017 again).  Rows of at most this many keys take the sum itself, in a pass of
+// its own over keys that are close by then; with more of them o's part is below 0.0007.
+constexpr int kExactKeys = 128;
+
 template <typename T, int NT, bool VEC, int W>
 __global__ __launch_bounds__(64 * W, NT == 1 ? 4 : sizeof(T) * NT == 4 ? 3 : sizeof(T) * NT < 16 ? 2 : 1) void attn_dq_kernel(AttnBwd<T> g, int tiles) {
     using Tl = Tile<T, NT>;
@@ -28,12 +34,38 @@ __global__ __launch_bounds__(64 * W, NT == 1 ? 4 : sizeof(T) * NT == 4 ? 3 : siz
     const int lane = threadIdx.x & 63, kh = rt.kh, h = kh * w.group + wr.head;
     const auto pl = Tl::place();
     const KeyTiles<T, NT, VEC, W> kt(w, reach, g.k, g.v, c, kh);
+    int first_buf = 0;  // where the first tile is
     if (reach.n > 0) kt.load(lds, 0, 0);
     typename Tl::Frag q[Tl::kSteps], dout[Tl::kSteps];
     Tl::template load_row<VEC>(q, g.q.at(c.q0 + wr.query, h, w.dim), w.dim, wr.there, w.scale < 0.f);
     Tl::template load_row<VEC>(dout, g.dout.at(c.q0 + wr.query, h, w.dim), w.dim, wr.there, false);
+    const int64_t stat = (int64_t)(c.q0 + wr.query) * w.heads + h;
+    const float l2 = wr.there ? g.lse[stat] * kLog2e : 0.f, c2 = exponent_scale(w);
     float delta = 0.f;
-    {
+    if (sizeof(T) == 2 && min(w.left + w.right + 1 + w.sinks, c.b) <= kExactKeys) {
+        for (int slot = 0, buf = 0; slot < reach.n; slot += kN, buf ^= 1) {
+            const char *keys = lds + buf * 2 * kTileBytes, *values = keys + kTileBytes;
+            wait_tiles();
+            kt.load(lds, slot + kN < reach.n ? slot + kN : 0, buf ^ 1);  // at last the first again
+            const SeenInTile seen(w, reach, slot, wr.p);
+#pragma unroll 1
+            for (int b = 0; b < kB; ++b) {
+                f32x16 s = {}, dp = {};
+#pragma unroll
+                for (int st = 0; st < Tl::kSteps; ++st) {
+                    s = Tl::mma(Tl::direct(keys, pl, b, st), q[st], s);
+                    dp = Tl::mma(Tl::direct(values, pl, b, st), dout[st], dp);
+                }
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float x = __builtin_amdgcn_exp2f(fmaf(s[i], c2, -l2)) * dp[i];
+                    delta += seen.sees(b * 32 + 8 * (i / 4) + i % 4) ? x : 0.f;
+                }
+            }
+            first_buf = buf ^ 1;
+        }
+        delta = halves<Add>(delta);
+    } else {
         typename Tl::Frag o[Tl::kSteps];
         Tl::template load_row<VEC>(o, g.o.at(c.q0 + wr.query, h, w.dim), w.dim, wr.there, false);
 #pragma unroll
@@ -42,15 +74,13 @@ __global__ __launch_bounds__(64 * W, NT == 1 ? 4 : sizeof(T) * NT == 4 ? 3 : siz
             for (int i = 0; i < Tl::kPer; ++i) delta = fmaf((float)o[st][i], (float)dout[st][i], delta);
         delta = halves<Add>(delta);
     }
-    const int64_t stat = (int64_t)(c.q0 + wr.query) * w.heads + h;
     if (wr.there && lane < 32) g.delta[stat] = delta;
-    const float l2 = wr.there ? g.lse[stat] * kLog2e : 0.f, c2 = exponent_scale(w);
     f32x16 acc[NT];
     bool met = false;
     auto pass = [&](auto again) {  // as in the forward pass
 #pragma unroll
         for (int d = 0; d < NT; ++d) acc[d] = f32x16{};
-        for (int slot = 0, buf = 0; slot < reach.n; slot += kN, buf ^= 1) {
+        for (int slot = 0, buf = again ? 0 : first_buf; slot < reach.n; slot += kN, buf ^= 1) {
             char *keys = lds + buf * 2 * kTileBytes, *values = keys + kTileBytes;
             wait_tiles();
             if (slot + kN < reach.n) kt.load(lds, slot + kN, buf ^ 1);
