@@ -92,10 +92,9 @@ __global__ __launch_bounds__(64 * W, NT == 1 ? 4 : sizeof(T) * NT == 4 ? 3 : siz
             for (int b = 0; b < kB; ++b) {
                 f32x16 s = {}, dp = {};
 #pragma unroll
-                for (int st = 0; st < Tl::kSteps; ++st) {
-                    s = Tl::mma(Tl::direct(keys, pl, b, st), q[st], s);
-                    dp = Tl::mma(Tl::direct(values, pl, b, st), dout[st], dp);
-                }
+                for (int st = 0; st < Tl::kSteps; ++st) s = Tl::mma(Tl::direct(keys, pl, b, st), q[st], s);
+#pragma unroll
+                for (int st = 0; st < Tl::kSteps; ++st) dp = Tl::mma(Tl::direct(values, pl, b, st), dout[st], dp);
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c2, -l2)) * (dp[i] - delta);
                 if (!all) {
@@ -166,9 +165,9 @@ struct QueryTiles {
     const AttnBwd<T>& g;
     const Cloud& c;
     int kh, step;
-    int64_t end;  // the rows' end, a multiple of `group`
+    int end;  // the rows' end, a multiple of `group`
     TileLoads<T, NT, N, THREADS> lq, ld;
-    __device__ __forceinline__ QueryTiles(const AttnBwd<T>& g_, const Cloud& c_, int kh_, int64_t end_) : g(g_), c(c_), kh(kh_), end(end_) {
+    __device__ __forceinline__ QueryTiles(const AttnBwd<T>& g_, const Cloud& c_, int kh_, int end_) : g(g_), c(c_), kh(kh_), end(end_) {
         const int group = g.w.group, row = g.w.dim * (int)sizeof(T);
         step = group <= N ? N / group * group : N;
         if constexpr (VEC) {
@@ -177,10 +176,10 @@ struct QueryTiles {
             ld.place(g.w.dim, [&](int r) { return r < step ? r / group * ldd + r % group * row : kOutside; });
         }
     }
-    __device__ __forceinline__ void one(char* tile, const TileLoads<T, NT, N, THREADS>& l, const Rows<const T>& t, int64_t row) const {
+    __device__ __forceinline__ void one(char* tile, const TileLoads<T, NT, N, THREADS>& l, const Rows<const T>& t, int row) const {
         const int group = g.w.group;
         if constexpr (VEC) {
-            const int64_t i = row / group, left = min((int64_t)step, end - row) / group;  // queries
+            const uint32_t i = (uint32_t)row / (uint32_t)group, left = (uint32_t)min(step, end - row) / (uint32_t)group;  // queries
             l.load(lds_address(tile), memory_of(t.at(c.q0 + i, kh * group, g.w.dim),
                                                 (uint32_t)((left - 1) * t.ld + group * g.w.dim) * (uint32_t)sizeof(T)));
         } else {
@@ -189,7 +188,7 @@ struct QueryTiles {
             });
         }
     }
-    __device__ __forceinline__ void load(char* tiles, int64_t row) const {
+    __device__ __forceinline__ void load(char* tiles, int row) const {
         one(tiles, lq, g.q, row);
         one(tiles + kTileBytes, ld, g.dout, row);
     }
@@ -201,7 +200,7 @@ struct RowStat {
     int p;
 };
 template <typename T>
-__device__ __forceinline__ RowStat row_stat(const AttnBwd<T>& g, const Cloud& c, int kh, int64_t row, bool there) {
+__device__ __forceinline__ RowStat row_stat(const AttnBwd<T>& g, const Cloud& c, int kh, int row, bool there) {
     RowStat r{0.f, 0.f, kNowhere};
     if (there) {
         const int i = (int)((uint32_t)row / (uint32_t)g.w.group);
@@ -242,10 +241,10 @@ struct KeyGrads {
             for (int i = 0; i < 4; ++i) dp[4 * g + i] = de[i];
         }
 #pragma unroll
-        for (int st = 0; st < Tl::kSteps; ++st) {
-            s = Tl::mma(Tl::direct(q, pl, b, st), k[st], s);
+        for (int st = 0; st < Tl::kSteps; ++st) s = Tl::mma(Tl::direct(q, pl, b, st), k[st], s);
+#pragma unroll
+        for (int st = 0; st < Tl::kSteps; ++st)
             dp = Tl::mma(Tl::direct(dout, pl, b, st), VLDS ? Tl::direct(v_tile, pl, 0, st) : v[VLDS ? 0 : st], dp);
-        }
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
             const f32x4 l = *reinterpret_cast<const f32x4*>(stats.l2 + half + 8 * g);
@@ -305,19 +304,24 @@ __global__ __launch_bounds__(64 * W, NT == 1 ? (sizeof(T) == 2 ? 4 : 3) : sizeof
     // the rows that see a key of the workgroup's
     const int a = c.partners ? c.a : 0;
     const int i0 = min(max(j0 - w.right - c.off, 0), a), i1 = j0 < sinks ? a : max(i0, min(max(min(j0 + kRows, c.b) + w.left - c.off, 0), a));
-    const int64_t begin = (int64_t)i0 * w.group, end = (int64_t)i1 * w.group;
+    const int begin = i0 * w.group, end = i1 * w.group;
     const auto pl = Tl::place();
     const QueryTiles<T, NT, VEC, kN, 64 * W> qt(g, c, kh, end);
     KeyGrads<T, NT, kVLds> kg;
     const float c2 = exponent_scale(w);
     bool met = false;
-    auto stat_of = [&](int64_t row) {
-        return row_stat(g, c, kh, row + threadIdx.x, (int)threadIdx.x < qt.step && row + threadIdx.x < end);
+    auto stat_of = [&](int row) {
+        const int thread = threadIdx.x;
+        return row_stat(g, c, kh, row + thread, (thread < qt.step) & (row + thread < end));
     };
+    // Workgroups of neighbouring keys see mostly the same rows, more of them than a chiplet's L2 holds.  Each goes round its steps from
+    // the one whose number among all rows' steps is a multiple of their count, so that those that run together read a row together.
+    const int steps = (end - begin + qt.step - 1) / qt.step, past = steps > 0 ? begin / qt.step % steps : 0, turn = past ? steps - past : 0;
+    auto row_of = [&](int n) { return begin + (n + turn < steps ? n + turn : n + turn - steps) * qt.step; };
     auto start = [&] {
         if (begin < end) {
-            qt.load(lds, begin);
-            const RowStat r = stat_of(begin);
+            qt.load(lds, row_of(0));
+            const RowStat r = stat_of(row_of(0));
             if (threadIdx.x < kN) stats[0].put(r, threadIdx.x);
         }
     };
@@ -345,14 +349,15 @@ __global__ __launch_bounds__(64 * W, NT == 1 ? (sizeof(T) == 2 ? 4 : 3) : sizeof
 #pragma unroll
         for (int d = 0; d < NT; ++d) kg.dk[d] = kg.dv[d] = f32x16{};
         int buf = 0;
-        for (int64_t row = begin; row < end; row += qt.step, buf ^= 1) {
+        for (int n = 0; n < steps; ++n, buf ^= 1) {
+            const int row = row_of(n);
             char *q = lds + buf * 2 * kTileBytes, *dout = q + kTileBytes;
             wait_tiles();
             RowStat next{};
-            const bool more = row + qt.step < end;
+            const bool more = n + 1 < steps;
             if (more) {
-                qt.load(lds + (buf ^ 1) * 2 * kTileBytes, row + qt.step);
-                next = stat_of(row + qt.step);
+                qt.load(lds + (buf ^ 1) * 2 * kTileBytes, row_of(n + 1));
+                next = stat_of(row_of(n + 1));
             }
             if constexpr (again) clean_tiles<T, NT, kN, 64 * W>(q, dout, marks);
             const int p_min = (int)((uint32_t)row / (uint32_t)w.group) + c.off;
@@ -407,14 +412,15 @@ __global__ __launch_bounds__(64, 1) void attn_far_kernel(AttnBwd<T> g, Split spl
     const int cn = cloud_of_tile(w.q_starts, w.clouds, w.n_q, t, w.group, split.chunk);
     const Cloud c(w, cn);
     const int64_t r0 = (t - first_tile(w.q_starts, w.clouds, w.n_q, cn, w.group, split.chunk)) * split.chunk;
-    const int64_t begin = max(r0, far_begin(w, c, key0)), end = min(r0 + split.chunk, (int64_t)c.a * w.group);
-    if (!c.partners || begin >= end || key0 >= c.b) return;
+    const int64_t from = max(r0, far_begin(w, c, key0)), to_row = min(r0 + split.chunk, (int64_t)c.a * w.group);
+    if (!c.partners || from >= to_row || key0 >= c.b) return;
+    const int begin = (int)from, end = (int)to_row;
     const int lane = threadIdx.x, j = key0 + (lane & 31);
     const bool there = j < min(split.sinks, c.b);
     const auto pl = Tl::place();
     const QueryTiles<T, NT, VEC, 32, 64> qt(g, c, kh, end);
     KeyGrads<T, NT, false> kg;
-    auto stat_of = [&](int64_t row) { return row_stat(g, c, kh, row + lane, lane < qt.step && row + lane < end); };
+    auto stat_of = [&](int row) { return row_stat(g, c, kh, row + lane, (lane < qt.step) & (row + lane < end)); };
     qt.load(lds, begin);
     {
         const RowStat r = stat_of(begin);
@@ -426,7 +432,7 @@ __global__ __launch_bounds__(64, 1) void attn_far_kernel(AttnBwd<T> g, Split spl
 #pragma unroll
     for (int d = 0; d < NT; ++d) kg.dk[d] = kg.dv[d] = f32x16{};
     int buf = 0;
-    for (int64_t row = begin; row < end; row += qt.step, buf ^= 1) {
+    for (int row = begin; row < end; row += qt.step, buf ^= 1) {
         wait_own_tiles();
         RowStat next{};
         const bool more = row + qt.step < end;

@@ -48,9 +48,9 @@ constexpr int kStepBufs = Tile<T, NT>::kRowBytes > 256 ? 1 : 2;
 // and values, the next on its way while one is used), with no barrier until their sums are joined.  The new token's rows are read
 // from k_new and v_new: another workgroup may be writing them to the cache.
 template <typename T, int NT, bool VEC>
-__global__ __launch_bounds__(kThreads, 1) void attn_step_kernel(StepArgs<T> a, int parts, float* __restrict__ partial) {
+__global__ __launch_bounds__(kThreads, 1) void attn_step_kernel(StepArgs<T> a, int parts, int bufs, float* __restrict__ partial) {
     using Tl = Tile<T, NT>;
-    constexpr int kTileBytes = kKeys * Tl::kRowBytes, kBufs = kStepBufs<T, NT>;
+    constexpr int kTileBytes = kKeys * Tl::kRowBytes;
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int part = blockIdx.x, columns = (a.group + kHeads - 1) / kHeads, kh = blockIdx.y / columns, h0 = blockIdx.y % columns * kHeads, b = blockIdx.z;
@@ -64,7 +64,7 @@ __global__ __launch_bounds__(kThreads, 1) void attn_step_kernel(StepArgs<T> a, i
             a.v_cache[cache + seen.row(seen.p) * slot_step + e] = a.v_new[fresh + e];
         }
     const int each = ((seen.n + parts - 1) / parts + kKeys - 1) / kKeys * kKeys, begin = min(part * each, seen.n), end = min(begin + each, seen.n);
-    char* mine = lds + wave * 2 * kBufs * kTileBytes;
+    char* mine = lds + wave * 2 * bufs * kTileBytes;
     const auto pl = Tl::place();
     typename Tl::Frag q[Tl::kSteps];
     const int column = lane & 31;
@@ -107,9 +107,9 @@ __global__ __launch_bounds__(kThreads, 1) void attn_step_kernel(StepArgs<T> a, i
     float m = -INFINITY, l = 0.f;
     int t = begin + wave * kKeys, buf = 0;
     if (t < end) load(t, 0);
-    for (; t < end; t += 4 * kKeys, buf ^= kBufs - 1) {
+    for (; t < end; t += 4 * kKeys, buf ^= bufs - 1) {
         wait_own_tiles();
-        if (kBufs == 2 && t + 4 * kKeys < end) load(t + 4 * kKeys, buf ^ 1);
+        if (bufs == 2 && t + 4 * kKeys < end) load(t + 4 * kKeys, buf ^ 1);
         const char *keys = mine + buf * 2 * kTileBytes, *values = keys + kTileBytes;
         f32x16 s = {};
 #pragma unroll
@@ -137,7 +137,7 @@ __global__ __launch_bounds__(kThreads, 1) void attn_step_kernel(StepArgs<T> a, i
 #pragma unroll
             for (int d = 0; d < NT; ++d) acc[d] = Tl::mma(Tl::turned(values, pl, 0, st, d), pr, acc[d]);
         }
-        if (kBufs == 1 && t + 4 * kKeys < end) {
+        if (bufs == 1 && t + 4 * kKeys < end) {
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             load(t + 4 * kKeys, 0);
         }
@@ -219,9 +219,11 @@ int step_sized(const StepArgs<T>& a, hipStream_t s) {
         if (!partial) return SP_ERR_ALLOC;
     }
     auto kernel = attn_step_kernel<T, NT, VEC>;
-    const size_t lds = std::max<size_t>((size_t)8 * kStepBufs<T, NT> * kKeys * Tl::kRowBytes, (size_t)4 * kHeads * (NT * 32 + 2) * 4);
+    // one tile a wavefront leaves a CU room for two workgroups: 264 of them, one sequence of 8 key heads, run at a time
+    const int bufs = (most + parts - 1) / parts <= 4 * kKeys ? 1 : kStepBufs<T, NT>;
+    const size_t lds = std::max<size_t>((size_t)8 * bufs * kKeys * Tl::kRowBytes, (size_t)4 * kHeads * (NT * 32 + 2) * 4);
     if (lds > 64 * 1024) SP_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-    hipLaunchKernelGGL(kernel, dim3(parts, a.kv_heads * columns, a.batch), dim3(kThreads), lds, s, a, parts, ptr<float>(partial));
+    hipLaunchKernelGGL(kernel, dim3(parts, a.kv_heads * columns, a.batch), dim3(kThreads), lds, s, a, parts, bufs, ptr<float>(partial));
     if (parts > 1) hipLaunchKernelGGL(attn_step_join_kernel<T>, dim3(a.heads, a.batch), dim3(128), 0, s, a, parts, ptr<float>(partial));
     SP_HIP(hipGetLastError());
     return SP_OK;
