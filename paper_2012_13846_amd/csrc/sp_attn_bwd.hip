@@ -18,6 +18,8 @@ constexpr int kThreads = 256;  // of a workgroup that joins
 // its own over keys that are close by then; with more of them o's part is below 0.0007.
 constexpr int kExactKeys = 128;
 
+// Three products a pair of tiles: scores, dout . v, dS . k; accumulators, q and dout stay in registers.  The forward pass's case: 445 us
+// (870 TFLOP/s of the three products), matrix pipe busy 39 %, vector pipe 37 %; heads of 32: 705 - 760 us, vector pipe 80 %.
 template <typename T, int NT, bool VEC, int W>
 __global__ __launch_bounds__(64 * W, NT == 1 ? 4 : sizeof(T) * NT == 4 ? 3 : sizeof(T) * NT < 16 ? 2 : 1) void attn_dq_kernel(AttnBwd<T> g, int tiles) {
     using Tl = Tile<T, NT>;
@@ -279,9 +281,15 @@ struct KeyGrads {
 
 template <typename T, int NT>
 constexpr bool kValuesInLds = sizeof(T) == 2 && NT >= 3;
+// rows of a step: 32 where 64 do not fit the LDS beside the values of two workgroups
 template <typename T, int NT, int W>
 constexpr int kStepRows = sizeof(T) == 2 && NT <= 2 && W > 1 ? 64 : 32;
 
+// Four products a pair of tiles.  A wavefront has 32 keys: 128 registers of accumulators and 32 of keys at a width of 128, which with
+// the values in LDS leaves room for two wavefronts a SIMD (1455 -> 697 us on the forward pass's case; 670 now).  Bound by the latency of
+// LDS reads, each right before its product for want of registers to read ahead: matrix pipe busy 30 %, vector pipe 19 %.  Reads asked
+// for ahead of their products spill (2103 us in all against 1538), a higher priority for products costs 15 %; the two score products one
+// after another instead of by turns give 1 - 7 %.  Heads of 32: 775 - 825 us.
 template <typename T, int NT, bool VEC, int W>
 __global__ __launch_bounds__(64 * W, NT == 1 ? (sizeof(T) == 2 ? 4 : 3) : sizeof(T) * NT == 4 ? 3 : sizeof(T) * NT <= 8 ? 2 : 1) void attn_dkv_kernel(AttnBwd<T> g, Split split, int tiles) {
     using Tl = Tile<T, NT>;
@@ -400,6 +408,8 @@ __global__ __launch_bounds__(64 * W, NT == 1 ? (sizeof(T) == 2 ? 4 : 3) : sizeof
     for (uint32_t bad = by_row; bad; bad &= bad - 1) key_gradient_row(g, c, jw + __builtin_ctz(bad), kh);
 }
 
+// Reads every row once for a few keys: bound by memory's latency at one or two wavefronts a SIMD (373601 rows of 8 heads of 32: 146 us,
+// 2.6 TB/s; 16384 of 32 of 128: 55 us, 4.9 TB/s).  Without the split the tile of the first keys alone would go over all rows.
 template <typename T, int NT, bool VEC>
 __global__ __launch_bounds__(64, 1) void attn_far_kernel(AttnBwd<T> g, Split split, int tiles) {
     using Tl = Tile<T, NT>;
@@ -510,6 +520,8 @@ int backward_sized(AttnBwd<T> g, hipStream_t s) {
     Split split{0, (chunk + w.group - 1) / w.group * w.group, nullptr, nullptr};
     const int groups = (w.sinks + 31) / 32;
     int64_t chunks = 0;
+    // Clouds of 561 more rows than the window: 103 us without the split, 123 with it (eight rows' heads of 32, fp32); of 745: 88 and 81
+    // (8 heads of 64, bf16); of 1745: 144 and 119.
     if (w.sinks > 0 && w.sinks <= kSplitSinks && w.n_q > 0 && w.clouds > 0 && w.n_k / w.clouds - w.left > 640) {
         chunks = tile_numbers(w.n_q, w.clouds, w.group, split.chunk);
         const size_t each = (size_t)w.kv_heads * w.sinks * 2 * w.dim;

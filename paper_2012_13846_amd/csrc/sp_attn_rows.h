@@ -141,7 +141,8 @@ template <typename T>
 bool in_pieces(const Rows<T>& r) { return r.ld * (int64_t)sizeof(T) % 16 == 0 && r.ld * (int64_t)sizeof(T) <= kMostRowBytes && aligned16(r.p); }
 
 // Workgroups of four wavefronts share what they read; where they are fewer than the chip's compute units, workgroups of one are four
-// times as many, each with a shorter way.
+// times as many, each with a shorter way.  Forward and backward in us, four / one: 1601 rows in 8 clouds, 4 heads of 16, fp32 79 / 68; 2500
+// rows in 4 clouds, 4 heads of 32, fp32 124 / 104; 256 rows, 8 heads of 64, bf16 55 / 55.
 inline bool few_tiles(int64_t tiles_of_four, int kv_heads) { return tiles_of_four * kv_heads <= 256; }
 
 }  // namespace sp

@@ -43,7 +43,9 @@ struct StepSeen {
 template <typename T, int NT>
 constexpr int kStepBufs = Tile<T, NT>::kRowBytes > 256 ? 1 : 2;
 
-// Reads a sequence's window once and does little else: bound by memory.  A workgroup has up to 32 query heads of one key head and a
+// Reads a sequence's window once and does little else: bound by memory (96 sequences of up to 30000 tokens, 8 key heads of 128, window
+// 4096: 243 us, 5.4 TB/s, as a large copy).  Keys as the first operand of 32 x 32 products waste the columns that have no query head; even
+// one in 32 leaves the matrix pipes idle nine tenths of the time.  A workgroup has up to 32 query heads of one key head and a
 // part of the sequence's keys; its four wavefronts take tiles of 32 keys by turns, each through LDS of its own (two tiles of keys
 // and values, the next on its way while one is used), with no barrier until their sums are joined.  The new token's rows are read
 // from k_new and v_new: another workgroup may be writing them to the cache.
