@@ -271,6 +271,7 @@ int sp_layer_norm_bwd(const void* d_x, const void* d_dy, int64_t n, int32_t c, c
  * right = 0: causal.  o = softmax over the keys seen of scale * q.k, times v; lse = log of the sum of exponentials (natural), fp32
  * [n_q][heads].  A query that sees nothing, and a row that belongs to no cloud, has o = 0 and lse = -infinity, and zero gradients.
  * Keys that a query does not see do not reach its results, whatever they hold (infinities and NaN too).
+ * Infinities and NaN that are seen give such results where they come in.
  * Starts that are not ascending or out of range give undefined values, but no access outside of the arrays.
  * Row r, head h, element e of an array lies at [r * ld + h * dim + e] (ld in elements, at least heads * dim or kv_heads * dim): views
  * of a fused projection are read and written in place.  Arrays that are written overlap no other array.

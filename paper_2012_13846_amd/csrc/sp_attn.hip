@@ -125,17 +125,23 @@ __global__ __launch_bounds__(64 * W, NT <= 2 ? 3 : 2) void attn_fwd_kernel(AttnF
             for (int i = 0; i < 16; ++i) check = fmaf(acc[d][i] *= inv, 0.f, check);
         return __syncthreads_or(wr.there & (halves<Add>(check) != 0.f));
     };
+    auto store = [&](uint32_t but) {
+        if (wr.there && !(but >> (lane & 31) & 1)) {
+            put_column<T, NT, VEC>(f.o.at(c.q0 + wr.query, h, w.dim), acc, w.dim);
+            if (lane < 32)
+                f.lse[(int64_t)(c.q0 + wr.query) * w.heads + h] = none ? -INFINITY : (m * c2 + __builtin_amdgcn_logf(l)) * kLn2;
+        }
+    };
+    uint32_t bad_rows = 0, by_row = 0;  // rows that see what is not finite; those of them to be computed key by key
     if (pass(std::false_type{})) {
+        store(0);
         kt.load(lds, 0, 0);
         pass(std::true_type{});
+        const uint64_t seen_by = __ballot(wr.there && met);
+        bad_rows = (uint32_t)seen_by | (uint32_t)(seen_by >> 32);
+        by_row = __popc(bad_rows) <= kMostByRow ? bad_rows : 0;
     }
-    const uint64_t seen_by = __ballot(wr.there && met);
-    const uint32_t by_row = (uint32_t)seen_by | (uint32_t)(seen_by >> 32);  // rows that see what is not finite: key by key
-    if (wr.there && !(by_row >> (lane & 31) & 1)) {
-        put_column<T, NT, VEC>(f.o.at(c.q0 + wr.query, h, w.dim), acc, w.dim);
-        if (lane < 32)
-            f.lse[(int64_t)(c.q0 + wr.query) * w.heads + h] = none ? -INFINITY : (m * c2 + __builtin_amdgcn_logf(l)) * kLn2;
-    }
+    store(bad_rows);
     for (uint32_t bad = by_row; bad; bad &= bad - 1) {
         const uint32_t r = wr.w0 + __builtin_ctz(bad);
         forward_row(f, c, (int)(r / w.group), kh * w.group + (int)(r % w.group));

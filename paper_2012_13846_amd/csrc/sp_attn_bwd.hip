@@ -128,13 +128,19 @@ __global__ __launch_bounds__(64 * W, NT == 1 ? 4 : sizeof(T) * NT == 4 ? 3 : siz
             for (int i = 0; i < 16; ++i) check = fmaf(acc[d][i] *= w.scale, 0.f, check);
         return __syncthreads_or(wr.there & (halves<Add>(check) != 0.f));
     };
+    auto store = [&](uint32_t but) {
+        if (wr.there && !(but >> (lane & 31) & 1)) put_column<T, NT, VEC>(g.dq.at(c.q0 + wr.query, h, w.dim), acc, w.dim);
+    };
+    uint32_t bad_rows = 0, by_row = 0;
     if (pass(std::false_type{})) {
+        store(0);
         kt.load(lds, 0, 0);
         pass(std::true_type{});
+        const uint64_t seen_by = __ballot(wr.there && met);
+        bad_rows = (uint32_t)seen_by | (uint32_t)(seen_by >> 32);
+        by_row = __popc(bad_rows) <= kMostByRow ? bad_rows : 0;
     }
-    const uint64_t seen_by = __ballot(wr.there && met);
-    const uint32_t by_row = (uint32_t)seen_by | (uint32_t)(seen_by >> 32);
-    if (wr.there && !(by_row >> (lane & 31) & 1)) put_column<T, NT, VEC>(g.dq.at(c.q0 + wr.query, h, w.dim), acc, w.dim);
+    store(bad_rows);
     __threadfence_block();  // delta, which other lanes read
     for (uint32_t bad = by_row; bad; bad &= bad - 1) {
         const uint32_t r = wr.w0 + __builtin_ctz(bad);
@@ -389,22 +395,28 @@ __global__ __launch_bounds__(64 * W, NT == 1 ? (sizeof(T) == 2 ? 4 : 3) : sizeof
             for (int i = 0; i < 16; ++i) check = fmaf(kg.dk[d][i] *= w.scale, 0.f, fmaf(kg.dv[d][i], 0.f, check));
         return __syncthreads_or(there & (halves<Add>(check) != 0.f));
     };
+    const bool part = split_here && j < split.sinks && c.partners;
+    auto store = [&](uint32_t but) {
+        if (there && part) {
+            float* to = split.first + split_at(w, split, cn - 1, kh, j);
+            if (met) kg.dk[0][0] = NAN;  // sends attn_join_kernel over the rows one by one
+            put_column<float, NT, false>(to, kg.dk, w.dim);
+            put_column<float, NT, false>(to + w.dim, kg.dv, w.dim);
+        } else if (there && !(but >> (lane & 31) & 1)) {
+            put_column<T, NT, VEC>(g.dk.at(c.k0 + j, kh, w.dim), kg.dk, w.dim);
+            put_column<T, NT, VEC>(g.dv.at(c.k0 + j, kh, w.dim), kg.dv, w.dim);
+        }
+    };
+    uint32_t bad_rows = 0, by_row = 0;
     if (pass(std::false_type{})) {
+        store(0);
         start();
         pass(std::true_type{});
+        const uint64_t seen_by = __ballot(there && !part && met);
+        bad_rows = (uint32_t)seen_by | (uint32_t)(seen_by >> 32);
+        by_row = __popc(bad_rows) <= kMostByRow ? bad_rows : 0;
     }
-    const bool part = split_here && j < split.sinks && c.partners;
-    const uint64_t seen_by = __ballot(there && !part && met);
-    const uint32_t by_row = (uint32_t)seen_by | (uint32_t)(seen_by >> 32);
-    if (there && part) {
-        float* to = split.first + split_at(w, split, cn - 1, kh, j);
-        if (met) kg.dk[0][0] = NAN;  // sends attn_join_kernel over the rows one by one
-        put_column<float, NT, false>(to, kg.dk, w.dim);
-        put_column<float, NT, false>(to + w.dim, kg.dv, w.dim);
-    } else if (there && !(by_row >> (lane & 31) & 1)) {
-        put_column<T, NT, VEC>(g.dk.at(c.k0 + j, kh, w.dim), kg.dk, w.dim);
-        put_column<T, NT, VEC>(g.dv.at(c.k0 + j, kh, w.dim), kg.dv, w.dim);
-    }
+    store(bad_rows);
     for (uint32_t bad = by_row; bad; bad &= bad - 1) key_gradient_row(g, c, jw + __builtin_ctz(bad), kh);
 }
 

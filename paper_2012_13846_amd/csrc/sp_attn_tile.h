@@ -236,6 +236,9 @@ __device__ __forceinline__ void clean_tiles(char* a, char* b, int* marks) {
     __syncthreads();
 }
 
+// Rows that see what is not finite are computed one by one where they are few: each costs about what a wavefront's 32 rows cost
+// together.  More of them (a key that a whole window sees, a run that has diverged) keep the first sums, whose finite ones are right.
+constexpr int kMostByRow = 8;
 // the two halves of a wavefront combined, in both
 template <typename Op>
 __device__ __forceinline__ float halves(float v) {

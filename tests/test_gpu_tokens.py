@@ -300,6 +300,28 @@ def test_what_is_not_seen_does_not_reach_results(sp, dt, dim, kv):
 
 
 @pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("dim,kv", [(64, 2), (128, 50)])
+def test_infinities_that_many_rows_see(sp, dt, dim, kv):
+    """Results are finite exactly where the definition's are: one column of what sees a value's infinity, all of what sees a key's."""
+    rng = np.random.default_rng(dim + 1)
+    n, h, left = 200, 2 * kv, 90
+    q, do = rows(rng, dt, n, h, dim), rows(rng, dt, n, h, dim)
+    k, v = rows(rng, dt, n, kv, dim), rows(rng, dt, n, kv, dim)
+    starts = torch.tensor([0, n], dtype=torch.int32, device="cuda")
+    v[30, 0, 5], k[150, 1, 3], do[190, 2, 7] = float("inf"), float("nan"), float("nan")   # seen by 30..120, 150..199; do: keys 100..190
+    o, lse = sp.sp_window_attn_fwd(q, k, v, starts, starts, left=left)
+    dq, dk, dv = sp.sp_window_attn_bwd(q, k, v, o, do, lse, starts, starts, left=left)
+    bad = torch.zeros((n, h, dim), dtype=torch.bool, device="cuda")
+    bad[30:121, :2, 5] = True
+    bad[150:, 2:4] = True
+    assert torch.equal(~torch.isfinite(o), bad)
+    assert torch.equal(~torch.isfinite(lse), bad[:, :, 0])
+    assert torch.isfinite(dq[:30]).all() and torch.isfinite(dq[:, 4:]).all() and not torch.isfinite(dq[30:121, :2]).any()
+    assert torch.isfinite(dv[:, 2:]).all() and torch.isfinite(dk[:, 2:]).all()
+    assert not torch.isfinite(dv[100:191, 1, 7]).any() and not torch.isfinite(dk[100:191, 1]).any()
+
+
+@pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
 def test_scores_of_extreme_size(sp, dt):
     """One key far above the others takes all of the weight; scores far below zero leave finite results."""
     n, d = 130, 64
