@@ -275,7 +275,7 @@ int sp_layer_norm_bwd(const void* d_x, const void* d_dy, int64_t n, int32_t c, c
  * Starts that are not ascending or out of range give undefined values, but no access outside of the arrays.
  * Row r, head h, element e of an array lies at [r * ld + h * dim + e] (ld in elements, at least heads * dim or kv_heads * dim): views
  * of a fused projection are read and written in place.  Arrays that are written overlap no other array.
- * 1 <= dim <= 128 (SP_ERR_UNSUPPORTED beyond), n_q, n_k <= 2^29, n_q * heads / kv_heads <= 2^30, left, right, sinks >= 0.  Rows of whole 16-byte pieces, 16-byte
+ * 1 <= dim <= 128 (SP_ERR_UNSUPPORTED beyond), n_q, n_k, n_clouds <= 2^29, n_q * heads / kv_heads <= 2^30, left, right, sinks >= 0.  Rows of whole 16-byte pieces, 16-byte
  * aligned, are read in such pieces, others element by element.  In bf16 probabilities and their gradients are rounded to bf16
  * before they are multiplied with rows; scores, sums and accumulators are fp32. */
 typedef struct {

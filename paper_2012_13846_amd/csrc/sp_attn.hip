@@ -180,8 +180,8 @@ int check(const sp_window_attn* a, Window* w) {
     if (a->dim < 1) return fail(SP_ERR_INVALID_ARG, "bad head width");
     if (a->left < 0 || a->right < 0 || a->sinks < 0) return fail(SP_ERR_INVALID_ARG, "left, right and sinks must not be negative");
     if (!(a->scale > -3.0e38f && a->scale < 3.0e38f)) return fail(SP_ERR_INVALID_ARG, "the scale must be finite");
-    if (a->dim > kMaxDim || a->heads > 65535 || a->n_q > 1 << 29 || a->n_k > 1 << 29)
-        return fail(SP_ERR_UNSUPPORTED, "head widths above %d, more than 65535 heads or more than 2^29 rows", kMaxDim);
+    if (a->dim > kMaxDim || a->heads > 65535 || a->n_q > 1 << 29 || a->n_k > 1 << 29 || a->n_clouds > 1 << 29)
+        return fail(SP_ERR_UNSUPPORTED, "head widths above %d, more than 65535 heads or more than 2^29 rows or clouds", kMaxDim);
     if (a->n_q * (a->heads / a->kv_heads) > 1 << 30) return fail(SP_ERR_UNSUPPORTED, "more than 2^30 rows and heads that share a key head");
     if (!a->d_q_starts || !a->d_k_starts) return fail(SP_ERR_INVALID_ARG, "the starts are NULL");
     w->q_starts = a->d_q_starts;

@@ -407,17 +407,15 @@ __global__ __launch_bounds__(64 * W, NT == 1 ? (sizeof(T) == 2 ? 4 : 3) : sizeof
             put_column<T, NT, VEC>(g.dv.at(c.k0 + j, kh, w.dim), kg.dv, w.dim);
         }
     };
-    uint32_t bad_rows = 0, by_row = 0;
+    uint32_t bad_rows = 0;  // keys that such rows see keep the first sums, whose finite ones are right
     if (pass(std::false_type{})) {
         store(0);
         start();
         pass(std::true_type{});
         const uint64_t seen_by = __ballot(there && !part && met);
         bad_rows = (uint32_t)seen_by | (uint32_t)(seen_by >> 32);
-        by_row = __popc(bad_rows) <= kMostByRow ? bad_rows : 0;
     }
     store(bad_rows);
-    for (uint32_t bad = by_row; bad; bad &= bad - 1) key_gradient_row(g, c, jw + __builtin_ctz(bad), kh);
 }
 
 // Reads every row once for a few keys: bound by memory's latency at one or two wavefronts a SIMD (373601 rows of 8 heads of 32: 146 us,
@@ -538,10 +536,11 @@ int backward_sized(AttnBwd<T> g, hipStream_t s) {
         chunks = tile_numbers(w.n_q, w.clouds, w.group, split.chunk);
         const size_t each = (size_t)w.kv_heads * w.sinks * 2 * w.dim;
         parts = dev_alloc((chunks + w.clouds) * each * 4, s);
-        if (!parts) return SP_ERR_ALLOC;
-        split.sinks = w.sinks;
-        split.first = ptr<float>(parts);
-        split.far = split.first + w.clouds * each;
+        if (parts) {  // else the slow way, which needs no memory
+            split.sinks = w.sinks;
+            split.first = ptr<float>(parts);
+            split.far = split.first + w.clouds * each;
+        }
     }
     if (w.n_q > 0)
         hipLaunchKernelGGL((attn_dq_kernel<T, NT, VEC, W>), dim3((unsigned)(q_tiles * w.kv_heads)), dim3(64 * W), 0, s, g, (int)q_tiles);

@@ -27,7 +27,7 @@ struct StepSeen {
     __device__ __forceinline__ StepSeen(const StepArgs<T>& a, int b) : p(a.lens[b]), sinks(a.sinks), ring(a.cap - a.sinks) {
         lo = max(max(p - a.left, p - ring + 1), 0);
         first = min(sinks, lo);
-        n = p < 0 ? 0 : first + p + 1 - lo;
+        n = p < 0 ? 0 : first + (p - lo + 1);
         from = max(lo, sinks);
         at = (from - sinks) % ring;
     }
@@ -224,7 +224,15 @@ int step_sized(const StepArgs<T>& a, hipStream_t s) {
     // one tile a wavefront leaves a CU room for two workgroups: 264 of them, one sequence of 8 key heads, run at a time
     const int bufs = (most + parts - 1) / parts <= 4 * kKeys ? 1 : kStepBufs<T, NT>;
     const size_t lds = std::max<size_t>((size_t)8 * bufs * kKeys * Tl::kRowBytes, (size_t)4 * kHeads * (NT * 32 + 2) * 4);
-    if (lds > 64 * 1024) SP_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+    {
+        static std::mutex mu;
+        static size_t attr_lds = 64 * 1024;  // largest dynamic LDS size opted into so far
+        std::lock_guard<std::mutex> lk(mu);
+        if (lds > attr_lds) {
+            SP_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+            attr_lds = lds;
+        }
+    }
     hipLaunchKernelGGL(kernel, dim3(parts, a.kv_heads * columns, a.batch), dim3(kThreads), lds, s, a, parts, bufs, ptr<float>(partial));
     if (parts > 1) hipLaunchKernelGGL(attn_step_join_kernel<T>, dim3(a.heads, a.batch), dim3(128), 0, s, a, parts, ptr<float>(partial));
     SP_HIP(hipGetLastError());
