@@ -336,6 +336,33 @@ def test_scores_of_extreme_size(sp, dt):
     assert torch.isfinite(o).all() and torch.isfinite(lse).all()
 
 
+def test_attention_refuses_what_it_cannot_read(sp):
+    q, k = torch.zeros((6, 4, 16), device="cuda"), torch.zeros((6, 2, 16), device="cuda")
+    st = torch.tensor([0, 6], dtype=torch.int32, device="cuda")
+    fwd = lambda q=q, k=k, v=k, a=st, b=st, **more: sp.sp_window_attn_fwd(q, k, v, a, b, **{"left": 2, **more})  # noqa: E731
+    o, lse = fwd()
+    assert o.shape == (6, 4, 16) and lse.shape == (6, 4)
+    for bad in (dict(v=k[:5]), dict(k=k.bfloat16()), dict(q=q.transpose(0, 1)), dict(q=q[:, :, ::2]), dict(q=q.expand(6, 4, 16)[:1].expand(6, 4, 16)),
+                dict(a=st.long()), dict(b=torch.tensor([0, 3, 6], dtype=torch.int32, device="cuda")), dict(q=q.double(), k=k.double(), v=k.double())):
+        with pytest.raises(ValueError):
+            fwd(**bad)
+    for bad in (dict(left=-1), dict(right=-2), dict(sinks=-1), dict(scale=float("nan")), dict(k=torch.zeros((6, 3, 16), device="cuda"), v=torch.zeros((6, 3, 16), device="cuda"))):
+        with pytest.raises(sp.SpError) as e:
+            fwd(**bad)
+        assert e.value.code == -1
+    wide = torch.zeros((6, 2, 136), device="cuda")
+    with pytest.raises(sp.SpError) as e:
+        fwd(q=wide, k=wide, v=wide)
+    assert e.value.code == -5
+    with pytest.raises(ValueError):
+        sp.sp_window_attn_bwd(q, k, k, o, q[:5], lse, st, st, left=2)
+    cache = torch.zeros((6, 9, 2, 16), device="cuda")
+    with pytest.raises(ValueError):
+        sp.sp_window_attn_step(q, k, k, cache, cache[:, :8], torch.zeros(6, dtype=torch.int32, device="cuda"), left=3)
+    with pytest.raises(sp.SpError):
+        sp.sp_window_attn_step(q, k, k, cache, cache.clone(), torch.zeros(6, dtype=torch.int32, device="cuda"), left=3, sinks=9)
+
+
 def test_attention_gradients_against_differences(sp):
     q, k, v, do, starts, hs, shape = attn_inputs("both_sides", F32)
     o, lse = sp.sp_window_attn_fwd(q, k, v, *starts, **shape)
