@@ -530,8 +530,8 @@ int backward_sized(AttnBwd<T> g, hipStream_t s) {
     Split split{0, (chunk + w.group - 1) / w.group * w.group, nullptr, nullptr};
     const int groups = (w.sinks + 31) / 32;
     int64_t chunks = 0;
-    // Clouds of 561 more rows than the window: 103 us without the split, 123 with it (eight rows' heads of 32, fp32); of 745: 88 and 81
-    // (8 heads of 64, bf16); of 1745: 144 and 119.
+    // Clouds of 561 rows beyond the window: 103 us without the split, 123 with it (four clouds, 4 heads of 32, fp32, forward and
+    // backward); of 745 rows: 88 and 81 (one cloud, 8 heads of 64, bf16); of 1745: 144 and 119.
     if (w.sinks > 0 && w.sinks <= kSplitSinks && w.n_q > 0 && w.clouds > 0 && w.n_k / w.clouds - w.left > 640) {
         chunks = tile_numbers(w.n_q, w.clouds, w.group, split.chunk);
         const size_t each = (size_t)w.kv_heads * w.sinks * 2 * w.dim;
