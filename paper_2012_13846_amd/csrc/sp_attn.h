@@ -4,6 +4,8 @@
 
 #include "sp_elem.h"
 
+#include "sp_attn_cut.h"
+
 namespace sp {
 
 constexpr int kMaxDim = 128;
@@ -46,38 +48,28 @@ struct AttnBwd {
 template <typename T>
 int attn_backward(const AttnBwd<T>& g, hipStream_t s);  // sp_attn_bwd.hip
 
-// Clouds 1 .. clouds are the caller's; 0 and clouds + 1 hold the rows before the first and after the last.
-__device__ __forceinline__ int cloud_begin(const int32_t* starts, int clouds, int n, int c) {
-    if (c <= 0) return 0;
-    if (c > clouds + 1) return n;
-    return min(max(starts[c - 1], 0), n);
-}
-// Rows cut cloud by cloud into tiles of `tile`, each row of the array standing for `per` rows of the cut: cloud c has the tile
-// numbers from begin(c) * per / tile + c on, which are at least as many as its tiles.
-__device__ __forceinline__ int64_t first_tile(const int32_t* starts, int clouds, int n, int c, int per, int tile) {
-    return (int64_t)cloud_begin(starts, clouds, n, c) * per / tile + c;
-}
-// The last cloud whose first tile is <= t: a wavefront looks at 64 clouds at a time.  All lanes must come here together.
-__device__ __forceinline__ int cloud_of_tile(const int32_t* starts, int clouds, int n, int64_t t, int per, int tile) {
-    int lo = 0, hi = clouds + 1;
-    while (lo < hi) {
-        const int step = (hi - lo + 63) / 64, c = lo + ((int)(threadIdx.x & 63) + 1) * step;
-        const bool behind = c <= hi && first_tile(starts, clouds, n, c, per, tile) <= t;
-        lo += step * __popcll(__ballot(behind));
-        hi = min(hi, lo + step - 1);
+// A tile number's cloud and the tile's first row, counted from the cloud's (see in_cloud).  All lanes must come here together.
+struct CloudTile {
+    int cloud;
+    int64_t row;
+    __device__ __forceinline__ CloudTile(const int32_t* starts, int clouds, int n, int64_t t, int per, int tile) {
+        const int c = last_cloud(clouds, [&](int lo, int step, int hi) {
+            const int at = lo + ((int)(threadIdx.x & 63) + 1) * step;
+            return (int)__popcll(__ballot(at <= hi && first_tile(starts, clouds, n, at, per, tile) <= t));
+        });
+        cloud = __builtin_amdgcn_readfirstlane(c);
+        row = (t - first_tile(starts, clouds, n, cloud, per, tile)) * tile;
     }
-    return __builtin_amdgcn_readfirstlane(lo);
-}
-inline int64_t tile_numbers(int64_t n, int clouds, int per, int tile) { return n * per / tile + clouds + 2; }
+};
 
 struct Cloud {
     int q0, a, k0, b;  // first query row, queries, first key row, keys
     int off;           // query i stands at position i + off
     __device__ __forceinline__ Cloud(const Window& w, int c) {
         q0 = cloud_begin(w.q_starts, w.clouds, w.n_q, c);
-        a = max(0, cloud_begin(w.q_starts, w.clouds, w.n_q, c + 1) - q0);
+        a = cloud_rows(w.q_starts, w.clouds, w.n_q, c);
         k0 = cloud_begin(w.k_starts, w.clouds, w.n_k, c);
-        b = max(0, cloud_begin(w.k_starts, w.clouds, w.n_k, c + 1) - k0);
+        b = cloud_rows(w.k_starts, w.clouds, w.n_k, c);
         off = b - a;
         partners = c >= 1 && c <= w.clouds;
     }

@@ -23,7 +23,7 @@ __global__ __launch_bounds__(64 * W, NT <= 2 ? 3 : 2) void attn_fwd_kernel(AttnF
     const RowTile<W> rt(w, tiles);
     const Cloud c(w, rt.cloud);
     const int64_t rows = (int64_t)c.a * w.group;
-    if (rt.r0 >= rows) return;
+    if (!in_cloud(rt.r0, rows)) return;
     const WaveRows<W> wr(w, c, (uint32_t)rt.r0, (uint32_t)rows);
     const Reach& reach = wr.reach;
     const int lane = threadIdx.x & 63, kh = rt.kh, h = kh * w.group + wr.head;

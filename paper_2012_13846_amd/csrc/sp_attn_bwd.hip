@@ -30,7 +30,7 @@ __global__ __launch_bounds__(64 * W, NT == 1 ? 4 : sizeof(T) * NT == 4 ? 3 : siz
     const RowTile<W> rt(w, tiles);
     const Cloud c(w, rt.cloud);
     const int64_t rows = (int64_t)c.a * w.group;
-    if (rt.r0 >= rows) return;
+    if (!in_cloud(rt.r0, rows)) return;
     const WaveRows<W> wr(w, c, (uint32_t)rt.r0, (uint32_t)rows);
     const Reach& reach = wr.reach;
     const int lane = threadIdx.x & 63, kh = rt.kh, h = kh * w.group + wr.head;
@@ -157,7 +157,7 @@ struct Split {
     float *first, *far;  // [cloud or chunk][kv_heads][sinks][dk, dv][dim]
 };
 __device__ __forceinline__ int64_t split_at(const Window& w, const Split& sp, int64_t part, int kh, int key) {
-    return (((part * w.kv_heads + kh) * sp.sinks + key) * 2) * w.dim;
+    return sums_at(w.kv_heads, sp.sinks, w.dim, part, kh, key);
 }
 // the first row that sees a key of the 32 from `key` on beyond its window
 __device__ __forceinline__ int64_t far_begin(const Window& w, const Cloud& c, int key) {
@@ -307,11 +307,12 @@ __global__ __launch_bounds__(64 * W, NT == 1 ? (sizeof(T) == 2 ? 4 : 3) : sizeof
     __shared__ int marks[kN];
     const Window& w = g.w;
     const uint32_t item = item_of_block(blockIdx.x, gridDim.x), t = item % (uint32_t)tiles;
-    const int kh = (int)(item / (uint32_t)tiles), cn = cloud_of_tile(w.k_starts, w.clouds, w.n_k, t, 1, kRows);
+    const int kh = (int)(item / (uint32_t)tiles);
+    const CloudTile ct(w.k_starts, w.clouds, w.n_k, t, 1, kRows);
+    const int cn = ct.cloud;
     const Cloud c(w, cn);
-    const int64_t tile0 = (t - first_tile(w.k_starts, w.clouds, w.n_k, cn, 1, kRows)) * kRows;
-    if (tile0 >= c.b) return;
-    const int j0 = (int)tile0, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (!in_cloud(ct.row, c.b)) return;
+    const int j0 = (int)ct.row, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int jw = j0 + wave * kWaveRows, j = jw + (lane & 31);
     const bool there = j < c.b, split_here = split.sinks > 0;
     const int sinks = split_here ? 0 : w.sinks;
@@ -429,11 +430,12 @@ __global__ __launch_bounds__(64, 1) void attn_far_kernel(AttnBwd<T> g, Split spl
     const Window& w = g.w;
     const uint32_t item = item_of_block(blockIdx.x, gridDim.x), t = item % (uint32_t)tiles;
     const int groups = (split.sinks + 31) / 32, key0 = (int)(item / (uint32_t)tiles) % groups * 32, kh = (int)(item / (uint32_t)tiles) / groups;
-    const int cn = cloud_of_tile(w.q_starts, w.clouds, w.n_q, t, w.group, split.chunk);
-    const Cloud c(w, cn);
-    const int64_t r0 = (t - first_tile(w.q_starts, w.clouds, w.n_q, cn, w.group, split.chunk)) * split.chunk;
-    const int64_t from = max(r0, far_begin(w, c, key0)), to_row = min(r0 + split.chunk, (int64_t)c.a * w.group);
-    if (!c.partners || from >= to_row || key0 >= c.b) return;
+    const CloudTile ct(w.q_starts, w.clouds, w.n_q, t, w.group, split.chunk);
+    const Cloud c(w, ct.cloud);
+    const int64_t rows = (int64_t)c.a * w.group;
+    if (!c.partners || !in_cloud(ct.row, rows) || key0 >= c.b) return;
+    const int64_t from = max(ct.row, far_begin(w, c, key0)), to_row = min(ct.row + split.chunk, rows);
+    if (from >= to_row) return;
     const int begin = (int)from, end = (int)to_row;
     const int lane = threadIdx.x, j = key0 + (lane & 31);
     const bool there = j < min(split.sinks, c.b);

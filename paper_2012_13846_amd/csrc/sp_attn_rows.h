@@ -70,8 +70,9 @@ struct RowTile {
     __device__ __forceinline__ RowTile(const Window& w, int tiles) {
         const uint32_t item = item_of_block(blockIdx.x, gridDim.x), t = item % (uint32_t)tiles;
         kh = (int)(item / (uint32_t)tiles);
-        cloud = cloud_of_tile(w.q_starts, w.clouds, w.n_q, t, w.group, W * kWaveRows);
-        r0 = (t - first_tile(w.q_starts, w.clouds, w.n_q, cloud, w.group, W * kWaveRows)) * (W * kWaveRows);
+        const CloudTile ct(w.q_starts, w.clouds, w.n_q, t, w.group, W * kWaveRows);
+        cloud = ct.cloud;
+        r0 = ct.row;
     }
 };
 

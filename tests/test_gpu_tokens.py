@@ -551,3 +551,19 @@ def test_captured_steps_replay(sp, dt):
         for a, b in zip(out, token_step(sp, fresh)):
             assert torch.equal(a, b)
         torch.cuda.synchronize()
+
+
+# ---- attention: starts, infinities and first keys at sizes that split the first keys' sums -----------------------
+@pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
+def test_wrong_starts_of_many_rows_stay_inside_of_the_arrays(sp, dt):
+    """Enough rows that the first keys' sums have scratch memory; tests/test_attn_cut.py shows the indexes.  Afterwards a legal call is right."""
+    n, h, d = 2000, 2, 32
+    room = torch.full((3 * n, h, d), 0.25, dtype=dt, device="cuda")
+    q, grad = room[n:2 * n], torch.full((3, 3 * n, h, d), 7.0, dtype=dt, device="cuda")
+    for bad in ([2000, 0, 2000], [0, 1800, 100], [-50, 2 ** 31 - 1], [1900, 20, 1990], [2000] * 40 + [0] * 30):
+        st = torch.tensor(bad, dtype=torch.int32, device="cuda")
+        o, lse = sp.sp_window_attn_fwd(q, q, q, st, st, left=9, right=3, sinks=4)
+        sp.sp_window_attn_bwd(q, q, q, o, q, lse, st, st, left=9, right=3, sinks=4, out=[g[n:2 * n] for g in grad])
+    assert (grad[:, :n] == 7).all() and (grad[:, 2 * n:] == 7).all() and (room == 0.25).all()
+    q, k, v, do, starts, hs, shape = attn_inputs("far_first_keys", dt)
+    check_attention(sp, q, k, v, do, starts, hs, shape, dt, "after wrong starts")
