@@ -120,33 +120,6 @@ __device__ __forceinline__ void put_row(T* row, const float (&acc)[2], int dim) 
 }
 
 template <typename T>
-__device__ __forceinline__ void forward_row(const AttnFwd<T>& f, const Cloud& c, int i, int h) {
-    const Window& w = f.w;
-    const int lane = threadIdx.x & 63, kh = h / w.group;
-    const Seen seen(w, c, i);
-    const float c2 = w.scale * kLog2e;
-    const T* q = f.q.at(c.q0 + i, h, w.dim);
-    float m = -INFINITY, l = 0.f, acc[2] = {0.f, 0.f};  // m: the largest score times c2 so far
-    for (int t0 = 0; t0 < seen.n; t0 += 64) {
-        const bool in = t0 + lane < seen.n;
-        const float s = in ? dot(q, f.k.at(c.k0 + seen.key(t0 + lane), kh, w.dim), w.dim) * c2 : -INFINITY;
-        const float top = fmaxf(m, lanes_reduce<64, Max>(s));
-        const float base = top == -INFINITY ? 0.f : top;
-        const float old = __builtin_amdgcn_exp2f(m - base), p = in ? __builtin_amdgcn_exp2f(s - base) : 0.f;
-        l = l * old + lanes_reduce<64, Add>(p);
-        acc[0] *= old;
-        acc[1] *= old;
-        add_rows<T>(acc, p, min(64, seen.n - t0), w.dim, [&](int t) { return f.v.at(c.k0 + seen.key(t0 + t), kh, w.dim); });
-        m = top;
-    }
-    const float inv = seen.n > 0 ? 1.f / l : 0.f;
-    acc[0] *= inv;
-    acc[1] *= inv;
-    put_row(f.o.at(c.q0 + i, h, w.dim), acc, w.dim);
-    if (lane == 0) f.lse[(int64_t)(c.q0 + i) * w.heads + h] = seen.n > 0 ? m * kLn2 + logf(l) : -INFINITY;
-}
-
-template <typename T>
 __device__ __forceinline__ void query_gradient_row(const AttnBwd<T>& g, const Cloud& c, int i, int h) {
     const Window& w = g.w;
     const int lane = threadIdx.x & 63, kh = h / w.group;

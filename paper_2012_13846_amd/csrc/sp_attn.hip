@@ -18,7 +18,6 @@ __global__ __launch_bounds__(64 * W, NT <= 2 ? 3 : 2) void attn_fwd_kernel(AttnF
     using Tl = Tile<T, NT>;
     constexpr int kN = kKeys<T, W>, kB = kN / 32, kTileBytes = kN * Tl::kRowBytes;
     __shared__ __attribute__((aligned(1024))) char lds[4 * kTileBytes];  // keys and values, two of each
-    __shared__ int marks[kN];
     const Window& w = f.w;
     const RowTile<W> rt(w, tiles);
     const Cloud c(w, rt.cloud);
@@ -36,85 +35,95 @@ __global__ __launch_bounds__(64 * W, NT <= 2 ? 3 : 2) void attn_fwd_kernel(AttnF
     const bool none = reach.n == 0 || wr.p + w.right < 0;  // the row sees nothing (else the last of its keys is seen at least)
 
     f32x16 acc[NT];
-    float m, l;        // at most 8 powers of two below the row's largest score so far; this lane's half of the sum of exponentials
-    bool met = false;  // this row sees something that is not finite
-    // again: sums that were not finite, a second time without what rows do not see
-    auto pass = [&](auto again) {
+    float m, l;          // at most 8 powers of two below the row's largest score so far; this lane's half of the sum of exponentials
+    bool other = false;  // there are values that are not finite
+    // again: sums that were not finite, by `part` of the values
+    auto pass = [&](auto again, int part) {
 #pragma unroll
         for (int d = 0; d < NT; ++d) acc[d] = f32x16{};
         m = -INFINITY;
         l = 0.f;
         for (int slot = 0, buf = 0; slot < reach.n; slot += kN, buf ^= 1) {
-            char *keys = lds + buf * 2 * kTileBytes, *values = keys + kTileBytes;
+            const char *keys = lds + buf * 2 * kTileBytes, *values = keys + kTileBytes;
             wait_tiles();
             if (slot + kN < reach.n) kt.load(lds, slot + kN, buf ^ 1);
-            if constexpr (again) clean_tiles<T, NT, kN, 64 * W>(keys, values, marks);
             if (reach.none(w, slot, kN, wr.p_min, wr.p_max)) continue;
             f32x16 s[kB] = {};
-#pragma unroll
-            for (int st = 0; st < Tl::kSteps; ++st)
-#pragma unroll
-                for (int b = 0; b < kB; ++b) s[b] = Tl::mma(Tl::direct(keys, pl, b, st), q[st], s[b]);
-            if (again || !(wr.whole & reach.all(w, slot, kN, wr.p_min, wr.p_max))) {
+            if (again && part != kFinite) {
                 const SeenInTile seen(w, reach, slot, wr.p);
-                if (!again && !seen.heads) {
-#pragma unroll
-                    for (int b = 0; b < kB; ++b)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) s[b][i] = seen.in_range(b * 32 + 8 * (i / 4) + i % 4) ? s[b][i] : -INFINITY;
-                } else {
-#pragma unroll
-                    for (int b = 0; b < kB; ++b)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const int r = b * 32 + 8 * (i / 4) + i % 4;
-                            const bool sees = seen.sees(r);
-                            s[b][i] = sees ? s[b][i] : -INFINITY;
-                            if constexpr (again) met |= sees & (marks[r + 4 * (lane >> 5)] != 0);
-                        }
-                }
-            }
-            float top = m;
-#pragma unroll
-            for (int b = 0; b < kB; ++b)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
-            top = halves<Max>(top);
-            if (__any((top - m) * c2 > 8.f)) {
-                const float old = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - top) * c2);
-                l *= old;
-#pragma unroll
-                for (int d = 0; d < NT; ++d) acc[d] *= old;
-                m = top;
-            }
-            const float m2 = m == -INFINITY ? 0.f : m * c2;
-            // one operation less than the difference first; m2's rounding, which stands in the exponents and in lse, is below 2^-17 then
-            if (__all(fabsf(m2) < 64.f)) {
 #pragma unroll
                 for (int b = 0; b < kB; ++b)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], c2, -m2));
+                    for (int i = 0; i < 16; ++i) s[b][i] = seen.sees(b * 32 + 8 * (i / 4) + i % 4) ? 1.f : 0.f;
             } else {
-                const float from = m == -INFINITY ? 0.f : m;
+#pragma unroll
+                for (int st = 0; st < Tl::kSteps; ++st)
+#pragma unroll
+                    for (int b = 0; b < kB; ++b) s[b] = Tl::mma(Tl::direct(keys, pl, b, st), q[st], s[b]);
+                if (again || !(wr.whole & reach.all(w, slot, kN, wr.p_min, wr.p_max))) {
+                    const SeenInTile seen(w, reach, slot, wr.p);
+                    if (!again && !seen.heads) {
+#pragma unroll
+                        for (int b = 0; b < kB; ++b)
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) s[b][i] = seen.in_range(b * 32 + 8 * (i / 4) + i % 4) ? s[b][i] : -INFINITY;
+                    } else {
+#pragma unroll
+                        for (int b = 0; b < kB; ++b)
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) s[b][i] = seen.sees(b * 32 + 8 * (i / 4) + i % 4) ? s[b][i] : -INFINITY;
+                    }
+                }
+                float top = m;
 #pragma unroll
                 for (int b = 0; b < kB; ++b)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) s[b][i] = __builtin_amdgcn_exp2f((s[b][i] - from) * c2);
+                    for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
+                top = halves<Max>(top);
+                if (__any((top - m) * c2 > 8.f)) {
+                    const float old = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - top) * c2);
+                    l *= old;
+#pragma unroll
+                    for (int d = 0; d < NT; ++d) acc[d] *= old;
+                    m = top;
+                }
+                const float m2 = m == -INFINITY ? 0.f : m * c2;
+                // one operation less than the difference first; m2's rounding, which stands in the exponents and in lse, is below 2^-17 then
+                if (__all(fabsf(m2) < 64.f)) {
+#pragma unroll
+                    for (int b = 0; b < kB; ++b)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], c2, -m2));
+                } else {
+                    const float from = m == -INFINITY ? 0.f : m;
+#pragma unroll
+                    for (int b = 0; b < kB; ++b)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) s[b][i] = __builtin_amdgcn_exp2f((s[b][i] - from) * c2);
+                }
+                float sum[4] = {};
+#pragma unroll
+                for (int b = 0; b < kB; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) sum[i % 4] += s[b][i];
+                l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
             }
-            float sum[4] = {};
-#pragma unroll
-            for (int b = 0; b < kB; ++b)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) sum[i % 4] += s[b][i];
-            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
 #pragma unroll
             for (int b = 0; b < kB; ++b)
 #pragma unroll
                 for (int st = 0; st < Tl::kTSteps; ++st) {
                     const auto pr = Tl::operand(s[b], st);
 #pragma unroll
-                    for (int d = 0; d < NT; ++d) acc[d] = Tl::mma(Tl::turned(values, pl, b, st, d), pr, acc[d]);
+                    for (int d = 0; d < NT; ++d) {
+                        auto rows = Tl::turned(values, pl, b, st, d);
+                        if constexpr (again) rows = Tl::part_of(rows, part, &other);
+                        acc[d] = Tl::mma(rows, pr, acc[d]);
+                    }
                 }
+        }
+        if (again && part != kFinite) {
+            __syncthreads();
+            return false;
         }
         l = halves<Add>(l);
         const float inv = none ? 0.f : 1.f / l;
@@ -123,28 +132,24 @@ __global__ __launch_bounds__(64 * W, NT <= 2 ? 3 : 2) void attn_fwd_kernel(AttnF
         for (int d = 0; d < NT; ++d)
 #pragma unroll
             for (int i = 0; i < 16; ++i) check = fmaf(acc[d][i] *= inv, 0.f, check);
-        return __syncthreads_or(wr.there & (halves<Add>(check) != 0.f));
+        return any_of_workgroup(wr.there & (halves<Add>(check) != 0.f));
     };
-    auto store = [&](uint32_t but) {
-        if (wr.there && !(but >> (lane & 31) & 1)) {
-            put_column<T, NT, VEC>(f.o.at(c.q0 + wr.query, h, w.dim), acc, w.dim);
-            if (lane < 32)
-                f.lse[(int64_t)(c.q0 + wr.query) * w.heads + h] = none ? -INFINITY : (m * c2 + __builtin_amdgcn_logf(l)) * kLn2;
-        }
+    auto store = [&] {
+        if (!wr.there) return;
+        put_column<T, NT, VEC>(f.o.at(c.q0 + wr.query, h, w.dim), acc, w.dim);
+        if (lane < 32) f.lse[(int64_t)(c.q0 + wr.query) * w.heads + h] = none ? -INFINITY : (m * c2 + __builtin_amdgcn_logf(l)) * kLn2;
     };
-    uint32_t bad_rows = 0, by_row = 0;  // rows that see what is not finite; those of them to be computed key by key
-    if (pass(std::false_type{})) {
-        store(0);
+    if (__builtin_expect(!pass(std::false_type{}, kFinite), 1)) return store();
+    kt.load(lds, 0, 0);
+    pass(std::true_type{}, kFinite);
+    store();
+    // a row whose sum of exponentials is NaN is that altogether
+    if (!any_of_workgroup(other) || !any_of_workgroup(wr.there & (l == l))) return;
+#pragma unroll 1
+    for (int part = kPlus; part <= kMinus; ++part) {
         kt.load(lds, 0, 0);
-        pass(std::true_type{});
-        const uint64_t seen_by = __ballot(wr.there && met);
-        bad_rows = (uint32_t)seen_by | (uint32_t)(seen_by >> 32);
-        by_row = __popc(bad_rows) <= kMostByRow ? bad_rows : 0;
-    }
-    store(bad_rows);
-    for (uint32_t bad = by_row; bad; bad &= bad - 1) {
-        const uint32_t r = wr.w0 + __builtin_ctz(bad);
-        forward_row(f, c, (int)(r / w.group), kh * w.group + (int)(r % w.group));
+        pass(std::true_type{}, part);
+        if (wr.there) join_column<T, NT>(f.o.at(c.q0 + wr.query, h, w.dim), acc, w.dim, part == kPlus ? INFINITY : -INFINITY);
     }
 }
 

@@ -33,6 +33,11 @@ __device__ __forceinline__ int swizzle(int row) {
     else return (row >> 2) & 3;
 }
 
+// A sum over rows adds, for rows that do not take part, 0 times their elements: NaN where these are infinities or NaN.  A workgroup whose
+// sums are not finite therefore takes them again in parts: of the elements that are finite; and how often those that do take part are +infinity
+// or NaN, and -infinity or NaN (1 for each), for infinity to be added with that sign where there are any.
+enum Part { kFinite, kPlus, kMinus };
+
 // NT: head width in 32s, rounded up.  What is beyond `dim` is zero in LDS and registers.
 template <typename T, int NT>
 struct Tile {
@@ -94,6 +99,21 @@ struct Tile {
             }
             return v;
         }
+    }
+    // what `part` of a first operand's elements are (Part)
+    static __device__ __forceinline__ Frag part_of(Frag v, int part, bool* bad) {
+        using Bits = typename std::conditional<kBf16, uint16_t, uint32_t>::type;
+        constexpr int kMantissa = kBf16 ? 7 : 23;
+        constexpr Bits kInf = (Bits)(0xffu << kMantissa), kOne = (Bits)(0x7fu << kMantissa), kSign = (Bits)(0x100u << kMantissa);
+        struct All { Bits e[kPer]; } b = __builtin_bit_cast(All, v);
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const Bits size = b.e[i] & (Bits)~kSign;
+            const bool other = size >= kInf, counts = size > kInf || (b.e[i] == kInf) == (part == kPlus);
+            *bad |= other;
+            b.e[i] = part == kFinite ? (other ? (Bits)0 : b.e[i]) : other && counts ? kOne : (Bits)0;
+        }
+        return __builtin_bit_cast(Frag, b);
     }
     // accumulators of 32 rows as the second operand of step s of a contraction over them
     static __device__ __forceinline__ Frag operand(const f32x16& v, int s) {
@@ -204,6 +224,8 @@ __device__ __forceinline__ void wait_tiles() {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     __syncthreads();
 }
+// Whether any thread of the workgroup says so: a scalar, so that nothing is kept for the other way
+__device__ __forceinline__ bool any_of_workgroup(bool x) { return __builtin_amdgcn_readfirstlane(__syncthreads_or(x)) != 0; }
 // A wavefront's loads into LDS of its own
 __device__ __forceinline__ void wait_own_tiles() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
 
@@ -265,6 +287,19 @@ __device__ __forceinline__ void put_column(T* row, const f32x16 (&acc)[NT], int 
                 for (int i = 0; i < 4; ++i)
                     if (at + i < dim) row[at + i] = to_elem<T>(acc[d][4 * g + i]);
             }
+        }
+}
+
+// Infinities and NaN join a row of the result where `counts` (Part) are not zero.  The thread itself has written these elements.
+template <typename T, int NT>
+__device__ __forceinline__ void join_column(T* row, const f32x16 (&counts)[NT], int dim, float infinity) {
+    const int h = (threadIdx.x & 63) >> 5;
+#pragma unroll
+    for (int d = 0; d < NT; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int at = d * 32 + 8 * (i / 4) + 4 * h + i % 4;
+            if (at < dim && counts[d][i] != 0.f) row[at] = to_elem<T>(elem(row[at]) + infinity);
         }
 }
 

@@ -567,3 +567,38 @@ def test_wrong_starts_of_many_rows_stay_inside_of_the_arrays(sp, dt):
     assert (grad[:, :n] == 7).all() and (grad[:, 2 * n:] == 7).all() and (room == 0.25).all()
     q, k, v, do, starts, hs, shape = attn_inputs("far_first_keys", dt)
     check_attention(sp, q, k, v, do, starts, hs, shape, dt, "after wrong starts")
+
+
+def finite_of(t):
+    return t.nan_to_num(0, 0, 0)
+
+
+def check_forward(sp, q, k, v, starts, hs, shape, dt, what):
+    """Inputs may hold infinities and NaN; results have the definition's in the same places."""
+    o, lse = sp.sp_window_attn_fwd(q, k, v, *starts, **shape)
+    u, g = attn_errors(dt, finite_of(q), finite_of(k), int(np.diff(hs[1]).max(initial=0)), shape["scale"])
+    O, LSE, bound = tokens.window_attn_fwd(host(q), host(k), host(v), *hs, shape["left"], shape["right"], shape["sinks"], shape["scale"], u, g)
+    within(lse, LSE, g * (1 + np.where(np.isfinite(LSE), np.abs(LSE), 0)), what + " lse")
+    within(o, O, bound, what + " o")
+    return o, lse
+
+
+def rows_with_infinities(rng, dt, kv, dim, n=200, left=90, sinks=0):
+    """Values that many rows see beside values, in the same tiles, that these rows do not see; in other elements."""
+    q, k, v = rows(rng, dt, n, 2 * kv, dim), rows(rng, dt, n, kv, dim), rows(rng, dt, n, kv, dim)
+    last = dim - 1
+    v[95, 0, 0], v[125, 0, last] = float("inf"), float("nan")              # seen by 95..185 and 125..
+    v[10, 0, 1], v[30, 0, 1], v[31, 0, 2] = float("inf"), float("-inf"), float("-inf")   # both signs for 30..100: NaN
+    v[100, 1, 1], k[170, 1, last] = float("-inf"), float("nan")
+    hs = (np.array([0, n]), np.array([0, n]))
+    starts = [torch.tensor([0, n], dtype=torch.int32, device="cuda")] * 2
+    return q, k, v, starts, hs, dict(left=left, right=0, sinks=sinks, scale=1 / math.sqrt(dim))
+
+
+@pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("dim,kv", [(24, 2), (64, 2), (33, 2), (128, 2), (32, 50), (64, 50), (96, 50), (128, 50)])
+def test_values_that_a_row_does_not_see_beside_ones_that_it_sees(sp, dt, dim, kv):
+    rng = np.random.default_rng(dim + kv)
+    for sinks in (0, 12):
+        q, k, v, starts, hs, shape = rows_with_infinities(rng, dt, kv, dim, sinks=sinks)
+        check_forward(sp, q, k, v, starts, hs, shape, dt, f"sinks {sinks}")
