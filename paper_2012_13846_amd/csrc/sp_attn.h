@@ -120,26 +120,6 @@ __device__ __forceinline__ void put_row(T* row, const float (&acc)[2], int dim) 
 }
 
 template <typename T>
-__device__ __forceinline__ void query_gradient_row(const AttnBwd<T>& g, const Cloud& c, int i, int h) {
-    const Window& w = g.w;
-    const int lane = threadIdx.x & 63, kh = h / w.group;
-    const Seen seen(w, c, i);
-    const int64_t r = c.q0 + i;
-    const float lse = g.lse[r * w.heads + h], delta = g.delta[r * w.heads + h];
-    float acc[2] = {0.f, 0.f};
-    for (int t0 = 0; t0 < seen.n; t0 += 64) {
-        float ds = 0.f;
-        if (t0 + lane < seen.n) {
-            const int64_t j = c.k0 + seen.key(t0 + lane);
-            const float p = __builtin_amdgcn_exp2f((dot(g.q.at(r, h, w.dim), g.k.at(j, kh, w.dim), w.dim) * w.scale - lse) * kLog2e);
-            ds = p * (dot(g.dout.at(r, h, w.dim), g.v.at(j, kh, w.dim), w.dim) - delta) * w.scale;
-        }
-        add_rows<T>(acc, ds, min(64, seen.n - t0), w.dim, [&](int t) { return g.k.at(c.k0 + seen.key(t0 + t), kh, w.dim); });
-    }
-    put_row(g.dq.at(r, h, w.dim), acc, w.dim);
-}
-
-template <typename T>
 __device__ __forceinline__ void key_gradient_row(const AttnBwd<T>& g, const Cloud& c, int j, int kh) {
     const Window& w = g.w;
     const int lane = threadIdx.x & 63;

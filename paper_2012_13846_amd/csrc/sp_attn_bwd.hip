@@ -25,7 +25,6 @@ __global__ __launch_bounds__(64 * W, NT == 1 ? 4 : sizeof(T) * NT == 4 ? 3 : siz
     using Tl = Tile<T, NT>;
     constexpr int kN = kKeys<T, W>, kB = kN / 32, kTileBytes = kN * Tl::kRowBytes;
     __shared__ __attribute__((aligned(1024))) char lds[4 * kTileBytes];
-    __shared__ int marks[kN];
     const Window& w = g.w;
     const RowTile<W> rt(w, tiles);
     const Cloud c(w, rt.cloud);
@@ -78,15 +77,15 @@ __global__ __launch_bounds__(64 * W, NT == 1 ? 4 : sizeof(T) * NT == 4 ? 3 : siz
     }
     if (wr.there && lane < 32) g.delta[stat] = delta;
     f32x16 acc[NT];
-    bool met = false;
-    auto pass = [&](auto again) {  // as in the forward pass
+    bool other = false;  // there are keys that are not finite
+    // As in the forward pass.  Such a key's score is -infinity, its dS 0 and the product NaN, or all of the row is NaN: no signs.
+    auto pass = [&](auto again, int part) {
 #pragma unroll
         for (int d = 0; d < NT; ++d) acc[d] = f32x16{};
         for (int slot = 0, buf = again ? 0 : first_buf; slot < reach.n; slot += kN, buf ^= 1) {
-            char *keys = lds + buf * 2 * kTileBytes, *values = keys + kTileBytes;
+            const char *keys = lds + buf * 2 * kTileBytes, *values = keys + kTileBytes;
             wait_tiles();
             if (slot + kN < reach.n) kt.load(lds, slot + kN, buf ^ 1);
-            if constexpr (again) clean_tiles<T, NT, kN, 64 * W>(keys, values, marks);
             if (reach.none(w, slot, kN, wr.p_min, wr.p_max)) continue;
             const bool all = !again && (wr.whole & reach.all(w, slot, kN, wr.p_min, wr.p_max));
             const SeenInTile seen(w, reach, slot, wr.p);
@@ -106,10 +105,8 @@ __global__ __launch_bounds__(64 * W, NT == 1 ? 4 : sizeof(T) * NT == 4 ? 3 : siz
                     } else {
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
-                            const int r = b * 32 + 8 * (i / 4) + i % 4;
-                            const bool sees = seen.sees(r);
-                            s[i] = sees ? s[i] : 0.f;
-                            if constexpr (again) met |= sees & (marks[r + 4 * (lane >> 5)] != 0);
+                            const float x = again && part != kFinite ? 1.f : s[i];
+                            s[i] = seen.sees(b * 32 + 8 * (i / 4) + i % 4) ? x : 0.f;
                         }
                     }
                 }
@@ -117,35 +114,33 @@ __global__ __launch_bounds__(64 * W, NT == 1 ? 4 : sizeof(T) * NT == 4 ? 3 : siz
                 for (int st = 0; st < Tl::kTSteps; ++st) {
                     const auto ds = Tl::operand(s, st);
 #pragma unroll
-                    for (int d = 0; d < NT; ++d) acc[d] = Tl::mma(Tl::turned(keys, pl, b, st, d), ds, acc[d]);
+                    for (int d = 0; d < NT; ++d) {
+                        auto rows = Tl::turned(keys, pl, b, st, d);
+                        if constexpr (again) rows = Tl::part_of(rows, part, &other);
+                        acc[d] = Tl::mma(rows, ds, acc[d]);
+                    }
                 }
             }
         }
+        if (again && part != kFinite) return false;
         float check = 0.f;
 #pragma unroll
         for (int d = 0; d < NT; ++d)
 #pragma unroll
             for (int i = 0; i < 16; ++i) check = fmaf(acc[d][i] *= w.scale, 0.f, check);
-        return __syncthreads_or(wr.there & (halves<Add>(check) != 0.f));
+        return any_of_workgroup(wr.there & (halves<Add>(check) != 0.f));
     };
-    auto store = [&](uint32_t but) {
-        if (wr.there && !(but >> (lane & 31) & 1)) put_column<T, NT, VEC>(g.dq.at(c.q0 + wr.query, h, w.dim), acc, w.dim);
+    auto store = [&] {
+        if (wr.there) put_column<T, NT, VEC>(g.dq.at(c.q0 + wr.query, h, w.dim), acc, w.dim);
     };
-    uint32_t bad_rows = 0, by_row = 0;
-    if (pass(std::false_type{})) {
-        store(0);
-        kt.load(lds, 0, 0);
-        pass(std::true_type{});
-        const uint64_t seen_by = __ballot(wr.there && met);
-        bad_rows = (uint32_t)seen_by | (uint32_t)(seen_by >> 32);
-        by_row = __popc(bad_rows) <= kMostByRow ? bad_rows : 0;
-    }
-    store(bad_rows);
-    __threadfence_block();  // delta, which other lanes read
-    for (uint32_t bad = by_row; bad; bad &= bad - 1) {
-        const uint32_t r = wr.w0 + __builtin_ctz(bad);
-        query_gradient_row(g, c, (int)(r / w.group), kh * w.group + (int)(r % w.group));
-    }
+    if (__builtin_expect(!pass(std::false_type{}, kFinite), 1)) return store();
+    kt.load(lds, 0, 0);
+    pass(std::true_type{}, kFinite);
+    store();
+    if (!any_of_workgroup(other) || !any_of_workgroup(wr.there & (fabsf(l2) < INFINITY))) return;
+    kt.load(lds, 0, 0);
+    pass(std::true_type{}, kEither);
+    if (wr.there) join_column<T, NT>(g.dq.at(c.q0 + wr.query, h, w.dim), acc, w.dim, NAN);
 }
 
 // The first keys of a cloud are seen by all later queries: a tile with them would take many times the others' time.  With few of them

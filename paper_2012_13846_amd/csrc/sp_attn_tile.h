@@ -35,8 +35,8 @@ __device__ __forceinline__ int swizzle(int row) {
 
 // A sum over rows adds, for rows that do not take part, 0 times their elements: NaN where these are infinities or NaN.  A workgroup whose
 // sums are not finite therefore takes them again in parts: of the elements that are finite; and how often those that do take part are +infinity
-// or NaN, and -infinity or NaN (1 for each), for infinity to be added with that sign where there are any.
-enum Part { kFinite, kPlus, kMinus };
+// or NaN, and -infinity or NaN (1 for each), for infinity to be added with that sign where there are any; or are either.
+enum Part { kFinite, kPlus, kMinus, kEither };
 
 // NT: head width in 32s, rounded up.  What is beyond `dim` is zero in LDS and registers.
 template <typename T, int NT>
@@ -109,7 +109,7 @@ struct Tile {
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             const Bits size = b.e[i] & (Bits)~kSign;
-            const bool other = size >= kInf, counts = size > kInf || (b.e[i] == kInf) == (part == kPlus);
+            const bool other = size >= kInf, counts = size > kInf || part == kEither || (b.e[i] == kInf) == (part == kPlus);
             *bad |= other;
             b.e[i] = part == kFinite ? (other ? (Bits)0 : b.e[i]) : other && counts ? kOne : (Bits)0;
         }
@@ -290,16 +290,16 @@ __device__ __forceinline__ void put_column(T* row, const f32x16 (&acc)[NT], int 
         }
 }
 
-// Infinities and NaN join a row of the result where `counts` (Part) are not zero.  The thread itself has written these elements.
+// `other` (an infinity, NaN) joins a row of the result where `counts` (Part) are not zero.  The thread itself has written these elements.
 template <typename T, int NT>
-__device__ __forceinline__ void join_column(T* row, const f32x16 (&counts)[NT], int dim, float infinity) {
+__device__ __forceinline__ void join_column(T* row, const f32x16 (&counts)[NT], int dim, float other) {
     const int h = (threadIdx.x & 63) >> 5;
 #pragma unroll
     for (int d = 0; d < NT; ++d)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             const int at = d * 32 + 8 * (i / 4) + 4 * h + i % 4;
-            if (at < dim && counts[d][i] != 0.f) row[at] = to_elem<T>(elem(row[at]) + infinity);
+            if (at < dim && counts[d][i] != 0.f) row[at] = to_elem<T>(elem(row[at]) + other);
         }
 }
 

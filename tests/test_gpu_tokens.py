@@ -602,3 +602,33 @@ def test_values_that_a_row_does_not_see_beside_ones_that_it_sees(sp, dt, dim, kv
     for sinks in (0, 12):
         q, k, v, starts, hs, shape = rows_with_infinities(rng, dt, kv, dim, sinks=sinks)
         check_forward(sp, q, k, v, starts, hs, shape, dt, f"sinks {sinks}")
+
+
+def check_gradients(sp, q, k, v, do, starts, hs, shape, dt, names, what):
+    """From the definition's o and lse, as check_attention; inputs may hold infinities and NaN."""
+    u, g = attn_errors(dt, finite_of(q), finite_of(k), int(np.diff(hs[1]).max(initial=0)), shape["scale"])
+    s = (shape["left"], shape["right"], shape["sinks"], shape["scale"])
+    O, LSE, _ = tokens.window_attn_fwd(host(q), host(k), host(v), *hs, *s, u, g)
+    o, lse = torch.from_numpy(O).to(dt).cuda(), torch.from_numpy(LSE).to(F32).cuda()
+    grads = sp.sp_window_attn_bwd(q, k, v, o, do, lse, *starts, **shape)
+    queries = int(np.diff(hs[0]).max(initial=0)) * (q.shape[1] // k.shape[1])
+    g += 2 * U32 * (float(np.abs(LSE[np.isfinite(LSE)]).max(initial=0)) + queries)
+    with np.errstate(invalid="ignore"):
+        want, bounds = tokens.window_attn_bwd(host(q), host(k), host(v), host(o), host(do), host(lse), *hs, *s, u, g)
+    for got, ref, b, name in zip(grads, want, bounds, ("dq", "dk", "dv")):
+        if name in names:
+            within(got, ref, b, f"{what} {name}")
+
+
+@pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("dim,kv", [(24, 2), (64, 2), (33, 2), (128, 2), (32, 50), (64, 50), (96, 50), (128, 50)])
+def test_query_gradients_beside_keys_that_are_not_seen(sp, dt, dim, kv):
+    """Among the keys is one of score -infinity: it has no share, but 0 times its infinity is NaN in this element of those that see it."""
+    rng = np.random.default_rng(dim * kv)
+    for left, sinks in ((90, 0), (90, 12), (150, 0)):         # in bf16 with the sum dout . v of few keys, and with dout . o
+        q, k, v, starts, hs, shape = rows_with_infinities(rng, dt, kv, dim, left=left, sinks=sinks)
+        q[:, :, 3] = q[:, :, 3].abs() + 0.5
+        k[80, 0, 3], k[140, 1, 3] = float("-inf"), float("-inf")
+        do = rows(rng, dt, *q.shape)
+        check_gradients(sp, q, k, v, do, starts, hs, shape, dt, ("dq",), f"left {left} sinks {sinks}")
+        check_gradients(sp, q, k, finite_of(v), do, starts, hs, shape, dt, ("dq",), f"left {left} sinks {sinks}, finite values")
