@@ -231,12 +231,12 @@ struct KeyGrads {
     typename Tl::Frag k[Tl::kSteps], v[VLDS ? 1 : Tl::kSteps];
     const char* v_tile;  // this wavefront's 32 rows
     f32x16 dk[NT], dv[NT];
-    // rows 32 b .. of the tiles q and dout
+    // Probabilities and dS of rows 32 b .. of the tiles q and dout; `counts`: 1 for each pair that is seen
     template <int N, typename Seen>
-    __device__ __forceinline__ void add(const char* q, const char* dout, const RowStats<N>& stats, const typename Tl::Place& pl, int b, float c2,
-                                        bool all, Seen seen) {
+    __device__ __forceinline__ void scores(f32x16& s, f32x16& dp, const char* q, const char* dout, const RowStats<N>& stats,
+                                           const typename Tl::Place& pl, int b, float c2, bool all, Seen seen, bool counts = false) const {
         const int half = b * 32 + 4 * ((threadIdx.x & 63) >> 5);
-        f32x16 s = {}, dp;  // dp begins at -delta
+        s = f32x16{};  // dp begins at -delta
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
             const f32x4 de = *reinterpret_cast<const f32x4*>(stats.minus_delta + half + 8 * g);
@@ -263,11 +263,13 @@ struct KeyGrads {
                 const int4 p = *reinterpret_cast<const int4*>(stats.p + half + 8 * g);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const bool sees = seen(i == 0 ? p.x : i == 1 ? p.y : i == 2 ? p.z : p.w, half + 8 * g + i);
-                    s[4 * g + i] = sees ? s[4 * g + i] : 0.f;
-                    dp[4 * g + i] = sees ? dp[4 * g + i] : 0.f;
+                    const bool sees = seen(i == 0 ? p.x : i == 1 ? p.y : i == 2 ? p.z : p.w);
+                    s[4 * g + i] = !sees ? 0.f : counts ? 1.f : s[4 * g + i];
+                    dp[4 * g + i] = !sees ? 0.f : counts ? 1.f : dp[4 * g + i];
                 }
             }
+    }
+    __device__ __forceinline__ void products(const f32x16& s, const f32x16& dp, const char* q, const char* dout, const typename Tl::Place& pl, int b) {
 #pragma unroll
         for (int st = 0; st < Tl::kTSteps; ++st) {
             const auto p = Tl::operand(s, st), ds = Tl::operand(dp, st);
@@ -278,7 +280,23 @@ struct KeyGrads {
             }
         }
     }
+    // Where sums were not finite, one of these instead (Part): into `dv`, from rows 32 b .. of `rows`, q's or dout's.  Returns whether they had others.
+    __device__ __forceinline__ bool product_of(const f32x16& shares, const char* rows, const typename Tl::Place& pl, int b, int part) {
+        bool other = false;
+#pragma unroll
+        for (int st = 0; st < Tl::kTSteps; ++st) {
+            const auto x = Tl::operand(shares, st);
+#pragma unroll
+            for (int d = 0; d < NT; ++d) dv[d] = Tl::mma(Tl::part_of(Tl::turned(rows, pl, b, st, d), part, &other), x, dv[d]);
+        }
+        return other;
+    }
 };
+
+// The sums that a workgroup takes again, one after another, where they were not finite: dk's and dv's finite part; and, where rows of dout are not
+// finite, how often +infinity and -infinity join dv.  A query that is not finite has scores that are not, and all of its shares are NaN: no signs.
+enum Again { kDk, kDv, kDvPlus, kDvMinus, kAgain };
+__device__ __forceinline__ int part_of_again(int what) { return what <= kDv ? kFinite : what == kDvPlus ? kPlus : kMinus; }
 
 template <typename T, int NT>
 constexpr bool kValuesInLds = sizeof(T) == 2 && NT >= 3;
@@ -299,7 +317,6 @@ __global__ __launch_bounds__(64 * W, NT == 1 ? (sizeof(T) == 2 ? 4 : 3) : sizeof
     __shared__ __attribute__((aligned(1024))) char lds[4 * kTileBytes];
     __shared__ __attribute__((aligned(1024))) char values[kVLds ? kRows * Tl::kRowBytes : 16];
     __shared__ RowStats<kN> stats[2];
-    __shared__ int marks[kN];
     const Window& w = g.w;
     const uint32_t item = item_of_block(blockIdx.x, gridDim.x), t = item % (uint32_t)tiles;
     const int kh = (int)(item / (uint32_t)tiles);
@@ -319,7 +336,7 @@ __global__ __launch_bounds__(64 * W, NT == 1 ? (sizeof(T) == 2 ? 4 : 3) : sizeof
     const QueryTiles<T, NT, VEC, kN, 64 * W> qt(g, c, kh, end);
     KeyGrads<T, NT, kVLds> kg;
     const float c2 = exponent_scale(w);
-    bool met = false;
+    bool other = false;  // there are rows of dout that are not finite
     auto stat_of = [&](int row) {
         const int thread = threadIdx.x;
         return row_stat(g, c, kh, row + thread, (thread < qt.step) & (row + thread < end));
@@ -355,13 +372,13 @@ __global__ __launch_bounds__(64 * W, NT == 1 ? (sizeof(T) == 2 ? 4 : 3) : sizeof
     // j - right <= p <= j + left, for the first keys all p behind
     const int low = j - w.right;
     const uint32_t width = j < sinks ? 0x7fffffffu : (uint32_t)(w.left + w.right);
-    auto pass = [&](auto again) {
+    auto pass = [&](auto again, int what) {
 #pragma unroll
         for (int d = 0; d < NT; ++d) kg.dk[d] = kg.dv[d] = f32x16{};
         int buf = 0;
         for (int n = 0; n < steps; ++n, buf ^= 1) {
             const int row = row_of(n);
-            char *q = lds + buf * 2 * kTileBytes, *dout = q + kTileBytes;
+            const char *q = lds + buf * 2 * kTileBytes, *dout = q + kTileBytes;
             wait_tiles();
             RowStat next{};
             const bool more = n + 1 < steps;
@@ -369,49 +386,58 @@ __global__ __launch_bounds__(64 * W, NT == 1 ? (sizeof(T) == 2 ? 4 : 3) : sizeof
                 qt.load(lds + (buf ^ 1) * 2 * kTileBytes, row_of(n + 1));
                 next = stat_of(row_of(n + 1));
             }
-            if constexpr (again) clean_tiles<T, NT, kN, 64 * W>(q, dout, marks);
             const int p_min = (int)((uint32_t)row / (uint32_t)w.group) + c.off;
             const int p_max = (int)((uint32_t)(min(row + qt.step, end) - 1) / (uint32_t)w.group) + c.off;
             const bool none = (jw >= c.b) | (jw > p_max + w.right) | ((jw + kWaveRows - 1 < p_min - w.left) & (jw >= sinks));
             const bool all = !again && ((row + kN <= end) & (qt.step == kN) & (jw + kWaveRows - 1 <= p_min + w.right) & (jw >= p_max - w.left));
+            const auto seen = [&](int p) { return (uint32_t)(p - low) <= width; };
             if (!none)
 #pragma unroll 1
-                for (int b = 0; b < kB; ++b)
-                    kg.add(q, dout, stats[buf], pl, b, c2, all, [&](int p, int r) {
-                        const bool seen = (uint32_t)(p - low) <= width;
-                        if constexpr (again) met |= seen & (marks[r] != 0);
-                        return seen;
-                    });
+                for (int b = 0; b < kB; ++b) {
+                    f32x16 s, dp;
+                    kg.scores(s, dp, q, dout, stats[buf], pl, b, c2, all, seen, again && what > kDv);
+                    if constexpr (again) other |= kg.product_of(what == kDk ? dp : s, what == kDk ? q : dout, pl, b, part_of_again(what)) & (what == kDv);
+                    else kg.products(s, dp, q, dout, pl, b);
+                }
             if (more && threadIdx.x < kN) stats[buf ^ 1].put(next, threadIdx.x);
         }
+        if (again) return __syncthreads(), false;
         float check = 0.f;
 #pragma unroll
         for (int d = 0; d < NT; ++d)
 #pragma unroll
             for (int i = 0; i < 16; ++i) check = fmaf(kg.dk[d][i] *= w.scale, 0.f, fmaf(kg.dv[d][i], 0.f, check));
-        return __syncthreads_or(there & (halves<Add>(check) != 0.f));
+        return any_of_workgroup(there & (halves<Add>(check) != 0.f));
     };
     const bool part = split_here && j < split.sinks && c.partners;
-    auto store = [&](uint32_t but) {
-        if (there && part) {
-            float* to = split.first + split_at(w, split, cn - 1, kh, j);
-            if (met) kg.dk[0][0] = NAN;  // sends attn_join_kernel over the rows one by one
-            put_column<float, NT, false>(to, kg.dk, w.dim);
-            put_column<float, NT, false>(to + w.dim, kg.dv, w.dim);
-        } else if (there && !(but >> (lane & 31) & 1)) {
-            put_column<T, NT, VEC>(g.dk.at(c.k0 + j, kh, w.dim), kg.dk, w.dim);
-            put_column<T, NT, VEC>(g.dv.at(c.k0 + j, kh, w.dim), kg.dv, w.dim);
-        }
+    // of this key's dk (0) and dv (1)
+    auto sums = [&](int which) { return split.first + split_at(w, split, cn - 1, kh, j) + which * w.dim; };
+    auto row = [&](int which) { return which ? g.dv.at(c.k0 + j, kh, w.dim) : g.dk.at(c.k0 + j, kh, w.dim); };
+    auto store = [&](int which, const f32x16(&acc)[NT]) {
+        if (there && part) put_column<float, NT, false>(sums(which), acc, w.dim);
+        else if (there) put_column<T, NT, VEC>(row(which), acc, w.dim);
     };
-    uint32_t bad_rows = 0;  // keys that such rows see keep the first sums, whose finite ones are right
-    if (pass(std::false_type{})) {
-        store(0);
-        start();
-        pass(std::true_type{});
-        const uint64_t seen_by = __ballot(there && !part && met);
-        bad_rows = (uint32_t)seen_by | (uint32_t)(seen_by >> 32);
+    if (__builtin_expect(!pass(std::false_type{}, 0), 1)) {
+        store(0, kg.dk);
+        store(1, kg.dv);
+        return;
     }
-    store(bad_rows);
+#pragma unroll 1
+    for (int what = kDk; what < kAgain; ++what) {
+        if (what == kDvPlus && !any_of_workgroup(other)) break;
+        start();
+        pass(std::true_type{}, what);
+        if (what <= kDv) {
+            if (what == kDk)
+#pragma unroll
+                for (int d = 0; d < NT; ++d) kg.dv[d] *= w.scale;
+            store(what, kg.dv);
+        } else if (there && part) {
+            join_column<float, NT>(sums(1), kg.dv, w.dim, what == kDvPlus ? INFINITY : -INFINITY);
+        } else if (there) {
+            join_column<T, NT>(row(1), kg.dv, w.dim, what == kDvPlus ? INFINITY : -INFINITY);
+        }
+    }
 }
 
 // Reads every row once for a few keys: bound by memory's latency at one or two wavefronts a SIMD (373601 rows of 8 heads of 32: 146 us,
@@ -459,7 +485,9 @@ __global__ __launch_bounds__(64, 1) void attn_far_kernel(AttnBwd<T> g, Split spl
         }
         const char* q = lds + buf * 2 * kTileBytes;
         const bool all = (row + 32 <= end) & (qt.step == 32) & (key0 + 31 < (int)((uint32_t)row / (uint32_t)w.group) + c.off - w.left);
-        kg.add(q, q + kTileBytes, stats[buf], pl, 0, c2, all, [&](int p, int) { return j < p - w.left; });
+        f32x16 s, dp;
+        kg.scores(s, dp, q, q + kTileBytes, stats[buf], pl, 0, c2, all, [&](int p) { return j < p - w.left; });
+        kg.products(s, dp, q, q + kTileBytes, pl, 0);
         if (more && lane < 32) stats[buf ^ 1].put(next, lane);
     }
     if (there) {

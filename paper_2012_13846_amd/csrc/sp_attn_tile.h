@@ -229,38 +229,6 @@ __device__ __forceinline__ bool any_of_workgroup(bool x) { return __builtin_amdg
 // A wavefront's loads into LDS of its own
 __device__ __forceinline__ void wait_own_tiles() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
 
-// Infinities and not-a-numbers of a tile become zero, and their rows are marked: for the second run of a workgroup whose results are
-// not finite (0 * infinity), which takes what a row does not see out of its sums.
-template <typename T, int NT, int THREADS>
-__device__ __forceinline__ void clean_tile(char* tile, int rows, int* marks) {
-    using Tl = Tile<T, NT>;
-    for (int p = threadIdx.x; p < rows * Tl::kC; p += THREADS) {
-        auto e = __builtin_bit_cast(typename Tl::Raw, *reinterpret_cast<const uint4*>(tile + p * 16));
-        bool bad = false;
-#pragma unroll
-        for (int i = 0; i < Tl::kPer; ++i)
-            if (!(fabsf(elem(e.e[i])) < INFINITY)) {
-                bad = true;
-                e.e[i] = 0;
-            }
-        if (bad) {
-            *reinterpret_cast<uint4*>(tile + p * 16) = __builtin_bit_cast(uint4, e);
-            marks[p / Tl::kC] = 1;
-        }
-    }
-}
-template <typename T, int NT, int ROWS, int THREADS>
-__device__ __forceinline__ void clean_tiles(char* a, char* b, int* marks) {
-    if (threadIdx.x < ROWS) marks[threadIdx.x] = 0;
-    __syncthreads();
-    clean_tile<T, NT, THREADS>(a, ROWS, marks);
-    clean_tile<T, NT, THREADS>(b, ROWS, marks);
-    __syncthreads();
-}
-
-// Rows that see what is not finite are computed one by one where they are few: each costs about what a wavefront's 32 rows cost
-// together.  More of them (a key that a whole window sees, a run that has diverged) keep the first sums, whose finite ones are right.
-constexpr int kMostByRow = 8;
 // the two halves of a wavefront combined, in both
 template <typename Op>
 __device__ __forceinline__ float halves(float v) {

@@ -616,8 +616,11 @@ def check_gradients(sp, q, k, v, do, starts, hs, shape, dt, names, what):
     with np.errstate(invalid="ignore"):
         want, bounds = tokens.window_attn_bwd(host(q), host(k), host(v), host(o), host(do), host(lse), *hs, *s, u, g)
     for got, ref, b, name in zip(grads, want, bounds, ("dq", "dk", "dv")):
-        if name in names:
-            within(got, ref, b, f"{what} {name}")
+        if name not in names:
+            continue
+        if name != "dv":                                      # dout . o of an infinity has a sign, but not as a sum over keys
+            got, ref = torch.where(torch.isfinite(got), got, float("nan")), np.where(np.isfinite(ref), ref, np.nan)
+        within(got, ref, b, f"{what} {name}")
 
 
 @pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
@@ -632,3 +635,18 @@ def test_query_gradients_beside_keys_that_are_not_seen(sp, dt, dim, kv):
         do = rows(rng, dt, *q.shape)
         check_gradients(sp, q, k, v, do, starts, hs, shape, dt, ("dq",), f"left {left} sinks {sinks}")
         check_gradients(sp, q, k, finite_of(v), do, starts, hs, shape, dt, ("dq",), f"left {left} sinks {sinks}, finite values")
+
+
+@pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("dim,kv", [(24, 2), (64, 2), (33, 2), (128, 2), (32, 50), (64, 50), (96, 50), (128, 50)])
+def test_key_gradients_beside_queries_that_do_not_see_the_key(sp, dt, dim, kv):
+    rng = np.random.default_rng(dim - kv + 100)
+    for left, sinks in ((90, 0), (60, 7)):
+        n, last = 200, dim - 1
+        q, do = rows(rng, dt, n, 2 * kv, dim), rows(rng, dt, n, 2 * kv, dim)
+        k, v = rows(rng, dt, n, kv, dim), rows(rng, dt, n, kv, dim)
+        do[99, 0, 2], do[40, 1, 4], do[45, 0, 4], do[130, 0, last] = float("inf"), float("inf"), float("-inf"), float("nan")
+        do[97, 2, 1], q[103, 3, last], k[120, 0, 0] = float("-inf"), float("nan"), float("nan")
+        hs, starts = (np.array([0, n]), np.array([0, n])), [torch.tensor([0, n], dtype=torch.int32, device="cuda")] * 2
+        check_gradients(sp, q, k, v, do, starts, hs, dict(left=left, right=0, sinks=sinks, scale=1 / math.sqrt(dim)), dt, ("dq", "dk", "dv"),
+                        f"left {left} sinks {sinks}")
