@@ -464,38 +464,65 @@ __global__ __launch_bounds__(64, 1) void attn_far_kernel(AttnBwd<T> g, Split spl
     const QueryTiles<T, NT, VEC, 32, 64> qt(g, c, kh, end);
     KeyGrads<T, NT, false> kg;
     auto stat_of = [&](int row) { return row_stat(g, c, kh, row + lane, (lane < qt.step) & (row + lane < end)); };
-    qt.load(lds, begin);
-    {
+    auto start = [&] {
+        wait_own_tiles();  // nothing of an earlier pass is still read
+        qt.load(lds, begin);
         const RowStat r = stat_of(begin);
         if (lane < 32) stats[0].put(r, lane);
-    }
+    };
+    start();
     Tl::template load_row<VEC>(kg.k, g.k.at(c.k0 + j, kh, w.dim), w.dim, there, w.scale < 0.f);
     Tl::template load_row<VEC>(kg.v, g.v.at(c.k0 + j, kh, w.dim), w.dim, there, false);
     const float c2 = exponent_scale(w);
+    bool other = false;
+    auto pass = [&](auto again, int what) {  // as in the keys' kernel
 #pragma unroll
-    for (int d = 0; d < NT; ++d) kg.dk[d] = kg.dv[d] = f32x16{};
-    int buf = 0;
-    for (int row = begin; row < end; row += qt.step, buf ^= 1) {
-        wait_own_tiles();
-        RowStat next{};
-        const bool more = row + qt.step < end;
-        if (more) {
-            qt.load(lds + (buf ^ 1) * 2 * kTileBytes, row + qt.step);
-            next = stat_of(row + qt.step);
+        for (int d = 0; d < NT; ++d) kg.dk[d] = kg.dv[d] = f32x16{};
+        int buf = 0;
+        for (int row = begin; row < end; row += qt.step, buf ^= 1) {
+            wait_own_tiles();
+            RowStat next{};
+            const bool more = row + qt.step < end;
+            if (more) {
+                qt.load(lds + (buf ^ 1) * 2 * kTileBytes, row + qt.step);
+                next = stat_of(row + qt.step);
+            }
+            const char *q = lds + buf * 2 * kTileBytes, *dout = q + kTileBytes;
+            const bool all = !again && ((row + 32 <= end) & (qt.step == 32) & (key0 + 31 < (int)((uint32_t)row / (uint32_t)w.group) + c.off - w.left));
+            f32x16 s, dp;
+            kg.scores(s, dp, q, dout, stats[buf], pl, 0, c2, all, [&](int p) { return j < p - w.left; }, again && what > kDv);
+            if constexpr (again) other |= kg.product_of(what == kDk ? dp : s, what == kDk ? q : dout, pl, 0, part_of_again(what)) & (what == kDv);
+            else kg.products(s, dp, q, dout, pl, 0);
+            if (more && lane < 32) stats[buf ^ 1].put(next, lane);
         }
-        const char* q = lds + buf * 2 * kTileBytes;
-        const bool all = (row + 32 <= end) & (qt.step == 32) & (key0 + 31 < (int)((uint32_t)row / (uint32_t)w.group) + c.off - w.left);
-        f32x16 s, dp;
-        kg.scores(s, dp, q, q + kTileBytes, stats[buf], pl, 0, c2, all, [&](int p) { return j < p - w.left; });
-        kg.products(s, dp, q, q + kTileBytes, pl, 0);
-        if (more && lane < 32) stats[buf ^ 1].put(next, lane);
-    }
-    if (there) {
+    };
+    float* const sums = split.far + split_at(w, split, t, kh, j);  // dk's, then dv's
+    auto scaled = [&](f32x16(&acc)[NT]) {
 #pragma unroll
-        for (int d = 0; d < NT; ++d) kg.dk[d] *= w.scale;
-        float* to = split.far + split_at(w, split, t, kh, j);
-        put_column<float, NT, false>(to, kg.dk, w.dim);
-        put_column<float, NT, false>(to + w.dim, kg.dv, w.dim);
+        for (int d = 0; d < NT; ++d) acc[d] *= w.scale;
+    };
+    pass(std::false_type{}, 0);
+    scaled(kg.dk);
+    float check = 0.f;
+#pragma unroll
+    for (int d = 0; d < NT; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) check = fmaf(kg.dk[d][i], 0.f, fmaf(kg.dv[d][i], 0.f, check));
+    if (__builtin_expect(!__any(there & (check != 0.f)), 1)) {
+        if (!there) return;
+        put_column<float, NT, false>(sums, kg.dk, w.dim);
+        put_column<float, NT, false>(sums + w.dim, kg.dv, w.dim);
+        return;
+    }
+#pragma unroll 1
+    for (int what = kDk; what < kAgain; ++what) {
+        if (what == kDvPlus && !__any(other)) break;
+        start();
+        pass(std::true_type{}, what);
+        if (what == kDk) scaled(kg.dv);
+        if (!there) continue;
+        if (what <= kDv) put_column<float, NT, false>(sums + what * w.dim, kg.dv, w.dim);
+        else join_column<float, NT>(sums + w.dim, kg.dv, w.dim, what == kDvPlus ? INFINITY : -INFINITY);
     }
 }
 
@@ -523,22 +550,14 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnBwd<T> g, Split
     __syncthreads();
     if (wave) return;
     const float* first = split.first + split_at(w, split, cn - 1, kh, j);
-    float sum[2][2] = {}, check = 0.f;
+    T* const to[2] = {g.dk.at(c.k0 + j, kh, w.dim), g.dv.at(c.k0 + j, kh, w.dim)};
     for (int q = 0; q < 2; ++q)
-        for (int e = 0; e < 2; ++e)
-            if (lane + 64 * e < w.dim) {
-                const int at = q * w.dim + lane + 64 * e;
-                float s = first[at];
-                for (int k = 0; k < 4; ++k) s += sums[k][at];
-                sum[q][e] = s;
-                check = fmaf(s, 0.f, check);
-            }
-    if (__any(check != 0.f)) {
-        key_gradient_row(g, c, j, kh);
-        return;
-    }
-    put_row(g.dk.at(c.k0 + j, kh, w.dim), sum[0], w.dim);
-    put_row(g.dv.at(c.k0 + j, kh, w.dim), sum[1], w.dim);
+        for (int e = lane; e < w.dim; e += 64) {
+            const int at = q * w.dim + e;
+            float s = first[at];
+            for (int k = 0; k < 4; ++k) s += sums[k][at];
+            to[q][e] = to_elem<T>(s);
+        }
 }
 
 template <typename T, int NT, bool VEC, int W>

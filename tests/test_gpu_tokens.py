@@ -650,3 +650,52 @@ def test_key_gradients_beside_queries_that_do_not_see_the_key(sp, dt, dim, kv):
         hs, starts = (np.array([0, n]), np.array([0, n])), [torch.tensor([0, n], dtype=torch.int32, device="cuda")] * 2
         check_gradients(sp, q, k, v, do, starts, hs, dict(left=left, right=0, sinks=sinks, scale=1 / math.sqrt(dim)), dt, ("dq", "dk", "dv"),
                         f"left {left} sinks {sinks}")
+
+
+def far_first_keys(dt, n, heads, kv, dim, left, sinks, seed=5):
+    """Clouds so long that the first keys' sums are split, one of them short."""
+    rng = np.random.default_rng(seed)
+    hs = (np.array([0, n, n + 30]),) * 2
+    q, do = rows(rng, dt, n + 30, heads, dim), rows(rng, dt, n + 30, heads, dim)
+    k, v = rows(rng, dt, n + 30, kv, dim), rows(rng, dt, n + 30, kv, dim)
+    starts = [torch.tensor(hs[0], dtype=torch.int32, device="cuda")] * 2
+    return q, k, v, do, starts, hs, dict(left=left, right=0, sinks=sinks, scale=1 / math.sqrt(dim))
+
+
+@pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("heads,kv,dim,sinks", [(2, 1, 64, 4), (4, 2, 24, 40), (16, 4, 128, 4), (3, 3, 33, 5)])
+def test_first_keys_gradients_of_rows_with_infinities(sp, dt, heads, kv, dim, sinks):
+    """Queries and output gradients that are not finite, inside of the first keys' window, behind it, and in chunks where other first keys do
+    not see them yet."""
+    q, k, v, do, starts, hs, shape = far_first_keys(dt, 2300, heads, kv, dim, 20, sinks)
+    check_gradients(sp, q, k, v, do, starts, hs, shape, dt, ("dq", "dk", "dv"), "finite")
+    do[1700, 0, 1], do[1200, 0, 1], do[900, heads - 1, 2], do[15, heads - 1, 3] = float("inf"), float("-inf"), float("inf"), float("nan")
+    do[23, 0, 4] = float("-inf")
+    check_gradients(sp, q, k, v, do, starts, hs, shape, dt, ("dq", "dk", "dv"), "dout")
+    q[1500, 0, 0], k[2, kv - 1, 0] = float("nan"), float("nan")
+    check_gradients(sp, q, k, v, do, starts, hs, shape, dt, ("dq", "dk", "dv"), "queries and keys")
+
+
+def test_first_keys_gradients_of_a_diverged_run_take_a_bounded_time(sp):
+    """Sums that are not finite are taken again, four times at most: no more than five times the time in all (and what two clocks differ)."""
+    n = 20000
+    q, k, v, do, starts, hs, shape = far_first_keys(BF16, n, 8, 2, 64, 100, 4)
+    o, lse = sp.sp_window_attn_fwd(q, k, v, *starts, **shape)
+
+    def milliseconds(q, do, o, lse):
+        times = []
+        for _ in range(4):
+            begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            begin.record()
+            sp.sp_window_attn_bwd(q, k, v, o, do, lse, *starts, **shape)
+            end.record()
+            torch.cuda.synchronize()
+            times.append(begin.elapsed_time(end))
+        return min(times[1:])
+
+    usual = milliseconds(q, do, o, lse)
+    one = do.clone()
+    one[n - 5, 3, 7] = float("inf")
+    assert milliseconds(q, one, o, lse) < 6 * usual
+    none = torch.full_like(q, float("nan"))
+    assert milliseconds(none, none, none, torch.full_like(lse, float("nan"))) < 6 * usual
