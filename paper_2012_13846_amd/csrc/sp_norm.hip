@@ -18,6 +18,10 @@ namespace {
 template <int LANES>
 constexpr int kBlock = LANES > 256 ? LANES : 256;
 
+// A row with an infinity or NaN has neither spread nor scale: NaN, which a maximum with zero would lose.  Its mean is its sum's.
+__device__ __forceinline__ float rstd_of(float var, float eps) { return 1.f / sqrtf((var < 0.f ? 0.f : var) + eps); }
+__device__ __forceinline__ float mean_of(float m0, float delta) { return delta == delta ? m0 + delta : m0; }
+
 template <typename T, int V, int LANES, int P>
 __global__ __launch_bounds__(kBlock<LANES>) void layer_norm_fwd_kernel(const T* __restrict__ x, int64_t n, int c,
                                                                        const float* __restrict__ gamma, const float* __restrict__ beta,
@@ -69,9 +73,9 @@ __global__ __launch_bounds__(kBlock<LANES>) void layer_norm_fwd_kernel(const T* 
             }
         reduce_lanes<LANES, Add>(q, room, &turn);
         const float delta = q[0] * inv;
-        const float r = 1.f / sqrtf(fmaxf(q[1] * inv - delta * delta, 0.f) + eps);
+        const float r = rstd_of(q[1] * inv - delta * delta, eps);
         if (l == 0) {
-            mean[row] = m0 + delta;
+            mean[row] = mean_of(m0, delta);
             rstd[row] = r;
         }
 #pragma unroll
@@ -206,9 +210,9 @@ __global__ __launch_bounds__(kWide) void layer_norm_fwd_wide_kernel(const T* __r
         }
         reduce_lanes<kWide, Add>(q, room, &turn);
         const float delta = q[0] / (float)c;
-        const float r = 1.f / sqrtf(fmaxf(q[1] / (float)c - delta * delta, 0.f) + eps);
+        const float r = rstd_of(q[1] / (float)c - delta * delta, eps);
         if (threadIdx.x == 0) {
-            mean[row] = m0 + delta;
+            mean[row] = mean_of(m0, delta);
             rstd[row] = r;
         }
         for (int j = threadIdx.x; j < c; j += kWide) y[row * c + j] = to_elem<T>((elem(xr[j]) - m0 - delta) * r * gamma[j] + beta[j]);

@@ -699,3 +699,18 @@ def test_first_keys_gradients_of_a_diverged_run_take_a_bounded_time(sp):
     assert milliseconds(q, one, o, lse) < 6 * usual
     none = torch.full_like(q, float("nan"))
     assert milliseconds(none, none, none, torch.full_like(lse, float("nan"))) < 6 * usual
+
+
+# ---- statistics and teachers that are not finite, extreme temperatures and windows -------------------------------
+@pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("c", [16, 77, 1024, 40001])
+def test_layer_norm_statistics_of_rows_with_infinities(sp, c, dt):
+    rng = np.random.default_rng(c)
+    x, gamma, beta = rows(rng, dt, 8, c), rows(rng, F32, c, scale=0.1, shift=1), rows(rng, F32, c)
+    x[1, 3], x[3, c - 1], x[4, 0], x[6, 1], x[6, 9] = float("nan"), float("inf"), float("-inf"), float("inf"), float("-inf")
+    y, mean, rstd = sp.sp_layer_norm_fwd(x, gamma, beta)
+    with np.errstate(invalid="ignore"):
+        Y, M, R = tokens.layer_norm_fwd(host(x), host(gamma), host(beta), 1e-5)
+    for got, want in ((y, Y), (mean, M), (rstd, R)):
+        assert np.array_equal(np.isnan(host(got)), np.isnan(want)) and np.array_equal(np.isinf(host(got)), np.isinf(want))
+    assert float(mean[3]) == float("inf") and float(mean[4]) == float("-inf") and torch.isnan(rstd[[1, 3, 4, 6]]).all()
