@@ -162,7 +162,7 @@ def distill(z, top, index, temperature, weight=None):
         lse = s.max() + np.log(np.exp(s - s.max()).sum())
         with np.errstate(divide="ignore"):
             log_a = np.log(a)
-        some = a > 0
+        some = a != 0
         loss += w * temperature ** 2 * (a[some] * (log_a[some] - s[index[r, ok][some]] + lse)).sum()
         dz[r] = np.exp(s - lse)
         np.subtract.at(dz[r], index[r, ok], a)

@@ -55,7 +55,7 @@ constexpr int kLead = LANES < 64 ? LANES : 64;
 __device__ __forceinline__ float exp2_of(float v) { return __builtin_amdgcn_exp2f(v); }
 __device__ __forceinline__ float log_of(float v) { return __builtin_amdgcn_logf(v) * 0.6931471805599453f; }
 
-// a_j = softmax(top / T) over the row's entries; whether there are any.  By the leading lanes.
+// a_j = softmax(top / T) over the row's entries; whether there are any (NaN is one).  By the leading lanes.
 template <typename T, int L>
 __device__ __forceinline__ bool teacher(const Entries& e, const T* z, int64_t row, int m, const float* top, const int32_t* index, float inv_t,
                                         int l) {
@@ -75,8 +75,8 @@ __device__ __forceinline__ bool teacher(const Entries& e, const T* z, int64_t ro
     }
     mx = lanes_reduce<L, Max>(mx);
     for (int j = l; j < e.k; j += L) {
-        const float t = (e.log_a[j] - mx) * inv_t;
-        const float a = e.col[j] < 0 || t == -INFINITY ? 0.f : exp2_of(t * kLog2e);
+        const float top_j = e.log_a[j], t = (top_j - mx) * inv_t;
+        const float a = top_j == -INFINITY ? 0.f : exp2_of(t * kLog2e);  // -infinity: no entry, too
         e.log_a[j] = t;
         e.a[j] = a;
         s += a;
@@ -87,7 +87,7 @@ __device__ __forceinline__ bool teacher(const Entries& e, const T* z, int64_t ro
         e.a[j] *= inv;
         e.log_a[j] -= log_s;
     }
-    return mx != -INFINITY;
+    return s != 0.f;  // the largest entry adds 1
 }
 
 // sum over j of a_j (log a_j - (z_j - max) / T), by the leading lanes

@@ -714,3 +714,25 @@ def test_layer_norm_statistics_of_rows_with_infinities(sp, c, dt):
     for got, want in ((y, Y), (mean, M), (rstd, R)):
         assert np.array_equal(np.isnan(host(got)), np.isnan(want)) and np.array_equal(np.isinf(host(got)), np.isinf(want))
     assert float(mean[3]) == float("inf") and float(mean[4]) == float("-inf") and torch.isnan(rstd[[1, 3, 4, 6]]).all()
+
+
+@pytest.mark.parametrize("m", [40, 1000, 4100, 40000])
+def test_a_teacher_of_nan_is_not_dropped(sp, m):
+    """NaN in all or some of a row's entries: the loss, and the gradient in the columns of its entries; other rows and columns as they are."""
+    z, weight = torch.randn((5, m), device="cuda"), torch.full((5,), 0.2, device="cuda")
+    top, index = torch.zeros((5, 3), device="cuda"), torch.tensor([[1, 2, 5]] * 5, dtype=torch.int32, device="cuda")
+    _, usual = sp.sp_distill(z, top, index, 2.0, weight)
+    for bad in ([0, 1, 2], [1]):
+        t = top.clone()
+        t[3, bad] = float("nan")
+        loss, dz = sp.sp_distill(z, t, index, 2.0, weight)
+        other = torch.ones_like(dz, dtype=torch.bool)
+        other[3, [1, 2, 5]] = False
+        assert torch.isnan(loss).all() and torch.isnan(dz[~other]).all() and torch.equal(dz[other], usual[other])
+    one, dz = sp.sp_distill(z, torch.full((5, 1), float("nan"), device="cuda"), index[:, :1].contiguous(), 2.0, weight)
+    assert torch.isnan(one).all() and torch.isnan(dz[:, 1]).all() and torch.isfinite(dz[:, 2:]).all()
+    # absent entries beside -infinity, and -infinity alone, are no entries as before
+    t, i = torch.full((5, 3), float("-inf"), device="cuda"), index.clone()
+    i[:, 0] = -1
+    loss, dz = sp.sp_distill(z, t, i, 2.0, weight)
+    assert float(loss) == 0 and not dz.any()
