@@ -313,7 +313,7 @@ int sp_window_attn_step(const void* d_q, const void* d_k_new, const void* d_v_ne
  *   loss = T^2 * sum over rows of w * sum_j a_j * (log a_j - log softmax(logits / T)[index_j])          -> d_loss [1]
  *   dlogits[c] = w * T * (softmax(logits / T)[c] - sum of a_j with index_j = c)                         -> d_dlogits [n][m]
  * A row without entries (or with -infinity in all of them) adds nothing and has a zero gradient.  d_dlogits may be NULL (the loss
- * alone), or d_logits itself.  1 <= k <= 256, T > 0.  n = 0 gives loss 0. */
+ * alone), or d_logits itself.  1 <= k <= 256, T >= 1e-37.  n = 0 gives loss 0. */
 int sp_distill(const void* d_logits, int64_t n, int32_t m, const float* d_top, const int32_t* d_index, int32_t k, float temperature,
                const float* d_weight, float* d_loss, void* d_dlogits, sp_dtype dt, void* stream);
 

@@ -132,7 +132,7 @@ __device__ __forceinline__ void meet() {
 // R pieces of V logits a lane.  160000 x 40 fp32 with five entries: 18 us, 3.2 TB/s; eight lanes a row: 16 take 24 us.
 template <typename T, int V, int LANES, int R>
 __global__ __launch_bounds__(kBlock<LANES>) void distill_kernel(const T* z, int64_t n, int m, const float* __restrict__ top,
-                                                                const int32_t* __restrict__ index, int k, float inv_t, float tt,
+                                                                const int32_t* __restrict__ index, int k, float temperature, float inv_t,
                                                                 const float* __restrict__ weight, float each,
                                                                 double* __restrict__ partial, T* dz) {
     constexpr int kGroups = kBlock<LANES> / LANES, L = kLead<LANES>;
@@ -172,7 +172,7 @@ __global__ __launch_bounds__(kBlock<LANES>) void distill_kernel(const T* z, int6
 #pragma unroll
                 for (int i = 0; i < V; ++i) sum[0] += exp2_of((elem(v[r].e[i]) - mx[0]) * c2);
         reduce_lanes<LANES, Add>(sum, room, &turn);
-        const float w = weight ? weight[row] : each, inv_sum = 1.f / sum[0], scale = w * tt * inv_t;
+        const float w = weight ? weight[row] : each, inv_sum = 1.f / sum[0], scale = w * temperature;
         if (dz) {
 #pragma unroll
             for (int r = 0; r < R; ++r) {
@@ -187,7 +187,7 @@ __global__ __launch_bounds__(kBlock<LANES>) void distill_kernel(const T* z, int6
         meet<LANES>();  // the row is written before its columns of the teacher are written again
         if (l < L) {
             const float part = teacher_loss<L>(e, mx[0], inv_t, l);
-            if (l == 0 && some) loss += (double)w * (double)tt * ((double)part + (double)log_of(sum[0]));
+            if (l == 0 && some) loss += (double)w * (double)temperature * (double)temperature * ((double)part + (double)log_of(sum[0]));
             if (dz && some) teacher_columns<T, L>(e, dz + row * m, c2, mx[0], inv_sum, scale, l);
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the leading lanes alone use the entries
@@ -207,7 +207,7 @@ __global__ __launch_bounds__(kBlock<LANES>) void distill_kernel(const T* z, int6
 constexpr int kWide = 512;
 template <typename T, int V>
 __global__ __launch_bounds__(kWide, 4) void distill_wide_kernel(const T* z, int64_t n, int m, const float* __restrict__ top,
-                                                                const int32_t* __restrict__ index, int k, float inv_t, float tt,
+                                                                const int32_t* __restrict__ index, int k, float temperature, float inv_t,
                                                                 const float* __restrict__ weight, float each,
                                                                 double* __restrict__ partial, T* dz) {
     constexpr int kAhead = sizeof(T) * V == 16 && V == 8 ? 4 : 8;  // pieces asked for at a time: 8 of bf16 spill
@@ -268,7 +268,7 @@ __global__ __launch_bounds__(kWide, 4) void distill_wide_kernel(const T* z, int6
             sum = all == -INFINITY ? NAN : s;  // nothing but -infinity: there is no softmax
         }
         some = any;
-        const float w = weight ? weight[row] : each, inv_sum = 1.f / sum, scale = w * tt * inv_t, p_scale = scale * inv_sum;
+        const float w = weight ? weight[row] : each, inv_sum = 1.f / sum, scale = w * temperature, p_scale = scale * inv_sum;
         if (dz) {
             for (int64_t c0 = (int64_t)l * V; c0 < m; c0 += (int64_t)kWide * V * kAhead) {
                 Piece<T, V> v[kAhead];
@@ -289,7 +289,7 @@ __global__ __launch_bounds__(kWide, 4) void distill_wide_kernel(const T* z, int6
         __syncthreads();
         if (l < 64) {
             const float part = teacher_loss<64>(e, mx, inv_t, l);
-            if (l == 0 && some) loss += (double)w * (double)tt * ((double)part + (double)log_of(sum));
+            if (l == 0 && some) loss += (double)w * (double)temperature * (double)temperature * ((double)part + (double)log_of(sum));
             if (dz && some) teacher_columns<T, 64>(e, dz + row * m, c2, mx, inv_sum, scale, l);
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -321,10 +321,10 @@ int launch(const DistillArgs& a) {
     const int blocks = (int)std::min<int64_t>((a.n + kGroups - 1) / kGroups, LANES > 256 ? 1024 : 4096);
     Buf partial = dev_alloc((size_t)blocks * 8, a.s);
     if (!partial) return SP_ERR_ALLOC;
-    const float inv_t = 1.f / a.temperature, tt = a.temperature * a.temperature, each = 1.f / (float)a.n;
+    const float inv_t = 1.f / a.temperature, each = 1.f / (float)a.n;
     auto kernel = distill_kernel<T, V, LANES, R>;
     hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kBlock<LANES>), (size_t)kGroups * Entries::kWords * ((a.k + 3) & ~3) * 4, a.s, static_cast<const T*>(a.z), a.n, a.m,
-                       a.top, a.index, a.k, inv_t, tt, a.weight, each, ptr<double>(partial), static_cast<T*>(a.dz));
+                       a.top, a.index, a.k, a.temperature, inv_t, a.weight, each, ptr<double>(partial), static_cast<T*>(a.dz));
     return finish(a, ptr<double>(partial), blocks);
 }
 
@@ -333,10 +333,10 @@ int launch_wide(const DistillArgs& a) {
     const int blocks = (int)std::min<int64_t>(a.n, 1024);
     Buf partial = dev_alloc((size_t)blocks * 8, a.s);
     if (!partial) return SP_ERR_ALLOC;
-    const float inv_t = 1.f / a.temperature, tt = a.temperature * a.temperature, each = 1.f / (float)a.n;
+    const float inv_t = 1.f / a.temperature, each = 1.f / (float)a.n;
     auto kernel = distill_wide_kernel<T, V>;
     hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kWide), (size_t)Entries::kWords * ((a.k + 3) & ~3) * 4, a.s, static_cast<const T*>(a.z), a.n, a.m, a.top, a.index, a.k,
-                       inv_t, tt, a.weight, each, ptr<double>(partial), static_cast<T*>(a.dz));
+                       a.temperature, inv_t, a.weight, each, ptr<double>(partial), static_cast<T*>(a.dz));
     return finish(a, ptr<double>(partial), blocks);
 }
 
@@ -369,7 +369,8 @@ extern "C" int sp_distill(const void* d_logits, int64_t n, int32_t m, const floa
                           float temperature, const float* d_weight, float* d_loss, void* d_dlogits, sp_dtype dt, void* stream) {
     if (n < 0 || n > (int64_t)1 << 40 || m < 1 || k < 1 || k > kMaxTop) return fail(SP_ERR_INVALID_ARG, "bad row, class or entry count");
     if (dt != SP_F32 && dt != SP_BF16) return fail(SP_ERR_INVALID_ARG, "bad dtype");
-    if (!(temperature > 0.f) || !(temperature <= 3.0e38f)) return fail(SP_ERR_INVALID_ARG, "the temperature must be positive and finite");
+    // 1 / T and log2(e) / T are fp32 numbers, too
+    if (!(temperature >= 1e-37f) || !(temperature <= 3.0e38f)) return fail(SP_ERR_INVALID_ARG, "the temperature must be positive and finite (at least 1e-37)");
     if (!d_loss || (n > 0 && (!d_logits || !d_top || !d_index))) return fail(SP_ERR_INVALID_ARG, "a logit/teacher/loss pointer is NULL");
     const DistillArgs a{d_logits, n, m, d_top, d_index, k, temperature, d_weight, d_loss, d_dlogits, (hipStream_t)stream};
     if (n == 0) return finish(a, nullptr, 0);

@@ -736,3 +736,19 @@ def test_a_teacher_of_nan_is_not_dropped(sp, m):
     i[:, 0] = -1
     loss, dz = sp.sp_distill(z, t, i, 2.0, weight)
     assert float(loss) == 0 and not dz.any()
+
+
+@pytest.mark.parametrize("m", [40, 40000])
+@pytest.mark.parametrize("temp", [1e20, 1e-20, 2e30, 1e-30])
+def test_distillation_at_extreme_temperatures(sp, m, temp):
+    """T^2 is out of fp32's range; w * T, which the gradient has, is not."""
+    rng = np.random.default_rng(int(math.log10(temp)) % 100)
+    z, top = rows(rng, F32, 3, m), rows(rng, F32, 3, 2)
+    index = torch.tensor([[1, 7]] * 3, dtype=torch.int32, device="cuda")
+    loss, dz = sp.sp_distill(z, top, index, temp)
+    _, want = tokens.distill(host(z), host(top), host(index).astype(np.int32), float(np.float32(temp)))
+    # logits of size 10 over T: shares are uniform to 2^-24 for large T, 0 or 1 for small ones (if the first two do not tie, which they do not)
+    w = float(np.float32(temp)) / 3
+    within(dz, want, (160 * U32) * w * (np.abs(want) / w + 1 / m) + 4 * U32 * np.abs(want), "dz")
+    if temp < 1:
+        assert np.isfinite(host(loss)).all()

@@ -142,3 +142,10 @@ def test_refusals_need_no_gpu():
     assert distill(n=-1) == -1 and distill(m=0) == -1 and distill(k=0) == -1 and distill(k=257) == -1 and distill(temp=0.0) == -1
     assert distill(temp=float("nan")) == -1 and distill(temp=float("inf")) == -1 and distill(loss=None) == -1 and distill(dt=5) == -1
     assert distill(z=None) == -1
+
+
+def test_a_temperature_without_an_fp32_reciprocal_is_refused():
+    lib = ctypes.CDLL(LIB)
+    x = ctypes.c_void_p(4096)                              # never read
+    for temp in (1e-38, 1e-40, -1e-30, 3.2e38):
+        assert lib.sp_distill(x, ctypes.c_int64(2), 8, x, x, 2, ctypes.c_float(temp), None, x, x, 0, None) == -1
