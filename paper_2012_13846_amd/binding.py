@@ -7,6 +7,7 @@ missing this module raises: there is no fallback.
 from __future__ import annotations
 
 import ctypes as C
+import operator
 import os
 
 import numpy as np
@@ -595,6 +596,11 @@ def _head_rows(t: torch.Tensor, dtype, name: str):
     return t.data_ptr(), (sn if n > 1 else h * d)
 
 
+def _reach(v: int) -> int:
+    """A window's reach as the library's int32: more than it holds is as far as it goes, not what is left of the number's bits."""
+    return max(-1, min(operator.index(v), 2 ** 31 - 1))
+
+
 def _window(q, k, v, q_starts, k_starts, left, right, sinks, scale):
     _need_cuda(q_starts, torch.int32, "q_starts"), _need_cuda(k_starts, torch.int32, "k_starts")
     if q_starts.ndim != 1 or k_starts.shape != q_starts.shape or q_starts.numel() < 1:
@@ -602,7 +608,7 @@ def _window(q, k, v, q_starts, k_starts, left, right, sinks, scale):
     n_q, heads, dim = q.shape
     n_k, kv_heads, _ = k.shape
     _need_shape(k, (n_k, kv_heads, dim), "k"), _need_shape(v, (n_k, kv_heads, dim), "v")
-    return _WindowAttn(n_q, n_k, q_starts.numel() - 1, heads, kv_heads, dim, left, right, sinks,
+    return _WindowAttn(n_q, n_k, q_starts.numel() - 1, heads, kv_heads, dim, _reach(left), _reach(right), _reach(sinks),
                        dim ** -0.5 if scale is None else scale, _dt(q), q_starts.data_ptr(), k_starts.data_ptr())
 
 
@@ -646,7 +652,7 @@ def sp_window_attn_step(q, k_new, v_new, k_cache, v_cache, lens, left: int, sink
     _need_shape(lens, (batch,), "lens")
     o = torch.empty_like(q)
     _check(_token_argtypes().sp_window_attn_step(q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
-                                                 lens.data_ptr(), batch, cap, heads, kv_heads, dim, left, sinks,
+                                                 lens.data_ptr(), batch, cap, heads, kv_heads, dim, _reach(left), _reach(sinks),
                                                  dim ** -0.5 if scale is None else scale, o.data_ptr(), _dt(q), _stream()))
     return o
 

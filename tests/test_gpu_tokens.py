@@ -752,3 +752,19 @@ def test_distillation_at_extreme_temperatures(sp, m, temp):
     within(dz, want, (160 * U32) * w * (np.abs(want) / w + 1 / m) + 4 * U32 * np.abs(want), "dz")
     if temp < 1:
         assert np.isfinite(host(loss)).all()
+
+
+@pytest.mark.parametrize("wide", [2 ** 31 - 1, 2 ** 31, 2 ** 32 + 3, 2 ** 63 - 1])
+def test_windows_wider_than_any_cloud(sp, wide):
+    q, k, v, do, starts, hs, shape = attn_inputs("both_sides", BF16)
+    shape = dict(shape, left=1000, right=1000, sinks=1000)
+    want = sp.sp_window_attn_fwd(q, k, v, *starts, **shape)
+    grads = sp.sp_window_attn_bwd(q, k, v, want[0], do, want[1], *starts, **shape)
+    shape = dict(shape, left=wide, right=wide, sinks=wide)
+    got = sp.sp_window_attn_fwd(q, k, v, *starts, **shape)
+    for a, b in zip(got + sp.sp_window_attn_bwd(q, k, v, got[0], do, got[1], *starts, **shape), want + grads):
+        assert torch.equal(a, b)
+    cache = [torch.randn((2, 40, 2, 16), device="cuda") for _ in range(2)]
+    q1, k1, lens = torch.randn((2, 4, 16), device="cuda"), torch.randn((2, 2, 16), device="cuda"), torch.tensor([39, 3], dtype=torch.int32, device="cuda")
+    a = sp.sp_window_attn_step(q1, k1, k1, cache[0].clone(), cache[1].clone(), lens, left=100)
+    assert torch.equal(a, sp.sp_window_attn_step(q1, k1, k1, cache[0].clone(), cache[1].clone(), lens, left=wide))

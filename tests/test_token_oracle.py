@@ -149,3 +149,9 @@ def test_a_temperature_without_an_fp32_reciprocal_is_refused():
     x = ctypes.c_void_p(4096)                              # never read
     for temp in (1e-38, 1e-40, -1e-30, 3.2e38):
         assert lib.sp_distill(x, ctypes.c_int64(2), 8, x, x, 2, ctypes.c_float(temp), None, x, x, 0, None) == -1
+
+
+def test_a_window_wider_than_an_int32_is_no_narrow_one():
+    from paper_2012_13846_amd.binding import _reach
+    assert [_reach(v) for v in (0, 5, 2 ** 31 - 1, 2 ** 31, 2 ** 32, 2 ** 32 + 7, 2 ** 63)] == [0, 5] + [2 ** 31 - 1] * 5
+    assert [_reach(v) for v in (-1, -2 ** 31, -2 ** 32, -2 ** 32 + 9)] == [-1] * 4   # refused by the library
