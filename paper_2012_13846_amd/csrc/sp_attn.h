@@ -47,16 +47,20 @@ struct AttnBwd {
 template <typename T>
 int attn_backward(const AttnBwd<T>& g, hipStream_t s);  // sp_attn_bwd.hip
 
-// A tile number's cloud and the tile's first row, counted from the cloud's (see in_cloud).  All lanes must come here together.
+// The last cloud c of which first(c) <= t, by a wavefront.  All lanes must come here together.
+template <typename First>
+__device__ __forceinline__ int find_cloud(int clouds, int64_t t, First first) {
+    return __builtin_amdgcn_readfirstlane(last_cloud(clouds, [&](int lo, int step, int hi) {
+        const int at = lo + ((int)(threadIdx.x & 63) + 1) * step;
+        return (int)__popcll(__ballot(at <= hi && first(at) <= t));
+    }));
+}
+// A tile number's cloud and the tile's first row, counted from the cloud's (see in_cloud).
 struct CloudTile {
     int cloud;
     int64_t row;
     __device__ __forceinline__ CloudTile(const int32_t* starts, int clouds, int n, int64_t t, int per, int tile) {
-        const int c = last_cloud(clouds, [&](int lo, int step, int hi) {
-            const int at = lo + ((int)(threadIdx.x & 63) + 1) * step;
-            return (int)__popcll(__ballot(at <= hi && first_tile(starts, clouds, n, at, per, tile) <= t));
-        });
-        cloud = __builtin_amdgcn_readfirstlane(c);
+        cloud = find_cloud(clouds, t, [&](int c) { return first_tile(starts, clouds, n, c, per, tile); });
         row = (t - first_tile(starts, clouds, n, cloud, per, tile)) * tile;
     }
 };

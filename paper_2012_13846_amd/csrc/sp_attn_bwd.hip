@@ -143,13 +143,21 @@ __global__ __launch_bounds__(64 * W, NT == 1 ? 4 : sizeof(T) * NT == 4 ? 3 : siz
     if (wr.there) join_column<T, NT>(g.dq.at(c.q0 + wr.query, h, w.dim), acc, w.dim, NAN);
 }
 
-// The first keys of a cloud are seen by all later queries: a tile with them would take many times the others' time.  With few of them
-// (at most kSplitSinks) the keys' kernel leaves their pairs beyond the window out and its sums in fp32 (`first`); attn_far_kernel adds
-// up those pairs, `chunk` rows to a wavefront (`far`), and attn_join_kernel adds both, the chunks in order.
+// The first keys of a cloud are seen by all later queries: a tile with them would take many times the others' time.  For few of them
+// (at most kSplitSinks) in a long cloud the keys' kernel leaves their pairs beyond the window out and its sums in fp32 (`first`);
+// attn_far_kernel adds up those pairs, a chunk of rows to a wavefront (`far`), and attn_join_kernel adds both, the chunks in order.
 constexpr int kSplitSinks = 128;
+// Clouds of 561 rows beyond the window: 103 us without the split, 123 with it (four clouds, 4 heads of 32, fp32, forward and
+// backward); of 745 rows: 88 and 81 (one cloud, 8 heads of 64, bf16); of 1745: 144 and 119.
+constexpr int kLongBeyond = 640;
+// The host knows the clouds' mean, not the longest: with a lower mean the kernels look for long clouds in calls of more keys beyond the window than
+// this.  Where there are none that costs 5 us (2048 to 65536 keys in clouds of 128 and 256: 29 - 1288 us in all); a cloud of 4000 keys among 100 of
+// 100 takes 132 us instead of 645 (8 heads of 64 over 2), one of 60000 370 instead of 9800, with 32 heads of 128 over 8 5.1 ms instead of 21.
+constexpr int kLongTotal = 2048;
 struct Split {
-    int sinks, chunk;    // 0: not split; a multiple of `group`
-    float *first, *far;  // [cloud or chunk][kv_heads][sinks][dk, dv][dim]
+    int sinks;           // 0: not split
+    LongClouds clouds;
+    float *first, *far;  // by sums_at(): [place or chunk]...
 };
 __device__ __forceinline__ int64_t split_at(const Window& w, const Split& sp, int64_t part, int kh, int key) {
     return sums_at(w.kv_heads, sp.sinks, w.dim, part, kh, key);
@@ -326,7 +334,7 @@ __global__ __launch_bounds__(64 * W, NT == 1 ? (sizeof(T) == 2 ? 4 : 3) : sizeof
     if (!in_cloud(ct.row, c.b)) return;
     const int j0 = (int)ct.row, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int jw = j0 + wave * kWaveRows, j = jw + (lane & 31);
-    const bool there = j < c.b, split_here = split.sinks > 0;
+    const bool there = j < c.b, split_here = split.sinks > 0 && split.clouds.has(cn);
     const int sinks = split_here ? 0 : w.sinks;
     // the rows that see a key of the workgroup's
     const int a = c.partners ? c.a : 0;
@@ -409,9 +417,9 @@ __global__ __launch_bounds__(64 * W, NT == 1 ? (sizeof(T) == 2 ? 4 : 3) : sizeof
             for (int i = 0; i < 16; ++i) check = fmaf(kg.dk[d][i] *= w.scale, 0.f, fmaf(kg.dv[d][i], 0.f, check));
         return any_of_workgroup(there & (halves<Add>(check) != 0.f));
     };
-    const bool part = split_here && j < split.sinks && c.partners;
+    const bool part = split_here && j < split.sinks;
     // of this key's dk (0) and dv (1)
-    auto sums = [&](int which) { return split.first + split_at(w, split, cn - 1, kh, j) + which * w.dim; };
+    auto sums = [&](int which) { return split.first + split_at(w, split, split.clouds.place(cn), kh, j) + which * w.dim; };
     auto row = [&](int which) { return which ? g.dv.at(c.k0 + j, kh, w.dim) : g.dk.at(c.k0 + j, kh, w.dim); };
     auto store = [&](int which, const f32x16(&acc)[NT]) {
         if (there && part) put_column<float, NT, false>(sums(which), acc, w.dim);
@@ -451,11 +459,12 @@ __global__ __launch_bounds__(64, 1) void attn_far_kernel(AttnBwd<T> g, Split spl
     const Window& w = g.w;
     const uint32_t item = item_of_block(blockIdx.x, gridDim.x), t = item % (uint32_t)tiles;
     const int groups = (split.sinks + 31) / 32, key0 = (int)(item / (uint32_t)tiles) % groups * 32, kh = (int)(item / (uint32_t)tiles) / groups;
-    const CloudTile ct(w.q_starts, w.clouds, w.n_q, t, w.group, split.chunk);
-    const Cloud c(w, ct.cloud);
-    const int64_t rows = (int64_t)c.a * w.group;
-    if (!c.partners || !in_cloud(ct.row, rows) || key0 >= c.b) return;
-    const int64_t from = max(ct.row, far_begin(w, c, key0)), to_row = min(ct.row + split.chunk, rows);
+    const LongClouds& lc = split.clouds;
+    const int cn = find_cloud(w.clouds, t, [&](int i) { return lc.first_chunk(i); });
+    const Cloud c(w, cn);
+    const int64_t r0 = (t - lc.first_chunk(cn)) * lc.chunk, rows = (int64_t)c.a * w.group;
+    if (!lc.has(cn) || !in_cloud(r0, rows)) return;
+    const int64_t from = max(r0, far_begin(w, c, key0)), to_row = min(r0 + lc.chunk, rows);
     if (from >= to_row) return;
     const int begin = (int)from, end = (int)to_row;
     const int lane = threadIdx.x, j = key0 + (lane & 31);
@@ -526,18 +535,21 @@ __global__ __launch_bounds__(64, 1) void attn_far_kernel(AttnBwd<T> g, Split spl
     }
 }
 
-// a workgroup a cloud, key head and one of the first keys: every wavefront a quarter of the chunks
+// a workgroup a place, key head and one of the first keys: every wavefront a quarter of the chunks
 template <typename T>
 __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnBwd<T> g, Split split) {
     __shared__ float sums[4][2 * kMaxDim];
     const Window& w = g.w;
-    const int cn = (int)blockIdx.x + 1, kh = blockIdx.y, j = blockIdx.z, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const LongClouds& lc = split.clouds;
+    const int place = blockIdx.x, kh = blockIdx.y, j = blockIdx.z, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int cn = lc.by_number() ? place + 1 : find_cloud(w.clouds, place, [&](int i) { return lc.place(i); });
+    if (!lc.has(cn) || lc.place(cn) != place) return;
     const Cloud c(w, cn);
     if (j >= c.b) return;
-    const int64_t t0 = first_tile(w.q_starts, w.clouds, w.n_q, cn, w.group, split.chunk), rows = (int64_t)c.a * w.group;
+    const int64_t t0 = lc.first_chunk(cn), rows = (int64_t)c.a * w.group;
     const int64_t far0 = far_begin(w, c, j / 32 * 32);
     // chunks with a row behind far0 were written
-    const int64_t u0 = min(far0, rows) / split.chunk, u1 = far0 < rows ? (rows + split.chunk - 1) / split.chunk : u0;
+    const int64_t u0 = min(far0, rows) / lc.chunk, u1 = far0 < rows ? (rows + lc.chunk - 1) / lc.chunk : u0;
     const int64_t quarter = (u1 - u0 + 3) / 4, v0 = min(u0 + wave * quarter, u1), v1 = min(v0 + quarter, u1);
     const float* far = split.far + split_at(w, split, t0, kh, j);
     const int64_t step = split_at(w, split, 1, 0, 0);
@@ -549,7 +561,7 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnBwd<T> g, Split
     }
     __syncthreads();
     if (wave) return;
-    const float* first = split.first + split_at(w, split, cn - 1, kh, j);
+    const float* first = split.first + split_at(w, split, place, kh, j);
     T* const to[2] = {g.dk.at(c.k0 + j, kh, w.dim), g.dv.at(c.k0 + j, kh, w.dim)};
     for (int q = 0; q < 2; ++q)
         for (int e = lane; e < w.dim; e += 64) {
@@ -571,19 +583,17 @@ int backward_sized(AttnBwd<T> g, hipStream_t s) {
     // rows of a chunk: enough chunks to fill the chip, whose sums are a quarter of the rows that they read at most
     const int64_t fill = (int64_t)w.n_q * w.heads / 1024;
     const int chunk = (int)std::min<int64_t>(std::max<int64_t>(fill, std::max(128, 8 * std::min(w.sinks, kSplitSinks))), 1024);
-    Split split{0, (chunk + w.group - 1) / w.group * w.group, nullptr, nullptr};
+    Split split{0, {w.q_starts, w.k_starts, w.n_q, w.n_k, w.clouds, w.group, (chunk + w.group - 1) / w.group * w.group, w.left + kLongBeyond + 1}, nullptr, nullptr};
+    const LongClouds& lc = split.clouds;
     const int groups = (w.sinks + 31) / 32;
-    int64_t chunks = 0;
-    // Clouds of 561 rows beyond the window: 103 us without the split, 123 with it (four clouds, 4 heads of 32, fp32, forward and
-    // backward); of 745 rows: 88 and 81 (one cloud, 8 heads of 64, bf16); of 1745: 144 and 119.
-    if (w.sinks > 0 && w.sinks <= kSplitSinks && w.n_q > 0 && w.clouds > 0 && w.n_k / w.clouds - w.left > 640) {
-        chunks = tile_numbers(w.n_q, w.clouds, w.group, split.chunk);
+    if (w.sinks > 0 && w.sinks <= kSplitSinks && w.n_q > 0 && w.clouds > 0 &&
+        (w.n_k / w.clouds >= lc.least || w.n_k - w.left > kLongTotal)) {
         const size_t each = (size_t)w.kv_heads * w.sinks * 2 * w.dim;
-        parts = dev_alloc((chunks + w.clouds) * each * 4, s);
+        parts = dev_alloc((lc.chunks() + lc.places()) * each * 4, s);
         if (parts) {  // else the slow way, which needs no memory
             split.sinks = w.sinks;
             split.first = ptr<float>(parts);
-            split.far = split.first + w.clouds * each;
+            split.far = split.first + lc.places() * each;
         }
     }
     if (w.n_q > 0)
@@ -591,8 +601,8 @@ int backward_sized(AttnBwd<T> g, hipStream_t s) {
     if (w.n_k > 0)
         hipLaunchKernelGGL((attn_dkv_kernel<T, NT, VEC, W>), dim3((unsigned)(k_tiles * w.kv_heads)), dim3(64 * W), 0, s, g, split, (int)k_tiles);
     if (split.sinks) {
-        hipLaunchKernelGGL((attn_far_kernel<T, NT, VEC>), dim3((unsigned)(chunks * w.kv_heads * groups)), dim3(64), 0, s, g, split, (int)chunks);
-        hipLaunchKernelGGL(attn_join_kernel<T>, dim3(w.clouds, w.kv_heads, split.sinks), dim3(kThreads), 0, s, g, split);
+        hipLaunchKernelGGL((attn_far_kernel<T, NT, VEC>), dim3((unsigned)(lc.chunks() * w.kv_heads * groups)), dim3(64), 0, s, g, split, (int)lc.chunks());
+        hipLaunchKernelGGL(attn_join_kernel<T>, dim3(lc.places(), w.kv_heads, split.sinks), dim3(kThreads), 0, s, g, split);
     }
     SP_HIP(hipGetLastError());
     return SP_OK;

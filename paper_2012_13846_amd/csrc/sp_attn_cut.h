@@ -57,4 +57,21 @@ SP_HOST_DEVICE int64_t sums_at(int kv_heads, int sinks, int dim, int64_t part, i
     return (((part * kv_heads + kh) * sinks + key) * 2) * dim;
 }
 
+// The clouds whose first keys' sums are split: those of at least `least` keys.  How many there are stands in device memory; they have places
+// (parts of the keys' own sums) by the clouds' numbers, or, of more clouds than there can be long ones, by where they begin: two that
+// begin in the same `least` keys are not both long.
+struct LongClouds {
+    const int32_t *q_starts, *k_starts;
+    int n_q, n_k, clouds;
+    int per, chunk;  // rows of a query; of a chunk
+    int least;
+    SP_HOST_DEVICE bool by_number() const { return clouds <= n_k / least + 1; }
+    SP_HOST_DEVICE int places() const { return by_number() ? clouds : n_k / least + 1; }
+    SP_HOST_DEVICE int place(int c) const { return by_number() ? c - 1 : cloud_begin(k_starts, clouds, n_k, c) / least; }
+    SP_HOST_DEVICE bool has(int c) const { return c >= 1 && c <= clouds && cloud_rows(k_starts, clouds, n_k, c) >= least; }
+    // Their rows cut into chunks: a long cloud has the numbers from here on, at least as many as its chunks before the next cloud's
+    SP_HOST_DEVICE int64_t first_chunk(int c) const { return (int64_t)cloud_begin(q_starts, clouds, n_q, c) * per / chunk + place(c); }
+    SP_HOST_DEVICE int64_t chunks() const { return (int64_t)n_q * per / chunk + places() + 1; }
+};
+
 }  // namespace sp

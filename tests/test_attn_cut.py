@@ -9,6 +9,9 @@ import pytest
 
 CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2012_13846_amd", "csrc")
 HARNESS = r"""
+#include <functional>
+#include <vector>
+
 #include "sp_attn_cut.h"
 using namespace sp;
 // the search of a wavefront of 64 lanes
@@ -37,19 +40,70 @@ extern "C" int tiles(const int32_t* starts, int clouds, int n, int per, int tile
     }
     return 0;
 }
-// The sums of the first keys that the keys' tiles write: 1: outside of `clouds` parts
-extern "C" int sums(const int32_t* starts, int clouds, int n, int tile, int kv_heads, int sinks, int dim) {
-    const int64_t count = tile_numbers(n, clouds, 1, tile), bytes = sums_at(kv_heads, sinks, dim, clouds, 0, 0);
+// The sums of the first keys that the keys' tiles write, 1: outside of their places, 2: two clouds at one place (starts that ascend)
+extern "C" int sums(const int32_t* starts, int clouds, int n, int tile, int kv_heads, int sinks, int dim, int least, int ascending) {
+    const LongClouds lc{starts, starts, n, n, clouds, 1, 128, least};
+    const int64_t count = tile_numbers(n, clouds, 1, tile), end = sums_at(kv_heads, sinks, dim, lc.places(), 0, 0);
+    std::vector<int> owner(lc.places(), -1);
     for (int64_t t = 0; t < count; ++t) {
         const int c = cloud_of(starts, clouds, n, t, 1, tile);
         const int64_t row = (t - first_tile(starts, clouds, n, c, 1, tile)) * tile;
         const int rows = cloud_rows(starts, clouds, n, c);
-        if (!in_cloud(row, rows) || c < 1 || c > clouds) continue;
+        if (!in_cloud(row, rows) || !lc.has(c)) continue;
+        if (lc.place(c) < 0 || lc.place(c) >= lc.places()) return 1;
+        if (ascending && owner[lc.place(c)] >= 0 && owner[lc.place(c)] != c) return 2;
+        owner[lc.place(c)] = c;
         for (int64_t j = row; j < row + tile && j < rows; ++j)
             for (int kh = 0; j < sinks && kh < kv_heads; ++kh) {
-                const int64_t at = sums_at(kv_heads, sinks, dim, c - 1, kh, (int)j);
-                if (at < 0 || at + 2 * dim > bytes) return 1;
+                const int64_t at = sums_at(kv_heads, sinks, dim, lc.place(c), kh, (int)j);
+                if (at < 0 || at + 2 * dim > end) return 1;
             }
+    }
+    return 0;
+}
+static int find(int clouds, int64_t t, const std::function<int64_t(int)>& first) {
+    return last_cloud(clouds, [&](int lo, int step, int hi) {
+        int k = 0;
+        for (int lane = 0; lane < 64; ++lane) {
+            const int at = lo + (lane + 1) * step;
+            k += at <= hi && first(at) <= t;
+        }
+        return k;
+    });
+}
+// Chunks that are written and joined.  1: a row outside of the array; 2: a chunk that is joined lies outside of their memory; starts that
+// ascend: 3: a long cloud's row without a chunk, or one of several; 4: a place finds another cloud than its own; 5: a chunk is joined that another cloud wrote
+extern "C" int chunks(const int32_t* qs, const int32_t* ks, int clouds, int n_q, int n_k, int per, int chunk, int least, int ascending) {
+    const LongClouds lc{qs, ks, n_q, n_k, clouds, per, chunk, least};
+    const int64_t count = lc.chunks();
+    std::vector<int> seen((size_t)n_q * per), writer(count, -1);
+    for (int64_t t = 0; t < count; ++t) {
+        const int c = find(clouds, t, [&](int i) { return lc.first_chunk(i); });
+        const int64_t row = (t - lc.first_chunk(c)) * chunk, rows = (int64_t)cloud_rows(qs, clouds, n_q, c) * per;
+        if (!lc.has(c) || !in_cloud(row, rows)) continue;
+        writer[t] = c;
+        for (int64_t r = row; r < row + chunk && r < rows; ++r) {
+            const int64_t at = (int64_t)cloud_begin(qs, clouds, n_q, c) * per + r;
+            if (at < 0 || at >= (int64_t)n_q * per) return 1;
+            ++seen[at];
+        }
+    }
+    std::vector<int> joined(clouds + 2);
+    for (int place = 0; place < lc.places(); ++place) {
+        const int c = lc.by_number() ? place + 1 : find(clouds, place, [&](int i) { return lc.place(i); });
+        if (!lc.has(c) || lc.place(c) != place) continue;
+        ++joined[c];
+        const int64_t rows = (int64_t)cloud_rows(qs, clouds, n_q, c) * per;
+        for (int64_t u = 0; u < (rows + chunk - 1) / chunk; ++u) {
+            const int64_t at = lc.first_chunk(c) + u;
+            if (at < 0 || at >= count) return 2;
+            if (ascending && writer[at] != c) return 5;
+        }
+    }
+    for (int c = 1; ascending && c <= clouds; ++c) {
+        if (joined[c] != lc.has(c)) return 4;
+        for (int64_t r = (int64_t)cloud_begin(qs, clouds, n_q, c) * per; r < (int64_t)cloud_begin(qs, clouds, n_q, c + 1) * per; ++r)
+            if (seen[r] != lc.has(c)) return 3;
     }
     return 0;
 }
@@ -106,8 +160,38 @@ def test_starts_that_do_not_ascend_lead_to_no_row_outside_of_the_array(lib):
             assert tiles(lib, starts, n, per, tile)[0] == 0, (list(starts), n)
 
 
+def pointer(a):
+    return a.ctypes.data_as(ctypes.c_void_p)
+
+
 def test_starts_that_do_not_ascend_lead_to_no_sum_outside_of_its_memory(lib):
     for starts, n in wrong_starts():
         s = as_starts(starts)
-        for tile in (32, 128):
-            assert lib.sums(s.ctypes.data_as(ctypes.c_void_p), len(s) - 1, n, tile, 8, 4, 128) == 0, (list(starts), n)
+        for tile, least in ((32, 1), (32, 650), (128, 1), (128, 1700)):
+            assert lib.sums(pointer(s), len(s) - 1, n, tile, 8, 4, 128, least, 0) == 0, (list(starts), n)
+            assert lib.chunks(pointer(s), pointer(s), len(s) - 1, n, n, 3, 129, least, 0) == 0, (list(starts), n)
+
+
+def test_starts_of_queries_and_keys_that_do_not_belong_together_stay_inside(lib):
+    rng = np.random.default_rng(12)
+    for _ in range(200):
+        n_q, n_k, clouds = int(rng.integers(1, 5000)), int(rng.integers(1, 5000)), int(rng.integers(1, 100))
+        qs, ks = as_starts(rng.integers(-50, 2 * n_q, clouds + 1)), as_starts(rng.integers(-50, 2 * n_k, clouds + 1))
+        assert lib.chunks(pointer(qs), pointer(ks), clouds, n_q, n_k, 2, 128, int(rng.integers(1, 900)), 0) == 0
+
+
+@pytest.mark.parametrize("per,chunk", [(1, 128), (4, 128), (5, 130), (1, 1024)])
+def test_every_long_cloud_has_a_place_and_chunks_of_its_own(lib, per, chunk):
+    """Long clouds among many short and empty ones, more and fewer than there can be long ones; queries the last of a cloud's keys, or none."""
+    rng = np.random.default_rng(per + chunk)
+    for case in range(120):
+        clouds = int(rng.choice([1, 3, 20, 300]))
+        lens = np.where(rng.random(clouds) < 0.1, rng.integers(600, 3000, clouds), rng.integers(0, 30, clouds))
+        if case % 3 == 0:
+            lens = np.where(lens > 600, 641, lens)             # exactly the least
+        asked = np.minimum(lens, rng.integers(0, 2000, clouds)) if case % 2 else lens
+        gap = int(rng.integers(0, 700)) if case % 5 == 0 else 0
+        ks, qs = as_starts(np.concatenate([[0], np.cumsum(lens)]) + gap), as_starts(np.concatenate([[0], np.cumsum(asked)]) + gap)
+        n_k, n_q = int(ks[-1]) + gap, int(qs[-1]) + gap
+        assert lib.sums(pointer(ks), clouds, n_k, 128, 2, 4, 8, 641, 1) == 0
+        assert lib.chunks(pointer(qs), pointer(ks), clouds, n_q, n_k, per, chunk, 641, 1) == 0, case

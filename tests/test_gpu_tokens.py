@@ -768,3 +768,40 @@ def test_windows_wider_than_any_cloud(sp, wide):
     q1, k1, lens = torch.randn((2, 4, 16), device="cuda"), torch.randn((2, 2, 16), device="cuda"), torch.tensor([39, 3], dtype=torch.int32, device="cuda")
     a = sp.sp_window_attn_step(q1, k1, k1, cache[0].clone(), cache[1].clone(), lens, left=100)
     assert torch.equal(a, sp.sp_window_attn_step(q1, k1, k1, cache[0].clone(), cache[1].clone(), lens, left=wide))
+
+
+# ---- first keys of long clouds among short ones ------------------------------------------------------------------
+@pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("heads,kv,dim,sinks,clouds", [(2, 1, 64, 4, 1), (2, 1, 24, 40, 20), (12, 12, 33, 3, 20), (16, 4, 128, 4, 1), (8, 8, 64, 100, 20)])
+def test_first_keys_of_long_clouds_among_short_ones(sp, dt, heads, kv, dim, sinks, clouds):
+    """More clouds than there can be long ones, and fewer; empty ones; rows of no cloud; some clouds are asked by their last rows only."""
+    rng = np.random.default_rng(clouds + dim)
+    b = np.array([30] * clouds + [1300] + [0, 17] * clouds + [900, 5])
+    a = np.where(np.arange(len(b)) % 3 == 2, np.minimum(b, 7), b)
+    hs = tuple(np.concatenate([[0], np.cumsum(x)]) + 9 for x in (a, b))
+    n_q, n_k = int(hs[0][-1]) + 9, int(hs[1][-1]) + 9
+    q, do, k, v = rows(rng, dt, n_q, heads, dim), rows(rng, dt, n_q, heads, dim), rows(rng, dt, n_k, kv, dim), rows(rng, dt, n_k, kv, dim)
+    starts = [torch.tensor(s, dtype=torch.int32, device="cuda") for s in hs]
+    shape = dict(left=40, right=0, sinks=sinks, scale=1 / math.sqrt(dim))
+    assert n_k // len(b) - 40 <= 640 and n_k - 40 > 2048       # not split by the mean
+    check_attention(sp, q, k, v, do, starts, hs, shape, dt, "long among short")
+
+
+def test_a_long_cloud_among_short_ones_takes_no_longer_than_equal_ones(sp):
+    """Its first keys' sums are split as those of equal clouds: 26000 rows in both.  (Chosen by the mean length it took 2.6 ms, now 0.18.)"""
+    def milliseconds(lens):
+        n = sum(lens)
+        starts = torch.tensor(np.concatenate([[0], np.cumsum(lens)]), dtype=torch.int32, device="cuda")
+        q, k, v, do = (torch.randn((n, h, 64), device="cuda").bfloat16() for h in (8, 2, 2, 8))
+        o, lse = sp.sp_window_attn_fwd(q, k, v, starts, starts, left=256, sinks=4)
+        times = []
+        for _ in range(5):
+            begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            begin.record()
+            sp.sp_window_attn_bwd(q, k, v, o, do, lse, starts, starts, left=256, sinks=4)
+            end.record()
+            torch.cuda.synchronize()
+            times.append(begin.elapsed_time(end))
+        return min(times[1:])
+
+    assert milliseconds([100] * 50 + [16000] + [100] * 50) < 4 * milliseconds([2600] * 10)
