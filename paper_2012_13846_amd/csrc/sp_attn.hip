@@ -123,26 +123,20 @@ __global__ __launch_bounds__(64 * W, NT <= 2 ? 3 : 2) void attn_fwd_kernel(AttnF
         }
         if (again && part != kFinite) {
             __syncthreads();
-            return false;
+            return;
         }
         l = halves<Add>(l);
         const float inv = none ? 0.f : 1.f / l;
-        float check = 0.f;
 #pragma unroll
-        for (int d = 0; d < NT; ++d)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) check = fmaf(acc[d][i] *= inv, 0.f, check);
-        return any_of_workgroup(wr.there & (halves<Add>(check) != 0.f));
-    };
-    auto store = [&] {
+        for (int d = 0; d < NT; ++d) acc[d] *= inv;
         if (!wr.there) return;
         put_column<T, NT, VEC>(f.o.at(c.q0 + wr.query, h, w.dim), acc, w.dim);
         if (lane < 32) f.lse[(int64_t)(c.q0 + wr.query) * w.heads + h] = none ? -INFINITY : (m * c2 + __builtin_amdgcn_logf(l)) * kLn2;
     };
-    if (__builtin_expect(!pass(std::false_type{}, kFinite), 1)) return store();
+    pass(std::false_type{}, kFinite);
+    if (__builtin_expect(!any_of_workgroup(wr.there & other_than_finite(acc)), 1)) return;
     kt.load(lds, 0, 0);
     pass(std::true_type{}, kFinite);
-    store();
     // a row whose sum of exponentials is NaN is that altogether
     if (!any_of_workgroup(other) || !any_of_workgroup(wr.there & (l == l))) return;
 #pragma unroll 1

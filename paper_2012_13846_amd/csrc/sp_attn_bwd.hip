@@ -122,21 +122,15 @@ __global__ __launch_bounds__(64 * W, NT == 1 ? 4 : sizeof(T) * NT == 4 ? 3 : siz
                 }
             }
         }
-        if (again && part != kFinite) return false;
-        float check = 0.f;
+        if (again && part != kFinite) return;
 #pragma unroll
-        for (int d = 0; d < NT; ++d)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) check = fmaf(acc[d][i] *= w.scale, 0.f, check);
-        return any_of_workgroup(wr.there & (halves<Add>(check) != 0.f));
-    };
-    auto store = [&] {
+        for (int d = 0; d < NT; ++d) acc[d] *= w.scale;
         if (wr.there) put_column<T, NT, VEC>(g.dq.at(c.q0 + wr.query, h, w.dim), acc, w.dim);
     };
-    if (__builtin_expect(!pass(std::false_type{}, kFinite), 1)) return store();
+    pass(std::false_type{}, kFinite);
+    if (__builtin_expect(!any_of_workgroup(wr.there & other_than_finite(acc)), 1)) return;
     kt.load(lds, 0, 0);
     pass(std::true_type{}, kFinite);
-    store();
     if (!any_of_workgroup(other) || !any_of_workgroup(wr.there & (fabsf(l2) < INFINITY))) return;
     kt.load(lds, 0, 0);
     pass(std::true_type{}, kEither);
@@ -151,9 +145,10 @@ constexpr int kSplitSinks = 128;
 // backward); of 745 rows: 88 and 81 (one cloud, 8 heads of 64, bf16); of 1745: 144 and 119.
 constexpr int kLongBeyond = 640;
 // The host knows the clouds' mean, not the longest: with a lower mean the kernels look for long clouds in calls of more keys beyond the window than
-// this.  Where there are none that costs 5 us (2048 to 65536 keys in clouds of 128 and 256: 29 - 1288 us in all); a cloud of 4000 keys among 100 of
+// this.  Where there are none that costs 5 us (4096 to 65536 keys in clouds of 256: 31 - 1288 us in all); a cloud of 4000 keys among 100 of
 // 100 takes 132 us instead of 645 (8 heads of 64 over 2), one of 60000 370 instead of 9800, with 32 heads of 128 over 8 5.1 ms instead of 21.
-constexpr int kLongTotal = 2048;
+// In fewer keys in all, one long cloud loses 0.2 - 0.6 ms at most, and clouds a little beyond kLongBeyond gain nothing (2500 keys: 109 us, 118 split).
+constexpr int kLongTotal = 4096;
 struct Split {
     int sinks;           // 0: not split
     LongClouds clouds;
@@ -409,13 +404,7 @@ __global__ __launch_bounds__(64 * W, NT == 1 ? (sizeof(T) == 2 ? 4 : 3) : sizeof
                 }
             if (more && threadIdx.x < kN) stats[buf ^ 1].put(next, threadIdx.x);
         }
-        if (again) return __syncthreads(), false;
-        float check = 0.f;
-#pragma unroll
-        for (int d = 0; d < NT; ++d)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) check = fmaf(kg.dk[d][i] *= w.scale, 0.f, fmaf(kg.dv[d][i], 0.f, check));
-        return any_of_workgroup(there & (halves<Add>(check) != 0.f));
+        if (again) __syncthreads();
     };
     const bool part = split_here && j < split.sinks;
     // of this key's dk (0) and dv (1)
@@ -425,20 +414,22 @@ __global__ __launch_bounds__(64 * W, NT == 1 ? (sizeof(T) == 2 ? 4 : 3) : sizeof
         if (there && part) put_column<float, NT, false>(sums(which), acc, w.dim);
         else if (there) put_column<T, NT, VEC>(row(which), acc, w.dim);
     };
-    if (__builtin_expect(!pass(std::false_type{}, 0), 1)) {
-        store(0, kg.dk);
-        store(1, kg.dv);
-        return;
-    }
+    auto scaled = [&](f32x16(&acc)[NT]) {
+#pragma unroll
+        for (int d = 0; d < NT; ++d) acc[d] *= w.scale;
+    };
+    pass(std::false_type{}, 0);
+    scaled(kg.dk);
+    store(0, kg.dk);
+    store(1, kg.dv);
+    if (__builtin_expect(!any_of_workgroup(there & other_than_finite(kg.dk, kg.dv)), 1)) return;
 #pragma unroll 1
     for (int what = kDk; what < kAgain; ++what) {
         if (what == kDvPlus && !any_of_workgroup(other)) break;
         start();
         pass(std::true_type{}, what);
         if (what <= kDv) {
-            if (what == kDk)
-#pragma unroll
-                for (int d = 0; d < NT; ++d) kg.dv[d] *= w.scale;
+            if (what == kDk) scaled(kg.dv);
             store(what, kg.dv);
         } else if (there && part) {
             join_column<float, NT>(sums(1), kg.dv, w.dim, what == kDvPlus ? INFINITY : -INFINITY);
@@ -512,17 +503,11 @@ __global__ __launch_bounds__(64, 1) void attn_far_kernel(AttnBwd<T> g, Split spl
     };
     pass(std::false_type{}, 0);
     scaled(kg.dk);
-    float check = 0.f;
-#pragma unroll
-    for (int d = 0; d < NT; ++d)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) check = fmaf(kg.dk[d][i], 0.f, fmaf(kg.dv[d][i], 0.f, check));
-    if (__builtin_expect(!__any(there & (check != 0.f)), 1)) {
-        if (!there) return;
+    if (there) {
         put_column<float, NT, false>(sums, kg.dk, w.dim);
         put_column<float, NT, false>(sums + w.dim, kg.dv, w.dim);
-        return;
     }
+    if (__builtin_expect(!__any(there & other_than_finite(kg.dk, kg.dv)), 1)) return;
 #pragma unroll 1
     for (int what = kDk; what < kAgain; ++what) {
         if (what == kDvPlus && !__any(other)) break;

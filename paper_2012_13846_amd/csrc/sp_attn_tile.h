@@ -258,6 +258,20 @@ __device__ __forceinline__ void put_column(T* row, const f32x16 (&acc)[NT], int 
         }
 }
 
+// Whether a column of accumulators holds an infinity or NaN.  After they are stored, so that they need not be kept for it.
+template <int NT, typename... More>
+__device__ __forceinline__ bool other_than_finite(const f32x16 (&acc)[NT], const More&... more) {
+    float check = 0.f;
+    auto add = [&](const f32x16 (&a)[NT]) {
+#pragma unroll
+        for (int d = 0; d < NT; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) check = fmaf(a[d][i], 0.f, check);
+    };
+    add(acc);
+    (add(more), ...);
+    return halves<Add>(check) != 0.f;
+}
 // `other` (an infinity, NaN) joins a row of the result where `counts` (Part) are not zero.  The thread itself has written these elements.
 template <typename T, int NT>
 __device__ __forceinline__ void join_column(T* row, const f32x16 (&counts)[NT], int dim, float other) {

@@ -776,14 +776,14 @@ def test_windows_wider_than_any_cloud(sp, wide):
 def test_first_keys_of_long_clouds_among_short_ones(sp, dt, heads, kv, dim, sinks, clouds):
     """More clouds than there can be long ones, and fewer; empty ones; rows of no cloud; some clouds are asked by their last rows only."""
     rng = np.random.default_rng(clouds + dim)
-    b = np.array([30] * clouds + [1300] + [0, 17] * clouds + [900, 5])
+    b = np.array([30] * clouds + [1300] + [0, 17] * clouds + [900, 5] + [100] * 25)
     a = np.where(np.arange(len(b)) % 3 == 2, np.minimum(b, 7), b)
     hs = tuple(np.concatenate([[0], np.cumsum(x)]) + 9 for x in (a, b))
     n_q, n_k = int(hs[0][-1]) + 9, int(hs[1][-1]) + 9
     q, do, k, v = rows(rng, dt, n_q, heads, dim), rows(rng, dt, n_q, heads, dim), rows(rng, dt, n_k, kv, dim), rows(rng, dt, n_k, kv, dim)
     starts = [torch.tensor(s, dtype=torch.int32, device="cuda") for s in hs]
     shape = dict(left=40, right=0, sinks=sinks, scale=1 / math.sqrt(dim))
-    assert n_k // len(b) - 40 <= 640 and n_k - 40 > 2048       # not split by the mean
+    assert n_k // len(b) - 40 <= 640 and n_k - 40 > 4096       # not split by the mean
     check_attention(sp, q, k, v, do, starts, hs, shape, dt, "long among short")
 
 
