@@ -271,12 +271,13 @@ int sp_layer_norm_bwd(const void* d_x, const void* d_dy, int64_t n, int32_t c, c
  * right = 0: causal.  o = softmax over the keys seen of scale * q.k, times v; lse = log of the sum of exponentials (natural), fp32
  * [n_q][heads].  A query that sees nothing, and a row that belongs to no cloud, has o = 0 and lse = -infinity, and zero gradients.
  * Keys that a query does not see do not reach its results, whatever they hold (infinities and NaN too).
- * Infinities and NaN that are seen give such results where they come in.
+ * Infinities and NaN that are seen give such results in the elements where the definition has them (of dq and dk whether by sign is not said:
+ * dout . o of an infinity is one of either sign, as a sum over keys NaN).  They cost up to five times a call's usual time.
  * Starts that are not ascending or out of range give undefined values, but no access outside of the arrays.
  * Row r, head h, element e of an array lies at [r * ld + h * dim + e] (ld in elements, at least heads * dim or kv_heads * dim): views
  * of a fused projection are read and written in place.  Arrays that are written overlap no other array.
- * 1 <= dim <= 128 (SP_ERR_UNSUPPORTED beyond), n_q, n_k, n_clouds <= 2^29, n_q * heads / kv_heads <= 2^30, left, right, sinks >= 0.  Rows of whole 16-byte pieces, 16-byte
- * aligned, are read in such pieces, others element by element.  In bf16 probabilities and their gradients are rounded to bf16
+ * 1 <= dim <= 128 (SP_ERR_UNSUPPORTED beyond), n_q, n_k, n_clouds <= 2^29, n_q * heads / kv_heads <= 2^30, left, right, sinks >= 0.
+ * Rows of whole 16-byte pieces, 16-byte aligned, are read in such pieces, others element by element.  In bf16 probabilities and their gradients are rounded to bf16
  * before they are multiplied with rows; scores, sums and accumulators are fp32. */
 typedef struct {
     int64_t n_q, n_k;          /* rows of q and o; rows of k and v */
@@ -291,7 +292,8 @@ typedef struct {
 int sp_window_attn_fwd(const sp_window_attn* a, const void* d_q, int64_t ldq, const void* d_k, int64_t ldk, const void* d_v,
                        int64_t ldv, void* d_o, int64_t ldo, float* d_lse, void* stream);
 /* Gradients of sum(o * dout): d_dq like q, d_dk and d_dv like k and v (summed over the query heads that share them); d_o and d_lse
- * are the forward pass's results (dout . o is taken from o, or in bf16 for rows of few keys from the sums that o was rounded from). */
+ * are the forward pass's results.  dout . o is taken from o, or in bf16 for rows that see at most 128 keys from the sums that o was rounded
+ * from: o's rounding, half a step, stands in all of a row's gradients, and averages out only where many keys share the row. */
 int sp_window_attn_bwd(const sp_window_attn* a, const void* d_q, int64_t ldq, const void* d_k, int64_t ldk, const void* d_v,
                        int64_t ldv, const void* d_o, int64_t ldo, const void* d_dout, int64_t lddout, const float* d_lse, void* d_dq,
                        int64_t lddq, void* d_dk, int64_t lddk, void* d_dv, int64_t lddv, void* stream);
@@ -302,7 +304,8 @@ int sp_window_attn_bwd(const sp_window_attn* a, const void* d_q, int64_t ldq, co
  * else in row sinks + (j - sinks) % (cap - sinks): with cap > p nothing is overwritten, else the rows behind the first `sinks`
  * are a ring.  The call writes k_new and v_new to p's row of the caches, then attends over
  *   max(p - left, p + 1 - (cap - sinks)) <= j <= p  and  j < min(sinks, p + 1).
- * lens[b] < 0: no sequence in this slot; o = 0, its caches stay as they are.  cap > sinks >= 0.  lens is not changed. */
+ * lens[b] < 0: no sequence in this slot; o = 0, its caches stay as they are.  cap > sinks >= 0.  lens is not changed.
+ * In bf16 probabilities are rounded to bf16 before they are multiplied with values, as in the packed form. */
 int sp_window_attn_step(const void* d_q, const void* d_k_new, const void* d_v_new, void* d_k_cache, void* d_v_cache,
                         const int32_t* d_lens, int32_t batch, int32_t cap, int32_t heads, int32_t kv_heads, int32_t dim, int32_t left,
                         int32_t sinks, float scale, void* d_o, sp_dtype dt, void* stream);

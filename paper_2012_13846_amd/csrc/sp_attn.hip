@@ -8,10 +8,10 @@ namespace {
 
 // One pass over the keys with a running maximum and sum.  The maximum in use may lag the true one by 8 powers of two (probabilities up
 // to 256, sums in fp32): the accumulators are multiplied again only when it falls behind, not whenever one of 32 rows has a new one.
-// Bound by the vector pipe and the matrix pipe together: 16384 tokens, 32 heads of 128 over 8, window 1024: 326 - 342 us, 780 TFLOP/s, matrix
-// pipe busy 34 %, vector pipe 43 %, no LDS bank conflicts; heads of 32 (373601 rows, 8 heads, 513 keys a row): 660 - 700 us, vector pipe
-// 75 % (an exponential and four operations a pair against 128 multiply-adds).  64 keys a step: 32 leave a barrier for every 16 products;
-// three wavefronts a SIMD for heads up to 64: at four (128 registers) the mask's borders spill, twice the time.  Row sums as products
+// Bound by the vector pipe and the matrix pipe together: 16384 tokens, 32 heads of 128 over 8, window 1024: 316 - 343 us, 760 - 820 TFLOP/s, matrix
+// pipe busy 37 %, vector pipe 43 %, no LDS bank conflicts; heads of 32 (373601 rows, 8 heads, 513 keys a row): 600 - 660 us, vector pipe
+// 83 % (an exponential and four operations a pair against 128 multiply-adds).  64 keys a step: 32 leave a barrier for every 16 products;
+// three wavefronts a SIMD for heads of 64, which need 165 registers; heads of 32 take 122 and get a fourth.  Row sums as products
 // with ones would be free on the matrix pipe, but of probabilities rounded to bf16: lse must not be.
 template <typename T, int NT, bool VEC, int W>
 __global__ __launch_bounds__(64 * W, NT <= 2 ? 3 : 2) void attn_fwd_kernel(AttnFwd<T> f, int tiles) {

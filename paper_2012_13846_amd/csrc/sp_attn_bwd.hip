@@ -18,8 +18,8 @@ constexpr int kThreads = 256;  // of a workgroup that joins
 // its own over keys that are close by then; with more of them o's part is below 0.0007.
 constexpr int kExactKeys = 128;
 
-// Three products a pair of tiles: scores, dout . v, dS . k; accumulators, q and dout stay in registers.  The forward pass's case: 442 - 462 us
-// (860 TFLOP/s of the three products), matrix pipe busy 39 %, vector pipe 37 %; heads of 32: 705 - 760 us, vector pipe 80 %.
+// Three products a pair of tiles: scores, dout . v, dS . k; accumulators, q and dout stay in registers.  The forward pass's case: 440 - 475 us
+// (840 - 900 TFLOP/s of the three products), matrix pipe busy 40 %, vector pipe 36 %; heads of 32: 710 - 790 us, vector pipe 80 %.
 template <typename T, int NT, bool VEC, int W>
 __global__ __launch_bounds__(64 * W, NT == 1 ? 4 : sizeof(T) * NT == 4 ? 3 : sizeof(T) * NT < 16 ? 2 : 1) void attn_dq_kernel(AttnBwd<T> g, int tiles) {
     using Tl = Tile<T, NT>;
@@ -308,10 +308,10 @@ template <typename T, int NT, int W>
 constexpr int kStepRows = sizeof(T) == 2 && NT <= 2 && W > 1 ? 64 : 32;
 
 // Four products a pair of tiles.  A wavefront has 32 keys: 128 registers of accumulators and 32 of keys at a width of 128, which with
-// the values in LDS leaves room for two wavefronts a SIMD (1455 -> 697 us on the forward pass's case; 660 - 720 now).  Bound by the latency of
-// LDS reads, each right before its product for want of registers to read ahead: matrix pipe busy 30 %, vector pipe 19 %.  Reads asked
+// the values in LDS leaves room for two wavefronts a SIMD (1455 -> 697 us on the forward pass's case; 680 - 750 now).  Bound by the latency of
+// LDS reads, each right before its product for want of registers to read ahead: matrix pipe busy 31 %, vector pipe 19 %.  Reads asked
 // for ahead of their products spill (2103 us in all against 1538), a higher priority for products costs 15 %; the two score products one
-// after another instead of by turns give 1 - 7 %.  Heads of 32: 775 - 825 us.
+// after another instead of by turns give 1 - 7 %.  Heads of 32: 770 - 850 us.
 template <typename T, int NT, bool VEC, int W>
 __global__ __launch_bounds__(64 * W, NT == 1 ? (sizeof(T) == 2 ? 4 : 3) : sizeof(T) * NT == 4 ? 3 : sizeof(T) * NT <= 8 ? 2 : 1) void attn_dkv_kernel(AttnBwd<T> g, Split split, int tiles) {
     using Tl = Tile<T, NT>;
@@ -439,8 +439,8 @@ __global__ __launch_bounds__(64 * W, NT == 1 ? (sizeof(T) == 2 ? 4 : 3) : sizeof
     }
 }
 
-// Reads every row once for a few keys: bound by memory's latency at one or two wavefronts a SIMD (373601 rows of 8 heads of 32: 146 us,
-// 2.6 TB/s; 16384 of 32 of 128: 55 us, 4.9 TB/s).  Without the split the tile of the first keys alone would go over all rows.
+// Reads every row once for a few keys: bound by memory's latency at one or two wavefronts a SIMD (373601 rows of 8 heads of 32: 147 us,
+// 2.6 TB/s; 16384 of 32 of 128: 55 - 59 us, 4.6 - 4.9 TB/s).  Without the split the tile of the first keys alone would go over all rows.
 template <typename T, int NT, bool VEC>
 __global__ __launch_bounds__(64, 1) void attn_far_kernel(AttnBwd<T> g, Split split, int tiles) {
     using Tl = Tile<T, NT>;

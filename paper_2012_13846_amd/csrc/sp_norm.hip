@@ -7,7 +7,8 @@
 // the registers of the lanes that own the columns, over all rows of a workgroup (the grid is no larger than the chip's fill), then
 // over its row groups through LDS, and the workgroups' partial sums are added in fp64 in a fixed order by a second kernel.
 // Rows that no workgroup can hold (more than 16 elements a thread of 1024) are read again from cache for every statistic.
-// Measured: 373601 x 256 bf16 forward 76 us, backward 114 + 5 (5.0 TB/s each; a large copy 5.0 - 6.3); 16384 x 4096 67 and 86.
+// Measured: 373601 x 256 bf16 forward 80 - 86 us (4.5 - 4.8 TB/s; a large copy 5.0 - 6.3), backward 114 - 117 + 5 (4.9 - 5.0); 16384 x 4096
+// 54 - 56 (4.8) and 86 - 88 + 5 (4.6).
 #include <algorithm>
 
 #include "sp_elem.h"
