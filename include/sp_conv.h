@@ -272,7 +272,7 @@ int sp_layer_norm_bwd(const void* d_x, const void* d_dy, int64_t n, int32_t c, c
  * [n_q][heads].  A query that sees nothing, and a row that belongs to no cloud, has o = 0 and lse = -infinity, and zero gradients.
  * Keys that a query does not see do not reach its results, whatever they hold (infinities and NaN too).
  * Infinities and NaN that are seen give such results in the elements where the definition has them (of dq and dk whether by sign is not said:
- * dout . o of an infinity is one of either sign, as a sum over keys NaN).  They cost up to five times a call's usual time.
+ * dout . o of an infinity is one of either sign, as a sum over keys NaN).  They cost a call up to seven times its usual time.
  * Starts that are not ascending or out of range give undefined values, but no access outside of the arrays.
  * Row r, head h, element e of an array lies at [r * ld + h * dim + e] (ld in elements, at least heads * dim or kv_heads * dim): views
  * of a fused projection are read and written in place.  Arrays that are written overlap no other array.

@@ -677,7 +677,7 @@ def test_first_keys_gradients_of_rows_with_infinities(sp, dt, heads, kv, dim, si
 
 
 def test_first_keys_gradients_of_a_diverged_run_take_a_bounded_time(sp):
-    """Sums that are not finite are taken again, four times at most: no more than five times the time in all (and what two clocks differ)."""
+    """Sums that are not finite are taken again, four times at most: four times the usual time is measured here, by one wavefront a key it was 172."""
     n = 20000
     q, k, v, do, starts, hs, shape = far_first_keys(BF16, n, 8, 2, 64, 100, 4)
     o, lse = sp.sp_window_attn_fwd(q, k, v, *starts, **shape)
