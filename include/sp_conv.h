@@ -320,6 +320,74 @@ int sp_window_attn_step(const void* d_q, const void* d_k_new, const void* d_v_ne
 int sp_distill(const void* d_logits, int64_t n, int32_t m, const float* d_top, const int32_t* d_index, int32_t k, float temperature,
                const float* d_weight, float* d_loss, void* d_dlogits, sp_dtype dt, void* stream);
 
+/* Rotary positions.  Axis a (a row has a position on each: its place in a sequence, or a voxel's x, y, z) turns part[a] elements of every
+ * head, those of axis 0 first; what is left of the head stays.  Pair i of an axis turns by angle = position * scale * base^(-2 i / part):
+ *   y1 = x1 cos - x2 sin, y2 = x1 sin + x2 cos
+ * The pairs of an axis are neighbours (elements 2 i, 2 i + 1) or, with split != 0, halves (i, i + part / 2).  Angles are reduced in fp64, so any
+ * int32 position is as exact as a near one.  Position of row r on axis a: d_pos[r * ld_pos + a], so that columns 1..3 of a coordinate matrix are read
+ * in place (d_coords + 1, ld_pos 4).  Rows [heads][dim] as in sp_window_attn: row r, head h, element e at [r * ld + h * dim + e]; y may be x (with the
+ * same ld), else the two do not overlap.  sp_rope_bwd turns back, which is the gradient.  1 <= dim <= 256, 1 to 4 axes, parts even. */
+typedef struct {
+    int64_t n;
+    int32_t heads, dim, axes;
+    int32_t part[4];
+    int32_t split;
+    double base, scale;
+    sp_dtype dt;
+    const int32_t* d_pos;
+    int64_t ld_pos;
+} sp_rope;
+int sp_rope_fwd(const sp_rope* a, const void* d_x, int64_t ldx, void* d_y, int64_t ldy, void* stream);
+int sp_rope_bwd(const sp_rope* a, const void* d_dy, int64_t lddy, void* d_dx, int64_t lddx, void* stream);
+
+/* Work memory of the calls below is the caller's: the size that the function beside them says (-1: such a call is refused), 256-byte aligned, used
+ * until the stream has passed the call.  No call allocates, so calls may be captured into graphs, each with work memory of its own.
+ *
+ * Root-mean-square norm with the residual's addition, every row of x [n][c] by itself:
+ *   h = x + res, as it is stored in dt;  rstd = 1/sqrt(mean(h^2) + eps);  y = gamma * h * rstd
+ * d_res NULL: h = x, and d_h must be NULL.  d_h may be d_x or d_res, d_y either of them that d_h is not.  rstd [n] is an output.
+ * sp_rms_norm_q8: y in 8 bits (below) instead, rounded once.
+ * sp_rms_norm_bwd: with hhat = h * rstd, g = dy * gamma and a mean over the row, dx = dh + rstd * (g - hhat * mean(g * hhat)) is the gradient of x
+ * and of the residual; dh (NULL: none) is the gradient that reaches h past the norm.  dgamma [c] = sum dy * hhat.  dx may be dy or dh.
+ * Any 1 <= c <= 65536. */
+int sp_rms_norm_fwd(const void* d_x, const void* d_res, int64_t n, int32_t c, const float* d_gamma, float eps, void* d_h, void* d_y,
+                    float* d_rstd, sp_dtype dt, void* stream);
+int sp_rms_norm_q8(const void* d_x, const void* d_res, int64_t n, int32_t c, const float* d_gamma, float eps, void* d_h, uint8_t* d_q,
+                   uint8_t* d_scales, sp_dtype dt, void* stream);
+int64_t sp_rms_norm_bwd_work(int64_t n, int32_t c, sp_dtype dt);
+int sp_rms_norm_bwd(const void* d_h, const void* d_dy, const void* d_dh, int64_t n, int32_t c, const float* d_gamma, const float* d_rstd,
+                    void* d_dx, float* d_dgamma, void* d_work, sp_dtype dt, void* stream);
+
+/* Rows in 8 bits: e4m3 codes [n][128 * blocks] with blocks = ceil(c / 128), zeros behind c, and one power of two for each block of 128 elements,
+ * e8m0 (exponent + 127) [n][blocks rounded up to 4] with 127 in the places behind: the least 2^e, -127 <= e, with every element at most 448 * 2^e.
+ * A block of zeros has 127; one that holds an infinity or NaN has 255, which makes NaN of every product with it.
+ * sp_q8_rows: of x (rows ldx elements apart), to nearest even; transposed != 0: of the c rows of the transposed matrix, n elements each.
+ * sp_q8_linear: y [n][m] of type dt = x w^T for x [n][c] and w [m][c] in 8 bits, sums fp32 on the scaled matrix instruction.  For gradients
+ * (dx = dy w, dw = dy^T x) it is given operands in 8 bits along the other axis.  c <= 2^22. */
+int64_t sp_q8_codes_bytes(int64_t n, int64_t c);
+int64_t sp_q8_scales_bytes(int64_t n, int64_t c);
+int sp_q8_rows(const void* d_x, int64_t ldx, int64_t n, int32_t c, int32_t transposed, uint8_t* d_q, uint8_t* d_scales, sp_dtype dt, void* stream);
+int64_t sp_q8_linear_work(int64_t n, int64_t c, int64_t m);
+int sp_q8_linear(const uint8_t* d_q, const uint8_t* d_scales, int64_t n, int64_t c, const uint8_t* d_wq, const uint8_t* d_wscales, int64_t m,
+                 void* d_y, sp_dtype dt, void* d_work, void* stream);
+
+/* Gated feed-forward block on rows x [n][c], with w_in [2 m][c] (m rows of gates, then m of ups) and w_out [c][m]:
+ *   [g u] = x w_in^T;  y = (act(g) * u) w_out^T,   act silu (g / (1 + e^-g)) or gelu (g * the normal distribution function of g)
+ * sp_ffn_fwd writes y [n][c] and, unless d_kept is NULL, g, u and act(g) * u [n][3 m], which the backward pass reads.  sp_ffn_bwd: gradients of sum(y * dy): dx like
+ * x, dw_in and dw_out like the weights, of type dt.  Sums fp32; in bf16 act(g) * u and the gradients of g and u are rounded before they are multiplied
+ * again.  All arrays dense; outputs overlap nothing. */
+typedef enum { SP_GATE_SILU = 0, SP_GATE_GELU = 1 } sp_gate;
+typedef struct {
+    int64_t n;
+    int32_t c, m;
+    sp_gate act;
+    sp_dtype dt;
+} sp_ffn;
+int64_t sp_ffn_work_bytes(const sp_ffn* f, int32_t backward);
+int sp_ffn_fwd(const sp_ffn* f, const void* d_x, const void* d_w_in, const void* d_w_out, void* d_kept, void* d_y, void* d_work, void* stream);
+int sp_ffn_bwd(const sp_ffn* f, const void* d_x, const void* d_w_in, const void* d_w_out, const void* d_kept, const void* d_dy, void* d_dx,
+               void* d_dw_in, void* d_dw_out, void* d_work, void* stream);
+
 /* ---- stage-boundary packing of a sparse tensor (Sec. III-B, last paragraph: the coordinate matrix and the
  * feature matrix are what is exchanged between pipeline stages) ---------------------------------------------
  * (C, F) -> one contiguous device buffer that any transport can send as a single message, and back.  Layout,

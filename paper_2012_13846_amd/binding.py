@@ -671,3 +671,221 @@ def sp_distill(logits, top, index, temperature: float = 1.0, weight=None, want_g
                                         weight.data_ptr() if weight is not None else None, loss.data_ptr(),
                                         d.data_ptr() if want_grad else None, _dt(logits), _stream()))
     return loss, d
+
+
+class _Rope(C.Structure):
+    _fields_ = [("n", C.c_int64), ("heads", C.c_int32), ("dim", C.c_int32), ("axes", C.c_int32), ("part", C.c_int32 * 4), ("split", C.c_int32),
+                ("base", C.c_double), ("scale", C.c_double), ("dt", C.c_int32), ("d_pos", _vp), ("ld_pos", C.c_int64)]
+
+
+class _Ffn(C.Structure):
+    _fields_ = [("n", C.c_int64), ("c", C.c_int32), ("m", C.c_int32), ("act", C.c_int32), ("dt", C.c_int32)]
+
+
+def _block_argtypes():
+    l = lib()
+    if getattr(l, "_block_ready", False):
+        return l
+    f, i4, i8 = C.c_float, C.c_int32, C.c_int64
+    l.sp_rope_fwd.argtypes = l.sp_rope_bwd.argtypes = [C.POINTER(_Rope), _vp, i8, _vp, i8, _vp]
+    l.sp_rms_norm_fwd.argtypes = [_vp, _vp, i8, i4, _vp, f, _vp, _vp, _vp, i4, _vp]
+    l.sp_rms_norm_q8.argtypes = [_vp, _vp, i8, i4, _vp, f, _vp, _vp, _vp, i4, _vp]
+    l.sp_rms_norm_bwd.argtypes = [_vp, _vp, _vp, i8, i4, _vp, _vp, _vp, _vp, _vp, i4, _vp]
+    l.sp_rms_norm_bwd_work.argtypes = [i8, i4, i4]
+    l.sp_q8_codes_bytes.argtypes = l.sp_q8_scales_bytes.argtypes = [i8, i8]
+    l.sp_q8_rows.argtypes = [_vp, i8, i8, i4, i4, _vp, _vp, i4, _vp]
+    l.sp_q8_linear_work.argtypes = [i8, i8, i8]
+    l.sp_q8_linear.argtypes = [_vp, _vp, i8, i8, _vp, _vp, i8, _vp, i4, _vp, _vp]
+    l.sp_ffn_work_bytes.argtypes = [C.POINTER(_Ffn), i4]
+    l.sp_ffn_fwd.argtypes = [C.POINTER(_Ffn)] + [_vp] * 7
+    l.sp_ffn_bwd.argtypes = [C.POINTER(_Ffn)] + [_vp] * 10
+    for name in ("sp_rms_norm_bwd_work", "sp_q8_codes_bytes", "sp_q8_scales_bytes", "sp_q8_linear_work", "sp_ffn_work_bytes"):
+        getattr(l, name).restype = i8
+    l._block_ready = True
+    return l
+
+
+def _here(*tensors):
+    """All on the device whose stream the call goes to."""
+    device = _cur_device() if _cur_device is not None else torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"every tensor must be on the current device (cuda:{device}), not {t.device}")
+
+
+def _work(nbytes: int, device) -> torch.Tensor:
+    """Work memory of one call: from torch's allocator, so that a captured graph owns its own."""
+    if nbytes < 0:
+        raise ValueError("sizes that the library does not take")
+    return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+def _rope(name, x, pos, parts, base, split, scale, out):
+    ptr, ld = _head_rows(x, x.dtype, "x")
+    n, heads, dim = x.shape
+    parts = [operator.index(p) for p in parts]
+    if not 1 <= len(parts) <= 4 or any(not 0 <= p <= dim for p in parts):
+        raise ValueError("1 to 4 axes, each turning at most a head's elements")
+    if not pos.is_cuda or pos.dtype != torch.int32 or pos.shape != (n, len(parts)):
+        raise ValueError(f"pos must be a CUDA int32 tensor {(n, len(parts))}")
+    if n > 1 and pos.stride(0) < len(parts) or (len(parts) > 1 and pos.stride(1) != 1):
+        raise ValueError("the positions of a row must lie one after another, and rows must not overlap")
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    _need_shape(out, x.shape, "out")
+    to, ldo = _head_rows(out, x.dtype, "out")
+    _here(x, pos, out)
+    a = _Rope(n, heads, dim, len(parts), (C.c_int32 * 4)(*parts), int(bool(split)), base, scale, _dt(x), pos.data_ptr(),
+              pos.stride(0) if n > 1 else len(parts))
+    _check(getattr(_block_argtypes(), name)(C.byref(a), ptr, ld, to, ldo, _stream()))
+    return out
+
+
+def sp_rope_fwd(x, pos, parts, base: float = 10000.0, split: bool = False, scale: float = 1.0, out=None):
+    """x [n][heads][dim] (a view of a fused projection too), pos int32 [n][axes] (a sparse tensor's coords()[:, 1:] too), parts: elements of a
+    head that each axis turns.  Returns the turned rows, new or in `out` (x itself: in place)."""
+    return _rope("sp_rope_fwd", x, pos, parts, base, split, scale, out)
+
+
+def sp_rope_bwd(dy, pos, parts, base: float = 10000.0, split: bool = False, scale: float = 1.0, out=None):
+    """The gradient of sp_rope_fwd's x: dy turned back."""
+    return _rope("sp_rope_bwd", dy, pos, parts, base, split, scale, out)
+
+
+def _rms_check(x, gamma, residual):
+    _need_cuda(x, None, "x"), _need_cuda(gamma, torch.float32, "gamma")
+    if x.ndim != 2:
+        raise ValueError("x must be [n][c]")
+    _need_shape(gamma, (x.shape[1],), "gamma")
+    if residual is not None:
+        _need_cuda(residual, x.dtype, "residual"), _need_shape(residual, x.shape, "residual")
+    _here(x, gamma, residual)
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def sp_rms_norm_fwd(x, gamma, residual=None, eps: float = 1e-5):
+    """x [n][c], gamma fp32 [c].  Returns (h = x + residual, or x itself without one; y; rstd fp32 [n])."""
+    _rms_check(x, gamma, residual)
+    n, c = x.shape
+    h = None if residual is None else torch.empty_like(x)
+    y, rstd = torch.empty_like(x), _f32((n,), x.device)
+    _check(_block_argtypes().sp_rms_norm_fwd(x.data_ptr(), _ptr(residual), n, c, gamma.data_ptr(), eps, _ptr(h), y.data_ptr(), rstd.data_ptr(),
+                                             _dt(x), _stream()))
+    return (x if h is None else h), y, rstd
+
+
+def sp_rms_norm_q8(x, gamma, residual=None, eps: float = 1e-5):
+    """Returns (h, y in 8 bits: see sp_q8_rows)."""
+    _rms_check(x, gamma, residual)
+    n, c = x.shape
+    h = None if residual is None else torch.empty_like(x)
+    q, scales = _q8_new(n, c, x.device)
+    _check(_block_argtypes().sp_rms_norm_q8(x.data_ptr(), _ptr(residual), n, c, gamma.data_ptr(), eps, _ptr(h), q.data_ptr(), scales.data_ptr(),
+                                            _dt(x), _stream()))
+    return (x if h is None else h), (q, scales)
+
+
+def sp_rms_norm_bwd(h, dy, gamma, rstd, dh=None):
+    """Returns (dx, which is the residual's gradient too; dgamma fp32 [c]).  dh: the gradient that reaches h past the norm."""
+    _rms_check(h, gamma, dh)
+    _need_cuda(dy, h.dtype, "dy"), _need_cuda(rstd, torch.float32, "rstd")
+    n, c = h.shape
+    _need_shape(dy, (n, c), "dy"), _need_shape(rstd, (n,), "rstd")
+    _here(dy, rstd)
+    l = _block_argtypes()
+    dx, dgamma, work = torch.empty_like(h), _f32((c,), h.device), _work(l.sp_rms_norm_bwd_work(n, c, _dt(h)), h.device)
+    _check(l.sp_rms_norm_bwd(h.data_ptr(), dy.data_ptr(), _ptr(dh), n, c, gamma.data_ptr(), rstd.data_ptr(), dx.data_ptr(), dgamma.data_ptr(),
+                             work.data_ptr(), _dt(h), _stream()))
+    return dx, dgamma
+
+
+def _q8_new(n: int, c: int, device):
+    blocks = (c + 127) // 128
+    return (torch.empty((n, blocks * 128), dtype=torch.float8_e4m3fn, device=device),
+            torch.empty((n, (blocks + 3) // 4 * 4), dtype=torch.float8_e8m0fnu, device=device))
+
+
+def sp_q8_rows(x, transposed: bool = False):
+    """Rows x [n][c] (rows may be further apart) in 8 bits: (codes float8_e4m3fn [n][c rounded up to 128], scales float8_e8m0fnu [n][one for each
+    128, rounded up to 4]).  transposed: of x's columns, [c][n]."""
+    if not x.is_cuda or x.ndim != 2 or x.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("x must be a CUDA tensor [n][c] of float32 or bfloat16")
+    n, c = x.shape
+    if (c > 1 and x.stride(1) != 1) or (n > 1 and x.stride(0) < c):
+        raise ValueError("the elements of a row of x must lie one after another, and rows must not overlap")
+    if transposed and n == 0:
+        raise ValueError("rows without elements have no codes")
+    _here(x)
+    q, scales = _q8_new(c, n, x.device) if transposed else _q8_new(n, c, x.device)
+    _check(_block_argtypes().sp_q8_rows(x.data_ptr(), x.stride(0) if n > 1 else c, n, c, int(bool(transposed)), q.data_ptr(), scales.data_ptr(),
+                                        _dt(x), _stream()))
+    return q, scales
+
+
+def sp_q8_linear(x, w, dtype=torch.bfloat16):
+    """x w^T [n][m] in `dtype` for x [n][c] and w [m][c], both as (codes, scales)."""
+    (q, s), (wq, ws) = x, w
+    for t, name in ((q, "x's codes"), (wq, "w's codes")):
+        _need_cuda(t, torch.float8_e4m3fn, name)
+    for t, name in ((s, "x's scales"), (ws, "w's scales")):
+        _need_cuda(t, torch.float8_e8m0fnu, name)
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("dtype must be float32 or bfloat16")
+    if q.ndim != 2 or wq.ndim != 2 or q.shape[1] % 128 or q.shape[1] == 0:
+        raise ValueError("codes must be [rows][a multiple of 128]")
+    n, wide = q.shape
+    m = wq.shape[0]
+    _need_shape(wq, (m, wide), "w's codes")
+    _need_shape(s, (n, (wide // 128 + 3) // 4 * 4), "x's scales"), _need_shape(ws, (m, (wide // 128 + 3) // 4 * 4), "w's scales")
+    _here(q, s, wq, ws)
+    l = _block_argtypes()
+    y, work = torch.empty((n, m), dtype=dtype, device=q.device), _work(l.sp_q8_linear_work(n, wide, m), q.device)
+    _check(l.sp_q8_linear(q.data_ptr(), s.data_ptr(), n, wide, wq.data_ptr(), ws.data_ptr(), m, y.data_ptr(),
+                          SP_F32 if dtype == torch.float32 else SP_BF16, work.data_ptr(), _stream()))
+    return y
+
+
+_GATES = {"silu": 0, "gelu": 1}
+
+
+def _ffn(x, w_in, w_out, act):
+    for t, name in ((x, "x"), (w_in, "w_in"), (w_out, "w_out")):
+        _need_cuda(t, x.dtype, name)
+        if t.ndim != 2:
+            raise ValueError(f"{name} must have two dimensions")
+    if act not in _GATES:
+        raise ValueError(f"act must be one of {sorted(_GATES)}")
+    n, c = x.shape
+    m = w_out.shape[1]
+    _need_shape(w_in, (2 * m, c), "w_in"), _need_shape(w_out, (c, m), "w_out")
+    _here(x, w_in, w_out)
+    return _Ffn(n, c, m, _GATES[act], _dt(x))
+
+
+def sp_ffn_fwd(x, w_in, w_out, act: str = "silu", keep: bool = True):
+    """Gated feed-forward block: x [n][c], w_in [2 m][c] (gates, then ups), w_out [c][m].  Returns (y, what the backward pass reads: g, u and
+    act(g) * u, [n][3 m]), or y alone without `keep`."""
+    a = _ffn(x, w_in, w_out, act)
+    l = _block_argtypes()
+    y = torch.empty_like(x)
+    kept = torch.empty((a.n, 3 * a.m), dtype=x.dtype, device=x.device) if keep else None
+    work = _work(l.sp_ffn_work_bytes(C.byref(a), 0), x.device)
+    _check(l.sp_ffn_fwd(C.byref(a), x.data_ptr(), w_in.data_ptr(), w_out.data_ptr(), _ptr(kept), y.data_ptr(), work.data_ptr(), _stream()))
+    return (y, kept) if keep else y
+
+
+def sp_ffn_bwd(x, w_in, w_out, kept, dy, act: str = "silu"):
+    """Returns (dx, dw_in, dw_out) in the type of x."""
+    a = _ffn(x, w_in, w_out, act)
+    _need_cuda(kept, x.dtype, "kept"), _need_cuda(dy, x.dtype, "dy")
+    _need_shape(kept, (a.n, 3 * a.m), "kept"), _need_shape(dy, x.shape, "dy")
+    _here(kept, dy)
+    l = _block_argtypes()
+    dx, dw_in, dw_out = torch.empty_like(x), torch.empty_like(w_in), torch.empty_like(w_out)
+    work = _work(l.sp_ffn_work_bytes(C.byref(a), 1), x.device)
+    _check(l.sp_ffn_bwd(C.byref(a), x.data_ptr(), w_in.data_ptr(), w_out.data_ptr(), kept.data_ptr(), dy.data_ptr(), dx.data_ptr(), dw_in.data_ptr(),
+                        dw_out.data_ptr(), work.data_ptr(), _stream()))
+    return dx, dw_in, dw_out
