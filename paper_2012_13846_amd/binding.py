@@ -865,13 +865,19 @@ def _ffn(x, w_in, w_out, act):
     return _Ffn(n, c, m, _GATES[act], _dt(x))
 
 
+def _kept(a):
+    """Shape and type of what the forward pass keeps: fp32 values, or words of 16 bits that are not all bf16."""
+    return ((a.n, 3 * a.m), torch.float32) if a.dt == SP_F32 else ((a.n, 4 * a.m), torch.int16)
+
+
 def sp_ffn_fwd(x, w_in, w_out, act: str = "silu", keep: bool = True):
-    """Gated feed-forward block: x [n][c], w_in [2 m][c] (gates, then ups), w_out [c][m].  Returns (y, what the backward pass reads: g, u and
-    act(g) * u, [n][3 m]), or y alone without `keep`."""
+    """Gated feed-forward block: x [n][c], w_in [2 m][c] (gates, then ups), w_out [c][m].  Returns (y, what the backward pass reads), or y
+    alone without `keep`."""
     a = _ffn(x, w_in, w_out, act)
     l = _block_argtypes()
     y = torch.empty_like(x)
-    kept = torch.empty((a.n, 3 * a.m), dtype=x.dtype, device=x.device) if keep else None
+    shape, dtype = _kept(a)
+    kept = torch.empty(shape, dtype=dtype, device=x.device) if keep else None
     work = _work(l.sp_ffn_work_bytes(C.byref(a), 0), x.device)
     _check(l.sp_ffn_fwd(C.byref(a), x.data_ptr(), w_in.data_ptr(), w_out.data_ptr(), _ptr(kept), y.data_ptr(), work.data_ptr(), _stream()))
     return (y, kept) if keep else y
@@ -880,8 +886,9 @@ def sp_ffn_fwd(x, w_in, w_out, act: str = "silu", keep: bool = True):
 def sp_ffn_bwd(x, w_in, w_out, kept, dy, act: str = "silu"):
     """Returns (dx, dw_in, dw_out) in the type of x."""
     a = _ffn(x, w_in, w_out, act)
-    _need_cuda(kept, x.dtype, "kept"), _need_cuda(dy, x.dtype, "dy")
-    _need_shape(kept, (a.n, 3 * a.m), "kept"), _need_shape(dy, x.shape, "dy")
+    shape, dtype = _kept(a)
+    _need_cuda(kept, dtype, "kept"), _need_cuda(dy, x.dtype, "dy")
+    _need_shape(kept, shape, "kept"), _need_shape(dy, x.shape, "dy")
     _here(kept, dy)
     l = _block_argtypes()
     dx, dw_in, dw_out = torch.empty_like(x), torch.empty_like(w_in), torch.empty_like(w_out)

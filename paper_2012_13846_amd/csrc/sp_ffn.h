@@ -21,14 +21,14 @@ bool in_pieces(std::initializer_list<const void*> arrays, int c, int m) {
 template <typename T>
 int ffn_fwd(const Ffn& f, hipStream_t s) {
     constexpr int E = sizeof(T);
-    const bool pieces = in_pieces<T>({f.x, f.w_in, f.w_out, f.gu}, f.c, f.m);
-    const bool four_m = f.m % 4 == 0 && aligned16(f.gu), four_c = f.c % 4 == 0 && aligned16(f.y);
-    T* h = f.gu ? static_cast<T*>(f.gu) + 2 * f.m : reinterpret_cast<T*>(f.work);
-    const int64_t ldh = f.gu ? 3 * (int64_t)f.m : f.m;
-    float* part = reinterpret_cast<float*>(f.work + (f.gu ? 0 : up256(f.n * f.m * E)));
+    const bool pieces = in_pieces<T>({f.x, f.w_in, f.w_out, f.kept}, f.c, f.m);
+    const bool four_m = f.m % 4 == 0 && aligned16(f.kept), four_c = f.c % 4 == 0 && aligned16(f.y);
+    T* h = f.kept ? static_cast<T*>(f.kept) + 2 * f.m : reinterpret_cast<T*>(f.work);
+    const int64_t ldh = f.kept ? kKept<T> * (int64_t)f.m : f.m;
+    float* part = reinterpret_cast<float*>(f.work + (f.kept ? 0 : up256(f.n * f.m * E)));
     Mm a{};
     a.first = f.w_in, a.ld_first = (int64_t)f.c * E, a.second = f.x, a.ld_second = (int64_t)f.c * E;
-    a.m = f.m, a.n = (int)f.n, a.k = f.c, a.last = kGate, a.out = h, a.ld = ldh, a.gu = f.gu, a.act = f.act, a.four = four_m;
+    a.m = f.m, a.n = (int)f.n, a.k = f.c, a.last = kGate, a.out = h, a.ld = ldh, a.kept = f.kept, a.act = f.act, a.four = four_m;
     SP_TRY((mm<T, false, false>(a, pieces, part, s)));
     Mm b{};
     b.first = f.w_out, b.ld_first = (int64_t)f.m * E, b.second = h, b.ld_second = ldh * E;
@@ -39,16 +39,16 @@ int ffn_fwd(const Ffn& f, hipStream_t s) {
 template <typename T>
 int ffn_bwd(const Ffn& f, hipStream_t s) {
     constexpr int E = sizeof(T);
-    const bool pieces = in_pieces<T>({f.x, f.w_in, f.w_out, f.gu, f.dy}, f.c, f.m);
-    const bool four_m = f.m % 4 == 0 && aligned16(f.gu);
-    const T* h = static_cast<const T*>(f.gu) + 2 * f.m;
+    const bool pieces = in_pieces<T>({f.x, f.w_in, f.w_out, f.kept, f.dy}, f.c, f.m);
+    const bool four_m = f.m % 4 == 0 && aligned16(f.kept);
+    const T* h = static_cast<const T*>(f.kept) + 2 * f.m;
     T* dgu = reinterpret_cast<T*>(f.work);
     float* part = reinterpret_cast<float*>(f.work + up256(2 * f.n * f.m * E));
     const int64_t row_c = (int64_t)f.c * E, row_m = (int64_t)f.m * E;
     if (f.n > 0) {
         Mm a{};
         a.first = f.w_out, a.ld_first = row_m, a.second = f.dy, a.ld_second = row_c;
-        a.m = f.m, a.n = (int)f.n, a.k = f.c, a.last = kGateBack, a.gu = f.gu, a.dgu = dgu, a.act = f.act, a.four = four_m;
+        a.m = f.m, a.n = (int)f.n, a.k = f.c, a.last = kGateBack, a.kept = f.kept, a.dgu = dgu, a.act = f.act, a.four = four_m;
         SP_TRY((mm<T, true, false>(a, pieces, part, s)));
         Mm b{};
         b.first = f.w_in, b.ld_first = row_c, b.second = dgu, b.ld_second = 2 * row_m;
@@ -59,7 +59,7 @@ int ffn_bwd(const Ffn& f, hipStream_t s) {
     w.first = f.x, w.ld_first = row_c, w.second = dgu, w.ld_second = 2 * row_m;
     w.m = f.c, w.n = 2 * f.m, w.k = (int)f.n, w.last = kStore, w.out = f.dw_in, w.ld = f.c, w.four = f.c % 4 == 0 && aligned16(f.dw_in);
     SP_TRY((mm<T, true, true>(w, pieces, part, s)));
-    w.first = h, w.ld_first = 3 * row_m, w.second = f.dy, w.ld_second = row_c;
+    w.first = h, w.ld_first = kKept<T> * row_m, w.second = f.dy, w.ld_second = row_c;
     w.m = f.m, w.n = f.c, w.out = f.dw_out, w.ld = f.m, w.four = f.m % 4 == 0 && aligned16(f.dw_out);
     return mm<T, true, true>(w, pieces, part, s);
 }

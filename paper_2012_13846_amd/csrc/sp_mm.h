@@ -30,11 +30,11 @@ struct Mm {
     int steps, per_split, splits; // steps of 128 bytes; of each part
     int tiles_m, tiles_n;
     // kStore: out [n][m] in rows of ld elements.  kGate: m is the hidden width; first has rows of gates, then as many of ups; out = act(g) * u,
-    // and, if not NULL, gu [n][3 m] gets g and u.  kGateBack: results are the gradient of act(g) * u; gu is read, dgu [n][2 m] written.
+    // and, if not NULL, kept [n][kKept * m] gets g and u.  kGateBack: results are the gradient of act(g) * u; kept is read, dgu [n][2 m] written.
     Last last;
     void* out;
     int64_t ld;
-    void *gu, *dgu;
+    void *kept, *dgu;
     int act;
     bool out_f32;                 // kStore: of 8-bit operands
     bool four;                    // results' rows may be written four columns at a time
@@ -79,25 +79,75 @@ __device__ __forceinline__ float2 gate_of(float g, int act) {
     return float2{g * p, p + g * 0.39894228f * expf(-0.5f * g * g)};
 }
 
+// What the backward pass reads of a row, m values each: g | u | act(g) * u, in bf16 g and u cut off behind 16 bits and the next 8 bits of both in a
+// fourth part.  Rounded to bf16 alone they would put as much error into dx and dW_in as all that is rounded after them (0.0030 of the norm against
+// 0.0024, and 0.0017 for the one rounding that cannot be done without).
+template <typename T>
+constexpr int kKept = sizeof(T) == 2 ? 4 : 3;
+
+template <typename T>
+__device__ __forceinline__ void keep(const Mm& a, int64_t row, int col, const Four& g, const Four& u) {
+    const int left = a.m - col;
+    T* to = static_cast<T*>(a.kept) + row * kKept<T> * a.m + col;
+    if constexpr (sizeof(T) == 4) {
+        put_four(to, g, left, a.four);
+        put_four(to + a.m, u, left, a.four);
+    } else {
+        uint16_t hg[4], hu[4], lo[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t x = __float_as_uint(g.e[i]), y = __float_as_uint(u.e[i]);
+            hg[i] = (uint16_t)(x >> 16), hu[i] = (uint16_t)(y >> 16), lo[i] = (uint16_t)((x >> 8 & 255u) | (y & 0xff00u));
+        }
+        auto put = [&](T* p, const uint16_t (&v)[4]) {
+            if (a.four) *reinterpret_cast<uint2*>(p) = uint2{v[0] | (uint32_t)v[1] << 16, v[2] | (uint32_t)v[3] << 16};
+            else
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (i < left) p[i] = v[i];
+        };
+        put(to, hg), put(to + a.m, hu), put(to + 3 * (int64_t)a.m, lo);
+    }
+}
+template <typename T>
+__device__ __forceinline__ void kept_of(const Mm& a, int64_t row, int col, Four& g, Four& u) {
+    const int left = a.m - col;
+    const T* from = static_cast<const T*>(a.kept) + row * kKept<T> * a.m + col;
+    if constexpr (sizeof(T) == 4) {
+        g = get_four(from, left, a.four), u = get_four(from + a.m, left, a.four);
+    } else {
+        auto get = [&](const T* p, uint32_t (&v)[4]) {
+            if (a.four) {
+                const uint2 w = *reinterpret_cast<const uint2*>(p);
+                v[0] = w.x & 0xffffu, v[1] = w.x >> 16, v[2] = w.y & 0xffffu, v[3] = w.y >> 16;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] = i < left ? p[i] : 0u;
+            }
+        };
+        uint32_t hg[4], hu[4], lo[4];
+        get(from, hg), get(from + a.m, hu), get(from + 3 * (int64_t)a.m, lo);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            g.e[i] = __uint_as_float(hg[i] << 16 | (lo[i] & 255u) << 8);
+            u.e[i] = __uint_as_float(hu[i] << 16 | (lo[i] & 0xff00u));
+        }
+    }
+}
+
 template <typename T>
 __device__ __forceinline__ void put_gate(const Mm& a, int64_t row, int col, const Four& g, const Four& u) {
-    const int left = a.m - col;
     Four h;
 #pragma unroll
     for (int i = 0; i < 4; ++i) h.e[i] = gate_of(g.e[i], a.act).x * u.e[i];
-    put_four(static_cast<T*>(a.out) + row * a.ld + col, h, left, a.four);
-    if (a.gu) {
-        T* gu = static_cast<T*>(a.gu) + row * 3 * a.m + col;
-        put_four(gu, g, left, a.four);
-        put_four(gu + a.m, u, left, a.four);
-    }
+    put_four(static_cast<T*>(a.out) + row * a.ld + col, h, a.m - col, a.four);
+    if (a.kept) keep<T>(a, row, col, g, u);
 }
 template <typename T>
 __device__ __forceinline__ void put_gate_back(const Mm& a, int64_t row, int col, const Four& dh) {
     const int left = a.m - col;
-    const T* gu = static_cast<const T*>(a.gu) + row * 3 * a.m + col;
-    const Four g = get_four(gu, left, a.four), u = get_four(gu + a.m, left, a.four);
-    Four dg, du;
+    Four g, u, dg, du;
+    kept_of<T>(a, row, col, g, u);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const float2 p = gate_of(g.e[i], a.act);
@@ -313,9 +363,9 @@ constexpr int depth_of() {
     return sizeof(T) == 1 && Sh::ST == 4 ? 3 : Sh::ST;
 }
 
-// EXACT (8-bit operands): codes become bf16, which holds them and their scales exactly, for the bf16 products.  The 8-bit products themselves drop
-// what lies some 2^-16 below the largest of a sum (measured: 1.5e-5 of the result whatever its length, 1e-8 in bf16): less than a bf16 result's
-// rounding, but not an fp32 one's.
+// EXACT (8-bit operands): codes become bf16, which holds them and their scales exactly, for the bf16 products.  The 8-bit products themselves take
+// eight neighbouring elements at a time and cut their products off at 2^-13 of the largest's power of two (found by cancelling that one); of
+// random rows 1.5e-5 of the result, whatever their length, against 1e-8: far below a bf16 result's rounding (1.7e-3), but not an fp32 one's.
 template <typename T, typename Sh, bool TA, bool TB, bool VEC, bool EXACT>
 __global__ __launch_bounds__(Sh::kThreads) void mm_kernel(Mm a) {
     using K = Kind<T>;
@@ -562,7 +612,7 @@ struct Ffn {
     int64_t n;
     int c, m, act;
     const void *x, *w_in, *w_out, *dy;
-    void *gu, *y, *dx, *dw_in, *dw_out;
+    void *kept, *y, *dx, *dw_in, *dw_out;
     char* work;
 };
 template <typename T>

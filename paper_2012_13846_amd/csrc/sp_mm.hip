@@ -66,9 +66,8 @@ int check(const sp_ffn* f) {
     if (f->dt != SP_F32 && f->dt != SP_BF16) return fail(SP_ERR_INVALID_ARG, "bad dtype");
     if (f->act != SP_GATE_SILU && f->act != SP_GATE_GELU) return fail(SP_ERR_INVALID_ARG, "bad gate");
     if (f->n < 0 || f->c < 1 || f->m < 1) return fail(SP_ERR_INVALID_ARG, "bad row or channel count");
-    const int64_t size = f->dt == SP_F32 ? 4 : 2;
-    if (f->n > kMostRows || f->c * size > kMostRow || 3 * (int64_t)f->m * size > kMostRow)
-        return fail(SP_ERR_UNSUPPORTED, "more than 2^30 rows, or rows of more than 4 MB");
+    if (f->n > kMostRows || f->c > 1 << 18 || f->m > 1 << 18)
+        return fail(SP_ERR_UNSUPPORTED, "more than 2^30 rows, or a width beyond 2^18");
     return SP_OK;
 }
 

@@ -161,7 +161,11 @@ int rope(const sp_rope* r, bool back, const void* d_x, int64_t ldx, void* d_y, i
     for (int k = 0; k < r->axes; ++k) {
         const int half = r->part[k] / 2;
         a.first[k] = a.pairs;
-        for (int i = 0; i < half; ++i) a.freq[a.pairs++] = r->scale * std::pow(r->base, -(double)i / half) / 6.283185307179586476925;
+        // base^(-i / half) from powers for each bit of i: seven calls of pow instead of one a pair, at most seven roundings more
+        double bit[8], *f = a.freq + a.pairs;
+        for (int b = 0; b < 8 && (1 << b) < half; ++b) bit[b] = std::pow(r->base, -(double)(1 << b) / half);
+        for (int i = 0; i < half; ++i) f[i] = i ? f[i & (i - 1)] * bit[__builtin_ctz(i)] : r->scale / 6.283185307179586476925;
+        a.pairs += half;
         a.end[k] = a.pairs;
     }
     // Rows of a workgroup: about eight 16-byte pieces a thread, as far as the table has room, but no fewer than two workgroups a CU.
