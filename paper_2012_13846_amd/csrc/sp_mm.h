@@ -2,9 +2,10 @@
 //
 // out[n][m] = sum over k of first(m, k) * second(n, k).  An operand is "direct" if its contraction runs along its rows in memory ([m][k]), and
 // "turned" if it runs across them ([k][m]).  A workgroup makes BM x BN results (first x second): in steps of 128 bytes of a direct operand's rows
-// it takes both operands' tiles from memory to LDS past the registers, ST tiles deep, and multiplies 32 x 32 blocks; turned bf16 tiles are read
-// by the transposing LDS read, so no operand is ever copied transposed.  The first operand are the results' columns: a lane's accumulators are
-// then four neighbouring columns of one row at a time.  Pieces of LDS rows are swizzled (sp_attn_tile.h) so that reads are free of bank conflicts.
+// it takes both operands' tiles from memory to LDS past the registers, ST tiles deep, and multiplies 16 x 16 blocks; turned bf16 tiles are read
+// by the transposing LDS read, so no operand is ever copied transposed.  The first operand are the results' columns, and two blocks share 32 of
+// them in turns of four (column 8 h + 4 (block & 1) + e is row 4 h + e of a block), so that a lane's accumulators of both are eight neighbouring
+// columns of one row: 16 bytes a store in bf16.  Pieces of LDS rows are swizzled so that reads are free of bank conflicts.
 // Few results are split along the contraction; the parts' sums are added in order by a second kernel, which takes the same last step.
 // Operands that are no whole, aligned 16-byte pieces go through registers by unaligned loads, with zeros behind their ends.
 #pragma once
@@ -37,36 +38,50 @@ struct Mm {
     void *kept, *dgu;
     int act;
     bool out_f32;                 // kStore: of 8-bit operands
-    bool four;                    // results' rows may be written four columns at a time
     float* part;                  // kPartial: [splits][n][m]
     const uint8_t *first_scales, *second_scales;
     int scales;                   // bytes a row of them
 };
 
 // ---- the last step ---------------------------------------------------------------------------------------------
-struct Four {
-    float e[4];
-};
+// Eight neighbouring columns, of which `left` (1 or more) exist.
 template <typename T>
-__device__ __forceinline__ void put_four(T* p, const Four& v, int left, bool four) {
-    struct alignas(4 * sizeof(T)) Quad { T e[4]; } q;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) q.e[i] = to_elem<T>(v.e[i]);
-    if (four) *reinterpret_cast<Quad*>(p) = q;
+struct EightOf {
+    T e[8];
+};
+using Eight = EightOf<float>;
+template <typename T>
+__device__ __forceinline__ void put_eight(T* p, const EightOf<T>& v, int left) {
+    if (left >= 8) __builtin_memcpy(p, &v, sizeof v);
     else
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i < left) p[i] = q.e[i];
+        for (int i = 0; i < 8; ++i)
+            if (i < left) p[i] = v.e[i];
 }
 template <typename T>
-__device__ __forceinline__ Four get_four(const T* p, int left, bool four) {
-    struct alignas(4 * sizeof(T)) Quad { T e[4]; } q{};
-    if (four) q = *reinterpret_cast<const Quad*>(p);
+__device__ __forceinline__ void put_rounded(T* p, const Eight& v, int left) {
+    EightOf<T> q;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) q.e[i] = to_elem<T>(v.e[i]);
+    put_eight(p, q, left);
+}
+template <typename T>
+__device__ __forceinline__ EightOf<T> get_piece(const T* p, int left) {
+    EightOf<T> q{};
+    if (left >= 8) __builtin_memcpy(&q, p, sizeof q);
     else
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 8; ++i)
             if (i < left) q.e[i] = p[i];
-    return Four{{elem(q.e[0]), elem(q.e[1]), elem(q.e[2]), elem(q.e[3])}};
+    return q;
+}
+template <typename T>
+__device__ __forceinline__ Eight get_eight(const T* p, int left) {
+    const EightOf<T> q = get_piece(p, left);
+    Eight v;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v.e[i] = elem(q.e[i]);
+    return v;
 }
 
 // act(g) and its derivative
@@ -86,86 +101,69 @@ template <typename T>
 constexpr int kKept = sizeof(T) == 2 ? 4 : 3;
 
 template <typename T>
-__device__ __forceinline__ void keep(const Mm& a, int64_t row, int col, const Four& g, const Four& u) {
+__device__ __forceinline__ void keep(const Mm& a, int64_t row, int col, const Eight& g, const Eight& u) {
     const int left = a.m - col;
     T* to = static_cast<T*>(a.kept) + row * kKept<T> * a.m + col;
     if constexpr (sizeof(T) == 4) {
-        put_four(to, g, left, a.four);
-        put_four(to + a.m, u, left, a.four);
+        put_eight(to, g, left);
+        put_eight(to + a.m, u, left);
     } else {
-        uint16_t hg[4], hu[4], lo[4];
+        EightOf<T> hg, hu, lo;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < 8; ++i) {
             const uint32_t x = __float_as_uint(g.e[i]), y = __float_as_uint(u.e[i]);
-            hg[i] = (uint16_t)(x >> 16), hu[i] = (uint16_t)(y >> 16), lo[i] = (uint16_t)((x >> 8 & 255u) | (y & 0xff00u));
+            hg.e[i] = (uint16_t)(x >> 16), hu.e[i] = (uint16_t)(y >> 16), lo.e[i] = (uint16_t)((x >> 8 & 255u) | (y & 0xff00u));
         }
-        auto put = [&](T* p, const uint16_t (&v)[4]) {
-            if (a.four) *reinterpret_cast<uint2*>(p) = uint2{v[0] | (uint32_t)v[1] << 16, v[2] | (uint32_t)v[3] << 16};
-            else
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (i < left) p[i] = v[i];
-        };
-        put(to, hg), put(to + a.m, hu), put(to + 3 * (int64_t)a.m, lo);
+        put_eight(to, hg, left), put_eight(to + a.m, hu, left), put_eight(to + 3 * (int64_t)a.m, lo, left);
     }
 }
 template <typename T>
-__device__ __forceinline__ void kept_of(const Mm& a, int64_t row, int col, Four& g, Four& u) {
+__device__ __forceinline__ void kept_of(const Mm& a, int64_t row, int col, Eight& g, Eight& u) {
     const int left = a.m - col;
     const T* from = static_cast<const T*>(a.kept) + row * kKept<T> * a.m + col;
     if constexpr (sizeof(T) == 4) {
-        g = get_four(from, left, a.four), u = get_four(from + a.m, left, a.four);
+        g = get_eight(from, left), u = get_eight(from + a.m, left);
     } else {
-        auto get = [&](const T* p, uint32_t (&v)[4]) {
-            if (a.four) {
-                const uint2 w = *reinterpret_cast<const uint2*>(p);
-                v[0] = w.x & 0xffffu, v[1] = w.x >> 16, v[2] = w.y & 0xffffu, v[3] = w.y >> 16;
-            } else {
+        const EightOf<T> hg = get_piece(from, left), hu = get_piece(from + a.m, left), lo = get_piece(from + 3 * (int64_t)a.m, left);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) v[i] = i < left ? p[i] : 0u;
-            }
-        };
-        uint32_t hg[4], hu[4], lo[4];
-        get(from, hg), get(from + a.m, hu), get(from + 3 * (int64_t)a.m, lo);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            g.e[i] = __uint_as_float(hg[i] << 16 | (lo[i] & 255u) << 8);
-            u.e[i] = __uint_as_float(hu[i] << 16 | (lo[i] & 0xff00u));
+        for (int i = 0; i < 8; ++i) {
+            g.e[i] = __uint_as_float((uint32_t)hg.e[i] << 16 | (lo.e[i] & 255u) << 8);
+            u.e[i] = __uint_as_float((uint32_t)hu.e[i] << 16 | (lo.e[i] & 0xff00u));
         }
     }
 }
 
 template <typename T>
-__device__ __forceinline__ void put_gate(const Mm& a, int64_t row, int col, const Four& g, const Four& u) {
-    Four h;
+__device__ __forceinline__ void put_gate(const Mm& a, int64_t row, int col, const Eight& g, const Eight& u) {
+    Eight h;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) h.e[i] = gate_of(g.e[i], a.act).x * u.e[i];
-    put_four(static_cast<T*>(a.out) + row * a.ld + col, h, a.m - col, a.four);
+    for (int i = 0; i < 8; ++i) h.e[i] = gate_of(g.e[i], a.act).x * u.e[i];
+    put_rounded(static_cast<T*>(a.out) + row * a.ld + col, h, a.m - col);
     if (a.kept) keep<T>(a, row, col, g, u);
 }
 template <typename T>
-__device__ __forceinline__ void put_gate_back(const Mm& a, int64_t row, int col, const Four& dh) {
+__device__ __forceinline__ void put_gate_back(const Mm& a, int64_t row, int col, const Eight& dh) {
     const int left = a.m - col;
-    Four g, u, dg, du;
+    Eight g, u, dg, du;
     kept_of<T>(a, row, col, g, u);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 8; ++i) {
         const float2 p = gate_of(g.e[i], a.act);
         dg.e[i] = dh.e[i] * u.e[i] * p.y;
         du.e[i] = dh.e[i] * p.x;
     }
     T* dgu = static_cast<T*>(a.dgu) + row * 2 * a.m + col;
-    put_four(dgu, dg, left, a.four);
-    put_four(dgu + a.m, du, left, a.four);
+    put_rounded(dgu, dg, left);
+    put_rounded(dgu + a.m, du, left);
 }
 template <typename T>
-__device__ __forceinline__ void put_out(const Mm& a, int64_t row, int col, const Four& v) {
+__device__ __forceinline__ void put_out(const Mm& a, int64_t row, int col, const Eight& v) {
     const int left = a.m - col;
     if constexpr (sizeof(T) == 1) {
-        if (a.out_f32) put_four(static_cast<float*>(a.out) + row * a.ld + col, v, left, a.four);
-        else put_four(static_cast<bf16_t*>(a.out) + row * a.ld + col, v, left, a.four);
+        if (a.out_f32) put_eight(static_cast<float*>(a.out) + row * a.ld + col, v, left);
+        else put_rounded(static_cast<bf16_t*>(a.out) + row * a.ld + col, v, left);
     } else {
-        put_four(static_cast<T*>(a.out) + row * a.ld + col, v, left, a.four);
+        put_rounded(static_cast<T*>(a.out) + row * a.ld + col, v, left);
     }
 }
 
@@ -189,13 +187,14 @@ constexpr int kStepBytes = 128;
 
 template <typename T>
 struct Kind {
-    static constexpr int kPer = 16 / (int)sizeof(T);           // elements a piece
+    static constexpr int kPer = 16 / (int)sizeof(T);            // elements a piece
     static constexpr int kElems = kStepBytes / (int)sizeof(T);  // elements of the contraction a step
-    static constexpr int kSub = sizeof(T) == 1 ? 2 : 4;        // products of a block a step
+    static constexpr int kSub = sizeof(T) == 1 ? 1 : 2;         // fragments of a block a step
     using Frag = std::conditional_t<sizeof(T) == 1, i32x8, std::conditional_t<sizeof(T) == 2, bf16x8, f32x4>>;
 };
 
-// One operand's tile: ROWS results of kElems elements each.
+// One operand's tile: ROWS results of kElems elements each.  Lane l has row l % 16 of a block's fragment; of the contraction, 16 bytes a fragment
+// (8 bits: 32, the whole step), those of group l / 16.
 template <typename T, int ROWS, bool TURNED, int THREADS>
 struct Side {
     using K = Kind<T>;
@@ -206,52 +205,61 @@ struct Side {
     static_assert(kBytes / 16 % THREADS == 0, "every thread loads equally many pieces");
     static __device__ __forceinline__ int at(int j) { return j * THREADS + (int)threadIdx.x; }
     static __device__ __forceinline__ int row(int j) { return at(j) / kC; }  // of LDS: a result, or an element of the contraction if turned
-    static __device__ __forceinline__ int piece(int j) { return (at(j) % kC) ^ swizzle<kC>(row(j)); }
+    static __device__ __forceinline__ int piece(int j) { return (at(j) % kC) ^ swizzled(row(j)); }
+    // 64 banks are 16 pieces.  Direct: 16 lanes read the same piece of rows 8 q + e (q, e < 4), of which neighbours lie 32 banks apart.  Turned bf16:
+    // 16 lanes read half of 4 neighbouring pieces of 4 neighbouring rows; turned fp32: 64 lanes a word of every other of 8 pieces of rows 4 h.
+    static __device__ __forceinline__ int swizzled(int r) {
+        if constexpr (!TURNED) return (r >> 1 & 1) | (r >> 3 & 3) << 1;
+        else if constexpr (sizeof(T) == 2) return kC >= 16 ? (r & 3) << 2 : kC == 8 ? (r >> 1 & 1) << 2 : 0;
+        else return (r >> 2 & 1) | (kC >= 16 ? (r >> 3 & 1) << 3 : 0);
+    }
 
-    // A lane's place in fragments: of step 0 and block 0
-    int place[TURNED && sizeof(T) == 2 ? 2 : 1];
-    __device__ __forceinline__ void aim() {
-        const int l = threadIdx.x & 63, h = l >> 5;
+    // A lane's place in the fragments of step 0 of a wavefront's 32 `at` ..
+    int place;
+    __device__ __forceinline__ void aim(int from) {
+        const int l = threadIdx.x & 63, h = l >> 4, q = l >> 2 & 3, e = l & 3;
         if constexpr (!TURNED) {
-            place[0] = (l & 31) * kRowBytes + ((h ^ swizzle<kC>(l & 31)) << 4);
+            const int r = 32 * from + 8 * q + e;
+            place = r * kRowBytes + ((h ^ swizzled(r)) << 4);
         } else if constexpr (sizeof(T) == 2) {
-            // 4 elements of the contraction by a transposing read: the lane's half has elements 8 h .. 8 h + 7 of each 16, as in a direct tile
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const int r = 8 * h + 4 * j + ((l & 15) >> 2), p = ((l & 16) >> 3) + ((l & 3) >> 1);
-                place[j] = r * kRowBytes + ((p ^ swizzle<kC>(r)) << 4) + ((l & 1) << 3);
-            }
+            // a transposing read: lanes 4 q + e of a group address columns 4 e .. of a block in row q, and get column 4 q + e of all four rows
+            const int r = 8 * h + q;
+            place = r * kRowBytes + (((4 * from + e) ^ swizzled(r)) << 4);
         } else {
-            place[0] = 4 * h * kRowBytes + ((((l & 31) >> 2) ^ swizzle<kC>(4 * h)) << 4) + ((l & 3) << 2);
+            place = 4 * h * kRowBytes + (((8 * from + 2 * q) ^ swizzled(4 * h)) << 4) + (e << 2);
         }
     }
-    // results 32 blk .., step s
-    __device__ __forceinline__ typename K::Frag frag(const char* tile, int blk, int s) const {
+    // Bytes from a direct tile's block 0 to block i; `half`: rows from gates to ups, which blocks MT / 2 .. are (0: no gate)
+    template <int MT>
+    static __device__ __forceinline__ constexpr int block(int i, int half) {
+        const int b = half && i >= MT / 2 ? i - MT / 2 : i;
+        return ((half && i >= MT / 2 ? half : 0) + 32 * (b >> 1) + 4 * (b & 1)) * kRowBytes;
+    }
+    // block i of the wavefront (a direct tile: `off` bytes behind its first), fragment s
+    __device__ __forceinline__ typename K::Frag frag(const char* tile, int i, int off, int s) const {
         if constexpr (sizeof(T) == 1) {
-            const uint4 lo = *reinterpret_cast<const uint4*>(tile + (place[0] ^ (4 * s << 4)) + blk * 32 * kRowBytes);
-            const uint4 hi = *reinterpret_cast<const uint4*>(tile + (place[0] ^ ((4 * s + 2) << 4)) + blk * 32 * kRowBytes);
+            const uint4 lo = *reinterpret_cast<const uint4*>(tile + place + off);
+            const uint4 hi = *reinterpret_cast<const uint4*>(tile + (place ^ 64) + off);
             return i32x8{(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
         } else if constexpr (!TURNED) {
-            return __builtin_bit_cast(typename K::Frag, *reinterpret_cast<const uint4*>(tile + (place[0] ^ (2 * s << 4)) + blk * 32 * kRowBytes));
+            return __builtin_bit_cast(typename K::Frag, *reinterpret_cast<const uint4*>(tile + (place ^ (s << 6)) + off));
         } else if constexpr (sizeof(T) == 2) {
-            const char* from = tile + 16 * s * kRowBytes;
-            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((SP_LDS s16x4*)(from + (place[0] ^ (blk << 6))));
-            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((SP_LDS s16x4*)(from + (place[1] ^ (blk << 6))));
+            const char* from = tile + 32 * s * kRowBytes + (place ^ ((i >> 1) << 6)) + ((i & 1) << 3);
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((SP_LDS s16x4*)from);
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((SP_LDS s16x4*)(from + 4 * kRowBytes));
             return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
         } else {
+            const char* from = tile + 16 * s * kRowBytes + (place ^ ((8 * (i >> 1) + (i & 1)) << 4));
             f32x4 v;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int r = 8 * s + i, x = (blk << 3) ^ swizzle<kC>(r);  // without the half's part of the swizzle, which `place` has
-                v[i] = *reinterpret_cast<const float*>(tile + r * kRowBytes + (place[0] ^ (x << 4)));
-            }
+            for (int e = 0; e < 4; ++e) v[e] = *reinterpret_cast<const float*>(from + e * kRowBytes);
             return v;
         }
     }
 };
 
-// The tile of an operand in memory: results from `first` on (of `count`), contraction from `k0` on (of `k`).  Rows of a direct gate tile: the first
-// half of each wavefront's are gates, the second half ups, `ups` rows behind.
+// The tile of an operand in memory: results from `first` on (of `count`), contraction from `k0` on (of `k`).  The second half of a direct gate
+// tile are ups, as many rows as there are gates behind them.
 struct Place {
     const char* p;
     int64_t ld;
@@ -271,7 +279,7 @@ struct Direct {
                 const int col = S::piece(j) * S::K::kPer;
                 off[j] = o.first + col < o.count ? (uint32_t)(r * o.ld + S::piece(j) * 16) : kOutside;
             } else {
-                const int half = THREADS / 8, q = gate ? r % half + (j >> 1) * half : r;
+                const int q = gate && j >= S::kLoads / 2 ? r - ROWS / 2 : r;
                 off[j] = o.first + q < o.count ? (uint32_t)(q * o.ld + S::piece(j) * 16) : kOutside;
             }
         }
@@ -292,7 +300,7 @@ struct Direct {
 #pragma unroll
             for (int j = 0; j < S::kLoads; ++j) {
                 const uint32_t from = left == kStepBytes || S::piece(j) * 16 < left ? off[j] : kOutside;
-                memory_to_lds(j & 1 ? up : mem, from, to + j * THREADS * 16);
+                memory_to_lds(j >= S::kLoads / 2 ? up : mem, from, to + j * THREADS * 16);
             }
         }
     }
@@ -314,8 +322,8 @@ struct Through {
                 from = o.p + (k0 + r) * o.ld + (int64_t)(o.first + e) * sizeof(T);
                 left = k0 + r < o.k ? o.count - o.first - e : 0;
             } else {
-                const int half = THREADS / 8, q = gate ? r % half + (j >> 1) * half : r;
-                from = o.p + (int64_t)(o.first + q) * o.ld + (k0 + e) * sizeof(T) + (gate && (j & 1) ? ups : 0);
+                const int q = gate && j >= S::kLoads / 2 ? r - ROWS / 2 : r;
+                from = o.p + (int64_t)(o.first + q) * o.ld + (k0 + e) * sizeof(T) + (gate && j >= S::kLoads / 2 ? ups : 0);
                 left = o.first + q < o.count ? o.k - k0 - e : 0;
             }
             Piece<T, S::K::kPer> v{};
@@ -352,7 +360,7 @@ template <int BM_, int BN_, int WM_, int WN_, int ST_>
 struct Shape2 {
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, ST = ST_, kThreads = WM_ * WN_ * 64;
 };
-using Large = Shape2<256, 256, 2, 4, 2>;
+using Large = Shape2<256, 256, 4, 4, 2>;
 using Middle = Shape2<128, 128, 2, 2, 2>;
 using Narrow = Shape2<64, 128, 1, 4, 3>;
 using Few = Shape2<128, 32, 4, 1, 4>;
@@ -366,10 +374,13 @@ constexpr int depth_of() {
 // EXACT (8-bit operands): codes become bf16, which holds them and their scales exactly, for the bf16 products.  The 8-bit products themselves take
 // eight neighbouring elements at a time and cut their products off at 2^-13 of the largest's power of two (found by cancelling that one); of
 // random rows 1.5e-5 of the result, whatever their length, against 1e-8: far below a bf16 result's rounding (1.7e-3), but not an fp32 one's.
-template <typename T, typename Sh, bool TA, bool TB, bool VEC, bool EXACT>
+template <typename T, typename Sh, bool TA, bool TB, bool VEC, bool EXACT, Last LAST>
 __global__ __launch_bounds__(Sh::kThreads) void mm_kernel(Mm a) {
     using K = Kind<T>;
-    constexpr int kThreads = Sh::kThreads, MT = Sh::BM / Sh::WM / 32, NT = Sh::BN / Sh::WN / 32;
+    constexpr int kThreads = Sh::kThreads, MT = Sh::BM / Sh::WM / 16, NT = Sh::BN / Sh::WN / 16;
+    static_assert(MT % 2 == 0 && NT % 2 == 0, "blocks come in pairs");
+    constexpr bool gate = LAST == kGate;
+    static_assert(!gate || (MT % 4 == 0 && !TA), "a wavefront has as many pairs of gates as of ups");
     constexpr int kScaleLoads = sizeof(T) == 1 ? (Sh::BM + Sh::BN + kThreads - 1) / kThreads : 0;
     constexpr int kScaleBytes = kScaleLoads * kThreads * 4;
     constexpr int kStage = (Sh::BM + Sh::BN) * kStepBytes + kScaleBytes;
@@ -377,59 +388,70 @@ __global__ __launch_bounds__(Sh::kThreads) void mm_kernel(Mm a) {
     using A = Side<T, Sh::BM, TA, kThreads>;
     using B = Side<T, Sh::BN, TB, kThreads>;
     __shared__ char room[ST * kStage] __attribute__((aligned(16)));  // [ST][tile of the first operand, of the second, their scales]
-    const bool gate = a.last == kGate;
     // neighbouring workgroups of an XCD: up to eight tiles of rows, then the next tile of columns, so that its L2 serves both operands
     const uint32_t tiles = (uint32_t)a.tiles_m * a.tiles_n, item = item_of_block(blockIdx.x, tiles * a.splits);
     const uint32_t split = item / tiles, t = item - split * tiles;
     const uint32_t band = 8u * a.tiles_m, b = t / band, in = t - b * band, high = min(8u, a.tiles_n - 8u * b);
     const int tm = (int)(in / high), tn = (int)(8u * b + in % high);
     const int begin = (int)split * a.per_split, count = min(a.steps - begin, a.per_split);
-    const int cols = gate ? Sh::BM / 2 : Sh::BM;  // results' columns of a tile
+    constexpr int cols = gate ? Sh::BM / 2 : Sh::BM, half = gate ? Sh::BM / 2 : 0;  // results' columns of a tile; rows from gates to ups
+    constexpr int MP = gate ? MT / 4 : MT / 2, NP = NT / 2;                          // pairs of blocks of a wavefront
     const Place pa{static_cast<const char*>(a.first), a.ld_first, tm * cols, a.m, a.k};
     const Place pb{static_cast<const char*>(a.second), a.ld_second, tn * Sh::BN, a.n, a.k};
     const int64_t ups = (int64_t)a.m * a.ld_first;
     const int wave = threadIdx.x >> 6, wm = wave / Sh::WN, wn = wave % Sh::WN, l = threadIdx.x & 63;
 
-    f32x16 acc[MT][NT] = {};
+    f32x4 acc[MT][NT] = {};
     A fa;
     B fb;
-    fa.aim(), fb.aim();
+    fa.aim(wm * MP), fb.aim(wn * NP);
     auto multiply = [&](const char* stage, int step) {
         const char *ta = stage, *tb = stage + A::kBytes;
         int sa[MT], sb[NT];
         if constexpr (sizeof(T) == 1) {
             // this step's scales: one byte of the four steps that a row's word has
             const int shift = 8 * (step & 3);
-            const uint32_t* words = reinterpret_cast<const uint32_t*>(tb + B::kBytes);
+            const uint32_t* words = reinterpret_cast<const uint32_t*>(tb + B::kBytes) + 8 * (l >> 2 & 3) + (l & 3);
 #pragma unroll
-            for (int i = 0; i < MT; ++i) sa[i] = (int)(words[(wm * MT + i) * 32 + (l & 31)] >> shift);
+            for (int i = 0; i < MT; ++i) sa[i] = (int)(words[32 * (wm * MP + (i >> 1)) + 4 * (i & 1)] >> shift);
 #pragma unroll
-            for (int i = 0; i < NT; ++i) sb[i] = (int)(words[Sh::BM + (wn * NT + i) * 32 + (l & 31)] >> shift);
+            for (int i = 0; i < NT; ++i) sb[i] = (int)(words[Sh::BM + 32 * (wn * NP + (i >> 1)) + 4 * (i & 1)] >> shift);
         }
 #pragma unroll
         for (int s = 0; s < K::kSub; ++s) {
             typename K::Frag x[MT], y[NT];
 #pragma unroll
-            for (int i = 0; i < MT; ++i) x[i] = fa.frag(ta, wm * MT + i, s);
+            for (int i = 0; i < MT; ++i) x[i] = fa.frag(ta, i, A::template block<MT>(i, half), s);
 #pragma unroll
-            for (int i = 0; i < NT; ++i) y[i] = fb.frag(tb, wn * NT + i, s);
+            for (int i = 0; i < NT; ++i) y[i] = fb.frag(tb, i, B::template block<NT>(i, 0), s);
+            if constexpr (EXACT) {
 #pragma unroll
-            for (int i = 0; i < MT; ++i)
+                for (int e = 0; e < 4; ++e) {
+                    bf16x8 u[MT], v[NT];
 #pragma unroll
-                for (int j = 0; j < NT; ++j) {
-                    if constexpr (EXACT) {
+                    for (int i = 0; i < MT; ++i) u[i] = q8_values(x[i], e, sa[i]);
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q8_values(x[i], e, sa[i]), q8_values(y[j], e, sb[j]), acc[i][j], 0, 0, 0);
-                    } else if constexpr (sizeof(T) == 1) {
-                        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x[i], y[j], acc[i][j], 0, 0, 0, sa[i], 0, sb[j]);
-                    } else if constexpr (sizeof(T) == 2) {
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[i], y[j], acc[i][j], 0, 0, 0);
-                    } else {
+                    for (int j = 0; j < NT; ++j) v[j] = q8_values(y[j], e, sb[j]);
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[i][e], y[j][e], acc[i][j], 0, 0, 0);
-                    }
+                    for (int i = 0; i < MT; ++i)
+#pragma unroll
+                        for (int j = 0; j < NT; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(u[i], v[j], acc[i][j], 0, 0, 0);
                 }
+            } else {
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int j = 0; j < NT; ++j) {
+                        if constexpr (sizeof(T) == 1) {
+                            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x[i], y[j], acc[i][j], 0, 0, 0, sa[i], 0, sb[j]);
+                        } else if constexpr (sizeof(T) == 2) {
+                            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[i], y[j], acc[i][j], 0, 0, 0);
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[i][e], y[j][e], acc[i][j], 0, 0, 0);
+                        }
+                    }
+            }
         }
     };
 
@@ -486,33 +508,23 @@ __global__ __launch_bounds__(Sh::kThreads) void mm_kernel(Mm a) {
         }
     }
 
-    const int h = l >> 5;
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
-        const int64_t row = (int64_t)pb.first + (wn * NT + j) * 32 + (l & 31);
+        const int64_t row = (int64_t)pb.first + 32 * (wn * NP + (j >> 1)) + 8 * (l >> 2 & 3) + 4 * (j & 1) + (l & 3);
         if (row >= a.n) continue;
-        auto four = [&](int i, int g) { return Four{{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]}}; };
-        if (gate) {
-            if constexpr (sizeof(T) > 1 && MT > 1 && !TA && !TB)
+        auto eight = [&](int i) {
+            const f32x4 &p = acc[i][j], &q = acc[i + 1][j];
+            return Eight{{p[0], p[1], p[2], p[3], q[0], q[1], q[2], q[3]}};
+        };
 #pragma unroll
-                for (int i = 0; i < MT / 2; ++i)
-#pragma unroll
-                    for (int g = 0; g < 4; ++g) {
-                        const int col = pa.first + (wm * MT / 2 + i) * 32 + 8 * g + 4 * h;
-                        if (col < a.m) put_gate<T>(a, row, col, four(i, g), four(i + MT / 2, g));
-                    }
-            continue;
+        for (int p = 0; p < MP; ++p) {
+            const int col = pa.first + 32 * (wm * MP + p) + 8 * (l >> 4);
+            if (col >= a.m) continue;
+            if constexpr (gate) put_gate<T>(a, row, col, eight(2 * p), eight(MT / 2 + 2 * p));
+            else if constexpr (LAST == kGateBack) put_gate_back<T>(a, row, col, eight(2 * p));
+            else if (a.last == kPartial) put_eight(a.part + ((int64_t)split * a.n + row) * a.m + col, eight(2 * p), a.m - col);
+            else put_out<T>(a, row, col, eight(2 * p));
         }
-#pragma unroll
-        for (int i = 0; i < MT; ++i)
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int col = pa.first + (wm * MT + i) * 32 + 8 * g + 4 * h;
-                if (col >= a.m) continue;
-                if (a.last == kPartial) put_four(a.part + ((int64_t)split * a.n + row) * a.m + col, four(i, g), a.m - col, a.m % 4 == 0);
-                else if (a.last == kStore) put_out<T>(a, row, col, four(i, g));
-                else if constexpr (sizeof(T) > 1 && TA && !TB) put_gate_back<T>(a, row, col, four(i, g));
-            }
     }
 }
 
@@ -520,22 +532,22 @@ __global__ __launch_bounds__(Sh::kThreads) void mm_kernel(Mm a) {
 // a.m: the results' columns (of a gate: the hidden width, parts have 2 m columns)
 template <typename T>
 __global__ __launch_bounds__(256) void mm_join_kernel(Mm a) {
-    const int each = (a.m + 3) / 4;
+    const int each = (a.m + 7) / 8;
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / each;
     if (row >= a.n) return;
-    const int col = (int)(i - row * each) * 4, wide = a.last == kGate ? 2 * a.m : a.m;
-    auto sum = [&](int at, int left) {
-        Four s{};
+    const int col = (int)(i - row * each) * 8, wide = a.last == kGate ? 2 * a.m : a.m;
+    auto sum = [&](int at) {
+        Eight s{};
         for (int p = 0; p < a.splits; ++p) {
-            const Four v = get_four(a.part + ((int64_t)p * a.n + row) * wide + at, left, a.m % 4 == 0);
+            const Eight v = get_eight(a.part + ((int64_t)p * a.n + row) * wide + at, a.m - col);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s.e[e] += v.e[e];
+            for (int e = 0; e < 8; ++e) s.e[e] += v.e[e];
         }
         return s;
     };
-    const Four s = sum(col, a.m - col);
+    const Eight s = sum(col);
     if constexpr (sizeof(T) > 1) {
-        if (a.last == kGate) return put_gate<T>(a, row, col, s, sum(a.m + col, a.m - col));
+        if (a.last == kGate) return put_gate<T>(a, row, col, s, sum(a.m + col));
         if (a.last == kGateBack) return put_gate_back<T>(a, row, col, s);
     }
     put_out<T>(a, row, col, s);
@@ -555,11 +567,11 @@ inline int64_t mm_work(int64_t rows, int64_t n, int64_t k_bytes, int size, bool 
     return p.splits > 1 || (gate && p.shape == kFew) ? (int64_t)p.splits * rows * n * 4 : 0;
 }
 
-template <typename T, typename Sh, bool TA, bool TB, bool VEC, bool EXACT>
+template <typename T, typename Sh, bool TA, bool TB, bool VEC, bool EXACT, Last LAST>
 int mm_launch(const Mm& a, hipStream_t s) {
     const int64_t blocks = (int64_t)a.tiles_m * a.tiles_n * a.splits;
     if (blocks > 0x7fffffff) return fail(SP_ERR_UNSUPPORTED, "too many tiles");
-    hipLaunchKernelGGL((mm_kernel<T, Sh, TA, TB, VEC, EXACT>), dim3((unsigned)blocks), dim3(Sh::kThreads), 0, s, a);
+    hipLaunchKernelGGL((mm_kernel<T, Sh, TA, TB, VEC, EXACT, LAST>), dim3((unsigned)blocks), dim3(Sh::kThreads), 0, s, a);
     SP_HIP(hipGetLastError());
     return SP_OK;
 }
@@ -570,7 +582,7 @@ template <typename T, bool TA, bool TB>
 int mm(Mm a, bool pieces, float* part, hipStream_t s) {
     const bool gate = a.last == kGate;
     const int64_t k_bytes = (int64_t)a.k * (int)sizeof(T);
-    const Plan p = mm_plan(gate ? (int64_t)2 * a.m : a.m, a.n, k_bytes, sizeof(T), gate, pieces);
+    const Plan p = mm_plan(gate ? (int64_t)2 * a.m : a.m, a.n, k_bytes, sizeof(T), gate, pieces && !(sizeof(T) == 1 && a.out_f32));
     a.steps = (int)((k_bytes + kStepBytes - 1) / kStepBytes);
     a.per_split = p.per_split, a.splits = p.splits, a.tiles_m = p.tiles_m, a.tiles_n = p.tiles_n;
     Mm last = a;
@@ -581,15 +593,25 @@ int mm(Mm a, bool pieces, float* part, hipStream_t s) {
     }
     auto go = [&](auto vec, auto exact) -> int {
         constexpr bool V = decltype(vec)::value, X = decltype(exact)::value;
-        switch (p.shape) {
-            case kLarge:
-                if constexpr (V) return mm_launch<T, Large, TA, TB, V, X>(a, s);
-                break;
-            case kMiddle: return mm_launch<T, Middle, TA, TB, V, X>(a, s);
-            case kNarrow: return mm_launch<T, Narrow, TA, TB, V, X>(a, s);
-            case kFew: return mm_launch<T, Few, TA, TB, V, X>(a, s);
-        }
-        return fail(SP_ERR_UNSUPPORTED, "no kernel for this product");
+        auto with = [&](auto last) -> int {
+            constexpr Last L = (Last)decltype(last)::value;
+            switch (p.shape) {
+                case kLarge:
+                    if constexpr (V && !X) return mm_launch<T, Large, TA, TB, V, X, L>(a, s);
+                    break;
+                case kMiddle: return mm_launch<T, Middle, TA, TB, V, X, L>(a, s);
+                case kNarrow: return mm_launch<T, Narrow, TA, TB, V, X, L>(a, s);
+                case kFew:
+                    if constexpr (L != kGate) return mm_launch<T, Few, TA, TB, V, X, L>(a, s);
+                    break;
+            }
+            return fail(SP_ERR_UNSUPPORTED, "no kernel for this product");
+        };
+        if constexpr (sizeof(T) > 1 && !TA && !TB)
+            if (a.last == kGate) return with(std::integral_constant<int, kGate>{});
+        if constexpr (sizeof(T) > 1 && TA && !TB)
+            if (a.last == kGateBack) return with(std::integral_constant<int, kGateBack>{});
+        return with(std::integral_constant<int, kStore>{});
     };
     if constexpr (sizeof(T) == 1) {
         SP_TRY(a.out_f32 ? go(std::true_type{}, std::true_type{}) : go(std::true_type{}, std::false_type{}));
@@ -597,7 +619,7 @@ int mm(Mm a, bool pieces, float* part, hipStream_t s) {
         SP_TRY(pieces ? go(std::true_type{}, std::false_type{}) : go(std::false_type{}, std::false_type{}));
     }
     if (join) {
-        const int64_t blocks = ((int64_t)((last.m + 3) / 4) * last.n + 255) / 256;
+        const int64_t blocks = ((int64_t)((last.m + 7) / 8) * last.n + 255) / 256;
         if (blocks > 0x7fffffff) return fail(SP_ERR_UNSUPPORTED, "too many results");
         hipLaunchKernelGGL(mm_join_kernel<T>, dim3((unsigned)blocks), dim3(256), 0, s, last);
         SP_HIP(hipGetLastError());

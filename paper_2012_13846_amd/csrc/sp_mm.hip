@@ -104,7 +104,8 @@ int sp_ffn_bwd(const sp_ffn* f, const void* d_x, const void* d_w_in, const void*
 
 int64_t sp_q8_linear_work(int64_t n, int64_t c, int64_t m) {
     if (n < 0 || n > kMostRows || c < 1 || c > kMostRow || m < 1 || m > kMostRows) return -1;
-    return up256(mm_work(m, n, q8_blocks(c) * kQ8Block, 1, false, true)) + 256;
+    const int64_t wide = q8_blocks(c) * kQ8Block;  // the results' type is not known yet
+    return up256(std::max(mm_work(m, n, wide, 1, false, true), mm_work(m, n, wide, 1, false, false))) + 256;
 }
 
 int sp_q8_linear(const uint8_t* d_q, const uint8_t* d_scales, int64_t n, int64_t c, const uint8_t* d_wq, const uint8_t* d_wscales, int64_t m,
@@ -120,7 +121,6 @@ int sp_q8_linear(const uint8_t* d_q, const uint8_t* d_scales, int64_t n, int64_t
     const int64_t wide = q8_blocks(c) * kQ8Block;
     a.first = d_wq, a.ld_first = wide, a.second = d_q, a.ld_second = wide;
     a.m = (int)m, a.n = (int)n, a.k = (int)wide, a.last = kStore, a.out = d_y, a.ld = m, a.out_f32 = dt == SP_F32;
-    a.four = m % 4 == 0 && aligned16(d_y);
     a.first_scales = d_wscales, a.second_scales = d_scales, a.scales = (int)q8_scales(c);
     return mm<q8_t, false, false>(a, true, static_cast<float*>(d_work), (hipStream_t)stream);
 }
