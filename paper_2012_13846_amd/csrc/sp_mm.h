@@ -84,14 +84,17 @@ __device__ __forceinline__ Eight get_eight(const T* p, int left) {
     return v;
 }
 
-// act(g) and its derivative
+// act(g) and its derivative.  For bf16 by the exponential and reciprocal instructions (an ulp each; the exponential's argument is off by |g| 2^-24,
+// as its result is then in relation): 2^-20 where the gate is not yet 2^-16 of g, against the 2^-8 of a rounding.
+template <typename T>
 __device__ __forceinline__ float2 gate_of(float g, int act) {
+    constexpr bool kQuick = sizeof(T) == 2;
     if (act == SP_GATE_SILU) {
-        const float p = 1.f / (1.f + expf(-g));
+        const float p = kQuick ? __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504f * g)) : 1.f / (1.f + expf(-g));
         return float2{g * p, p * (1.f + g * (1.f - p))};
     }
-    const float p = 0.5f * (1.f + erff(g * 0.70710678f));
-    return float2{g * p, p + g * 0.39894228f * expf(-0.5f * g * g)};
+    const float p = 0.5f * (1.f + erff(g * 0.70710678f)), e = kQuick ? __builtin_amdgcn_exp2f(-0.72134752f * g * g) : expf(-0.5f * g * g);
+    return float2{g * p, p + g * 0.39894228f * e};
 }
 
 // What the backward pass reads of a row, m values each: g | u | act(g) * u, in bf16 g and u cut off behind 16 bits and the next 8 bits of both in a
@@ -117,39 +120,39 @@ __device__ __forceinline__ void keep(const Mm& a, int64_t row, int col, const Ei
         put_eight(to, hg, left), put_eight(to + a.m, hu, left), put_eight(to + 3 * (int64_t)a.m, lo, left);
     }
 }
+// The same as it lies in memory
 template <typename T>
-__device__ __forceinline__ void kept_of(const Mm& a, int64_t row, int col, Eight& g, Eight& u) {
-    const int left = a.m - col;
+struct KeptOf {
+    EightOf<T> g, u, lo;  // lo: bf16 only
+};
+template <typename T>
+__device__ __forceinline__ KeptOf<T> kept_at(const Mm& a, int64_t row, int col, int left) {
     const T* from = static_cast<const T*>(a.kept) + row * kKept<T> * a.m + col;
-    if constexpr (sizeof(T) == 4) {
-        g = get_eight(from, left), u = get_eight(from + a.m, left);
-    } else {
-        const EightOf<T> hg = get_piece(from, left), hu = get_piece(from + a.m, left), lo = get_piece(from + 3 * (int64_t)a.m, left);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            g.e[i] = __uint_as_float((uint32_t)hg.e[i] << 16 | (lo.e[i] & 255u) << 8);
-            u.e[i] = __uint_as_float((uint32_t)hu.e[i] << 16 | (lo.e[i] & 0xff00u));
-        }
-    }
+    KeptOf<T> k{get_piece(from, left), get_piece(from + a.m, left), EightOf<T>{}};
+    if constexpr (sizeof(T) == 2) k.lo = get_piece(from + 3 * (int64_t)a.m, left);
+    return k;
+}
+template <typename T>
+__device__ __forceinline__ float2 gate_and_up(const KeptOf<T>& k, int i) {
+    if constexpr (sizeof(T) == 4) return float2{k.g.e[i], k.u.e[i]};
+    else return float2{__uint_as_float((uint32_t)k.g.e[i] << 16 | (k.lo.e[i] & 255u) << 8), __uint_as_float((uint32_t)k.u.e[i] << 16 | (k.lo.e[i] & 0xff00u))};
 }
 
 template <typename T>
 __device__ __forceinline__ void put_gate(const Mm& a, int64_t row, int col, const Eight& g, const Eight& u) {
     Eight h;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) h.e[i] = gate_of(g.e[i], a.act).x * u.e[i];
+    for (int i = 0; i < 8; ++i) h.e[i] = gate_of<T>(g.e[i], a.act).x * u.e[i];
     put_rounded(static_cast<T*>(a.out) + row * a.ld + col, h, a.m - col);
     if (a.kept) keep<T>(a, row, col, g, u);
 }
 template <typename T>
-__device__ __forceinline__ void put_gate_back(const Mm& a, int64_t row, int col, const Eight& dh) {
-    const int left = a.m - col;
-    Eight g, u, dg, du;
-    kept_of<T>(a, row, col, g, u);
+__device__ __forceinline__ void put_gate_back(const Mm& a, int64_t row, int col, const Eight& dh, const KeptOf<T>& kept, int left) {
+    Eight dg, du;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const float2 p = gate_of(g.e[i], a.act);
-        dg.e[i] = dh.e[i] * u.e[i] * p.y;
+        const float2 gu = gate_and_up(kept, i), p = gate_of<T>(gu.x, a.act);
+        dg.e[i] = dh.e[i] * gu.y * p.y;
         du.e[i] = dh.e[i] * p.x;
     }
     T* dgu = static_cast<T*>(a.dgu) + row * 2 * a.m + col;
@@ -360,7 +363,8 @@ template <int BM_, int BN_, int WM_, int WN_, int ST_>
 struct Shape2 {
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, ST = ST_, kThreads = WM_ * WN_ * 64;
 };
-using Large = Shape2<256, 256, 4, 4, 2>;
+using Large = Shape2<256, 256, 2, 4, 2>;
+using Large8 = Shape2<256, 256, 4, 4, 2>;  // of 8-bit operands, whose fragments are twice as long: 64 x 64 results a wavefront
 using Middle = Shape2<128, 128, 2, 2, 2>;
 using Narrow = Shape2<64, 128, 1, 4, 3>;
 using Few = Shape2<128, 32, 4, 1, 4>;
@@ -385,6 +389,7 @@ __global__ __launch_bounds__(Sh::kThreads) void mm_kernel(Mm a) {
     constexpr int kScaleBytes = kScaleLoads * kThreads * 4;
     constexpr int kStage = (Sh::BM + Sh::BN) * kStepBytes + kScaleBytes;
     constexpr int ST = VEC ? depth_of<T, Sh>() : 2;
+    constexpr bool kAhead = VEC && ST == 2 && sizeof(T) > 1;
     using A = Side<T, Sh::BM, TA, kThreads>;
     using B = Side<T, Sh::BN, TB, kThreads>;
     __shared__ char room[ST * kStage] __attribute__((aligned(16)));  // [ST][tile of the first operand, of the second, their scales]
@@ -405,13 +410,41 @@ __global__ __launch_bounds__(Sh::kThreads) void mm_kernel(Mm a) {
     A fa;
     B fb;
     fa.aim(wm * MP), fb.aim(wn * NP);
+    using Frag = typename K::Frag;
+    // of an LDS read and products in turn
+    auto alternate = [] {
+        constexpr int kReads = (MT * (TA ? 2 : 1) + NT * (TB ? 2 : 1)) * (sizeof(T) == 4 && (TA || TB) ? 2 : 1);
+#pragma unroll
+        for (int i = 0; i < kReads; ++i) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0), __builtin_amdgcn_sched_group_barrier(0x8, 2, 0);
+        __builtin_amdgcn_sched_group_barrier(0x8, MT * NT * 4, 0);
+    };
+    auto take = [&](const char* stage, int s, Frag (&x)[MT], Frag (&y)[NT]) {
+#pragma unroll
+        for (int i = 0; i < NT; ++i) y[i] = fb.frag(stage + A::kBytes, i, B::template block<NT>(i, 0), s);
+#pragma unroll
+        for (int i = 0; i < MT; ++i) x[i] = fa.frag(stage, i, A::template block<MT>(i, half), s);
+    };
+    auto product = [&](const Frag (&x)[MT], const Frag (&y)[NT], const int* sa, const int* sb) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                if constexpr (sizeof(T) == 1) {
+                    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x[i], y[j], acc[i][j], 0, 0, 0, sa[i], 0, sb[j]);
+                } else if constexpr (sizeof(T) == 2) {
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[i], y[j], acc[i][j], 0, 0, 0);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[i][e], y[j][e], acc[i][j], 0, 0, 0);
+                }
+            }
+    };
     auto multiply = [&](const char* stage, int step) {
-        const char *ta = stage, *tb = stage + A::kBytes;
         int sa[MT], sb[NT];
         if constexpr (sizeof(T) == 1) {
             // this step's scales: one byte of the four steps that a row's word has
             const int shift = 8 * (step & 3);
-            const uint32_t* words = reinterpret_cast<const uint32_t*>(tb + B::kBytes) + 8 * (l >> 2 & 3) + (l & 3);
+            const uint32_t* words = reinterpret_cast<const uint32_t*>(stage + A::kBytes + B::kBytes) + 8 * (l >> 2 & 3) + (l & 3);
 #pragma unroll
             for (int i = 0; i < MT; ++i) sa[i] = (int)(words[32 * (wm * MP + (i >> 1)) + 4 * (i & 1)] >> shift);
 #pragma unroll
@@ -419,11 +452,8 @@ __global__ __launch_bounds__(Sh::kThreads) void mm_kernel(Mm a) {
         }
 #pragma unroll
         for (int s = 0; s < K::kSub; ++s) {
-            typename K::Frag x[MT], y[NT];
-#pragma unroll
-            for (int i = 0; i < MT; ++i) x[i] = fa.frag(ta, i, A::template block<MT>(i, half), s);
-#pragma unroll
-            for (int i = 0; i < NT; ++i) y[i] = fb.frag(tb, i, B::template block<NT>(i, 0), s);
+            Frag x[MT], y[NT];
+            take(stage, s, x, y);
             if constexpr (EXACT) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
@@ -438,19 +468,7 @@ __global__ __launch_bounds__(Sh::kThreads) void mm_kernel(Mm a) {
                         for (int j = 0; j < NT; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(u[i], v[j], acc[i][j], 0, 0, 0);
                 }
             } else {
-#pragma unroll
-                for (int i = 0; i < MT; ++i)
-#pragma unroll
-                    for (int j = 0; j < NT; ++j) {
-                        if constexpr (sizeof(T) == 1) {
-                            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x[i], y[j], acc[i][j], 0, 0, 0, sa[i], 0, sb[j]);
-                        } else if constexpr (sizeof(T) == 2) {
-                            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[i], y[j], acc[i][j], 0, 0, 0);
-                        } else {
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[i][e], y[j][e], acc[i][j], 0, 0, 0);
-                        }
-                    }
+                product(x, y, sa, sb);
             }
         }
     };
@@ -478,20 +496,46 @@ __global__ __launch_bounds__(Sh::kThreads) void mm_kernel(Mm a) {
                 }
             }
         };
-#pragma unroll
-        for (int s = 0; s < ST - 1; ++s)
-            if (s < count) load(begin + s, s);
-        int stage = 0, next = ST - 1;
-#pragma unroll 1
-        for (int k = 0; k < count; ++k) {
-            // this step's tiles are there; the ones behind it may still be under way
-            if (k + ST - 1 <= count) wait_loads<(ST - 2) * kLoads>();
+        if constexpr (kAhead) {
+            // Fragments are read while the ones before them are multiplied.  One meeting a step, between its two fragments: behind it nobody reads this
+            // step's tiles any more, and the next step's are there.
+            static_assert(ST == 2 && K::kSub == 2, "two tiles, two fragments a step");
+            Frag x[2][MT], y[2][NT];
+            if (count > 0) load(begin, 0);
+            if (count > 1) load(begin + 1, 1), wait_loads<kLoads>();
             else wait_loads<0>();
             meet();
-            if (k + ST - 1 < count) load(begin + k + ST - 1, next);
-            multiply(room + stage * kStage, begin + k);
-            stage = stage + 1 == ST ? 0 : stage + 1;
-            next = next + 1 == ST ? 0 : next + 1;
+            take(room, 0, x[0], y[0]);
+            int stage = 0;
+#pragma unroll 1
+            for (int k = 0; k < count; ++k) {
+                take(room + stage * kStage, 1, x[1], y[1]);
+                product(x[0], y[0], nullptr, nullptr);
+                alternate();
+                wait_loads<0>();
+                meet();
+                if (k + 2 < count) load(begin + k + 2, stage);
+                stage ^= 1;
+                take(room + stage * kStage, 0, x[0], y[0]);  // (behind the last step: a tile that is not used)
+                product(x[1], y[1], nullptr, nullptr);
+                alternate();
+            }
+        } else {
+#pragma unroll
+            for (int s = 0; s < ST - 1; ++s)
+                if (s < count) load(begin + s, s);
+            int stage = 0, next = ST - 1;
+#pragma unroll 1
+            for (int k = 0; k < count; ++k) {
+                // this step's tiles are there; the ones behind it may still be under way
+                if (k + ST - 1 <= count) wait_loads<(ST - 2) * kLoads>();
+                else wait_loads<0>();
+                meet();
+                if (k + ST - 1 < count) load(begin + k + ST - 1, next);
+                multiply(room + stage * kStage, begin + k);
+                stage = stage + 1 == ST ? 0 : stage + 1;
+                next = next + 1 == ST ? 0 : next + 1;
+            }
         }
     } else {
         Through<T, Sh::BM, TA, kThreads> la;
@@ -508,22 +552,66 @@ __global__ __launch_bounds__(Sh::kThreads) void mm_kernel(Mm a) {
         }
     }
 
+    // The last step's items of a lane: eight columns of a row each, item t = (t / MP)'s block of rows.  In 16 bits lanes r and r + 8 of a block swap a
+    // pair's half, so that a store writes 128 bytes of 8 rows instead of 64 of 16.
+    constexpr bool kWhole = sizeof(T) <= 2 && MP % 2 == 0;
+    auto row_at = [&](int t) {
+        const int j = t / MP, r = kWhole ? 8 * (t & 1) + (l & 7) : l & 15;
+        return (int64_t)pb.first + 32 * (wn * NP + (j >> 1)) + 8 * (r >> 2) + 4 * (j & 1) + (r & 3);
+    };
+    auto col_at = [&](int t) { return pa.first + 32 * (wm * MP + (kWhole ? t % MP / 2 * 2 + (l >> 3 & 1) : t % MP)) + 8 * (l >> 4); };
+    auto values = [&](int t, int from) {  // from: the first block of these columns
+        const int j = t / MP, p = t % MP;
+        Eight v;
 #pragma unroll
-    for (int j = 0; j < NT; ++j) {
-        const int64_t row = (int64_t)pb.first + 32 * (wn * NP + (j >> 1)) + 8 * (l >> 2 & 3) + 4 * (j & 1) + (l & 3);
-        if (row >= a.n) continue;
-        auto eight = [&](int i) {
-            const f32x4 &p = acc[i][j], &q = acc[i + 1][j];
-            return Eight{{p[0], p[1], p[2], p[3], q[0], q[1], q[2], q[3]}};
+        for (int e = 0; e < 8; ++e) {
+            if constexpr (kWhole) {
+                const float lo = acc[from + 2 * (p & ~1) + (e >> 2)][j][e & 3], hi = acc[from + 2 * (p | 1) + (e >> 2)][j][e & 3];
+                const bool high = l & 8;
+                const float swapped = __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, high ? lo : hi), 0x128, 0xf, 0xf, false));
+                v.e[e] = t & 1 ? (high ? hi : swapped) : (high ? swapped : lo);
+            } else {
+                v.e[e] = acc[from + 2 * p + (e >> 2)][j][e & 3];
+            }
+        }
+        return v;
+    };
+    constexpr int kItems = NT * MP;
+    if constexpr (LAST == kGateBack) {
+        // what was kept is read some items ahead: one after the other took 320 us longer in 8192 x 8192 results
+        constexpr int kAheadBy = sizeof(T) == 2 ? 4 : 2;
+        auto items = [&](auto inside) {
+            constexpr bool kInside = decltype(inside)::value;
+            KeptOf<T> kept[kAheadBy];
+            auto fetch = [&](int t) {
+                const int col = col_at(t);
+                if (kInside || col < a.m) kept[t % kAheadBy] = kept_at<T>(a, min(row_at(t), (int64_t)a.n - 1), col, kInside ? 8 : a.m - col);
+            };
+#pragma unroll
+            for (int t = 0; t < kAheadBy; ++t) fetch(t);
+#pragma unroll
+            for (int t = 0; t < kItems; ++t) {
+                const int64_t row = row_at(t);
+                const int col = col_at(t);
+                const Eight dh = values(t, 0);
+                if (row < a.n && (kInside || col < a.m)) put_gate_back<T>(a, row, col, dh, kept[t % kAheadBy], kInside ? 8 : a.m - col);
+                if (t + kAheadBy < kItems) fetch(t + kAheadBy);
+            }
         };
+        if (pa.first + cols <= a.m) items(std::true_type{});
+        else items(std::false_type{});
+    } else {
 #pragma unroll
-        for (int p = 0; p < MP; ++p) {
-            const int col = pa.first + 32 * (wm * MP + p) + 8 * (l >> 4);
-            if (col >= a.m) continue;
-            if constexpr (gate) put_gate<T>(a, row, col, eight(2 * p), eight(MT / 2 + 2 * p));
-            else if constexpr (LAST == kGateBack) put_gate_back<T>(a, row, col, eight(2 * p));
-            else if (a.last == kPartial) put_eight(a.part + ((int64_t)split * a.n + row) * a.m + col, eight(2 * p), a.m - col);
-            else put_out<T>(a, row, col, eight(2 * p));
+        for (int t = 0; t < kItems; ++t) {
+            const int64_t row = row_at(t);
+            const int col = col_at(t);
+            const Eight v = values(t, 0);
+            Eight u;
+            if constexpr (gate) u = values(t, MT / 2);
+            if (row >= a.n || col >= a.m) continue;
+            if constexpr (gate) put_gate<T>(a, row, col, v, u);
+            else if (a.last == kPartial) put_eight(a.part + ((int64_t)split * a.n + row) * a.m + col, v, a.m - col);
+            else put_out<T>(a, row, col, v);
         }
     }
 }
@@ -548,7 +636,7 @@ __global__ __launch_bounds__(256) void mm_join_kernel(Mm a) {
     const Eight s = sum(col);
     if constexpr (sizeof(T) > 1) {
         if (a.last == kGate) return put_gate<T>(a, row, col, s, sum(a.m + col));
-        if (a.last == kGateBack) return put_gate_back<T>(a, row, col, s);
+        if (a.last == kGateBack) return put_gate_back<T>(a, row, col, s, kept_at<T>(a, row, col, a.m - col), a.m - col);
     }
     put_out<T>(a, row, col, s);
 }
@@ -597,7 +685,7 @@ int mm(Mm a, bool pieces, float* part, hipStream_t s) {
             constexpr Last L = (Last)decltype(last)::value;
             switch (p.shape) {
                 case kLarge:
-                    if constexpr (V && !X) return mm_launch<T, Large, TA, TB, V, X, L>(a, s);
+                    if constexpr (V && !X) return mm_launch<T, std::conditional_t<sizeof(T) == 1, Large8, Large>, TA, TB, V, X, L>(a, s);
                     break;
                 case kMiddle: return mm_launch<T, Middle, TA, TB, V, X, L>(a, s);
                 case kNarrow: return mm_launch<T, Narrow, TA, TB, V, X, L>(a, s);
