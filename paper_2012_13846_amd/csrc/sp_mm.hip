@@ -5,7 +5,7 @@
 
 namespace sp {
 
-Plan mm_plan(int64_t rows, int64_t n, int64_t k_bytes, int size, bool gate, bool pieces) {
+Plan mm_plan(int64_t rows, int64_t n, int64_t k_bytes, int size, bool pieces) {
     const int64_t steps = (k_bytes + kStepBytes - 1) / kStepBytes;
     struct Kind2 {
         ShapeName name;
@@ -31,7 +31,7 @@ Plan mm_plan(int64_t rows, int64_t n, int64_t k_bytes, int size, bool gate, bool
             const int64_t each = std::max<int64_t>(1, (steps + want - 1) / want), splits = std::max<int64_t>(1, (steps + each - 1) / each);
             if (splits == last || tiles * splits > 0x7fffffff) continue;
             last = splits;
-            const bool join = splits > 1 || (gate && kind.name == kFew);
+            const bool join = splits > 1;
             const double rounds = (double)((tiles * splits + 255) / 256);
             const double time = rounds * each * (rounds > 1 ? kind.step : kind.alone) + 3000 + (join ? 8000 + 8.0 * splits * rows * n / 2300 : 0);
             if (time < least) {
@@ -47,7 +47,7 @@ static int64_t ffn_work(int64_t n, int c, int m, int size, bool backward) {
     int64_t part = 0;
     for (const bool pieces : {false, true}) {  // the arrays' alignment is not known yet
         if (!backward) {
-            part = std::max({part, mm_work(2 * (int64_t)m, n, (int64_t)c * size, size, true, pieces), mm_work(c, n, (int64_t)m * size, size, false, pieces)});
+            part = std::max({part, mm_work(2 * (int64_t)m, n, (int64_t)c * size, size, true, pieces), mm_work(c, n, (int64_t)m * size, size, true, pieces)});
         } else {
             part = std::max({part, mm_work(m, n, (int64_t)c * size, size, false, pieces), mm_work(c, n, 2 * (int64_t)m * size, size, false, pieces),
                              mm_work(c, 2 * (int64_t)m, n * size, size, false, pieces), mm_work(m, c, n * size, size, false, pieces)});
@@ -105,7 +105,7 @@ int sp_ffn_bwd(const sp_ffn* f, const void* d_x, const void* d_w_in, const void*
 int64_t sp_q8_linear_work(int64_t n, int64_t c, int64_t m) {
     if (n < 0 || n > kMostRows || c < 1 || c > kMostRow || m < 1 || m > kMostRows) return -1;
     const int64_t wide = q8_blocks(c) * kQ8Block;  // the results' type is not known yet
-    return up256(std::max(mm_work(m, n, wide, 1, false, true), mm_work(m, n, wide, 1, false, false))) + 256;
+    return up256(std::max(mm_work(m, n, wide, 1, true, true), mm_work(m, n, wide, 1, true, false))) + 256;
 }
 
 int sp_q8_linear(const uint8_t* d_q, const uint8_t* d_scales, int64_t n, int64_t c, const uint8_t* d_wq, const uint8_t* d_wscales, int64_t m,
