@@ -705,11 +705,22 @@ def _block_argtypes():
     return l
 
 
+def _device() -> int:
+    return _cur_device() if _cur_device is not None else torch.cuda.current_device()
+
+
+def _need(t, device: int, dtype, shape, name: str):
+    """Contiguous, of this type and shape, on the device whose stream the call goes to.  (One call a tensor: four checks by themselves were a
+    quarter of the time that a call of a few rows takes.)"""
+    if t.get_device() != device or t.dtype != dtype or t.shape != shape or not t.is_contiguous():
+        _need_cuda(t, dtype, name), _need_shape(t, shape, name)
+        raise ValueError(f"every tensor must be on the current device (cuda:{device}), not {t.device}")
+
+
 def _here(*tensors):
-    """All on the device whose stream the call goes to."""
-    device = _cur_device() if _cur_device is not None else torch.cuda.current_device()
+    device = _device()
     for t in tensors:
-        if t is not None and t.get_device() != device:
+        if t.get_device() != device:
             raise ValueError(f"every tensor must be on the current device (cuda:{device}), not {t.device}")
 
 
@@ -718,6 +729,9 @@ def _work(nbytes: int, device) -> torch.Tensor:
     if nbytes < 0:
         raise ValueError("sizes that the library does not take")
     return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+_Parts = C.c_int32 * 4
 
 
 def _rope(name, x, pos, parts, base, split, scale, out):
@@ -731,11 +745,14 @@ def _rope(name, x, pos, parts, base, split, scale, out):
     if n > 1 and pos.stride(0) < len(parts) or (len(parts) > 1 and pos.stride(1) != 1):
         raise ValueError("the positions of a row must lie one after another, and rows must not overlap")
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    _need_shape(out, x.shape, "out")
-    to, ldo = _head_rows(out, x.dtype, "out")
-    _here(x, pos, out)
-    a = _Rope(n, heads, dim, len(parts), (C.c_int32 * 4)(*parts), int(bool(split)), base, scale, _dt(x), pos.data_ptr(),
+        out = torch.empty_like(x, memory_format=torch.contiguous_format)
+        to, ldo = out.data_ptr(), heads * dim
+        _here(x, pos)
+    else:
+        _need_shape(out, x.shape, "out")
+        to, ldo = _head_rows(out, x.dtype, "out")
+        _here(x, pos, out)
+    a = _Rope(n, heads, dim, len(parts), _Parts(*parts), 1 if split else 0, base, scale, _dt(x), pos.data_ptr(),
               pos.stride(0) if n > 1 else len(parts))
     _check(getattr(_block_argtypes(), name)(C.byref(a), ptr, ld, to, ldo, _stream()))
     return out
@@ -753,13 +770,13 @@ def sp_rope_bwd(dy, pos, parts, base: float = 10000.0, split: bool = False, scal
 
 
 def _rms_check(x, gamma, residual):
-    _need_cuda(x, None, "x"), _need_cuda(gamma, torch.float32, "gamma")
     if x.ndim != 2:
         raise ValueError("x must be [n][c]")
-    _need_shape(gamma, (x.shape[1],), "gamma")
+    device, dtype, shape = _device(), x.dtype, x.shape
+    _need(x, device, dtype, shape, "x"), _need(gamma, device, torch.float32, shape[1:], "gamma")
     if residual is not None:
-        _need_cuda(residual, x.dtype, "residual"), _need_shape(residual, x.shape, "residual")
-    _here(x, gamma, residual)
+        _need(residual, device, dtype, shape, "residual")
+    return shape
 
 
 def _ptr(t):
@@ -768,10 +785,9 @@ def _ptr(t):
 
 def sp_rms_norm_fwd(x, gamma, residual=None, eps: float = 1e-5):
     """x [n][c], gamma fp32 [c].  Returns (h = x + residual, or x itself without one; y; rstd fp32 [n])."""
-    _rms_check(x, gamma, residual)
-    n, c = x.shape
+    n, c = _rms_check(x, gamma, residual)
     h = None if residual is None else torch.empty_like(x)
-    y, rstd = torch.empty_like(x), _f32((n,), x.device)
+    y, rstd = torch.empty_like(x), torch.empty(n, dtype=torch.float32, device=x.device)
     _check(_block_argtypes().sp_rms_norm_fwd(x.data_ptr(), _ptr(residual), n, c, gamma.data_ptr(), eps, _ptr(h), y.data_ptr(), rstd.data_ptr(),
                                              _dt(x), _stream()))
     return (x if h is None else h), y, rstd
@@ -779,8 +795,7 @@ def sp_rms_norm_fwd(x, gamma, residual=None, eps: float = 1e-5):
 
 def sp_rms_norm_q8(x, gamma, residual=None, eps: float = 1e-5):
     """Returns (h, y in 8 bits: see sp_q8_rows)."""
-    _rms_check(x, gamma, residual)
-    n, c = x.shape
+    n, c = _rms_check(x, gamma, residual)
     h = None if residual is None else torch.empty_like(x)
     q, scales = _q8_new(n, c, x.device)
     _check(_block_argtypes().sp_rms_norm_q8(x.data_ptr(), _ptr(residual), n, c, gamma.data_ptr(), eps, _ptr(h), q.data_ptr(), scales.data_ptr(),
@@ -790,13 +805,11 @@ def sp_rms_norm_q8(x, gamma, residual=None, eps: float = 1e-5):
 
 def sp_rms_norm_bwd(h, dy, gamma, rstd, dh=None):
     """Returns (dx, which is the residual's gradient too; dgamma fp32 [c]).  dh: the gradient that reaches h past the norm."""
-    _rms_check(h, gamma, dh)
-    _need_cuda(dy, h.dtype, "dy"), _need_cuda(rstd, torch.float32, "rstd")
-    n, c = h.shape
-    _need_shape(dy, (n, c), "dy"), _need_shape(rstd, (n,), "rstd")
-    _here(dy, rstd)
+    n, c = shape = _rms_check(h, gamma, dh)
+    device = _device()
+    _need(dy, device, h.dtype, shape, "dy"), _need(rstd, device, torch.float32, shape[:1], "rstd")
     l = _block_argtypes()
-    dx, dgamma, work = torch.empty_like(h), _f32((c,), h.device), _work(l.sp_rms_norm_bwd_work(n, c, _dt(h)), h.device)
+    dx, dgamma, work = torch.empty_like(h), torch.empty_like(gamma), _work(l.sp_rms_norm_bwd_work(n, c, _dt(h)), h.device)
     _check(l.sp_rms_norm_bwd(h.data_ptr(), dy.data_ptr(), _ptr(dh), n, c, gamma.data_ptr(), rstd.data_ptr(), dx.data_ptr(), dgamma.data_ptr(),
                              work.data_ptr(), _dt(h), _stream()))
     return dx, dgamma
@@ -804,8 +817,8 @@ def sp_rms_norm_bwd(h, dy, gamma, rstd, dh=None):
 
 def _q8_new(n: int, c: int, device):
     blocks = (c + 127) // 128
-    return (torch.empty((n, blocks * 128), dtype=torch.float8_e4m3fn, device=device),
-            torch.empty((n, (blocks + 3) // 4 * 4), dtype=torch.float8_e8m0fnu, device=device))
+    return (torch.empty(n, blocks * 128, dtype=torch.float8_e4m3fn, device=device),
+            torch.empty(n, (blocks + 3) // 4 * 4, dtype=torch.float8_e8m0fnu, device=device))
 
 
 def sp_q8_rows(x, transposed: bool = False):
@@ -828,21 +841,16 @@ def sp_q8_rows(x, transposed: bool = False):
 def sp_q8_linear(x, w, dtype=torch.bfloat16):
     """x w^T [n][m] in `dtype` for x [n][c] and w [m][c], both as (codes, scales)."""
     (q, s), (wq, ws) = x, w
-    for t, name in ((q, "x's codes"), (wq, "w's codes")):
-        _need_cuda(t, torch.float8_e4m3fn, name)
-    for t, name in ((s, "x's scales"), (ws, "w's scales")):
-        _need_cuda(t, torch.float8_e8m0fnu, name)
     if dtype not in (torch.float32, torch.bfloat16):
         raise ValueError("dtype must be float32 or bfloat16")
     if q.ndim != 2 or wq.ndim != 2 or q.shape[1] % 128 or q.shape[1] == 0:
         raise ValueError("codes must be [rows][a multiple of 128]")
-    n, wide = q.shape
-    m = wq.shape[0]
-    _need_shape(wq, (m, wide), "w's codes")
-    _need_shape(s, (n, (wide // 128 + 3) // 4 * 4), "x's scales"), _need_shape(ws, (m, (wide // 128 + 3) // 4 * 4), "w's scales")
-    _here(q, s, wq, ws)
+    device, (n, wide), m = _device(), q.shape, wq.shape[0]
+    blocks = (wide // 128 + 3) // 4 * 4
+    _need(q, device, torch.float8_e4m3fn, (n, wide), "x's codes"), _need(wq, device, torch.float8_e4m3fn, (m, wide), "w's codes")
+    _need(s, device, torch.float8_e8m0fnu, (n, blocks), "x's scales"), _need(ws, device, torch.float8_e8m0fnu, (m, blocks), "w's scales")
     l = _block_argtypes()
-    y, work = torch.empty((n, m), dtype=dtype, device=q.device), _work(l.sp_q8_linear_work(n, wide, m), q.device)
+    y, work = torch.empty(n, m, dtype=dtype, device=q.device), _work(l.sp_q8_linear_work(n, wide, m), q.device)
     _check(l.sp_q8_linear(q.data_ptr(), s.data_ptr(), n, wide, wq.data_ptr(), ws.data_ptr(), m, y.data_ptr(),
                           SP_F32 if dtype == torch.float32 else SP_BF16, work.data_ptr(), _stream()))
     return y
@@ -852,16 +860,13 @@ _GATES = {"silu": 0, "gelu": 1}
 
 
 def _ffn(x, w_in, w_out, act):
-    for t, name in ((x, "x"), (w_in, "w_in"), (w_out, "w_out")):
-        _need_cuda(t, x.dtype, name)
-        if t.ndim != 2:
-            raise ValueError(f"{name} must have two dimensions")
     if act not in _GATES:
         raise ValueError(f"act must be one of {sorted(_GATES)}")
-    n, c = x.shape
-    m = w_out.shape[1]
-    _need_shape(w_in, (2 * m, c), "w_in"), _need_shape(w_out, (c, m), "w_out")
-    _here(x, w_in, w_out)
+    for t, name in ((x, "x"), (w_in, "w_in"), (w_out, "w_out")):
+        if t.ndim != 2:
+            raise ValueError(f"{name} must have two dimensions")
+    device, dtype, (n, c), m = _device(), x.dtype, x.shape, w_out.shape[1]
+    _need(x, device, dtype, (n, c), "x"), _need(w_in, device, dtype, (2 * m, c), "w_in"), _need(w_out, device, dtype, (c, m), "w_out")
     return _Ffn(n, c, m, _GATES[act], _dt(x))
 
 
@@ -887,9 +892,8 @@ def sp_ffn_bwd(x, w_in, w_out, kept, dy, act: str = "silu"):
     """Returns (dx, dw_in, dw_out) in the type of x."""
     a = _ffn(x, w_in, w_out, act)
     shape, dtype = _kept(a)
-    _need_cuda(kept, dtype, "kept"), _need_cuda(dy, x.dtype, "dy")
-    _need_shape(kept, shape, "kept"), _need_shape(dy, x.shape, "dy")
-    _here(kept, dy)
+    device = _device()
+    _need(kept, device, dtype, shape, "kept"), _need(dy, device, x.dtype, x.shape, "dy")
     l = _block_argtypes()
     dx, dw_in, dw_out = torch.empty_like(x), torch.empty_like(w_in), torch.empty_like(w_out)
     work = _work(l.sp_ffn_work_bytes(C.byref(a), 1), x.device)
