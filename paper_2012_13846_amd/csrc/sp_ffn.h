@@ -5,40 +5,29 @@
 // h is kept beside g and u: made again from these as they were rounded it would be off by their rounding, too (dW_out 4e-3 instead of 2e-3).
 #pragma once
 
-#include <algorithm>
-
 #include "sp_mm.h"
 
 namespace sp {
 
 template <typename T>
-bool in_pieces(std::initializer_list<const void*> arrays, int c, int m) {
-    bool all = c % (16 / (int)sizeof(T)) == 0 && m % (16 / (int)sizeof(T)) == 0;
-    for (const void* p : arrays) all &= aligned16(p);
-    return all;
-}
-
-template <typename T>
 int ffn_fwd(const Ffn& f, hipStream_t s) {
     constexpr int E = sizeof(T);
-    const bool pieces = in_pieces<T>({f.x, f.w_in, f.w_out, f.kept}, f.c, f.m);
     T* h = f.kept ? static_cast<T*>(f.kept) + 2 * f.m : reinterpret_cast<T*>(f.work);
     const int64_t ldh = f.kept ? kKept<T> * (int64_t)f.m : f.m;
     float* part = reinterpret_cast<float*>(f.work + (f.kept ? 0 : up256(f.n * f.m * E)));
     Mm a{};
     a.first = f.w_in, a.ld_first = (int64_t)f.c * E, a.second = f.x, a.ld_second = (int64_t)f.c * E;
     a.m = f.m, a.n = (int)f.n, a.k = f.c, a.last = kGate, a.out = h, a.ld = ldh, a.kept = f.kept, a.act = f.act;
-    SP_TRY((mm<T, false, false>(a, pieces, part, s)));
+    SP_TRY((mm<T, false, false>(a, part, s)));
     Mm b{};
     b.first = f.w_out, b.ld_first = (int64_t)f.m * E, b.second = h, b.ld_second = ldh * E;
     b.m = f.c, b.n = (int)f.n, b.k = f.m, b.last = kStore, b.out = f.y, b.ld = f.c;
-    return mm<T, false, false>(b, pieces, part, s);
+    return mm<T, false, false>(b, part, s);
 }
 
 template <typename T>
 int ffn_bwd(const Ffn& f, hipStream_t s) {
     constexpr int E = sizeof(T);
-    const bool pieces = in_pieces<T>({f.x, f.w_in, f.w_out, f.kept, f.dy}, f.c, f.m);
     const T* h = static_cast<const T*>(f.kept) + 2 * f.m;
     T* dgu = reinterpret_cast<T*>(f.work);
     float* part = reinterpret_cast<float*>(f.work + up256(2 * f.n * f.m * E));
@@ -47,19 +36,19 @@ int ffn_bwd(const Ffn& f, hipStream_t s) {
         Mm a{};
         a.first = f.w_out, a.ld_first = row_m, a.second = f.dy, a.ld_second = row_c;
         a.m = f.m, a.n = (int)f.n, a.k = f.c, a.last = kGateBack, a.kept = f.kept, a.dgu = dgu, a.act = f.act;
-        SP_TRY((mm<T, true, false>(a, pieces, part, s)));
+        SP_TRY((mm<T, true, false>(a, part, s)));
         Mm b{};
         b.first = f.w_in, b.ld_first = row_c, b.second = dgu, b.ld_second = 2 * row_m;
         b.m = f.c, b.n = (int)f.n, b.k = 2 * f.m, b.last = kStore, b.out = f.dx, b.ld = f.c;
-        SP_TRY((mm<T, true, false>(b, pieces, part, s)));
+        SP_TRY((mm<T, true, false>(b, part, s)));
     }
     Mm w{};
     w.first = f.x, w.ld_first = row_c, w.second = dgu, w.ld_second = 2 * row_m;
     w.m = f.c, w.n = 2 * f.m, w.k = (int)f.n, w.last = kStore, w.out = f.dw_in, w.ld = f.c;
-    SP_TRY((mm<T, true, true>(w, pieces, part, s)));
+    SP_TRY((mm<T, true, true>(w, part, s)));
     w.first = h, w.ld_first = kKept<T> * row_m, w.second = f.dy, w.ld_second = row_c;
     w.m = f.m, w.n = f.c, w.out = f.dw_out, w.ld = f.m;
-    return mm<T, true, true>(w, pieces, part, s);
+    return mm<T, true, true>(w, part, s);
 }
 
 }  // namespace sp

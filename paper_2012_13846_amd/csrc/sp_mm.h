@@ -617,25 +617,39 @@ __global__ __launch_bounds__(Sh::kThreads) void mm_kernel(Mm a) {
 }
 
 // ---- the parts' sums, and the last step ---------------------------------------------------------------------------
-// a.m: the results' columns (of a gate: the hidden width, parts have 2 m columns)
-template <typename T>
+// a.m: the results' columns (of a gate: the hidden width, parts have 2 m columns).  GROUPS threads share the parts of eight columns, each GROUPS-th of
+// them in order, and the threads' sums are added in order: 42 parts of 540 x 100 results one after another took 20 us.
+template <typename T, int GROUPS>
 __global__ __launch_bounds__(256) void mm_join_kernel(Mm a) {
-    const int each = (a.m + 7) / 8;
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / each;
-    if (row >= a.n) return;
-    const int col = (int)(i - row * each) * 8, wide = a.last == kGate ? 2 * a.m : a.m;
+    constexpr int kItems = 256 / GROUPS;
+    __shared__ Eight room[GROUPS > 1 ? 2 * 256 : 1];
+    const int each = (a.m + 7) / 8, item = threadIdx.x % kItems, group = threadIdx.x / kItems;
+    const int64_t i = (int64_t)blockIdx.x * kItems + item, row = i / each;
+    const bool there = row < a.n, gate = a.last == kGate;
+    const int col = (int)(i - row * each) * 8, wide = gate ? 2 * a.m : a.m;
     auto sum = [&](int at) {
         Eight s{};
-        for (int p = 0; p < a.splits; ++p) {
-            const Eight v = get_eight(a.part + ((int64_t)p * a.n + row) * wide + at, a.m - col);
+        if (there)
+#pragma unroll 4
+            for (int p = group; p < a.splits; p += GROUPS) {
+                const Eight v = get_eight(a.part + ((int64_t)p * a.n + row) * wide + at, a.m - col);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) s.e[e] += v.e[e];
-        }
+                for (int e = 0; e < 8; ++e) s.e[e] += v.e[e];
+            }
         return s;
     };
-    const Eight s = sum(col);
+    Eight s = sum(col), u = gate ? sum(a.m + col) : Eight{};
+    if constexpr (GROUPS > 1) {
+        room[threadIdx.x] = s, room[256 + threadIdx.x] = u;
+        __syncthreads();
+        if (group) return;
+        for (int g = 1; g < GROUPS; ++g)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s.e[e] += room[g * kItems + item].e[e], u.e[e] += room[256 + g * kItems + item].e[e];
+    }
+    if (!there) return;
     if constexpr (sizeof(T) > 1) {
-        if (a.last == kGate) return put_gate<T>(a, row, col, s, sum(a.m + col));
+        if (gate) return put_gate<T>(a, row, col, s, u);
         if (a.last == kGateBack) return put_gate_back<T>(a, row, col, s, kept_at<T>(a, row, col, a.m - col), a.m - col);
     }
     put_out<T>(a, row, col, s);
@@ -796,11 +810,13 @@ int mm_launch(const Mm& a, hipStream_t s) {
     return SP_OK;
 }
 
-// Fills in what is left of `a` (steps, tiles, parts) and enqueues the product.  pieces: both operands are whole, aligned 16-byte pieces; part:
-// mm_work() bytes.
+// Fills in what is left of `a` (steps, tiles, parts) and enqueues the product.  part: mm_work() bytes.
 template <typename T, bool TA, bool TB>
-int mm(Mm a, bool pieces, float* part, hipStream_t s) {
+int mm(Mm a, float* part, hipStream_t s) {
     const bool gate = a.last == kGate;
+    // both operands' rows are whole, aligned 16-byte pieces
+    auto whole = [](const void* p, int64_t ld, int64_t row) { return aligned16(p) && ld % 16 == 0 && row * (int64_t)sizeof(T) % 16 == 0; };
+    const bool pieces = whole(a.first, a.ld_first, TA ? a.m : a.k) && whole(a.second, a.ld_second, TB ? a.n : a.k);
     const int64_t k_bytes = (int64_t)a.k * (int)sizeof(T);
     if constexpr (!TA && !TB)
         if (a.n <= kThinRows) {
@@ -848,10 +864,15 @@ int mm(Mm a, bool pieces, float* part, hipStream_t s) {
         SP_TRY(pieces ? go(std::true_type{}, std::false_type{}) : go(std::false_type{}, std::false_type{}));
     }
     if (join) {
-        const int64_t blocks = ((int64_t)((last.m + 7) / 8) * last.n + 255) / 256;
-        if (blocks > 0x7fffffff) return fail(SP_ERR_UNSUPPORTED, "too many results");
-        hipLaunchKernelGGL(mm_join_kernel<T>, dim3((unsigned)blocks), dim3(256), 0, s, last);
-        SP_HIP(hipGetLastError());
+        auto add = [&](auto groups) -> int {
+            constexpr int G = decltype(groups)::value;
+            const int64_t blocks = ((int64_t)((last.m + 7) / 8) * last.n + 256 / G - 1) / (256 / G);
+            if (blocks > 0x7fffffff) return fail(SP_ERR_UNSUPPORTED, "too many results");
+            hipLaunchKernelGGL((mm_join_kernel<T, G>), dim3((unsigned)blocks), dim3(256), 0, s, last);
+            SP_HIP(hipGetLastError());
+            return SP_OK;
+        };
+        SP_TRY(p.splits >= 8 ? add(std::integral_constant<int, 8>{}) : add(std::integral_constant<int, 1>{}));
     }
     return SP_OK;
 }

@@ -122,7 +122,7 @@ int sp_q8_linear(const uint8_t* d_q, const uint8_t* d_scales, int64_t n, int64_t
     a.first = d_wq, a.ld_first = wide, a.second = d_q, a.ld_second = wide;
     a.m = (int)m, a.n = (int)n, a.k = (int)wide, a.last = kStore, a.out = d_y, a.ld = m, a.out_f32 = dt == SP_F32;
     a.first_scales = d_wscales, a.second_scales = d_scales, a.scales = (int)q8_scales(c);
-    return mm<q8_t, false, false>(a, true, static_cast<float*>(d_work), (hipStream_t)stream);
+    return mm<q8_t, false, false>(a, static_cast<float*>(d_work), (hipStream_t)stream);
 }
 
 }  // extern "C"
