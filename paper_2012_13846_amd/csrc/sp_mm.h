@@ -389,7 +389,7 @@ __global__ __launch_bounds__(Sh::kThreads) void mm_kernel(Mm a) {
     constexpr int kScaleBytes = kScaleLoads * kThreads * 4;
     constexpr int kStage = (Sh::BM + Sh::BN) * kStepBytes + kScaleBytes;
     constexpr int ST = VEC ? depth_of<T, Sh>() : 2;
-    constexpr bool kAhead = VEC && ST == 2 && sizeof(T) > 1;
+    constexpr bool kAhead = VEC && sizeof(T) > 1;
     using A = Side<T, Sh::BM, TA, kThreads>;
     using B = Side<T, Sh::BN, TB, kThreads>;
     __shared__ char room[ST * kStage] __attribute__((aligned(16)));  // [ST][tile of the first operand, of the second, their scales]
@@ -499,10 +499,12 @@ __global__ __launch_bounds__(Sh::kThreads) void mm_kernel(Mm a) {
         if constexpr (kAhead) {
             // Fragments are read while the ones before them are multiplied.  One meeting a step, between its two fragments: behind it nobody reads this
             // step's tiles any more, and the next step's are there.
-            static_assert(ST == 2 && K::kSub == 2, "two tiles, two fragments a step");
+            static_assert(K::kSub == 2, "two fragments a step");
             Frag x[2][MT], y[2][NT];
-            if (count > 0) load(begin, 0);
-            if (count > 1) load(begin + 1, 1), wait_loads<kLoads>();
+#pragma unroll
+            for (int i = 0; i < ST; ++i)
+                if (i < count) load(begin + i, i);
+            if (ST <= count) wait_loads<(ST - 1) * kLoads>();
             else wait_loads<0>();
             meet();
             take(room, 0, x[0], y[0]);
@@ -512,10 +514,11 @@ __global__ __launch_bounds__(Sh::kThreads) void mm_kernel(Mm a) {
                 take(room + stage * kStage, 1, x[1], y[1]);
                 product(x[0], y[0], nullptr, nullptr);
                 alternate();
-                wait_loads<0>();
+                if (k + ST <= count) wait_loads<(ST - 2) * kLoads>();
+                else wait_loads<0>();
                 meet();
-                if (k + 2 < count) load(begin + k + 2, stage);
-                stage ^= 1;
+                if (k + ST < count) load(begin + k + ST, stage);
+                stage = stage + 1 == ST ? 0 : stage + 1;
                 take(room + stage * kStage, 0, x[0], y[0]);  // (behind the last step: a tile that is not used)
                 product(x[1], y[1], nullptr, nullptr);
                 alternate();
@@ -793,11 +796,12 @@ struct Plan {
     int splits, per_split, tiles_m, tiles_n;
 };
 // rows: of the first operand (a gate: 2 m); k_bytes: of a row of the contraction
-Plan mm_plan(int64_t rows, int64_t n, int64_t k_bytes, int size, bool pieces);
+enum MmType { kF32, kBf16, kQ8, kQ8Exact };
+Plan mm_plan(int64_t rows, int64_t n, int64_t k_bytes, MmType type, bool pieces);
 // Bytes of the parts' sums (0: none).  direct: both operands are.
-inline int64_t mm_work(int64_t rows, int64_t n, int64_t k_bytes, int size, bool direct, bool pieces) {
+inline int64_t mm_work(int64_t rows, int64_t n, int64_t k_bytes, MmType type, bool direct, bool pieces) {
     if (direct && n <= kThinRows) return 0;
-    const Plan p = mm_plan(rows, n, k_bytes, size, pieces);
+    const Plan p = mm_plan(rows, n, k_bytes, type, pieces);
     return p.splits > 1 ? (int64_t)p.splits * rows * n * 4 : 0;
 }
 
@@ -827,7 +831,8 @@ int mm(Mm a, float* part, hipStream_t s) {
                 return pieces ? mm_thin<T, false, true, false>(a, s) : mm_thin<T, false, false, false>(a, s);
             }
         }
-    const Plan p = mm_plan(gate ? (int64_t)2 * a.m : a.m, a.n, k_bytes, sizeof(T), pieces && !(sizeof(T) == 1 && a.out_f32));
+    const MmType type = sizeof(T) == 4 ? kF32 : sizeof(T) == 2 ? kBf16 : a.out_f32 ? kQ8Exact : kQ8;
+    const Plan p = mm_plan(gate ? (int64_t)2 * a.m : a.m, a.n, k_bytes, type, pieces);
     a.steps = (int)((k_bytes + kStepBytes - 1) / kStepBytes);
     a.per_split = p.per_split, a.splits = p.splits, a.tiles_m = p.tiles_m, a.tiles_n = p.tiles_n;
     Mm last = a;

@@ -5,35 +5,38 @@
 
 namespace sp {
 
-Plan mm_plan(int64_t rows, int64_t n, int64_t k_bytes, int size, bool pieces) {
-    const int64_t steps = (k_bytes + kStepBytes - 1) / kStepBytes;
-    struct Kind2 {
+// Workgroups of each shape, and the microseconds that a step of 128 bytes takes of one that has a CU to itself and of two that share it, as measured
+// over products of 64 to 70001 rows and widths of 64 to 8192; what a product takes beside them: 3.5 us, 2 us for each round of workgroups (what the
+// first tiles wait for, and the results' way out), and to join parts 3.5 us and their way to memory and back at 4 bytes a picosecond.
+Plan mm_plan(int64_t rows, int64_t n, int64_t k_bytes, MmType type, bool pieces) {
+    struct Cost {
         ShapeName name;
         int bm, bn;
-        double step;  // clocks a step of a workgroup takes of a CU that is full of them
-        double alone; // ... and of a CU that has no other
+        double alone[4], shared[4];  // by type; shared 0: a CU holds one
     };
-    // A CU multiplies 64 x 64 blocks of a step of 128 bytes in 128 clocks (fp32: 1024).
-    const double unit = size == 4 ? 1024 : 128;
-    const Kind2 kinds[] = {{kLarge, 256, 256, 16 * unit * 1.25, 16 * unit * 1.25},
-                           {kMiddle, 128, 128, 4 * unit * 1.5, std::max(4 * unit * 1.5, 1000.0)},
-                           {kNarrow, 64, 128, 2 * unit * 1.7, std::max(2 * unit * 1.7, 800.0)},
-                           {kFew, 128, 32, std::max(unit * 2, 2000.0), std::max(unit * 2, 2000.0)}};
+    //                              f32   bf16  8 bits, and exactly
+    static constexpr Cost kCosts[] = {{kLarge, 256, 256, {7.9, 1.35, 1.7, 0}, {0, 0, 0, 0}},
+                                      {kMiddle, 128, 128, {2.0, 0.6, 0.75, 1.15}, {4.06, 1.0, 1.13, 1.96}},
+                                      {kNarrow, 64, 128, {1.15, 0.37, 0.55, 0.85}, {2.1, 0.65, 0.81, 1.26}},
+                                      {kFew, 128, 32, {0.7, 0.35, 0, 0}, {1.1, 0.55, 0, 0}}};
+    const int64_t steps = (k_bytes + kStepBytes - 1) / kStepBytes;
     Plan best{kMiddle, 1, (int)steps, 1, 1};
     double least = 1e300;
-    for (const Kind2& kind : kinds) {
-        if (kind.name == kLarge && !pieces) continue;
-        if ((kind.name == kFew) != (n <= 32)) continue;
+    for (const Cost& kind : kCosts) {
+        if (kind.name == kLarge && (!pieces || type == kQ8Exact)) continue;
+        if ((kind.name == kFew) != (n <= kThinRows && type < kQ8)) continue;
         const int64_t tiles_m = (rows + kind.bm - 1) / kind.bm, tiles_n = (n + kind.bn - 1) / kind.bn, tiles = tiles_m * tiles_n;
         if (tiles > 0x7fffffff) continue;
+        const double alone = kind.alone[type], shared = kind.shared[type];
         int64_t last = 0;
-        for (int64_t want = 1; want <= 64 && want <= std::max<int64_t>(1, steps / 2); want = want < 4 ? want + 1 : want + want / 2) {
+        for (int64_t want = 1; want <= 128 && want <= std::max<int64_t>(1, steps / 2); want = want < 4 ? want + 1 : want + want / 3) {
             const int64_t each = std::max<int64_t>(1, (steps + want - 1) / want), splits = std::max<int64_t>(1, (steps + each - 1) / each);
             if (splits == last || tiles * splits > 0x7fffffff) continue;
             last = splits;
-            const bool join = splits > 1;
-            const double rounds = (double)((tiles * splits + 255) / 256);
-            const double time = rounds * each * (rounds > 1 ? kind.step : kind.alone) + 3000 + (join ? 8000 + 8.0 * splits * rows * n / 2300 : 0);
+            const int64_t groups = tiles * splits, slots = shared > 0 ? 512 : 256, rest = groups % slots;
+            double time = 3.5 + (double)(groups / slots) * ((double)each * (shared > 0 ? shared : alone) + 2);
+            if (rest) time += (double)each * (rest <= 256 ? alone : shared) + 2;
+            if (splits > 1) time += 3.5 + 8.0 * (double)splits * (double)rows * (double)n / 4e6;
             if (time < least) {
                 least = time;
                 best = Plan{kind.name, (int)splits, (int)each, (int)tiles_m, (int)tiles_n};
@@ -44,13 +47,14 @@ Plan mm_plan(int64_t rows, int64_t n, int64_t k_bytes, int size, bool pieces) {
 }
 
 static int64_t ffn_work(int64_t n, int c, int m, int size, bool backward) {
+    const MmType type = size == 4 ? kF32 : kBf16;
     int64_t part = 0;
     for (const bool pieces : {false, true}) {  // the arrays' alignment is not known yet
         if (!backward) {
-            part = std::max({part, mm_work(2 * (int64_t)m, n, (int64_t)c * size, size, true, pieces), mm_work(c, n, (int64_t)m * size, size, true, pieces)});
+            part = std::max({part, mm_work(2 * (int64_t)m, n, (int64_t)c * size, type, true, pieces), mm_work(c, n, (int64_t)m * size, type, true, pieces)});
         } else {
-            part = std::max({part, mm_work(m, n, (int64_t)c * size, size, false, pieces), mm_work(c, n, 2 * (int64_t)m * size, size, false, pieces),
-                             mm_work(c, 2 * (int64_t)m, n * size, size, false, pieces), mm_work(m, c, n * size, size, false, pieces)});
+            part = std::max({part, mm_work(m, n, (int64_t)c * size, type, false, pieces), mm_work(c, n, 2 * (int64_t)m * size, type, false, pieces),
+                             mm_work(c, 2 * (int64_t)m, n * size, type, false, pieces), mm_work(m, c, n * size, type, false, pieces)});
         }
     }
     return up256((backward ? 2 : 1) * n * m * size) + up256(part) + 256;
@@ -105,7 +109,7 @@ int sp_ffn_bwd(const sp_ffn* f, const void* d_x, const void* d_w_in, const void*
 int64_t sp_q8_linear_work(int64_t n, int64_t c, int64_t m) {
     if (n < 0 || n > kMostRows || c < 1 || c > kMostRow || m < 1 || m > kMostRows) return -1;
     const int64_t wide = q8_blocks(c) * kQ8Block;  // the results' type is not known yet
-    return up256(std::max(mm_work(m, n, wide, 1, true, true), mm_work(m, n, wide, 1, true, false))) + 256;
+    return up256(std::max(mm_work(m, n, wide, kQ8, true, true), mm_work(m, n, wide, kQ8Exact, true, true))) + 256;
 }
 
 int sp_q8_linear(const uint8_t* d_q, const uint8_t* d_scales, int64_t n, int64_t c, const uint8_t* d_wq, const uint8_t* d_wscales, int64_t m,
