@@ -364,7 +364,6 @@ struct Shape2 {
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, ST = ST_, kThreads = WM_ * WN_ * 64;
 };
 using Large = Shape2<256, 256, 2, 4, 2>;
-using Large8 = Shape2<256, 256, 4, 4, 2>;  // of 8-bit operands, whose fragments are twice as long: 64 x 64 results a wavefront
 using Middle = Shape2<128, 128, 2, 2, 2>;
 using Narrow = Shape2<64, 128, 1, 4, 3>;
 using Few = Shape2<128, 32, 4, 1, 4>;
@@ -385,14 +384,12 @@ __global__ __launch_bounds__(Sh::kThreads) void mm_kernel(Mm a) {
     static_assert(MT % 2 == 0 && NT % 2 == 0, "blocks come in pairs");
     constexpr bool gate = LAST == kGate;
     static_assert(!gate || (MT % 4 == 0 && !TA), "a wavefront has as many pairs of gates as of ups");
-    constexpr int kScaleLoads = sizeof(T) == 1 ? (Sh::BM + Sh::BN + kThreads - 1) / kThreads : 0;
-    constexpr int kScaleBytes = kScaleLoads * kThreads * 4;
-    constexpr int kStage = (Sh::BM + Sh::BN) * kStepBytes + kScaleBytes;
+    constexpr int kStage = (Sh::BM + Sh::BN) * kStepBytes, kWords = sizeof(T) == 1 ? Sh::BM + Sh::BN : 0;
     constexpr int ST = VEC ? depth_of<T, Sh>() : 2;
     constexpr bool kAhead = VEC && sizeof(T) > 1;
     using A = Side<T, Sh::BM, TA, kThreads>;
     using B = Side<T, Sh::BN, TB, kThreads>;
-    __shared__ char room[ST * kStage] __attribute__((aligned(16)));  // [ST][tile of the first operand, of the second, their scales]
+    __shared__ char room[ST * kStage + 2 * kWords * 4] __attribute__((aligned(16)));  // [ST][tile of the first operand, of the second], [2][scales]
     // neighbouring workgroups of an XCD: up to eight tiles of rows, then the next tile of columns, so that its L2 serves both operands
     const uint32_t tiles = (uint32_t)a.tiles_m * a.tiles_n, item = item_of_block(blockIdx.x, tiles * a.splits);
     const uint32_t split = item / tiles, t = item - split * tiles;
@@ -424,14 +421,12 @@ __global__ __launch_bounds__(Sh::kThreads) void mm_kernel(Mm a) {
 #pragma unroll
         for (int i = 0; i < MT; ++i) x[i] = fa.frag(stage, i, A::template block<MT>(i, half), s);
     };
-    auto product = [&](const Frag (&x)[MT], const Frag (&y)[NT], const int* sa, const int* sb) {
+    auto product = [&](const Frag (&x)[MT], const Frag (&y)[NT]) {
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
-                if constexpr (sizeof(T) == 1) {
-                    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x[i], y[j], acc[i][j], 0, 0, 0, sa[i], 0, sb[j]);
-                } else if constexpr (sizeof(T) == 2) {
+                if constexpr (sizeof(T) == 2) {
                     acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[i], y[j], acc[i][j], 0, 0, 0);
                 } else {
 #pragma unroll
@@ -439,17 +434,17 @@ __global__ __launch_bounds__(Sh::kThreads) void mm_kernel(Mm a) {
                 }
             }
     };
-    auto multiply = [&](const char* stage, int step) {
-        int sa[MT], sb[NT];
-        if constexpr (sizeof(T) == 1) {
-            // this step's scales: one byte of the four steps that a row's word has
-            const int shift = 8 * (step & 3);
-            const uint32_t* words = reinterpret_cast<const uint32_t*>(stage + A::kBytes + B::kBytes) + 8 * (l >> 2 & 3) + (l & 3);
+    // 8 bits: the scales of a row's next four steps, a byte each; step u's (opsel) is a constant of the matrix instruction
+    int sa[MT], sb[NT];
+    auto take_scales = [&](int step) {
+        const int* words = reinterpret_cast<const int*>(room + ST * kStage) + (step >> 2 & 1) * kWords + 8 * (l >> 2 & 3) + (l & 3);
 #pragma unroll
-            for (int i = 0; i < MT; ++i) sa[i] = (int)(words[32 * (wm * MP + (i >> 1)) + 4 * (i & 1)] >> shift);
+        for (int i = 0; i < MT; ++i) sa[i] = words[32 * (wm * MP + (i >> 1)) + 4 * (i & 1)];
 #pragma unroll
-            for (int i = 0; i < NT; ++i) sb[i] = (int)(words[Sh::BM + 32 * (wn * NP + (i >> 1)) + 4 * (i & 1)] >> shift);
-        }
+        for (int i = 0; i < NT; ++i) sb[i] = words[Sh::BM + 32 * (wn * NP + (i >> 1)) + 4 * (i & 1)];
+    };
+    auto multiply = [&](const char* stage, auto opsel) {
+        constexpr int U = decltype(opsel)::value;
 #pragma unroll
         for (int s = 0; s < K::kSub; ++s) {
             Frag x[MT], y[NT];
@@ -459,16 +454,22 @@ __global__ __launch_bounds__(Sh::kThreads) void mm_kernel(Mm a) {
                 for (int e = 0; e < 4; ++e) {
                     bf16x8 u[MT], v[NT];
 #pragma unroll
-                    for (int i = 0; i < MT; ++i) u[i] = q8_values(x[i], e, sa[i]);
+                    for (int i = 0; i < MT; ++i) u[i] = q8_values(x[i], e, sa[i] >> (8 * U));
 #pragma unroll
-                    for (int j = 0; j < NT; ++j) v[j] = q8_values(y[j], e, sb[j]);
+                    for (int j = 0; j < NT; ++j) v[j] = q8_values(y[j], e, sb[j] >> (8 * U));
 #pragma unroll
                     for (int i = 0; i < MT; ++i)
 #pragma unroll
                         for (int j = 0; j < NT; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(u[i], v[j], acc[i][j], 0, 0, 0);
                 }
+            } else if constexpr (sizeof(T) == 1) {
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int j = 0; j < NT; ++j)
+                        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x[i], y[j], acc[i][j], 0, 0, U, sa[i], U, sb[j]);
             } else {
-                product(x, y, sa, sb);
+                product(x, y);
             }
         }
     };
@@ -477,22 +478,25 @@ __global__ __launch_bounds__(Sh::kThreads) void mm_kernel(Mm a) {
         Direct<T, Sh::BM, TA, kThreads> la;
         Direct<T, Sh::BN, TB, kThreads> lb;
         la.aim(pa, gate), lb.aim(pb, false);
-        constexpr int kLoads = A::kLoads + B::kLoads + kScaleLoads;  // of a wavefront a step
+        constexpr int kLoads = A::kLoads + B::kLoads;  // of a wavefront a step (8 bits: at least)
         const uint32_t lds = lds_address(room);
         auto load = [&](int step, int stage) {
             const uint32_t to = lds + stage * kStage;
             la.load(pa, step, gate, ups, to);
             lb.load(pb, step, false, 0, to + A::kBytes);
             if constexpr (sizeof(T) == 1) {
-                // a word a row: four steps' scales.  Every wavefront loads equally often, so that waits can count (zeros behind the rows).
+                // a word a row, four steps' scales (zeros behind the rows)
+                if ((step & 3) == 0 || step == begin) {
 #pragma unroll
-                for (int j = 0; j < kScaleLoads; ++j) {
-                    const int base = __builtin_amdgcn_readfirstlane(j * kThreads + (int)(threadIdx.x & ~63u));
-                    const Place& o = base < Sh::BM ? pa : pb;
-                    const int q = (base < Sh::BM ? base : base - Sh::BM) + l, rows = base < Sh::BM ? Sh::BM : Sh::BN;
-                    const uint8_t* from = (base < Sh::BM ? a.first_scales : a.second_scales) + (int64_t)o.first * a.scales + (step >> 2) * 4;
-                    const uint32_t off = q < rows && o.first + q < o.count ? (uint32_t)(q * a.scales) : kOutside;
-                    word_to_lds(memory_of(from, 0x7fffffffu), off, to + A::kBytes + B::kBytes + base * 4);
+                    for (int j = 0; j < (kWords + kThreads - 1) / kThreads; ++j) {
+                        const int base = __builtin_amdgcn_readfirstlane(j * kThreads + (int)(threadIdx.x & ~63u));
+                        if (base >= kWords) continue;
+                        const Place& o = base < Sh::BM ? pa : pb;
+                        const int q = (base < Sh::BM ? base : base - Sh::BM) + l;
+                        const uint8_t* from = (base < Sh::BM ? a.first_scales : a.second_scales) + (int64_t)o.first * a.scales + (step >> 2) * 4;
+                        word_to_lds(memory_of(from, 0x7fffffffu), o.first + q < o.count ? (uint32_t)(q * a.scales) : kOutside,
+                                    lds + ST * kStage + ((step >> 2 & 1) * kWords + base) * 4);
+                    }
                 }
             }
         };
@@ -512,7 +516,7 @@ __global__ __launch_bounds__(Sh::kThreads) void mm_kernel(Mm a) {
 #pragma unroll 1
             for (int k = 0; k < count; ++k) {
                 take(room + stage * kStage, 1, x[1], y[1]);
-                product(x[0], y[0], nullptr, nullptr);
+                product(x[0], y[0]);
                 alternate();
                 if (k + ST <= count) wait_loads<(ST - 2) * kLoads>();
                 else wait_loads<0>();
@@ -520,7 +524,7 @@ __global__ __launch_bounds__(Sh::kThreads) void mm_kernel(Mm a) {
                 if (k + ST < count) load(begin + k + ST, stage);
                 stage = stage + 1 == ST ? 0 : stage + 1;
                 take(room + stage * kStage, 0, x[0], y[0]);  // (behind the last step: a tile that is not used)
-                product(x[1], y[1], nullptr, nullptr);
+                product(x[1], y[1]);
                 alternate();
             }
         } else {
@@ -528,16 +532,24 @@ __global__ __launch_bounds__(Sh::kThreads) void mm_kernel(Mm a) {
             for (int s = 0; s < ST - 1; ++s)
                 if (s < count) load(begin + s, s);
             int stage = 0, next = ST - 1;
-#pragma unroll 1
-            for (int k = 0; k < count; ++k) {
+            // (a part begins at a step whose scales are a word's first)
+            auto step = [&](int k, auto opsel) {
                 // this step's tiles are there; the ones behind it may still be under way
                 if (k + ST - 1 <= count) wait_loads<(ST - 2) * kLoads>();
                 else wait_loads<0>();
                 meet();
                 if (k + ST - 1 < count) load(begin + k + ST - 1, next);
-                multiply(room + stage * kStage, begin + k);
+                if constexpr (decltype(opsel)::value == 0) take_scales(begin + k);
+                multiply(room + stage * kStage, opsel);
                 stage = stage + 1 == ST ? 0 : stage + 1;
                 next = next + 1 == ST ? 0 : next + 1;
+            };
+#pragma unroll 1
+            for (int k = 0; k < count; k += 4) {
+                step(k, std::integral_constant<int, 0>{});
+                if (k + 1 < count) step(k + 1, std::integral_constant<int, 1>{});
+                if (k + 2 < count) step(k + 2, std::integral_constant<int, 2>{});
+                if (k + 3 < count) step(k + 3, std::integral_constant<int, 3>{});
             }
         }
     } else {
@@ -551,7 +563,7 @@ __global__ __launch_bounds__(Sh::kThreads) void mm_kernel(Mm a) {
             wait_loads<0>();
             meet();
             if (k + 1 < count) la.load(pa, begin + k + 1, gate, ups), lb.load(pb, begin + k + 1, false, 0);
-            multiply(stage, begin + k);
+            multiply(stage, std::integral_constant<int, 0>{});
         }
     }
 
@@ -847,7 +859,7 @@ int mm(Mm a, float* part, hipStream_t s) {
             constexpr Last L = (Last)decltype(last)::value;
             switch (p.shape) {
                 case kLarge:
-                    if constexpr (V && !X) return mm_launch<T, std::conditional_t<sizeof(T) == 1, Large8, Large>, TA, TB, V, X, L>(a, s);
+                    if constexpr (V && !X) return mm_launch<T, Large, TA, TB, V, X, L>(a, s);
                     break;
                 case kMiddle: return mm_launch<T, Middle, TA, TB, V, X, L>(a, s);
                 case kNarrow: return mm_launch<T, Narrow, TA, TB, V, X, L>(a, s);

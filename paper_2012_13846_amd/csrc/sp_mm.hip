@@ -30,7 +30,9 @@ Plan mm_plan(int64_t rows, int64_t n, int64_t k_bytes, MmType type, bool pieces)
         const double alone = kind.alone[type], shared = kind.shared[type];
         int64_t last = 0;
         for (int64_t want = 1; want <= 128 && want <= std::max<int64_t>(1, steps / 2); want = want < 4 ? want + 1 : want + want / 3) {
-            const int64_t each = std::max<int64_t>(1, (steps + want - 1) / want), splits = std::max<int64_t>(1, (steps + each - 1) / each);
+            int64_t each = std::max<int64_t>(1, (steps + want - 1) / want);
+            if (type >= kQ8 && want > 1) each = (each + 3) / 4 * 4;  // a word of scales is four steps'
+            const int64_t splits = std::max<int64_t>(1, (steps + each - 1) / each);
             if (splits == last || tiles * splits > 0x7fffffff) continue;
             last = splits;
             const int64_t groups = tiles * splits, slots = shared > 0 ? 512 : 256, rest = groups % slots;

@@ -500,35 +500,41 @@ __global__ __launch_bounds__(256) void q8_rows_kernel(const T* __restrict__ x, i
 constexpr int kTurnCols = 64;
 template <typename T, bool ALIGNED>
 __global__ __launch_bounds__(256) void q8_turned_kernel(const T* __restrict__ x, int64_t ldx, int64_t n, int c, uint8_t* q, uint8_t* qs) {
-    constexpr int V = 16 / (int)sizeof(T), kPieces = kTurnCols / V;
+    constexpr int V = 16 / (int)sizeof(T), kPieces = kTurnCols / V, kEach = kQ8Block * kPieces / 256;
     __shared__ float tile[kTurnCols][kQ8Block + 1];
     const int64_t blocks = (n + kQ8Block - 1) / kQ8Block, wide = blocks * kQ8Block, scales = (blocks + 3) / 4 * 4;
     const int64_t block = blockIdx.x, row0 = block * kQ8Block;
     const int col0 = blockIdx.y * kTurnCols;
-    for (int i = threadIdx.x; i < kQ8Block * kPieces; i += 256) {
-        const int r = i / kPieces, j = (i % kPieces) * V;
-        Piece<T, V> v{};
-        if (row0 + r < n && col0 + j < c) v = load_some<T, V, ALIGNED>(x + (row0 + r) * ldx + col0 + j, c - col0 - j);
+    Piece<T, V> in[kEach];
 #pragma unroll
-        for (int k = 0; k < V; ++k) tile[j + k][r] = elem(v.e[k]);
+    for (int k = 0; k < kEach; ++k) {
+        const int i = k * 256 + threadIdx.x, r = i / kPieces, j = (i % kPieces) * V;
+        in[k] = Piece<T, V>{};
+        if (row0 + r < n && col0 + j < c) in[k] = load_some<T, V, ALIGNED>(x + (row0 + r) * ldx + col0 + j, c - col0 - j);
+    }
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+        const int i = k * 256 + threadIdx.x, r = i / kPieces, j = (i % kPieces) * V;
+#pragma unroll
+        for (int e = 0; e < V; ++e) tile[j + e][r] = elem(in[k].e[e]);
     }
     __syncthreads();
-    // four lanes a column, 32 rows each
-    const int j = threadIdx.x / 4, part = threadIdx.x % 4;
-    float top = 0.f;
-#pragma unroll 8
-    for (int i = 0; i < 32; ++i) top = q8_larger(top, q8_size(tile[j][part * 32 + i]));
+    // four lanes a column, 32 rows each; lanes 2 and 3 begin at the second 16, since they share banks with lanes 0 and 1
+    const int j = threadIdx.x / 4, part = threadIdx.x % 4, swap = part >> 1;
+    float v[32], top = 0.f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+        v[i] = tile[j][part * 32 + (i ^ (swap << 4))];
+        top = q8_larger(top, q8_size(v[i]));
+    }
     const uint32_t code = q8_scale(q8_top<4>(top));
     if (col0 + j >= c) return;
     uint32_t w[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float* v = &tile[j][part * 32 + 4 * i];
-        w[i] = q8_codes(v[0], v[1], v[2], v[3], code);
-    }
+    for (int i = 0; i < 8; ++i) w[i] = q8_codes(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3], code);
     uint4* to = reinterpret_cast<uint4*>(q + (int64_t)(col0 + j) * wide + row0 + part * 32);
-    to[0] = uint4{w[0], w[1], w[2], w[3]};
-    to[1] = uint4{w[4], w[5], w[6], w[7]};
+    to[swap] = uint4{w[0], w[1], w[2], w[3]};
+    to[swap ^ 1] = uint4{w[4], w[5], w[6], w[7]};
     if (part == 0) {
         uint8_t* s = qs + (int64_t)(col0 + j) * scales;
         s[block] = (uint8_t)code;
