@@ -340,8 +340,8 @@ typedef struct {
 int sp_rope_fwd(const sp_rope* a, const void* d_x, int64_t ldx, void* d_y, int64_t ldy, void* stream);
 int sp_rope_bwd(const sp_rope* a, const void* d_dy, int64_t lddy, void* d_dx, int64_t lddx, void* stream);
 
-/* Work memory of the calls below is the caller's: the size that the function beside them says (-1: such a call is refused), 256-byte aligned, used
- * until the stream has passed the call.  No call allocates, so calls may be captured into graphs, each with work memory of its own.
+/* Work memory of the calls below is the caller's: the size that the function beside them says (-1: such a call is refused; up to 256 bytes: the
+ * call does not touch them), 256-byte aligned, used until the stream has passed the call.  No call allocates, so calls may be captured into graphs, each with work memory of its own.
  *
  * Root-mean-square norm with the residual's addition, every row of x [n][c] by itself:
  *   h = x + res, as it is stored in dt;  rstd = 1/sqrt(mean(h^2) + eps);  y = gamma * h * rstd

@@ -728,9 +728,15 @@ def _work(nbytes: int, device) -> torch.Tensor:
     """Work memory of one call: from torch's allocator, so that a captured graph owns its own."""
     if nbytes < 0:
         raise ValueError("sizes that the library does not take")
+    if nbytes <= 256:                                        # the call does not touch them: any memory will do
+        idle = _idle.get(device)
+        if idle is None:
+            idle = _idle[device] = torch.empty(256, dtype=torch.uint8, device=device)
+        return idle
     return torch.empty(nbytes, dtype=torch.uint8, device=device)
 
 
+_idle = {}
 _Parts = C.c_int32 * 4
 
 

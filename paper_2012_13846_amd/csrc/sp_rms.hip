@@ -212,17 +212,17 @@ struct RmsBwd {
     int c;
     const float *gamma, *rstd;
     T* dx;
-    float* partial;        // [workgroups][c]
+    float* partial;        // [workgroups][c], or NULL: dgamma comes from the rows themselves
 };
 
-template <typename T, int V, int LANES, int P, bool ALIGNED>
-__global__ __launch_bounds__(kBlock<LANES>) void rms_bwd_kernel(RmsBwd<T> a) {
+template <typename T, int V, int LANES, int P, bool ALIGNED, bool PARTIAL>
+__device__ __forceinline__ void rms_bwd_rows(const RmsBwd<T>& a, int blocks) {
     constexpr int kGroups = kBlock<LANES> / LANES;
     __shared__ float room[kReduceRoom<LANES>];
-    __shared__ float sums[kGroups > 1 ? kBlock<LANES> * V * P : 1];
+    __shared__ float sums[PARTIAL && kGroups > 1 ? kBlock<LANES> * V * P : 1];
     int turn = 0;
     const int l = threadIdx.x % LANES, c = a.c;
-    const int64_t step = (int64_t)gridDim.x * kGroups;
+    const int64_t step = (int64_t)blocks * kGroups;
     int64_t row = (int64_t)blockIdx.x * kGroups + threadIdx.x / LANES;
     float ga[P][V], dg[P][V];
     Piece<T, V> nh[P], nd[P], ns[P];
@@ -274,6 +274,7 @@ __global__ __launch_bounds__(kBlock<LANES>) void rms_bwd_kernel(RmsBwd<T> a) {
             if (col < c) store_some<T, V, ALIGNED>(a.dx + row * c + col, o, c - col);
         }
     }
+    if constexpr (!PARTIAL) return;
     float* out = a.partial + (size_t)blockIdx.x * c;
     if constexpr (kGroups > 1) {
         constexpr int kCols = LANES * V * P;  // [group][column], the groups added in order
@@ -296,6 +297,59 @@ __global__ __launch_bounds__(kBlock<LANES>) void rms_bwd_kernel(RmsBwd<T> a) {
             for (int i = 0; i < V; ++i)
                 if ((p * LANES + l) * V + i < c) out[(p * LANES + l) * V + i] = dg[p][i];
     }
+}
+
+template <typename T, int V, int LANES, int P, bool ALIGNED>
+__global__ __launch_bounds__(kBlock<LANES>) void rms_bwd_kernel(RmsBwd<T> a) {
+    rms_bwd_rows<T, V, LANES, P, ALIGNED, true>(a, gridDim.x);
+}
+
+// dgamma of 4 V columns, straight from the rows: 64 rows at a time, 4 of a thread's asked for at once, its sums in fp32, those of the threads in fp64.
+constexpr int kShort = 256;
+template <typename T, int V, bool ALIGNED>
+__device__ __forceinline__ void rms_bwd_columns(const RmsBwd<T>& a, int slab, float* dgamma) {
+    constexpr int kSide = 4, kGroups = kShort / kSide, kAtOnce = 4;
+    __shared__ float sums[kGroups][kSide * V + 1];
+    const int group = threadIdx.x / kSide, at = threadIdx.x % kSide * V, col = slab * kSide * V + at, c = a.c;
+    float dg[V] = {};
+    if (col < c)
+        for (int64_t row = group; row < a.n; row += kGroups * kAtOnce) {
+            Piece<T, V> h[kAtOnce], d[kAtOnce];
+            float r[kAtOnce];
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k) {
+                const int64_t from = min(row + kGroups * k, a.n - 1);
+                h[k] = load_some<T, V, ALIGNED>(a.h + from * c + col, c - col);
+                d[k] = load_some<T, V, ALIGNED>(a.dy + from * c + col, c - col);
+                r[k] = a.rstd[from];
+            }
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k)
+                if (row + kGroups * k < a.n)
+#pragma unroll
+                    for (int i = 0; i < V; ++i) dg[i] += elem(d[k].e[i]) * (elem(h[k].e[i]) * r[k]);
+        }
+#pragma unroll
+    for (int i = 0; i < V; ++i) sums[group][at + i] = dg[i];
+    __syncthreads();
+    const int t = threadIdx.x;
+    if (t < kSide * V && slab * kSide * V + t < c) {
+        double s = 0.0;
+#pragma unroll 16
+        for (int g = 0; g < kGroups; ++g) s += (double)sums[g][t];
+        dgamma[slab * kSide * V + t] = (float)s;
+    }
+}
+// A small matrix: the first `rows` workgroups take rows, the others columns, in one launch and without work memory.  (Two launches and a
+// workgroup's parts: 1428 rows of 128 in bf16 24.5 us a forward and backward pass, most of it the host's.)
+template <typename T, int V, int LANES, int P, bool ALIGNED>
+__global__ __launch_bounds__(kShort) void rms_bwd_short_kernel(RmsBwd<T> a, int rows, float* dgamma) {
+    if ((int)blockIdx.x < rows) rms_bwd_rows<T, V, LANES, P, ALIGNED, false>(a, rows);
+    else rms_bwd_columns<T, V, ALIGNED>(a, blockIdx.x - rows, dgamma);
+}
+template <typename T, int V, bool ALIGNED>
+__global__ __launch_bounds__(kShort) void rms_bwd_columns_kernel(RmsBwd<T> a, float* dgamma) {
+    rms_bwd_columns<T, V, ALIGNED>(a, blockIdx.x, dgamma);
 }
 
 template <typename T>
@@ -398,6 +452,9 @@ int bwd_blocks(int64_t n, Shape s, int v) {
 constexpr int kMostSlabs = 256;
 int64_t slab_of(int64_t n) { return std::max<int64_t>(64, (n + kMostSlabs - 1) / kMostSlabs); }
 
+// Reading h and dy again for dgamma costs less than a launch
+bool short_rows(int64_t n, int c, Shape s) { return n > 0 && s.lanes && s.lanes <= kShort && n <= 4096 && n * c <= (1 << 18); }
+
 template <typename T, bool ALIGNED, bool Q8>
 int rms_fwd(const RmsFwd<T>& a, hipStream_t s) {
     constexpr int V = 16 / (int)sizeof(T);
@@ -423,6 +480,21 @@ int rms_bwd(RmsBwd<T> a, float* dgamma, hipStream_t s) {
     constexpr int V = 16 / (int)sizeof(T);
     const Shape shape = shape_of((a.c + V - 1) / V, V, 1, true);
     int blocks;
+    if (short_rows(a.n, a.c, shape)) {
+        const int rows = bwd_blocks(a.n, shape, V), columns = (a.c + 4 * V - 1) / (4 * V);
+        const bool same = (const void*)a.dy == (const void*)a.dx;  // dgamma first
+        if (same) hipLaunchKernelGGL((rms_bwd_columns_kernel<T, V, ALIGNED>), dim3(columns), dim3(kShort), 0, s, a, dgamma);
+        SP_TRY((with_shape<V, true>(shape, [&](auto lanes, auto per) -> int {
+            constexpr int L = decltype(lanes)::value, P = decltype(per)::value;
+            if constexpr (L <= kShort) {
+                hipLaunchKernelGGL((rms_bwd_short_kernel<T, V, L, P, ALIGNED>), dim3(rows + (same ? 0 : columns)), dim3(kShort), 0, s, a, rows, dgamma);
+                return SP_OK;
+            }
+            return fail(SP_ERR_UNSUPPORTED, "no kernel for this width");
+        })));
+        SP_HIP(hipGetLastError());
+        return SP_OK;
+    }
     if (a.n == 0) {
         blocks = 0;
     } else if (!shape.lanes) {
@@ -589,7 +661,8 @@ int64_t sp_rms_norm_bwd_work(int64_t n, int32_t c, sp_dtype dt) {
     if (check(n, c, dt) != SP_OK) return -1;
     const int v = dt == SP_F32 ? 4 : 8;
     const Shape shape = shape_of((c + v - 1) / v, v, 1, true);
-    return std::max<int64_t>(16, (int64_t)(shape.lanes ? bwd_blocks(n, shape, v) : kMostSlabs) * c * 4);
+    if (n == 0 || short_rows(n, c, shape)) return 256;
+    return std::max<int64_t>(512, (int64_t)(shape.lanes ? bwd_blocks(n, shape, v) : kMostSlabs) * c * 4);
 }
 
 int sp_rms_norm_bwd(const void* d_h, const void* d_dy, const void* d_dh, int64_t n, int32_t c, const float* d_gamma, const float* d_rstd,
