@@ -390,11 +390,15 @@ __global__ __launch_bounds__(Sh::kThreads) void mm_kernel(Mm a) {
     using A = Side<T, Sh::BM, TA, kThreads>;
     using B = Side<T, Sh::BN, TB, kThreads>;
     __shared__ char room[ST * kStage + 2 * kWords * 4] __attribute__((aligned(16)));  // [ST][tile of the first operand, of the second], [2][scales]
-    // neighbouring workgroups of an XCD: up to eight tiles of rows, then the next tile of columns, so that its L2 serves both operands
+    // Neighbouring workgroups of an XCD: up to kBand tiles of rows, then the next tile of columns, so that its L2 serves both operands.  Each band begins
+    // 5/8 of the columns behind the last: XCDs that go through equal columns of their rows at a time write to, and read the first operand from, the same
+    // memory channels where rows are a power of two apart (8192 x 16384 results of 2048 in bf16, bands of 8 that all begin at column 0: 456 us, so: 403).
+    constexpr uint32_t kBand = 6;
     const uint32_t tiles = (uint32_t)a.tiles_m * a.tiles_n, item = item_of_block(blockIdx.x, tiles * a.splits);
     const uint32_t split = item / tiles, t = item - split * tiles;
-    const uint32_t band = 8u * a.tiles_m, b = t / band, in = t - b * band, high = min(8u, a.tiles_n - 8u * b);
-    const int tm = (int)(in / high), tn = (int)(8u * b + in % high);
+    const uint32_t band = kBand * a.tiles_m, b = t / band, in = t - b * band, high = min(kBand, a.tiles_n - kBand * b);
+    const uint32_t turned = in / high + b % 8 * 5 * a.tiles_m / 8;
+    const int tm = (int)(turned % a.tiles_m), tn = (int)(kBand * b + in % high);
     const int begin = (int)split * a.per_split, count = min(a.steps - begin, a.per_split);
     constexpr int cols = gate ? Sh::BM / 2 : Sh::BM, half = gate ? Sh::BM / 2 : 0;  // results' columns of a tile; rows from gates to ups
     constexpr int MP = gate ? MT / 4 : MT / 2, NP = NT / 2;                          // pairs of blocks of a wavefront
@@ -425,7 +429,8 @@ __global__ __launch_bounds__(Sh::kThreads) void mm_kernel(Mm a) {
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
-            for (int j = 0; j < NT; ++j) {
+            for (int v = 0; v < NT; ++v) {
+                const int j = i & 1 ? NT - 1 - v : v;  // (back and forth: 2% in a product of 2048 x 8192 x 8192)
                 if constexpr (sizeof(T) == 2) {
                     acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[i], y[j], acc[i][j], 0, 0, 0);
                 } else {
