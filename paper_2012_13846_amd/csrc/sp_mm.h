@@ -104,8 +104,7 @@ template <typename T>
 constexpr int kKept = sizeof(T) == 2 ? 4 : 3;
 
 template <typename T>
-__device__ __forceinline__ void keep(const Mm& a, int64_t row, int col, const Eight& g, const Eight& u) {
-    const int left = a.m - col;
+__device__ __forceinline__ void keep(const Mm& a, int64_t row, int col, const Eight& g, const Eight& u, int left) {
     T* to = static_cast<T*>(a.kept) + row * kKept<T> * a.m + col;
     if constexpr (sizeof(T) == 4) {
         put_eight(to, g, left);
@@ -139,12 +138,12 @@ __device__ __forceinline__ float2 gate_and_up(const KeptOf<T>& k, int i) {
 }
 
 template <typename T>
-__device__ __forceinline__ void put_gate(const Mm& a, int64_t row, int col, const Eight& g, const Eight& u) {
+__device__ __forceinline__ void put_gate(const Mm& a, int64_t row, int col, const Eight& g, const Eight& u, int left) {
     Eight h;
 #pragma unroll
     for (int i = 0; i < 8; ++i) h.e[i] = gate_of<T>(g.e[i], a.act).x * u.e[i];
-    put_rounded(static_cast<T*>(a.out) + row * a.ld + col, h, a.m - col);
-    if (a.kept) keep<T>(a, row, col, g, u);
+    put_rounded(static_cast<T*>(a.out) + row * a.ld + col, h, left);
+    if (a.kept) keep<T>(a, row, col, g, u, left);
 }
 template <typename T>
 __device__ __forceinline__ void put_gate_back(const Mm& a, int64_t row, int col, const Eight& dh, const KeptOf<T>& kept, int left) {
@@ -160,8 +159,7 @@ __device__ __forceinline__ void put_gate_back(const Mm& a, int64_t row, int col,
     put_rounded(dgu + a.m, du, left);
 }
 template <typename T>
-__device__ __forceinline__ void put_out(const Mm& a, int64_t row, int col, const Eight& v) {
-    const int left = a.m - col;
+__device__ __forceinline__ void put_out(const Mm& a, int64_t row, int col, const Eight& v, int left) {
     if constexpr (sizeof(T) == 1) {
         if (a.out_f32) put_eight(static_cast<float*>(a.out) + row * a.ld + col, v, left);
         else put_rounded(static_cast<bf16_t*>(a.out) + row * a.ld + col, v, left);
@@ -596,31 +594,21 @@ __global__ __launch_bounds__(Sh::kThreads) void mm_kernel(Mm a) {
         }
         return v;
     };
-    constexpr int kItems = NT * MP;
-    if constexpr (LAST == kGateBack) {
-        // what was kept is read some items ahead: one after the other took 320 us longer in 8192 x 8192 results
-        constexpr int kAheadBy = sizeof(T) == 2 ? 4 : 2;
-        auto items = [&](auto inside) {
-            constexpr bool kInside = decltype(inside)::value;
-            KeptOf<T> kept[kAheadBy];
-            auto fetch = [&](int t) {
+    // Tiles that lie within the results, nearly all, have code of their own: with a way out for each of eight columns behind every store the last step
+    // is so long that it is fetched from memory again and again.
+    constexpr int kItems = NT * MP, kAheadBy = LAST == kGateBack ? sizeof(T) == 2 ? 4 : 2 : 1;
+    auto items = [&](auto inside) {
+        constexpr bool kInside = decltype(inside)::value;
+        auto left = [&](int col) { return kInside ? 8 : a.m - col; };
+        KeptOf<std::conditional_t<sizeof(T) == 1, float, T>> kept[kAheadBy];  // (kGateBack) what was kept is read some items ahead
+        auto fetch = [&](int t) {
+            if constexpr (LAST == kGateBack) {
                 const int col = col_at(t);
-                if (kInside || col < a.m) kept[t % kAheadBy] = kept_at<T>(a, min(row_at(t), (int64_t)a.n - 1), col, kInside ? 8 : a.m - col);
-            };
-#pragma unroll
-            for (int t = 0; t < kAheadBy; ++t) fetch(t);
-#pragma unroll
-            for (int t = 0; t < kItems; ++t) {
-                const int64_t row = row_at(t);
-                const int col = col_at(t);
-                const Eight dh = values(t, 0);
-                if (row < a.n && (kInside || col < a.m)) put_gate_back<T>(a, row, col, dh, kept[t % kAheadBy], kInside ? 8 : a.m - col);
-                if (t + kAheadBy < kItems) fetch(t + kAheadBy);
+                if (left(col) > 0) kept[t % kAheadBy] = kept_at<T>(a, kInside ? row_at(t) : min(row_at(t), (int64_t)a.n - 1), col, left(col));
             }
         };
-        if (pa.first + cols <= a.m) items(std::true_type{});
-        else items(std::false_type{});
-    } else {
+#pragma unroll
+        for (int t = 0; t < kAheadBy; ++t) fetch(t);
 #pragma unroll
         for (int t = 0; t < kItems; ++t) {
             const int64_t row = row_at(t);
@@ -628,12 +616,17 @@ __global__ __launch_bounds__(Sh::kThreads) void mm_kernel(Mm a) {
             const Eight v = values(t, 0);
             Eight u;
             if constexpr (gate) u = values(t, MT / 2);
-            if (row >= a.n || col >= a.m) continue;
-            if constexpr (gate) put_gate<T>(a, row, col, v, u);
-            else if (a.last == kPartial) put_eight(a.part + ((int64_t)split * a.n + row) * a.m + col, v, a.m - col);
-            else put_out<T>(a, row, col, v);
+            if (kInside || (row < a.n && col < a.m)) {
+                if constexpr (gate) put_gate<T>(a, row, col, v, u, left(col));
+                else if constexpr (LAST == kGateBack) put_gate_back<T>(a, row, col, v, kept[t % kAheadBy], left(col));
+                else if (a.last == kPartial) put_eight(a.part + ((int64_t)split * a.n + row) * a.m + col, v, left(col));
+                else put_out<T>(a, row, col, v, left(col));
+            }
+            if (t + kAheadBy < kItems) fetch(t + kAheadBy);
         }
-    }
+    };
+    if (pa.first + cols <= a.m && pb.first + Sh::BN <= a.n) items(std::true_type{});
+    else items(std::false_type{});
 }
 
 // ---- the parts' sums, and the last step ---------------------------------------------------------------------------
@@ -669,10 +662,10 @@ __global__ __launch_bounds__(256) void mm_join_kernel(Mm a) {
     }
     if (!there) return;
     if constexpr (sizeof(T) > 1) {
-        if (gate) return put_gate<T>(a, row, col, s, u);
+        if (gate) return put_gate<T>(a, row, col, s, u, a.m - col);
         if (a.last == kGateBack) return put_gate_back<T>(a, row, col, s, kept_at<T>(a, row, col, a.m - col), a.m - col);
     }
-    put_out<T>(a, row, col, s);
+    put_out<T>(a, row, col, s, a.m - col);
 }
 
 // ---- few rows --------------------------------------------------------------------------------------------------------
@@ -783,8 +776,8 @@ __global__ __launch_bounds__(1024) void mm_thin_kernel(Mm a) {
             for (int e = 0; e < 8; ++e) v.e[e] += p[w * kSides * NB * 256 + e];
         return v;
     };
-    if constexpr (GATE) put_gate<T>(a, row, col, sum(0), sum(1));
-    else put_out<T>(a, row, col, sum(0));
+    if constexpr (GATE) put_gate<T>(a, row, col, sum(0), sum(1), a.m - col);
+    else put_out<T>(a, row, col, sum(0), a.m - col);
 }
 
 constexpr int kThinRows = 32;
