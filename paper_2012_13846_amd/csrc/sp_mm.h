@@ -307,12 +307,39 @@ struct Direct {
     }
 };
 
-// Through registers, element by element where a row ends
+// Through registers, by unaligned loads.  Steps but the last need no care: a direct operand's pieces lie within their rows, a turned one's may hold
+// elements of the next row, behind its own, which reach only results that there are not; rows and columns that there are not have another's
+// elements.  The last step is loaded with zeros behind the contraction's end, element by element where a row ends.
 template <typename T, int ROWS, bool TURNED, int THREADS>
 struct Through {
     using S = Side<T, ROWS, TURNED, THREADS>;
     uint4 held[S::kLoads];
+    uint32_t off[S::kLoads];
+    bool quick;
+    __device__ __forceinline__ void aim(const Place& o, bool gate) {
+        // (a turned piece of the last row but one, which may begin in the last column, ends within the last row)
+        quick = !TURNED || o.ld >= (S::K::kPer - 1) * (int64_t)sizeof(T);
+#pragma unroll
+        for (int j = 0; j < S::kLoads; ++j) {
+            const int r = S::row(j), e = S::piece(j) * S::K::kPer;
+            if constexpr (TURNED) {
+                off[j] = (uint32_t)(r * o.ld + (o.first + e < o.count ? e : 0) * (int)sizeof(T));
+            } else {
+                const int q = gate && j >= S::kLoads / 2 ? r - ROWS / 2 : r;
+                off[j] = (uint32_t)(min(q, o.count - 1 - o.first) * o.ld + e * (int)sizeof(T));
+            }
+        }
+    }
     __device__ __forceinline__ void load(const Place& o, int step, bool gate, int64_t ups) {
+        if (quick && (step + 1) * (int64_t)S::K::kElems < o.k) {
+            const char* at = TURNED ? o.p + (int64_t)step * S::K::kElems * o.ld + (int64_t)o.first * sizeof(T) : o.p + (int64_t)o.first * o.ld + (int64_t)step * kStepBytes;
+#pragma unroll
+            for (int j = 0; j < S::kLoads; ++j) __builtin_memcpy(&held[j], at + (gate && j >= S::kLoads / 2 ? ups : 0) + off[j], 16);
+        } else {
+            load_last(o, step, gate, ups);
+        }
+    }
+    __device__ __forceinline__ void load_last(const Place& o, int step, bool gate, int64_t ups) {
 #pragma unroll
         for (int j = 0; j < S::kLoads; ++j) {
             const int r = S::row(j), e = S::piece(j) * S::K::kPer;
@@ -558,6 +585,7 @@ __global__ __launch_bounds__(Sh::kThreads) void mm_kernel(Mm a) {
     } else {
         Through<T, Sh::BM, TA, kThreads> la;
         Through<T, Sh::BN, TB, kThreads> lb;
+        la.aim(pa, gate), lb.aim(pb, false);
         if (count > 0) la.load(pa, begin, gate, ups), lb.load(pb, begin, false, 0);
 #pragma unroll 1
         for (int k = 0; k < count; ++k) {
