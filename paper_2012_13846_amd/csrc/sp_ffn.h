@@ -30,25 +30,25 @@ int ffn_bwd(const Ffn& f, hipStream_t s) {
     constexpr int E = sizeof(T);
     const T* h = static_cast<const T*>(f.kept) + 2 * f.m;
     T* dgu = reinterpret_cast<T*>(f.work);
-    float* part = reinterpret_cast<float*>(f.work + up256(2 * f.n * f.m * E));
+    char* part = f.work + up256(2 * f.n * f.m * E);
     const int64_t row_c = (int64_t)f.c * E, row_m = (int64_t)f.m * E;
-    if (f.n > 0) {
-        Mm a{};
-        a.first = f.w_out, a.ld_first = row_m, a.second = f.dy, a.ld_second = row_c;
-        a.m = f.m, a.n = (int)f.n, a.k = f.c, a.last = kGateBack, a.kept = f.kept, a.dgu = dgu, a.act = f.act;
-        SP_TRY((mm<T, true, false>(a, part, s)));
-        Mm b{};
-        b.first = f.w_in, b.ld_first = row_c, b.second = dgu, b.ld_second = 2 * row_m;
-        b.m = f.c, b.n = (int)f.n, b.k = 2 * f.m, b.last = kStore, b.out = f.dx, b.ld = f.c;
-        SP_TRY((mm<T, true, false>(b, part, s)));
+    Mm of[3] = {};
+    Mm &x = of[0], &in = of[1], &out = of[2];
+    x.first = f.w_in, x.ld_first = row_c, x.second = dgu, x.ld_second = 2 * row_m;
+    x.m = f.c, x.n = (int)f.n, x.k = 2 * f.m, x.last = kStore, x.out = f.dx, x.ld = f.c;
+    in.first = f.x, in.ld_first = row_c, in.second = dgu, in.ld_second = 2 * row_m;
+    in.m = f.c, in.n = 2 * f.m, in.k = (int)f.n, in.last = kStore, in.out = f.dw_in, in.ld = f.c;
+    out.first = h, out.ld_first = kKept<T> * row_m, out.second = f.dy, out.ld_second = row_c;
+    out.m = f.m, out.n = f.c, out.k = (int)f.n, out.last = kStore, out.out = f.dw_out, out.ld = f.m;
+    if (f.n == 0) {
+        SP_TRY((mm<T, true, true>(in, reinterpret_cast<float*>(part), s)));
+        return mm<T, true, true>(out, reinterpret_cast<float*>(part), s);
     }
-    Mm w{};
-    w.first = f.x, w.ld_first = row_c, w.second = dgu, w.ld_second = 2 * row_m;
-    w.m = f.c, w.n = 2 * f.m, w.k = (int)f.n, w.last = kStore, w.out = f.dw_in, w.ld = f.c;
-    SP_TRY((mm<T, true, true>(w, part, s)));
-    w.first = h, w.ld_first = kKept<T> * row_m, w.second = f.dy, w.ld_second = row_c;
-    w.m = f.m, w.n = f.c, w.out = f.dw_out, w.ld = f.m;
-    return mm<T, true, true>(w, part, s);
+    Mm a{};
+    a.first = f.w_out, a.ld_first = row_m, a.second = f.dy, a.ld_second = row_c;
+    a.m = f.m, a.n = (int)f.n, a.k = f.c, a.last = kGateBack, a.kept = f.kept, a.dgu = dgu, a.act = f.act;
+    SP_TRY((mm<T, true, false>(a, reinterpret_cast<float*>(part), s)));
+    return mm_three<T>(of, part, s);
 }
 
 }  // namespace sp

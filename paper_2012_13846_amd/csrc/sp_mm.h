@@ -402,24 +402,28 @@ constexpr int depth_of() {
 // EXACT (8-bit operands): codes become bf16, which holds them and their scales exactly, for the bf16 products.  The 8-bit products themselves take
 // eight neighbouring elements at a time and cut their products off at 2^-13 of the largest's power of two (found by cancelling that one); of
 // random rows 1.5e-5 of the result, whatever their length, against 1e-8: far below a bf16 result's rounding (1.7e-3), but not an fp32 one's.
+template <typename T, typename Sh, bool VEC>
+struct Room {  // LDS: [ST][tile of the first operand, of the second], [2][scales]
+    static constexpr int kStage = (Sh::BM + Sh::BN) * kStepBytes, kWords = sizeof(T) == 1 ? Sh::BM + Sh::BN : 0;
+    static constexpr int ST = VEC ? depth_of<T, Sh>() : 2, kBytes = ST * kStage + 2 * kWords * 4;
+};
+
 template <typename T, typename Sh, bool TA, bool TB, bool VEC, bool EXACT, Last LAST>
-__global__ __launch_bounds__(Sh::kThreads) void mm_kernel(Mm a) {
+__device__ __forceinline__ void mm_body(const Mm& a, uint32_t block, char* room) {
     using K = Kind<T>;
     constexpr int kThreads = Sh::kThreads, MT = Sh::BM / Sh::WM / 16, NT = Sh::BN / Sh::WN / 16;
     static_assert(MT % 2 == 0 && NT % 2 == 0, "blocks come in pairs");
     constexpr bool gate = LAST == kGate;
     static_assert(!gate || (MT % 4 == 0 && !TA), "a wavefront has as many pairs of gates as of ups");
-    constexpr int kStage = (Sh::BM + Sh::BN) * kStepBytes, kWords = sizeof(T) == 1 ? Sh::BM + Sh::BN : 0;
-    constexpr int ST = VEC ? depth_of<T, Sh>() : 2;
+    constexpr int kStage = Room<T, Sh, VEC>::kStage, kWords = Room<T, Sh, VEC>::kWords, ST = Room<T, Sh, VEC>::ST;
     constexpr bool kAhead = VEC && sizeof(T) > 1;
     using A = Side<T, Sh::BM, TA, kThreads>;
     using B = Side<T, Sh::BN, TB, kThreads>;
-    __shared__ char room[ST * kStage + 2 * kWords * 4] __attribute__((aligned(16)));  // [ST][tile of the first operand, of the second], [2][scales]
     // Neighbouring workgroups of an XCD: up to kBand tiles of rows, then the next tile of columns, so that its L2 serves both operands.  Each band begins
     // 5/8 of the columns behind the last: XCDs that go through equal columns of their rows at a time write to, and read the first operand from, the same
     // memory channels where rows are a power of two apart (8192 x 16384 results of 2048 in bf16, bands of 8 that all begin at column 0: 456 us, so: 403).
     constexpr uint32_t kBand = 6;
-    const uint32_t tiles = (uint32_t)a.tiles_m * a.tiles_n, item = item_of_block(blockIdx.x, tiles * a.splits);
+    const uint32_t tiles = (uint32_t)a.tiles_m * a.tiles_n, item = item_of_block(block, tiles * a.splits);
     const uint32_t split = item / tiles, t = item - split * tiles;
     const uint32_t band = kBand * a.tiles_m, b = t / band, in = t - b * band, high = min(kBand, a.tiles_n - kBand * b);
     const uint32_t turned = in / high + b % 8 * 5 * a.tiles_m / 8;
@@ -657,15 +661,36 @@ __global__ __launch_bounds__(Sh::kThreads) void mm_kernel(Mm a) {
     else items(std::false_type{});
 }
 
+template <typename T, typename Sh, bool TA, bool TB, bool VEC, bool EXACT, Last LAST>
+__global__ __launch_bounds__(Sh::kThreads) void mm_kernel(Mm a) {
+    __shared__ char room[Room<T, Sh, VEC>::kBytes] __attribute__((aligned(16)));
+    mm_body<T, Sh, TA, TB, VEC, EXACT, LAST>(a, blockIdx.x, room);
+}
+
+// Three products that do not wait for each other, the first of a turned and a direct operand, the others of turned ones, in one launch: small ones
+// leave most of the chip idle, and a launch takes the host 2.7 us.
+struct Three {
+    Mm p[3];
+    uint32_t end[3];  // workgroups up to and with each
+};
+template <typename T, typename Sh, bool VEC0, bool VEC>
+__global__ __launch_bounds__(Sh::kThreads) void mm_three_kernel(Three t) {
+    constexpr int kRoom = Room<T, Sh, VEC0>::kBytes > Room<T, Sh, VEC>::kBytes ? Room<T, Sh, VEC0>::kBytes : Room<T, Sh, VEC>::kBytes;
+    __shared__ char room[kRoom] __attribute__((aligned(16)));
+    const uint32_t block = blockIdx.x;
+    if (block < t.end[0]) return mm_body<T, Sh, true, false, VEC0, false, kStore>(t.p[0], block, room);
+    const int i = block < t.end[1] ? 1 : 2;
+    mm_body<T, Sh, true, true, VEC, false, kStore>(t.p[i], block - t.end[i - 1], room);
+}
+
 // ---- the parts' sums, and the last step ---------------------------------------------------------------------------
 // a.m: the results' columns (of a gate: the hidden width, parts have 2 m columns).  GROUPS threads share the parts of eight columns, each GROUPS-th of
 // them in order, and the threads' sums are added in order: 42 parts of 540 x 100 results one after another took 20 us.
 template <typename T, int GROUPS>
-__global__ __launch_bounds__(256) void mm_join_kernel(Mm a) {
+__device__ __forceinline__ void mm_join(const Mm& a, uint32_t block, Eight* room) {
     constexpr int kItems = 256 / GROUPS;
-    __shared__ Eight room[GROUPS > 1 ? 2 * 256 : 1];
     const int each = (a.m + 7) / 8, item = threadIdx.x % kItems, group = threadIdx.x / kItems;
-    const int64_t i = (int64_t)blockIdx.x * kItems + item, row = i / each;
+    const int64_t i = (int64_t)block * kItems + item, row = i / each;
     const bool there = row < a.n, gate = a.last == kGate;
     const int col = (int)(i - row * each) * 8, wide = gate ? 2 * a.m : a.m;
     auto sum = [&](int at) {
@@ -694,6 +719,19 @@ __global__ __launch_bounds__(256) void mm_join_kernel(Mm a) {
         if (a.last == kGateBack) return put_gate_back<T>(a, row, col, s, kept_at<T>(a, row, col, a.m - col), a.m - col);
     }
     put_out<T>(a, row, col, s, a.m - col);
+}
+
+template <typename T, int GROUPS>
+__global__ __launch_bounds__(256) void mm_join_kernel(Mm a) {
+    __shared__ Eight room[GROUPS > 1 ? 2 * 256 : 1];
+    mm_join<T, GROUPS>(a, blockIdx.x, room);
+}
+template <typename T>
+__global__ __launch_bounds__(256) void mm_join_three_kernel(Three t) {
+    __shared__ Eight room[2 * 256];
+    const uint32_t block = blockIdx.x;
+    const int i = block < t.end[0] ? 0 : block < t.end[1] ? 1 : 2;
+    mm_join<T, 8>(t.p[i], i ? block - t.end[i - 1] : block, room);
 }
 
 // ---- few rows --------------------------------------------------------------------------------------------------------
@@ -832,6 +870,7 @@ enum ShapeName { kLarge, kMiddle, kNarrow, kFew };
 struct Plan {
     ShapeName shape;
     int splits, per_split, tiles_m, tiles_n;
+    double time;  // us, about
 };
 // rows: of the first operand (a gate: 2 m); k_bytes: of a row of the contraction
 enum MmType { kF32, kBf16, kQ8, kQ8Exact };
@@ -852,13 +891,18 @@ int mm_launch(const Mm& a, hipStream_t s) {
     return SP_OK;
 }
 
+// Are both operands' rows whole, aligned 16-byte pieces?
+template <typename T>
+bool mm_whole(const Mm& a, bool turned_first, bool turned_second) {
+    auto whole = [](const void* p, int64_t ld, int64_t row) { return aligned16(p) && ld % 16 == 0 && row * (int64_t)sizeof(T) % 16 == 0; };
+    return whole(a.first, a.ld_first, turned_first ? a.m : a.k) && whole(a.second, a.ld_second, turned_second ? a.n : a.k);
+}
+
 // Fills in what is left of `a` (steps, tiles, parts) and enqueues the product.  part: mm_work() bytes.
 template <typename T, bool TA, bool TB>
 int mm(Mm a, float* part, hipStream_t s) {
     const bool gate = a.last == kGate;
-    // both operands' rows are whole, aligned 16-byte pieces
-    auto whole = [](const void* p, int64_t ld, int64_t row) { return aligned16(p) && ld % 16 == 0 && row * (int64_t)sizeof(T) % 16 == 0; };
-    const bool pieces = whole(a.first, a.ld_first, TA ? a.m : a.k) && whole(a.second, a.ld_second, TB ? a.n : a.k);
+    const bool pieces = mm_whole<T>(a, TA, TB);
     const int64_t k_bytes = (int64_t)a.k * (int)sizeof(T);
     if constexpr (!TA && !TB)
         if (a.n <= kThinRows) {
@@ -921,6 +965,74 @@ int mm(Mm a, float* part, hipStream_t s) {
 }
 
 inline int64_t up256(int64_t b) { return (b + 255) / 256 * 256; }
+
+// Of three products rows x n over a contraction: one launch's workgroups, or none if three launches are as fast.
+struct Size {
+    int64_t rows, n, k_bytes;
+};
+struct PlanThree {
+    bool together;
+    Plan p[3];
+};
+PlanThree mm_plan_three(const Size (&of)[3], MmType type, bool pieces);
+inline int64_t mm_work_three(const Size (&of)[3], MmType type, bool pieces) {
+    const PlanThree t = mm_plan_three(of, type, pieces);
+    int64_t bytes = 0;
+    for (int i = 0; i < 3; ++i)
+        if (t.together && t.p[i].splits > 1) bytes += up256((int64_t)t.p[i].splits * of[i].rows * of[i].n * 4);
+    return bytes;
+}
+
+// The first of a turned and a direct operand, the others of turned ones; every one kStore.  part: mm_work_three() bytes, and mm_work() of each.
+template <typename T>
+int mm_three(const Mm (&of)[3], char* part, hipStream_t s) {
+    const MmType type = sizeof(T) == 4 ? kF32 : kBf16;
+    Size size[3];
+    bool whole[3];
+    for (int i = 0; i < 3; ++i) {
+        size[i] = Size{of[i].m, of[i].n, (int64_t)of[i].k * (int)sizeof(T)};
+        whole[i] = mm_whole<T>(of[i], true, i > 0);
+    }
+    const PlanThree plan = mm_plan_three(size, type, whole[0] && whole[1] && whole[2]);
+    if (!plan.together) {
+        SP_TRY((mm<T, true, false>(of[0], reinterpret_cast<float*>(part), s)));
+        SP_TRY((mm<T, true, true>(of[1], reinterpret_cast<float*>(part), s)));
+        return mm<T, true, true>(of[2], reinterpret_cast<float*>(part), s);
+    }
+    Three t{}, join{};
+    uint32_t blocks = 0, joins = 0;
+    for (int i = 0; i < 3; ++i) {
+        const Plan& p = plan.p[i];
+        Mm& a = t.p[i];
+        a = of[i];
+        a.steps = (int)((size[i].k_bytes + kStepBytes - 1) / kStepBytes);
+        a.per_split = p.per_split, a.splits = p.splits, a.tiles_m = p.tiles_m, a.tiles_n = p.tiles_n;
+        join.p[i] = a;
+        if (p.splits > 1) {
+            a.last = kPartial, a.part = join.p[i].part = reinterpret_cast<float*>(part);
+            part += up256((int64_t)p.splits * a.n * a.m * 4);
+            joins += (uint32_t)(((int64_t)((a.m + 7) / 8) * a.n + 31) / 32);
+        }
+        blocks += (uint32_t)p.tiles_m * p.tiles_n * p.splits;
+        t.end[i] = blocks, join.end[i] = joins;
+    }
+    auto go = [&](auto shape, auto vec0, auto vec) {
+        hipLaunchKernelGGL((mm_three_kernel<T, decltype(shape), decltype(vec0)::value, decltype(vec)::value>), dim3(blocks), dim3(256), 0, s, t);
+    };
+    auto with = [&](auto shape) {
+        const bool vec = whole[1] && whole[2];
+        if (whole[0]) vec ? go(shape, std::true_type{}, std::true_type{}) : go(shape, std::true_type{}, std::false_type{});
+        else vec ? go(shape, std::false_type{}, std::true_type{}) : go(shape, std::false_type{}, std::false_type{});
+    };
+    if (plan.p[0].shape == kMiddle) with(Middle{});
+    else with(Narrow{});
+    SP_HIP(hipGetLastError());
+    if (joins) {
+        hipLaunchKernelGGL(mm_join_three_kernel<T>, dim3(joins), dim3(256), 0, s, join);
+        SP_HIP(hipGetLastError());
+    }
+    return SP_OK;
+}
 
 // the feed-forward block's products (sp_ffn_f32.hip, sp_ffn_bf16.hip)
 struct Ffn {

@@ -8,20 +8,24 @@ namespace sp {
 // Workgroups of each shape, and the microseconds that a step of 128 bytes takes of one that has a CU to itself and of two that share it, as measured
 // over products of 64 to 70001 rows and widths of 64 to 8192; what a product takes beside them: 3.5 us, 2 us for each round of workgroups (what the
 // first tiles wait for, and the results' way out), and to join parts 3.5 us and their way to memory and back at 4 bytes a picosecond.
+namespace {
+struct Cost {
+    ShapeName name;
+    int bm, bn;
+    double alone[4], shared[4];  // by type; shared 0: a CU holds one
+};
+//                                f32   bf16  8 bits, and exactly
+constexpr Cost kCosts[] = {{kLarge, 256, 256, {7.9, 1.35, 1.7, 0}, {0, 0, 0, 0}},
+                           {kMiddle, 128, 128, {2.0, 0.6, 0.75, 1.15}, {4.06, 1.0, 1.13, 1.96}},
+                           {kNarrow, 64, 128, {1.15, 0.37, 0.55, 0.85}, {2.1, 0.65, 0.81, 1.26}},
+                           {kFew, 128, 32, {0.7, 0.35, 0, 0}, {1.1, 0.55, 0, 0}}};
+constexpr double kLaunch = 3.5, kRound = 2;
+double join_time(int64_t splits, int64_t rows, int64_t n) { return 8.0 * (double)splits * (double)rows * (double)n / 4e6; }
+}  // namespace
+
 Plan mm_plan(int64_t rows, int64_t n, int64_t k_bytes, MmType type, bool pieces) {
-    struct Cost {
-        ShapeName name;
-        int bm, bn;
-        double alone[4], shared[4];  // by type; shared 0: a CU holds one
-    };
-    //                              f32   bf16  8 bits, and exactly
-    static constexpr Cost kCosts[] = {{kLarge, 256, 256, {7.9, 1.35, 1.7, 0}, {0, 0, 0, 0}},
-                                      {kMiddle, 128, 128, {2.0, 0.6, 0.75, 1.15}, {4.06, 1.0, 1.13, 1.96}},
-                                      {kNarrow, 64, 128, {1.15, 0.37, 0.55, 0.85}, {2.1, 0.65, 0.81, 1.26}},
-                                      {kFew, 128, 32, {0.7, 0.35, 0, 0}, {1.1, 0.55, 0, 0}}};
     const int64_t steps = (k_bytes + kStepBytes - 1) / kStepBytes;
-    Plan best{kMiddle, 1, (int)steps, 1, 1};
-    double least = 1e300;
+    Plan best{kMiddle, 1, (int)steps, 1, 1, 1e300};
     for (const Cost& kind : kCosts) {
         if (kind.name == kLarge && (!pieces || type == kQ8Exact)) continue;
         if ((kind.name == kFew) != (n <= kThinRows && type < kQ8)) continue;
@@ -29,20 +33,52 @@ Plan mm_plan(int64_t rows, int64_t n, int64_t k_bytes, MmType type, bool pieces)
         if (tiles > 0x7fffffff) continue;
         const double alone = kind.alone[type], shared = kind.shared[type];
         int64_t last = 0;
-        for (int64_t want = 1; want <= 128 && want <= std::max<int64_t>(1, steps / 2); want = want < 4 ? want + 1 : want + want / 3) {
+        for (int64_t want = 1; want <= 128 && want <= std::max<int64_t>(1, steps / 2); want = want < 4 ? want + 1 : want + want / 2) {
             int64_t each = std::max<int64_t>(1, (steps + want - 1) / want);
             if (type >= kQ8 && want > 1) each = (each + 3) / 4 * 4;  // a word of scales is four steps'
             const int64_t splits = std::max<int64_t>(1, (steps + each - 1) / each);
             if (splits == last || tiles * splits > 0x7fffffff) continue;
             last = splits;
             const int64_t groups = tiles * splits, slots = shared > 0 ? 512 : 256, rest = groups % slots;
-            double time = 3.5 + (double)(groups / slots) * ((double)each * (shared > 0 ? shared : alone) + 2);
-            if (rest) time += (double)each * (rest <= 256 ? alone : shared) + 2;
-            if (splits > 1) time += 3.5 + 8.0 * (double)splits * (double)rows * (double)n / 4e6;
-            if (time < least) {
-                least = time;
-                best = Plan{kind.name, (int)splits, (int)each, (int)tiles_m, (int)tiles_n};
+            double time = kLaunch + (double)(groups / slots) * ((double)each * (shared > 0 ? shared : alone) + kRound);
+            if (rest) time += (double)each * (rest <= 256 ? alone : shared) + kRound;
+            if (splits > 1) time += kLaunch + join_time(splits, rows, n);
+            if (time < best.time) best = Plan{kind.name, (int)splits, (int)each, (int)tiles_m, (int)tiles_n, time};
+        }
+    }
+    return best;
+}
+
+// Every workgroup has at most so many steps, whichever product it is of: those are handed out as CUs come free.
+PlanThree mm_plan_three(const Size (&of)[3], MmType type, bool pieces) {
+    PlanThree best{};
+    double least = 0;
+    for (const Size& o : of) least += mm_plan(o.rows, o.n, o.k_bytes, type, pieces).time;
+    for (const Cost& kind : kCosts) {
+        if (kind.name != kMiddle && kind.name != kNarrow) continue;
+        const double alone = kind.alone[type], shared = kind.shared[type];
+        for (int64_t most = 4; most <= 4096; most += most < 16 ? 4 : most / 2) {
+            PlanThree t{true, {}};
+            double work = 0, joins = 0;
+            int64_t groups = 0, longest = 0;
+            for (int i = 0; i < 3; ++i) {
+                const int64_t steps = (of[i].k_bytes + kStepBytes - 1) / kStepBytes;
+                const int64_t tiles_m = (of[i].rows + kind.bm - 1) / kind.bm, tiles_n = (of[i].n + kind.bn - 1) / kind.bn;
+                const int64_t want = (steps + most - 1) / most, each = (steps + want - 1) / want, splits = (steps + each - 1) / each;
+                if (tiles_m > 1 << 20 || tiles_n > 1 << 20 || splits > 128) {
+                    groups = (int64_t)1 << 40;
+                    break;
+                }
+                groups += tiles_m * tiles_n * splits;
+                longest = std::max(longest, each);
+                work += (double)(tiles_m * tiles_n) * ((double)steps * shared + (double)splits * kRound);
+                if (splits > 1) joins += join_time(splits, of[i].rows, of[i].n) + (joins > 0 ? 0 : kLaunch);
+                t.p[i] = Plan{kind.name, (int)splits, (int)each, (int)tiles_m, (int)tiles_n, 0};
             }
+            if (groups > 1 << 20) continue;
+            // (an uneven end: half a workgroup's time)
+            const double time = kLaunch + joins + (groups <= 256 ? (double)longest * alone + kRound : std::max(work / 512 + (double)longest * shared / 2, (double)longest * shared + kRound));
+            if (time < least) least = time, best = t;
         }
     }
     return best;
@@ -55,8 +91,11 @@ static int64_t ffn_work(int64_t n, int c, int m, int size, bool backward) {
         if (!backward) {
             part = std::max({part, mm_work(2 * (int64_t)m, n, (int64_t)c * size, type, true, pieces), mm_work(c, n, (int64_t)m * size, type, true, pieces)});
         } else {
-            part = std::max({part, mm_work(m, n, (int64_t)c * size, type, false, pieces), mm_work(c, n, 2 * (int64_t)m * size, type, false, pieces),
-                             mm_work(c, 2 * (int64_t)m, n * size, type, false, pieces), mm_work(m, c, n * size, type, false, pieces)});
+            const int64_t c_bytes = (int64_t)c * size, n_bytes = n * size;
+            const Size of[3] = {{c, n, 2 * (int64_t)m * size}, {c, 2 * (int64_t)m, n_bytes}, {m, c, n_bytes}};
+            part = std::max(part, mm_work(m, n, c_bytes, type, false, pieces));
+            for (const Size& o : of) part = std::max(part, mm_work(o.rows, o.n, o.k_bytes, type, false, pieces));
+            if (n > 0) part = std::max(part, mm_work_three(of, type, pieces));
         }
     }
     return up256((backward ? 2 : 1) * n * m * size) + up256(part) + 256;
