@@ -85,16 +85,34 @@ __device__ __forceinline__ Eight get_eight(const T* p, int left) {
 }
 
 // act(g) and its derivative.  For bf16 by the exponential and reciprocal instructions (an ulp each; the exponential's argument is off by |g| 2^-24,
-// as its result is then in relation): 2^-20 where the gate is not yet 2^-16 of g, against the 2^-8 of a rounding.
-template <typename T>
-__device__ __forceinline__ float2 gate_of(float g, int act) {
+// as its result is then in relation): 2^-20 where the gate is not yet 2^-16 of g, against the 2^-8 of a rounding.  The normal distribution's tail
+// beyond |g| is then exp(-g^2 / 2) t q(t) with t = 1 / (1 + 0.28 |g|) and q of degree 8, fitted to erfcx in fp64 with the least largest relative
+// error, 1.8e-7: its exponential is the derivative's, too.
+template <typename T, int ACT>
+__device__ __forceinline__ float2 gate_of(float g) {
     constexpr bool kQuick = sizeof(T) == 2;
-    if (act == SP_GATE_SILU) {
+    if constexpr (ACT == SP_GATE_SILU) {
         const float p = kQuick ? __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504f * g)) : 1.f / (1.f + expf(-g));
         return float2{g * p, p * (1.f + g * (1.f - p))};
+    } else if constexpr (kQuick) {
+        const float e = __builtin_amdgcn_exp2f(-0.72134752f * g * g), t = __builtin_amdgcn_rcpf(fmaf(0.28f, fabsf(g), 1.f));
+        constexpr float q[9] = {0.111703858f, 0.111699802f, 0.103084684f, 0.0836305994f, 0.072775931f, -0.00645151077f, 0.0924313212f, -0.093595375f, 0.0247206059f};
+        float v = q[8];
+#pragma unroll
+        for (int i = 7; i >= 0; --i) v = fmaf(v, t, q[i]);
+        v *= e * t;
+        const float p = g < 0.f ? v : 1.f - v;
+        return float2{g * p, p + g * 0.39894228f * e};
+    } else {
+        const float p = 0.5f * (1.f + erff(g * 0.70710678f));
+        return float2{g * p, p + g * 0.39894228f * expf(-0.5f * g * g)};
     }
-    const float p = 0.5f * (1.f + erff(g * 0.70710678f)), e = kQuick ? __builtin_amdgcn_exp2f(-0.72134752f * g * g) : expf(-0.5f * g * g);
-    return float2{g * p, p + g * 0.39894228f * e};
+}
+// f(std::integral_constant): of the gate, once for many values (a question at each is a third of the last step's instructions)
+template <typename F>
+__device__ __forceinline__ void with_act(int act, F f) {
+    if (act == SP_GATE_SILU) f(std::integral_constant<int, SP_GATE_SILU>{});
+    else f(std::integral_constant<int, SP_GATE_GELU>{});
 }
 
 // What the backward pass reads of a row, m values each: g | u | act(g) * u, in bf16 g and u cut off behind 16 bits and the next 8 bits of both in a
@@ -119,38 +137,60 @@ __device__ __forceinline__ void keep(const Mm& a, int64_t row, int col, const Ei
         put_eight(to, hg, left), put_eight(to + a.m, hu, left), put_eight(to + 3 * (int64_t)a.m, lo, left);
     }
 }
-// The same as it lies in memory
+// The same as it lies in memory, in whole words: 16-bit elements by themselves take a register each
 template <typename T>
 struct KeptOf {
-    EightOf<T> g, u, lo;  // lo: bf16 only
+    static constexpr int kWords = 2 * (int)sizeof(T);
+    uint32_t g[kWords], u[kWords], lo[kWords];  // lo: bf16 only
 };
+template <typename T>
+__device__ __forceinline__ void get_words(const T* p, int left, uint32_t (&w)[2 * sizeof(T)]) {
+    if (left >= 8) {
+        __builtin_memcpy(w, p, sizeof w);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < (int)(2 * sizeof(T)); ++i) w[i] = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (i < left) {
+            if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(p[i]);
+            else w[i / 2] |= (uint32_t)p[i] << (16 * (i & 1));
+        }
+}
 template <typename T>
 __device__ __forceinline__ KeptOf<T> kept_at(const Mm& a, int64_t row, int col, int left) {
     const T* from = static_cast<const T*>(a.kept) + row * kKept<T> * a.m + col;
-    KeptOf<T> k{get_piece(from, left), get_piece(from + a.m, left), EightOf<T>{}};
-    if constexpr (sizeof(T) == 2) k.lo = get_piece(from + 3 * (int64_t)a.m, left);
+    KeptOf<T> k;
+    get_words(from, left, k.g), get_words(from + a.m, left, k.u);
+    if constexpr (sizeof(T) == 2) get_words(from + 3 * (int64_t)a.m, left, k.lo);
     return k;
 }
 template <typename T>
 __device__ __forceinline__ float2 gate_and_up(const KeptOf<T>& k, int i) {
-    if constexpr (sizeof(T) == 4) return float2{k.g.e[i], k.u.e[i]};
-    else return float2{__uint_as_float((uint32_t)k.g.e[i] << 16 | (k.lo.e[i] & 255u) << 8), __uint_as_float((uint32_t)k.u.e[i] << 16 | (k.lo.e[i] & 0xff00u))};
+    if constexpr (sizeof(T) == 4) {
+        return float2{__uint_as_float(k.g[i]), __uint_as_float(k.u[i])};
+    } else {
+        const uint32_t g = k.g[i / 2], u = k.u[i / 2], lo = k.lo[i / 2];
+        return i & 1 ? float2{__uint_as_float((g & 0xffff0000u) | (lo >> 8 & 0xff00u)), __uint_as_float((u & 0xffff0000u) | (lo >> 16 & 0xff00u))}
+                     : float2{__uint_as_float(g << 16 | (lo << 8 & 0xff00u)), __uint_as_float(u << 16 | (lo & 0xff00u))};
+    }
 }
 
-template <typename T>
+template <typename T, int ACT>
 __device__ __forceinline__ void put_gate(const Mm& a, int64_t row, int col, const Eight& g, const Eight& u, int left) {
     Eight h;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) h.e[i] = gate_of<T>(g.e[i], a.act).x * u.e[i];
+    for (int i = 0; i < 8; ++i) h.e[i] = gate_of<T, ACT>(g.e[i]).x * u.e[i];
     put_rounded(static_cast<T*>(a.out) + row * a.ld + col, h, left);
     if (a.kept) keep<T>(a, row, col, g, u, left);
 }
-template <typename T>
+template <typename T, int ACT>
 __device__ __forceinline__ void put_gate_back(const Mm& a, int64_t row, int col, const Eight& dh, const KeptOf<T>& kept, int left) {
     Eight dg, du;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const float2 gu = gate_and_up(kept, i), p = gate_of<T>(gu.x, a.act);
+        const float2 gu = gate_and_up(kept, i), p = gate_of<T, ACT>(gu.x);
         dg.e[i] = dh.e[i] * gu.y * p.y;
         du.e[i] = dh.e[i] * p.x;
     }
@@ -629,8 +669,9 @@ __device__ __forceinline__ void mm_body(const Mm& a, uint32_t block, char* room)
     // Tiles that lie within the results, nearly all, have code of their own: with a way out for each of eight columns behind every store the last step
     // is so long that it is fetched from memory again and again.
     constexpr int kItems = NT * MP, kAheadBy = LAST == kGateBack ? sizeof(T) == 2 ? 4 : 2 : 1;
-    auto items = [&](auto inside) {
+    auto items = [&](auto inside, auto act) {
         constexpr bool kInside = decltype(inside)::value;
+        constexpr int kAct = decltype(act)::value;
         auto left = [&](int col) { return kInside ? 8 : a.m - col; };
         KeptOf<std::conditional_t<sizeof(T) == 1, float, T>> kept[kAheadBy];  // (kGateBack) what was kept is read some items ahead
         auto fetch = [&](int t) {
@@ -649,16 +690,23 @@ __device__ __forceinline__ void mm_body(const Mm& a, uint32_t block, char* room)
             Eight u;
             if constexpr (gate) u = values(t, MT / 2);
             if (kInside || (row < a.n && col < a.m)) {
-                if constexpr (gate) put_gate<T>(a, row, col, v, u, left(col));
-                else if constexpr (LAST == kGateBack) put_gate_back<T>(a, row, col, v, kept[t % kAheadBy], left(col));
+                if constexpr (gate) put_gate<T, kAct>(a, row, col, v, u, left(col));
+                else if constexpr (LAST == kGateBack) put_gate_back<T, kAct>(a, row, col, v, kept[t % kAheadBy], left(col));
                 else if (a.last == kPartial) put_eight(a.part + ((int64_t)split * a.n + row) * a.m + col, v, left(col));
                 else put_out<T>(a, row, col, v, left(col));
             }
-            if (t + kAheadBy < kItems) fetch(t + kAheadBy);
+            if constexpr (LAST == kGateBack) {
+                if (t + kAheadBy < kItems) fetch(t + kAheadBy);
+                __builtin_amdgcn_sched_barrier(0);  // what is ahead stays ahead: the compiler would move it to where it is used, to save registers
+            }
         }
     };
-    if (pa.first + cols <= a.m && pb.first + Sh::BN <= a.n) items(std::true_type{});
-    else items(std::false_type{});
+    auto with = [&](auto act) {
+        if (pa.first + cols <= a.m && pb.first + Sh::BN <= a.n) items(std::true_type{}, act);
+        else items(std::false_type{}, act);
+    };
+    if constexpr (gate || LAST == kGateBack) with_act(a.act, with);
+    else with(std::integral_constant<int, 0>{});
 }
 
 template <typename T, typename Sh, bool TA, bool TB, bool VEC, bool EXACT, Last LAST>
@@ -715,8 +763,11 @@ __device__ __forceinline__ void mm_join(const Mm& a, uint32_t block, Eight* room
     }
     if (!there) return;
     if constexpr (sizeof(T) > 1) {
-        if (gate) return put_gate<T>(a, row, col, s, u, a.m - col);
-        if (a.last == kGateBack) return put_gate_back<T>(a, row, col, s, kept_at<T>(a, row, col, a.m - col), a.m - col);
+        if (gate || a.last == kGateBack)
+            return with_act(a.act, [&](auto act) {
+                if (gate) put_gate<T, decltype(act)::value>(a, row, col, s, u, a.m - col);
+                else put_gate_back<T, decltype(act)::value>(a, row, col, s, kept_at<T>(a, row, col, a.m - col), a.m - col);
+            });
     }
     put_out<T>(a, row, col, s, a.m - col);
 }
@@ -842,7 +893,7 @@ __global__ __launch_bounds__(1024) void mm_thin_kernel(Mm a) {
             for (int e = 0; e < 8; ++e) v.e[e] += p[w * kSides * NB * 256 + e];
         return v;
     };
-    if constexpr (GATE) put_gate<T>(a, row, col, sum(0), sum(1), a.m - col);
+    if constexpr (GATE) with_act(a.act, [&](auto act) { put_gate<T, decltype(act)::value>(a, row, col, sum(0), sum(1), a.m - col); });
     else put_out<T>(a, row, col, sum(0), a.m - col);
 }
 
