@@ -6,8 +6,9 @@
 namespace sp {
 
 // Workgroups of each shape, and the microseconds that a step of 128 bytes takes of one that has a CU to itself and of two that share it, as measured
-// over products of 64 to 70001 rows and widths of 64 to 8192; what a product takes beside them: 3.5 us, 2 us for each round of workgroups (what the
-// first tiles wait for, and the results' way out), and to join parts 3.5 us and their way to memory and back at 4 bytes a picosecond.
+// over products of 64 to 70001 rows and widths of 64 to 8192; what a product takes beside them: 3.5 us, for each round of workgroups what the first
+// tiles wait for and the results' way out (2 us, 8 us where no other workgroup of the CU works meanwhile), and to join parts 3.5 us and their way to
+// memory and back at 4 bytes a picosecond.
 namespace {
 struct Cost {
     ShapeName name;
@@ -19,7 +20,7 @@ constexpr Cost kCosts[] = {{kLarge, 256, 256, {7.9, 1.35, 1.7, 0}, {0, 0, 0, 0}}
                            {kMiddle, 128, 128, {2.0, 0.6, 0.75, 1.15}, {4.06, 1.0, 1.13, 1.96}},
                            {kNarrow, 64, 128, {1.15, 0.37, 0.55, 0.85}, {2.1, 0.65, 0.81, 1.26}},
                            {kFew, 128, 32, {0.7, 0.35, 0, 0}, {1.1, 0.55, 0, 0}}};
-constexpr double kLaunch = 3.5, kRound = 2;
+constexpr double kLaunch = 3.5, kRound = 2, kRoundAlone = 8;
 double join_time(int64_t splits, int64_t rows, int64_t n) { return 8.0 * (double)splits * (double)rows * (double)n / 4e6; }
 }  // namespace
 
@@ -40,8 +41,9 @@ Plan mm_plan(int64_t rows, int64_t n, int64_t k_bytes, MmType type, bool pieces)
             if (splits == last || tiles * splits > 0x7fffffff) continue;
             last = splits;
             const int64_t groups = tiles * splits, slots = shared > 0 ? 512 : 256, rest = groups % slots;
-            double time = kLaunch + (double)(groups / slots) * ((double)each * (shared > 0 ? shared : alone) + kRound);
-            if (rest) time += (double)each * (rest <= 256 ? alone : shared) + kRound;
+            const double round = shared > 0 ? kRound : kRoundAlone;
+            double time = kLaunch + (double)(groups / slots) * ((double)each * (shared > 0 ? shared : alone) + round);
+            if (rest) time += (double)each * (rest <= 256 ? alone : shared) + round;
             if (splits > 1) time += kLaunch + join_time(splits, rows, n);
             if (time < best.time) best = Plan{kind.name, (int)splits, (int)each, (int)tiles_m, (int)tiles_n, time};
         }
