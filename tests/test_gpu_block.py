@@ -564,3 +564,61 @@ def test_two_streams_at_once(sp):
         torch.cuda.synchronize()
         for a, b in zip(got, want):
             assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+# ---- rows that end inside a load, small matrices in one launch, gates of every size --------------------------------
+@TYPES
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("n,c,m", [(200, 3, 5), (400, 6, 10), (333, 7, 9), (2049, 33, 70), (600, 1030, 24), (96, 4, 2050), (40, 952, 330), (3000, 100, 270)])
+def test_ffn_of_rows_that_end_inside_a_load(sp, n, c, m, act, dt):
+    """Contractions of several steps over rows of no whole 16 bytes, down to rows shorter than a load."""
+    test_ffn(sp, n, c, m, act, dt)
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("n", [7, 4000])
+def test_gates_over_their_range(sp, act, n):
+    """u = 1, W_out = 1: y is act(g), rounded once; its own error is below 6 U32 |g|.  dx (dy = 1, W_in = (1, 0; 0, 1)) is (act'(g), act(g)) as dgu is
+    rounded: the slope's error is below 8 U32 (1 + |g|)."""
+    g = torch.linspace(-12, 12, n, device="cuda").bfloat16()
+    x = torch.stack([g, torch.ones_like(g)], 1)
+    w_in, w_out = torch.eye(2, device="cuda").bfloat16(), torch.tensor([[1.0], [0.0]], device="cuda").bfloat16()
+    y, kept = sp.sp_ffn_fwd(x, w_in, w_out, act)
+    G = host(g)
+    a, da = block.gate(G, act)
+    u = half_step(BF16)
+    err = 6 * U32 * np.abs(G)
+    within(y[:, 0], a, err + u * (np.abs(a) + err), "act")
+    dx, _, _ = sp.sp_ffn_bwd(x, w_in, w_out, kept, torch.ones_like(x), act)
+    err = 8 * U32 * (1 + np.abs(G))
+    within(dx[:, 0], da, err + u * (np.abs(da) + err), "slope")
+
+
+@TYPES
+@pytest.mark.parametrize("n,c", [(1428, 128), (60, 77), (4096, 64), (4097, 64), (900, 1024), (3, 16392)])
+def test_rms_norm_gradients_in_place(sp, n, c, dt):
+    """dx in dy's or dh's memory: the same results, in one launch or several."""
+    rng = np.random.default_rng(n + c)
+    h, dy, dh = (rows(rng, dt, n, c) for _ in range(3))
+    gamma = 1 + rows(rng, F32, c, scale=0.2)
+    rstd = 1 / torch.sqrt((h.float() ** 2).mean(1) + 1e-5)
+    dx, dgamma = sp.sp_rms_norm_bwd(h, dy, gamma, rstd, dh)
+    l = sp._block_argtypes()
+    for which in (0, 1):
+        a = [dy.clone(), dh.clone()]
+        got, work = torch.empty_like(gamma), torch.empty(l.sp_rms_norm_bwd_work(n, c, sp._dt(h)), dtype=torch.uint8, device="cuda")
+        assert l.sp_rms_norm_bwd(h.data_ptr(), a[0].data_ptr(), a[1].data_ptr(), n, c, gamma.data_ptr(), rstd.data_ptr(), a[which].data_ptr(),
+                                 got.data_ptr(), work.data_ptr(), sp._dt(h), sp._stream()) == 0
+        assert torch.equal(a[which], dx) and torch.equal(got, dgamma)
+
+
+@pytest.mark.parametrize("n,c,m", [(32, 640, 77), (33, 640, 77), (70, 3000, 40), (300, 12800, 24), (1, 12900, 9), (129, 130, 260)])
+def test_q8_linear_of_many_steps(sp, n, c, m):
+    """Four steps share a word of scales, and parts begin at one: scales that differ from step to step."""
+    g = torch.Generator(device="cuda").manual_seed(n + c)
+    grow = lambda k: torch.randn((k, c), device="cuda", generator=g) * 2.0 ** torch.randint(-6, 6, (k, -(-c // 128)), device="cuda", generator=g).float().repeat_interleave(128, 1)[:, :c]  # noqa: E731
+    (x, xs), (w, ws) = sp.sp_q8_rows(grow(n)), sp.sp_q8_rows(grow(m))
+    X, W = (block.q8_values(q.view(torch.uint8).cpu().numpy(), s.view(torch.uint8).cpu().numpy()) for q, s in ((x, xs), (w, ws)))
+    Y = X @ W.T
+    for out in (F32, BF16):
+        within(sp.sp_q8_linear((x, xs), (w, ws), out), Y, q8_bound(X, W, Y, out), "y")
