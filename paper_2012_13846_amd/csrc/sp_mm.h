@@ -3,9 +3,9 @@
 // out[n][m] = sum over k of first(m, k) * second(n, k).  An operand is "direct" if its contraction runs along its rows in memory ([m][k]), and
 // "turned" if it runs across them ([k][m]).  A workgroup makes BM x BN results (first x second): in steps of 128 bytes of a direct operand's rows
 // it takes both operands' tiles from memory to LDS past the registers, ST tiles deep, and multiplies 16 x 16 blocks; turned bf16 tiles are read
-// by the transposing LDS read, so no operand is ever copied transposed.  The first operand are the results' columns, and two blocks share 32 of
-// them in turns of four (column 8 h + 4 (block & 1) + e is row 4 h + e of a block), so that a lane's accumulators of both are eight neighbouring
-// columns of one row: 16 bytes a store in bf16.  Pieces of LDS rows are swizzled so that reads are free of bank conflicts.
+// by the transposing LDS read, so no operand is ever copied transposed.  The first operand are the results' columns; at the end groups of 16 lanes
+// swap halves of two neighbouring blocks, and a lane has eight neighbouring columns of one row: 16 bytes a store in bf16.  Pieces of LDS rows are
+// swizzled so that reads are free of bank conflicts.
 // Few results are split along the contraction; the parts' sums are added in order by a second kernel, which takes the same last step.
 // Operands that are no whole, aligned 16-byte pieces go through registers by unaligned loads, with zeros behind their ends.
 #pragma once
@@ -247,34 +247,34 @@ struct Side {
     static __device__ __forceinline__ int at(int j) { return j * THREADS + (int)threadIdx.x; }
     static __device__ __forceinline__ int row(int j) { return at(j) / kC; }  // of LDS: a result, or an element of the contraction if turned
     static __device__ __forceinline__ int piece(int j) { return (at(j) % kC) ^ swizzled(row(j)); }
-    // 64 banks are 16 pieces.  Direct: 16 lanes read the same piece of rows 8 q + e (q, e < 4), of which neighbours lie 32 banks apart.  Turned bf16:
-    // 16 lanes read half of 4 neighbouring pieces of 4 neighbouring rows; turned fp32: 64 lanes a word of every other of 8 pieces of rows 4 h.
+    // 64 banks are 16 pieces.  Direct: 16 lanes read the same piece of 16 rows, of which neighbours lie 32 banks apart.  Turned bf16: 32 lanes read 2
+    // neighbouring pieces of rows 0 .. 3 and 8 .. 11; turned fp32: 64 lanes 4 pieces of rows 0, 4, 8 and 12.
     static __device__ __forceinline__ int swizzled(int r) {
-        if constexpr (!TURNED) return (r >> 1 & 1) | (r >> 3 & 3) << 1;
-        else if constexpr (sizeof(T) == 2) return kC >= 16 ? (r & 3) << 2 : kC == 8 ? (r >> 1 & 1) << 2 : 0;
-        else return (r >> 2 & 1) | (kC >= 16 ? (r >> 3 & 1) << 3 : 0);
+        if constexpr (!TURNED) return r >> 1 & 7;
+        else if constexpr (sizeof(T) == 2) return kC >= 16 ? (r & 3) << 1 | (r >> 3 & 1) << 3 : kC == 8 ? (r >> 1 & 1) << 1 | (r >> 3 & 1) << 2 : (r >> 3 & 1) << 1;
+        else return kC >= 16 ? (r >> 2 & 3) << 2 : (r >> 2 & 1) << 2;
     }
 
-    // A lane's place in the fragments of step 0 of a wavefront's 32 `at` ..
+    // A lane's place in the first fragment of a wavefront's pairs of blocks `from` ..
     int place;
     __device__ __forceinline__ void aim(int from) {
         const int l = threadIdx.x & 63, h = l >> 4, q = l >> 2 & 3, e = l & 3;
         if constexpr (!TURNED) {
-            const int r = 32 * from + 8 * q + e;
+            const int r = 32 * from + (l & 15);
             place = r * kRowBytes + ((h ^ swizzled(r)) << 4);
         } else if constexpr (sizeof(T) == 2) {
             // a transposing read: lanes 4 q + e of a group address columns 4 e .. of a block in row q, and get column 4 q + e of all four rows
             const int r = 8 * h + q;
-            place = r * kRowBytes + (((4 * from + e) ^ swizzled(r)) << 4);
+            place = r * kRowBytes + (((4 * from + (e >> 1)) ^ swizzled(r)) << 4) + ((e & 1) << 3);
         } else {
-            place = 4 * h * kRowBytes + (((8 * from + 2 * q) ^ swizzled(4 * h)) << 4) + (e << 2);
+            place = 4 * h * kRowBytes + (((8 * from + q) ^ swizzled(4 * h)) << 4) + (e << 2);
         }
     }
     // Bytes from a direct tile's block 0 to block i; `half`: rows from gates to ups, which blocks MT / 2 .. are (0: no gate)
     template <int MT>
     static __device__ __forceinline__ constexpr int block(int i, int half) {
         const int b = half && i >= MT / 2 ? i - MT / 2 : i;
-        return ((half && i >= MT / 2 ? half : 0) + 32 * (b >> 1) + 4 * (b & 1)) * kRowBytes;
+        return ((half && i >= MT / 2 ? half : 0) + 16 * b) * kRowBytes;
     }
     // block i of the wavefront (a direct tile: `off` bytes behind its first), fragment s
     __device__ __forceinline__ typename K::Frag frag(const char* tile, int i, int off, int s) const {
@@ -285,12 +285,12 @@ struct Side {
         } else if constexpr (!TURNED) {
             return __builtin_bit_cast(typename K::Frag, *reinterpret_cast<const uint4*>(tile + (place ^ (s << 6)) + off));
         } else if constexpr (sizeof(T) == 2) {
-            const char* from = tile + 32 * s * kRowBytes + (place ^ ((i >> 1) << 6)) + ((i & 1) << 3);
+            const char* from = tile + 32 * s * kRowBytes + (place ^ (i << 5));
             const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((SP_LDS s16x4*)from);
             const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((SP_LDS s16x4*)(from + 4 * kRowBytes));
             return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
         } else {
-            const char* from = tile + 16 * s * kRowBytes + (place ^ ((8 * (i >> 1) + (i & 1)) << 4));
+            const char* from = tile + 16 * s * kRowBytes + (place ^ (i << 6));
             f32x4 v;
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] = *reinterpret_cast<const float*>(from + e * kRowBytes);
@@ -511,11 +511,11 @@ __device__ __forceinline__ void mm_body(const Mm& a, uint32_t block, char* room)
     // 8 bits: the scales of a row's next four steps, a byte each; step u's (opsel) is a constant of the matrix instruction
     int sa[MT], sb[NT];
     auto take_scales = [&](int step) {
-        const int* words = reinterpret_cast<const int*>(room + ST * kStage) + (step >> 2 & 1) * kWords + 8 * (l >> 2 & 3) + (l & 3);
+        const int* words = reinterpret_cast<const int*>(room + ST * kStage) + (step >> 2 & 1) * kWords + (l & 15);
 #pragma unroll
-        for (int i = 0; i < MT; ++i) sa[i] = words[32 * (wm * MP + (i >> 1)) + 4 * (i & 1)];
+        for (int i = 0; i < MT; ++i) sa[i] = words[32 * wm * MP + 16 * i];
 #pragma unroll
-        for (int i = 0; i < NT; ++i) sb[i] = words[Sh::BM + 32 * (wn * NP + (i >> 1)) + 4 * (i & 1)];
+        for (int i = 0; i < NT; ++i) sb[i] = words[Sh::BM + 32 * wn * NP + 16 * i];
     };
     auto multiply = [&](const char* stage, auto opsel) {
         constexpr int U = decltype(opsel)::value;
@@ -642,14 +642,24 @@ __device__ __forceinline__ void mm_body(const Mm& a, uint32_t block, char* room)
         }
     }
 
+    // Blocks 2 p and 2 p + 1 hold columns 4 h .. of 32 p and 32 p + 16, h the lane's group; lanes of odd groups swap the first's with the second's of
+    // the group before: 8 (h >> 1) .. of the first, or of the second.
+#pragma unroll
+    for (int i = 0; i < MT; i += 2)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const auto both = __builtin_amdgcn_permlane16_swap(__float_as_uint(acc[i][j][e]), __float_as_uint(acc[i + 1][j][e]), false, false);
+                acc[i][j][e] = __uint_as_float(both[0]), acc[i + 1][j][e] = __uint_as_float(both[1]);
+            }
     // The last step's items of a lane: eight columns of a row each, item t = (t / MP)'s block of rows.  In 16 bits lanes r and r + 8 of a block swap a
     // pair's half, so that a store writes 128 bytes of 8 rows instead of 64 of 16.
     constexpr bool kWhole = sizeof(T) <= 2 && MP % 2 == 0;
-    auto row_at = [&](int t) {
-        const int j = t / MP, r = kWhole ? 8 * (t & 1) + (l & 7) : l & 15;
-        return (int64_t)pb.first + 32 * (wn * NP + (j >> 1)) + 8 * (r >> 2) + 4 * (j & 1) + (r & 3);
+    auto row_at = [&](int t) { return (int64_t)pb.first + 32 * wn * NP + 16 * (t / MP) + (kWhole ? 8 * (t & 1) + (l & 7) : l & 15); };
+    auto col_at = [&](int t) {
+        return pa.first + 32 * (wm * MP + (kWhole ? t % MP / 2 * 2 + (l >> 3 & 1) : t % MP)) + 16 * (l >> 4 & 1) + 8 * (l >> 5);
     };
-    auto col_at = [&](int t) { return pa.first + 32 * (wm * MP + (kWhole ? t % MP / 2 * 2 + (l >> 3 & 1) : t % MP)) + 8 * (l >> 4); };
     auto values = [&](int t, int from) {  // from: the first block of these columns
         const int j = t / MP, p = t % MP;
         Eight v;
