@@ -494,9 +494,9 @@ __device__ __forceinline__ void mm_body(const Mm& a, uint32_t block, char* room)
 #pragma unroll
         for (int i = 0; i < MT; ++i) x[i] = fa.frag(stage, i, A::template block<MT>(i, half), s);
     };
-    auto product = [&](const Frag (&x)[MT], const Frag (&y)[NT]) {
+    auto product_of = [&](const Frag (&x)[MT], const Frag (&y)[NT], auto from, auto to) {
 #pragma unroll
-        for (int i = 0; i < MT; ++i)
+        for (int i = decltype(from)::value; i < decltype(to)::value; ++i)
 #pragma unroll
             for (int v = 0; v < NT; ++v) {
                 const int j = i & 1 ? NT - 1 - v : v;  // (back and forth: 2% in a product of 2048 x 8192 x 8192)
@@ -508,6 +508,7 @@ __device__ __forceinline__ void mm_body(const Mm& a, uint32_t block, char* room)
                 }
             }
     };
+    auto product = [&](const Frag (&x)[MT], const Frag (&y)[NT]) { product_of(x, y, std::integral_constant<int, 0>{}, std::integral_constant<int, MT>{}); };
     // 8 bits: the scales of a row's next four steps, a byte each; step u's (opsel) is a constant of the matrix instruction
     int sa[MT], sb[NT];
     auto take_scales = [&](int step) {
@@ -595,11 +596,14 @@ __device__ __forceinline__ void mm_body(const Mm& a, uint32_t block, char* room)
                 if (k + ST <= count) wait_loads<(ST - 2) * kLoads>();
                 else wait_loads<0>();
                 meet();
-                if (k + ST < count) load(begin + k + ST, stage);
+                const int free = stage;
+                if (k + ST < count) la.load(pa, begin + k + ST, gate, ups, lds + free * kStage);
                 stage = stage + 1 == ST ? 0 : stage + 1;
                 take(room + stage * kStage, 0, x[0], y[0]);  // (behind the last step: a tile that is not used)
-                product(x[1], y[1]);
+                product_of(x[1], y[1], std::integral_constant<int, 0>{}, std::integral_constant<int, MT / 2>{});
                 alternate();
+                if (k + ST < count) lb.load(pb, begin + k + ST, false, 0, lds + free * kStage + A::kBytes);
+                product_of(x[1], y[1], std::integral_constant<int, MT / 2>{}, std::integral_constant<int, MT>{});
             }
         } else {
 #pragma unroll
