@@ -374,9 +374,10 @@ int sp_q8_linear(const uint8_t* d_q, const uint8_t* d_scales, int64_t n, int64_t
 
 /* Gated feed-forward block on rows x [n][c], with w_in [2 m][c] (m rows of gates, then m of ups) and w_out [c][m]:
  *   [g u] = x w_in^T;  y = (act(g) * u) w_out^T,   act silu (g / (1 + e^-g)) or gelu (g * the normal distribution function of g)
- * sp_ffn_fwd writes y [n][c] and, unless d_kept is NULL, what the backward pass reads (g, u and act(g) * u in a layout of the library's own): [n][3 m] of fp32, or [n][4 m] of bf16.  sp_ffn_bwd: gradients of sum(y * dy): dx like
- * x, dw_in and dw_out like the weights, of type dt.  Sums fp32; in bf16 act(g) * u and the gradients of g and u are rounded before they are multiplied
- * again.  All arrays dense; outputs overlap nothing.  n <= 2^30, c, m <= 2^18 (SP_ERR_UNSUPPORTED beyond). */
+ * sp_ffn_fwd writes y [n][c] and, unless d_kept is NULL, what the backward pass reads (g, u and act(g) * u in a layout of the library's own):
+ * [n][3 m] of fp32, or [n][4 m] of bf16.  sp_ffn_bwd: gradients of sum(y * dy): dx like x, dw_in and dw_out like the weights, of type dt.  Sums fp32;
+ * in bf16 act(g) * u and the gradients of g and u are rounded before they are multiplied again, g and u are kept in 24 bits.  All arrays dense;
+ * outputs overlap nothing.  n <= 2^30, c, m <= 2^18 (SP_ERR_UNSUPPORTED beyond). */
 typedef enum { SP_GATE_SILU = 0, SP_GATE_GELU = 1 } sp_gate;
 typedef struct {
     int64_t n;

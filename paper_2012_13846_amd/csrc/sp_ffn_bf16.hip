@@ -1,4 +1,4 @@
-// The feed-forward block's products in bf16 (v_mfma_f32_32x32x16_bf16).
+// The feed-forward block's products in bf16 (v_mfma_f32_16x16x32_bf16).
 #include "sp_ffn.h"
 
 namespace sp {

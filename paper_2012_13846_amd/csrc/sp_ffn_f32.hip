@@ -1,4 +1,4 @@
-// The feed-forward block's products in fp32 (v_mfma_f32_32x32x2_f32).
+// The feed-forward block's products in fp32 (v_mfma_f32_16x16x4_f32).
 #include "sp_ffn.h"
 
 namespace sp {
