@@ -484,8 +484,9 @@ __device__ __forceinline__ void mm_body(const Mm& a, uint32_t block, char* room)
     // of an LDS read and products in turn
     auto alternate = [] {
         constexpr int kReads = (MT * (TA ? 2 : 1) + NT * (TB ? 2 : 1)) * (sizeof(T) == 4 && (TA || TB) ? 2 : 1);
+        constexpr int kEach = MT * NT / kReads > 1 ? 2 : 1;
 #pragma unroll
-        for (int i = 0; i < kReads; ++i) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0), __builtin_amdgcn_sched_group_barrier(0x8, 2, 0);
+        for (int i = 0; i < kReads; ++i) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0), __builtin_amdgcn_sched_group_barrier(0x8, kEach, 0);
         __builtin_amdgcn_sched_group_barrier(0x8, MT * NT * 4, 0);
     };
     auto take = [&](const char* stage, int s, Frag (&x)[MT], Frag (&y)[NT]) {
