@@ -7,6 +7,7 @@ missing this module raises: there is no fallback.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import operator
 import os
 
@@ -740,15 +741,23 @@ _idle = {}
 _Parts = C.c_int32 * 4
 
 
-def _rope(name, x, pos, parts, base, split, scale, out):
-    ptr, ld = _head_rows(x, x.dtype, "x")
-    n, heads, dim = x.shape
+@functools.lru_cache(maxsize=64)
+def _rope_parts(parts: tuple, dim: int):
+    """Their number, and the library's array of them."""
     parts = [operator.index(p) for p in parts]
     if not 1 <= len(parts) <= 4 or any(not 0 <= p <= dim for p in parts):
         raise ValueError("1 to 4 axes, each turning at most a head's elements")
-    if not pos.is_cuda or pos.dtype != torch.int32 or pos.shape != (n, len(parts)):
-        raise ValueError(f"pos must be a CUDA int32 tensor {(n, len(parts))}")
-    if n > 1 and pos.stride(0) < len(parts) or (len(parts) > 1 and pos.stride(1) != 1):
+    return len(parts), _Parts(*parts)
+
+
+def _rope(name, x, pos, parts, base, split, scale, out):
+    ptr, ld = _head_rows(x, x.dtype, "x")
+    n, heads, dim = x.shape
+    axes, parts = _rope_parts(tuple(parts), dim)
+    if not pos.is_cuda or pos.dtype != torch.int32 or pos.shape != (n, axes):
+        raise ValueError(f"pos must be a CUDA int32 tensor {(n, axes)}")
+    step, apart = pos.stride()
+    if n > 1 and step < axes or (axes > 1 and apart != 1):
         raise ValueError("the positions of a row must lie one after another, and rows must not overlap")
     if out is None:
         out = torch.empty_like(x, memory_format=torch.contiguous_format)
@@ -758,8 +767,7 @@ def _rope(name, x, pos, parts, base, split, scale, out):
         _need_shape(out, x.shape, "out")
         to, ldo = _head_rows(out, x.dtype, "out")
         _here(x, pos, out)
-    a = _Rope(n, heads, dim, len(parts), _Parts(*parts), 1 if split else 0, base, scale, _dt(x), pos.data_ptr(),
-              pos.stride(0) if n > 1 else len(parts))
+    a = _Rope(n, heads, dim, axes, parts, 1 if split else 0, base, scale, _dt(x), pos.data_ptr(), step if n > 1 else axes)
     _check(getattr(_block_argtypes(), name)(C.byref(a), ptr, ld, to, ldo, _stream()))
     return out
 
