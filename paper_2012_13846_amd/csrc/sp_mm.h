@@ -432,6 +432,11 @@ using Large = Shape2<256, 256, 2, 4, 2>;
 using Middle = Shape2<128, 128, 2, 2, 2>;
 using Narrow = Shape2<64, 128, 1, 4, 3>;
 using Few = Shape2<128, 32, 4, 1, 4>;
+// Middle where a workgroup has its CU to itself: twice the wavefronts, and all of the LDS for tiles further ahead.  bf16, 256 workgroups of 32 steps: 24.7
+// against 20.4 us, 216 of 51 steps 49.8 against 36.6; 8 bits 50.2 against 47.6; fp32, whose steps are longer than a load's way, the same.  (Narrow, six
+// tiles deep: the same, too.)
+using MiddleDeep = Shape2<128, 128, 2, 4, 4>;
+constexpr int64_t kCUs = 256;
 
 template <typename T, typename Sh, bool VEC>
 struct Room {  // LDS: [ST][tile of the first operand, of the second], [2][scales]
@@ -992,6 +997,7 @@ int mm(Mm a, float* part, hipStream_t s) {
         a.last = kPartial, a.part = last.part = part;
         if (gate) a.m *= 2;
     }
+    const bool alone = (int64_t)p.tiles_m * p.tiles_n * p.splits <= kCUs;
     auto go = [&](auto vec, auto exact) -> int {
         constexpr bool V = decltype(vec)::value, X = decltype(exact)::value;
         auto with = [&](auto last) -> int {
@@ -1000,7 +1006,10 @@ int mm(Mm a, float* part, hipStream_t s) {
                 case kLarge:
                     if constexpr (V && !X) return mm_launch<T, Large, TA, TB, V, X, L>(a, s);
                     break;
-                case kMiddle: return mm_launch<T, Middle, TA, TB, V, X, L>(a, s);
+                case kMiddle:
+                    if constexpr (V && !X && sizeof(T) < 4)
+                        if (alone) return mm_launch<T, MiddleDeep, TA, TB, V, X, L>(a, s);
+                    return mm_launch<T, Middle, TA, TB, V, X, L>(a, s);
                 case kNarrow: return mm_launch<T, Narrow, TA, TB, V, X, L>(a, s);
                 case kFew:
                     if constexpr (TA || TB) return mm_launch<T, Few, TA, TB, V, X, L>(a, s);
@@ -1086,15 +1095,21 @@ int mm_three(const Mm (&of)[3], char* part, hipStream_t s) {
         t.end[i] = blocks, join.end[i] = joins;
     }
     auto go = [&](auto shape, auto vec0, auto vec) {
-        hipLaunchKernelGGL((mm_three_kernel<T, decltype(shape), decltype(vec0)::value, decltype(vec)::value>), dim3(blocks), dim3(256), 0, s, t);
+        using Sh = decltype(shape);
+        hipLaunchKernelGGL((mm_three_kernel<T, Sh, decltype(vec0)::value, decltype(vec)::value>), dim3(blocks), dim3(Sh::kThreads), 0, s, t);
     };
     auto with = [&](auto shape) {
         const bool vec = whole[1] && whole[2];
         if (whole[0]) vec ? go(shape, std::true_type{}, std::true_type{}) : go(shape, std::true_type{}, std::false_type{});
         else vec ? go(shape, std::false_type{}, std::true_type{}) : go(shape, std::false_type{}, std::false_type{});
     };
-    if (plan.p[0].shape == kMiddle) with(Middle{});
-    else with(Narrow{});
+    const bool deep = sizeof(T) < 4 && blocks <= kCUs && whole[0] && whole[1] && whole[2];
+    if (plan.p[0].shape == kMiddle) {
+        if constexpr (sizeof(T) < 4) deep ? go(MiddleDeep{}, std::true_type{}, std::true_type{}) : with(Middle{});
+        else with(Middle{});
+    } else {
+        with(Narrow{});
+    }
     SP_HIP(hipGetLastError());
     if (joins) {
         hipLaunchKernelGGL(mm_join_three_kernel<T>, dim3(joins), dim3(256), 0, s, join);

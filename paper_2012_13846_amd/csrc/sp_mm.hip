@@ -17,7 +17,7 @@ struct Cost {
 };
 //                                f32   bf16  8 bits, and exactly
 constexpr Cost kCosts[] = {{kLarge, 256, 256, {7.9, 1.35, 1.7, 0}, {0, 0, 0, 0}},
-                           {kMiddle, 128, 128, {2.0, 0.6, 0.75, 1.15}, {4.06, 1.0, 1.13, 1.96}},
+                           {kMiddle, 128, 128, {2.0, 0.55, 0.68, 1.15}, {4.06, 1.0, 1.13, 1.96}},
                            {kNarrow, 64, 128, {1.15, 0.37, 0.55, 0.85}, {2.1, 0.65, 0.81, 1.26}},
                            {kFew, 128, 32, {0.7, 0.35, 0, 0}, {1.1, 0.55, 0, 0}}};
 constexpr double kLaunch = 3.5, kRound = 2, kRoundAlone = 8;
