@@ -622,3 +622,14 @@ def test_q8_linear_of_many_steps(sp, n, c, m):
     Y = X @ W.T
     for out in (F32, BF16):
         within(sp.sp_q8_linear((x, xs), (w, ws), out), Y, q8_bound(X, W, Y, out), "y")
+
+
+@pytest.mark.parametrize("n,c,m", [(600, 504, 1000), (700, 768, 3000), (6000, 256, 512), (300, 1024, 4096), (1697, 512, 1024)])
+def test_ffn_of_a_workgroup_a_cu(sp, n, c, m):
+    """Fewer workgroups than CUs, in one part and in several: the deeper tiles."""
+    test_large_ffn_by_samples(sp, n, c, m, BF16)
+
+
+@pytest.mark.parametrize("n,c,m", [(2048, 2048, 2048), (1000, 4096, 1024), (1500, 1800, 1900)])
+def test_q8_linear_of_a_workgroup_a_cu(sp, n, c, m):
+    test_large_q8_linear_by_samples(sp, n, c, m)
