@@ -569,12 +569,14 @@ __global__ __launch_bounds__(256) void q8_rows_kernel(const T* __restrict__ x, i
     }
 }
 
-// A workgroup: 128 rows and 64 columns of x, through LDS.
+// A workgroup: 128 rows and 64 columns of x, through LDS as they are stored, so that of bf16 eight workgroups share a CU (8192 x 2048: 11.5 us, 4.4 TB/s;
+// four of them, with 32 bits an element: 14.5).
 constexpr int kTurnCols = 64;
 template <typename T, bool ALIGNED>
 __global__ __launch_bounds__(256) void q8_turned_kernel(const T* __restrict__ x, int64_t ldx, int64_t n, int c, uint8_t* q, uint8_t* qs) {
     constexpr int V = 16 / (int)sizeof(T), kPieces = kTurnCols / V, kEach = kQ8Block * kPieces / 256;
-    __shared__ float tile[kTurnCols][kQ8Block + 1];
+    constexpr int kPad = 4 / (int)sizeof(T);  // a column is an odd number of banks behind the last
+    __shared__ __attribute__((aligned(4))) T tile[kTurnCols][kQ8Block + kPad];
     const int64_t blocks = (n + kQ8Block - 1) / kQ8Block, wide = blocks * kQ8Block, scales = (blocks + 3) / 4 * 4;
     const int64_t block = blockIdx.x, row0 = block * kQ8Block;
     const int col0 = blockIdx.y * kTurnCols;
@@ -589,15 +591,15 @@ __global__ __launch_bounds__(256) void q8_turned_kernel(const T* __restrict__ x,
     for (int k = 0; k < kEach; ++k) {
         const int i = k * 256 + threadIdx.x, r = i / kPieces, j = (i % kPieces) * V;
 #pragma unroll
-        for (int e = 0; e < V; ++e) tile[j + e][r] = elem(in[k].e[e]);
+        for (int e = 0; e < V; ++e) tile[j + e][r] = in[k].e[e];
     }
     __syncthreads();
-    // four lanes a column, 32 rows each; lanes 2 and 3 begin at the second 16, since they share banks with lanes 0 and 1
-    const int j = threadIdx.x / 4, part = threadIdx.x % 4, swap = part >> 1;
+    // four lanes a column, 32 rows each; of fp32, lanes 2 and 3 begin at the second 16, since they share banks with lanes 0 and 1
+    const int j = threadIdx.x / 4, part = threadIdx.x % 4, swap = sizeof(T) == 4 ? part >> 1 : 0;
     float v[32], top = 0.f;
 #pragma unroll
     for (int i = 0; i < 32; ++i) {
-        v[i] = tile[j][part * 32 + (i ^ (swap << 4))];
+        v[i] = elem(tile[j][part * 32 + (i ^ (swap << 4))]);
         top = q8_larger(top, q8_size(v[i]));
     }
     const uint32_t code = q8_scale(q8_top<4>(top));
