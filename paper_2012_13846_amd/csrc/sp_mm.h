@@ -690,7 +690,8 @@ __device__ __forceinline__ void mm_body(const Mm& a, uint32_t block, char* room)
     };
     // Tiles that lie within the results, nearly all, have code of their own: with a way out for each of eight columns behind every store the last step
     // is so long that it is fetched from memory again and again.
-    constexpr int kItems = NT * MP, kAheadBy = LAST == kGateBack ? sizeof(T) == 2 ? 4 : 2 : 1;
+    constexpr int kItems = NT * MP, kMostAhead = LAST == kGateBack ? sizeof(T) == 2 ? 4 : 2 : 1, kAheadBy = kMostAhead < kItems ? kMostAhead : kItems;
+    static_assert(kAheadBy <= kItems, "an item that is read ahead is one of the lane's: the rows behind a tile may be none of the matrix");
     auto items = [&](auto inside, auto act) {
         constexpr bool kInside = decltype(inside)::value;
         constexpr int kAct = decltype(act)::value;

@@ -633,3 +633,11 @@ def test_ffn_of_a_workgroup_a_cu(sp, n, c, m):
 @pytest.mark.parametrize("n,c,m", [(2048, 2048, 2048), (1000, 4096, 1024), (1500, 1800, 1900)])
 def test_q8_linear_of_a_workgroup_a_cu(sp, n, c, m):
     test_large_q8_linear_by_samples(sp, n, c, m)
+
+
+@TYPES
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("n,c,m", [(32, 136, 256), (32, 64, 128), (32, 512, 1024), (31, 136, 256)])
+def test_ffn_of_a_tile_of_32_rows(sp, n, c, m, act, dt):
+    """Tiles of 128 x 32 that lie within the results: the gradient's last step has two items a lane, and reads no more of them ahead."""
+    test_ffn(sp, n, c, m, act, dt)
