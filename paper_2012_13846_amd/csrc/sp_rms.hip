@@ -53,10 +53,12 @@ struct RmsFwd {
     uint8_t *q, *qs;   // codes [n][blocks * 128], scales [n][blocks rounded up to 4]
 };
 
-// 1 / sqrt(mean + eps) from a row's sum of squares; `again` sums them with the elements times 2^-70, where the sum overflows.
+// 1 / sqrt(mean + eps) from a row's sum of squares; `again` sums them with the elements times 2^kDown, where the sum overflows
+// (65536 squares of 2^(128 - 74) stay below 2^124, and the mean of a sum that overflowed is above 2^(112 - 148)).
+constexpr int kDown = -74;
 template <typename Again>
 __device__ __forceinline__ float rstd_of(float squares, float inv, float eps, Again again) {
-    if (squares > 3.4028234e38f) return ldexpf(1.f / sqrtf(again() * inv), -70);  // infinite squares: 0
+    if (squares > 3.4028234e38f) return ldexpf(1.f / sqrtf(again() * inv), kDown);  // infinite squares: 0
     return 1.f / sqrtf(squares * inv + eps);
 }
 
@@ -132,7 +134,7 @@ __global__ __launch_bounds__(kBlock<LANES>) void rms_fwd_kernel(RmsFwd<T> a) {
 #pragma unroll
             for (int p = 0; p < P; ++p)
 #pragma unroll
-                for (int i = 0; i < V; ++i) t[0] += ldexpf(v[p][i], -70) * ldexpf(v[p][i], -70);
+                for (int i = 0; i < V; ++i) t[0] += ldexpf(v[p][i], kDown) * ldexpf(v[p][i], kDown);
             reduce_lanes<LANES, Add>(t, room, &turn);
             return t[0];
         });
@@ -182,7 +184,7 @@ __global__ __launch_bounds__(kWide) void rms_fwd_wide_kernel(RmsFwd<T> a) {
             for (int j = threadIdx.x * V; j < c; j += kWide * V) {
                 const Piece<T, V> v = load_some<T, V, ALIGNED>(from + j, c - j);
 #pragma unroll
-                for (int i = 0; i < V; ++i) t[0] += ldexpf(elem(v.e[i]), -70) * ldexpf(elem(v.e[i]), -70);
+                for (int i = 0; i < V; ++i) t[0] += ldexpf(elem(v.e[i]), kDown) * ldexpf(elem(v.e[i]), kDown);
             }
             reduce_lanes<kWide, Add>(t, room, &turn);
             return t[0];

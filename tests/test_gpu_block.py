@@ -641,3 +641,22 @@ def test_q8_linear_of_a_workgroup_a_cu(sp, n, c, m):
 def test_ffn_of_a_tile_of_32_rows(sp, n, c, m, act, dt):
     """Tiles of 128 x 32 that lie within the results: the gradient's last step has two items a lane, and reads no more of them ahead."""
     test_ffn(sp, n, c, m, act, dt)
+
+
+@TYPES
+@pytest.mark.parametrize("c", [1, 77, 4096, 8192, 16392, 65536])
+def test_rms_norm_of_the_largest_values(sp, c, dt):
+    """Squares beyond fp32, whatever the width; rstd is then below 2^-126, where fp32 has steps of 2^-149."""
+    rng = np.random.default_rng(c)
+    x = torch.from_numpy((rng.uniform(1e38, 3.3e38, (3, c)) * rng.choice([-1, 1], (3, c))).astype(np.float32)).to(dt).cuda()
+    gamma = 1 + rows(rng, F32, c, scale=0.2)
+    _, y, rstd = sp.sp_rms_norm_fwd(x, gamma)
+    Y, R = block.rms_fwd(host(x), host(gamma), 1e-5)
+    rel = sum_error(c) / 2 + 4 * U32
+    within(rstd, R, rel * R + 2.0 ** -150, "rstd")
+    within(y, Y, (rel + 3 * U32 + half_step(dt) + 2.0 ** -150 / R.min()) * np.abs(Y), "y")
+    _, q8 = sp.sp_rms_norm_q8(x, gamma)
+    V = block.q8_values(*(t.view(torch.uint8).cpu().numpy() for t in q8))[:, :c]
+    err = (rel + 3 * U32 + 2.0 ** -150 / R.min()) * np.abs(Y)
+    # half a step of a code: 2^-4 of the value, or of the smallest step, 2^-9 of a scale that is below 2^-7 of the block's largest element
+    assert (np.abs(V - Y) <= err + np.maximum((np.abs(Y) + err) / 16, np.abs(Y).max() * 2.0 ** -17)).all()
