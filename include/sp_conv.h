@@ -346,6 +346,7 @@ int sp_rope_bwd(const sp_rope* a, const void* d_dy, int64_t lddy, void* d_dx, in
  * Root-mean-square norm with the residual's addition, every row of x [n][c] by itself:
  *   h = x + res, as it is stored in dt;  rstd = 1/sqrt(mean(h^2) + eps);  y = gamma * h * rstd
  * d_res NULL: h = x, and d_h must be NULL.  d_h may be d_x or d_res, d_y either of them that d_h is not.  rstd [n] is an output.
+ * eps may be 0, elements of any size: only a row of zeros then has no y (NaN).  rstd is infinite for rows whose root lies below 2^-128, which have a y, but no gradients.
  * sp_rms_norm_q8: y in 8 bits (below) instead, rounded once.
  * sp_rms_norm_bwd: with hhat = h * rstd, g = dy * gamma and a mean over the row, dx = dh + rstd * (g - hhat * mean(g * hhat)) is the gradient of x
  * and of the residual; dh (NULL: none) is the gradient that reaches h past the norm.  dgamma [c] = sum dy * hhat.  dx may be dy or dh.

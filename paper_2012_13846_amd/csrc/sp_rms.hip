@@ -6,9 +6,7 @@
 // the next row is asked for before this one is reduced.  Pieces that are not aligned (odd widths, views) are loaded and stored as wide by
 // unaligned instructions, but for the piece that holds a row's end.  What is normalised is the sum as it is stored, so that the backward
 // pass finds the same.  In 8 bits the 16 (fp32: 32) neighbouring lanes that hold 128 elements share their largest size.  The weight's gradient is
-// summed in the lanes that own the columns, then over a workgroup's row groups through LDS, and the workgroups' sums are added in fp64 in a
-// fixed order by a second kernel; small matrices read the rows again for it, in the same launch.  Squares are summed in fp32; where that overflows,
-// again with the row scaled down.  16384 x 4096 in bf16: 93 us forward (5.7 TB/s), 115 + 5 back (4.7).  Rows to 8 bits: 8192 x 2048 10.5 us, transposed 14.
+// summed in the lanes that own the columns, then over a workgroup's row groups through LDS, and the workgroups' sums are added in fp64 in X16384 x 4096 in bf16: 93 us forward (5.7 TB/s), 115 + 5 back (4.7).  Rows to 8 bits: 8192 x 2048 10.5 us, transposed 14.
 #include <algorithm>
 #include <type_traits>
 
@@ -53,13 +51,25 @@ struct RmsFwd {
     uint8_t *q, *qs;   // codes [n][blocks * 128], scales [n][blocks rounded up to 4]
 };
 
-// 1 / sqrt(mean + eps) from a row's sum of squares; `again` sums them with the elements times 2^kDown, where the sum overflows
-// (65536 squares of 2^(128 - 74) stay below 2^124, and the mean of a sum that overflowed is above 2^(112 - 148)).
-constexpr int kDown = -74;
+// 1 / sqrt(mean + eps) of a row from its sum of squares.  Where that overflows, `again` sums the squares of the elements times 2^kDown (65536 squares
+// of 2^(128 - 74) stay below 2^124, and the mean of a sum that overflowed is above 2^(112 - 148)).  Squares below 2^-126 lose bits, 65536 of them at most
+// 2^-134: nothing to a sum or an eps of 2^-100, else `again` sums the squares of the elements times 2^kUp, which lie between 2^-98 and 2^100.
+constexpr int kDown = -74, kUp = 100;
+constexpr float kFew = 0x1p-100f;
+struct Root {
+    float r, rstd;  // y = row * r * gamma (up: row * 2^kUp * r * gamma, since rstd is beyond fp32 for rows below 2^-128)
+    bool up;
+};
 template <typename Again>
-__device__ __forceinline__ float rstd_of(float squares, float inv, float eps, Again again) {
-    if (squares > 3.4028234e38f) return ldexpf(1.f / sqrtf(again() * inv), kDown);  // infinite squares: 0
-    return 1.f / sqrtf(squares * inv + eps);
+__device__ __forceinline__ Root rstd_of(float squares, float inv, float eps, Again again) {
+    const bool up = squares < kFew && eps < kFew;
+    if (up || squares > 3.4028234e38f) {
+        const int k = up ? kUp : kDown;
+        const float r = 1.f / sqrtf(again(k) * inv + ldexpf(eps, 2 * k)), rstd = ldexpf(r, k);  // infinite squares: 0
+        return Root{up ? r : rstd, rstd, up};
+    }
+    const float r = 1.f / sqrtf(squares * inv + eps);
+    return Root{r, r, false};
 }
 
 // A lane's V elements of a row in 8 bits: with the lanes of the same 128 elements, from column `col` on.
@@ -129,16 +139,21 @@ __global__ __launch_bounds__(kBlock<LANES>) void rms_fwd_kernel(RmsFwd<T> a) {
         }
         if (row + step < a.n) fetch(row + step);
         reduce_lanes<LANES, Add>(s, room, &turn);
-        const float r = rstd_of(s[0], inv, a.eps, [&] {
+        const Root root = rstd_of(s[0], inv, a.eps, [&](int k) {
             float t[1] = {0.f};
 #pragma unroll
             for (int p = 0; p < P; ++p)
 #pragma unroll
-                for (int i = 0; i < V; ++i) t[0] += ldexpf(v[p][i], kDown) * ldexpf(v[p][i], kDown);
+                for (int i = 0; i < V; ++i) {
+                    const float f = ldexpf(v[p][i], k);
+                    t[0] += f * f;
+                    if (k > 0) v[p][i] = f;
+                }
             reduce_lanes<LANES, Add>(t, room, &turn);
             return t[0];
         });
-        if (l == 0 && a.rstd) a.rstd[row] = r;
+        const float r = root.r;
+        if (l == 0 && a.rstd) a.rstd[row] = root.rstd;
 #pragma unroll
         for (int p = 0; p < P; ++p) {
             const int col = (p * LANES + l) * V;
@@ -179,17 +194,21 @@ __global__ __launch_bounds__(kWide) void rms_fwd_wide_kernel(RmsFwd<T> a) {
             for (int i = 0; i < V; ++i) s[0] += elem(v.e[i]) * elem(v.e[i]);
         }
         reduce_lanes<kWide, Add>(s, room, &turn);
-        const float r = rstd_of(s[0], inv, a.eps, [&] {
+        const Root root = rstd_of(s[0], inv, a.eps, [&](int k) {
             float t[1] = {0.f};
             for (int j = threadIdx.x * V; j < c; j += kWide * V) {
                 const Piece<T, V> v = load_some<T, V, ALIGNED>(from + j, c - j);
 #pragma unroll
-                for (int i = 0; i < V; ++i) t[0] += ldexpf(elem(v.e[i]), kDown) * ldexpf(elem(v.e[i]), kDown);
+                for (int i = 0; i < V; ++i) {
+                    const float f = ldexpf(elem(v.e[i]), k);
+                    t[0] += f * f;
+                }
             }
             reduce_lanes<kWide, Add>(t, room, &turn);
             return t[0];
         });
-        if (threadIdx.x == 0 && a.rstd) a.rstd[row] = r;
+        const float r = root.r, up = root.up ? ldexpf(1.f, kUp) : 1.f;
+        if (threadIdx.x == 0 && a.rstd) a.rstd[row] = root.rstd;
         // (the thread itself has written the piece of the sum that it reads)
         for (int col = threadIdx.x * V; col < (Q8 ? wide : c); col += kWide * V) {
             Piece<T, V> v{};
@@ -197,11 +216,11 @@ __global__ __launch_bounds__(kWide) void rms_fwd_wide_kernel(RmsFwd<T> a) {
             if constexpr (Q8) {
                 float f[V];
 #pragma unroll
-                for (int i = 0; i < V; ++i) f[i] = col + i < c ? elem(v.e[i]) * r * a.gamma[col + i] : 0.f;
+                for (int i = 0; i < V; ++i) f[i] = col + i < c ? elem(v.e[i]) * up * r * a.gamma[col + i] : 0.f;
                 put_q8<V>(f, col, wide, a.q + row * wide, a.qs + row * scales);
             } else {
 #pragma unroll
-                for (int i = 0; i < V; ++i) v.e[i] = col + i < c ? to_elem<T>(elem(v.e[i]) * r * a.gamma[col + i]) : T(0);
+                for (int i = 0; i < V; ++i) v.e[i] = col + i < c ? to_elem<T>(elem(v.e[i]) * up * r * a.gamma[col + i]) : T(0);
                 store_some<T, V, ALIGNED>(a.y + row * c + col, v, c - col);
             }
         }

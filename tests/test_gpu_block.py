@@ -660,3 +660,37 @@ def test_rms_norm_of_the_largest_values(sp, c, dt):
     err = (rel + 3 * U32 + 2.0 ** -150 / R.min()) * np.abs(Y)
     # half a step of a code: 2^-4 of the value, or of the smallest step, 2^-9 of a scale that is below 2^-7 of the block's largest element
     assert (np.abs(V - Y) <= err + np.maximum((np.abs(Y) + err) / 16, np.abs(Y).max() * 2.0 ** -17)).all()
+
+
+@TYPES
+@pytest.mark.parametrize("eps", [0.0, 1e-40, 1e-32])
+@pytest.mark.parametrize("c", [1, 13, 128, 1000, 4096, 16392])
+def test_rms_norm_of_small_values(sp, c, eps, dt):
+    """Squares that underflow, beside an eps that does not cover them: the definition all the same, rstd as far as fp32 goes."""
+    rng = np.random.default_rng(c)
+    sizes = np.array([1e-10, 1e-15, 1e-17, 1e-19, 1e-21, 1e-24, 1e-30, 1e-36, 1e-39, 0.0])[:, None]
+    x = torch.from_numpy((rng.uniform(0.5, 2, (10, c)) * rng.choice([-1, 1], (10, c)) * sizes).astype(np.float32)).to(dt).cuda()
+    dy = rows(rng, dt, 10, c)
+    gamma = 1 + rows(rng, F32, c, scale=0.2)
+    exact = float(np.float32(eps))
+    _, y, rstd = sp.sp_rms_norm_fwd(x, gamma, eps=eps)
+    with np.errstate(divide="ignore", invalid="ignore"):
+        Y, R = block.rms_fwd(host(x), host(gamma), exact)
+    assert torch.isnan(y[9]).all() if eps == 0 else not y[9].any()
+    rel = sum_error(c) / 2 + 4 * U32
+    within(rstd, np.where(R > 2.0 ** 128, np.inf, R), rel * R, "rstd")
+    within(y, Y, (rel + 3 * U32 + half_step(dt)) * np.abs(Y), "y")
+    _, q8 = sp.sp_rms_norm_q8(x, gamma, eps=eps)
+    V = block.q8_values(*(t.view(torch.uint8).cpu().numpy() for t in q8))[:9, :c]
+    err = (rel + 3 * U32) * np.abs(Y[:9])
+    # half a step of a code: 2^-4 of the value, or of the smallest step, 2^-9 of a scale that is below 2^-7 of the block's largest element
+    assert (np.abs(V - Y[:9]) <= err + np.maximum((np.abs(Y[:9]) + err) / 16, np.abs(Y[:9]).max(1, keepdims=True) * 2.0 ** -17)).all()
+    # gradients of the rows that have an rstd, from the GPU's own, where they are within fp32
+    live = slice(0, 6)
+    dx, dgamma = sp.sp_rms_norm_bwd(x[live].contiguous(), dy[live].contiguous(), gamma, rstd[live].contiguous())
+    H, D, S = host(x[live]), host(dy[live]), host(rstd[live])
+    DX, DG = block.rms_bwd(H, D, host(gamma), S)
+    hat, g = np.abs(H * S[:, None]), np.abs(D * host(gamma))
+    size = S[:, None] * (g + hat * (g * hat).mean(1)[:, None])
+    within(dx, DX, (sum_error(c) + 6 * U32) * size + (half_step(dt) + U32) * np.abs(DX), "dx")
+    within(dgamma, DG, 18 * U32 * np.abs(D * hat).sum(0) + U32 * np.abs(DG), "dgamma")
