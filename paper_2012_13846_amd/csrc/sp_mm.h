@@ -104,7 +104,7 @@ __device__ __forceinline__ float2 gate_of(float g) {
         const float p = g < 0.f ? v : 1.f - v;
         return float2{g * p, p + g * 0.39894228f * e};
     } else {
-        const float p = 0.5f * (1.f + erff(g * 0.70710678f));
+        const float p = 0.5f * erfcf(g * -0.70710678f);  // (of 1 + erf the tail would be what cancels)
         return float2{g * p, p + g * 0.39894228f * expf(-0.5f * g * g)};
     }
 }

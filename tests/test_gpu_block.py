@@ -694,3 +694,18 @@ def test_rms_norm_of_small_values(sp, c, eps, dt):
     size = S[:, None] * (g + hat * (g * hat).mean(1)[:, None])
     within(dx, DX, (sum_error(c) + 6 * U32) * size + (half_step(dt) + U32) * np.abs(DX), "dx")
     within(dgamma, DG, 18 * U32 * np.abs(D * hat).sum(0) + U32 * np.abs(DG), "dgamma")
+
+
+@pytest.mark.parametrize("n", [7, 4000])
+def test_gelu_keeps_its_tail_in_fp32(sp, n):
+    """u = 1, W_out = 1: y is gelu(g) = g p, dx its slope p + g f (p the normal distribution function, f its density).  erfc is within 16 steps of fp32 (32 U32) of
+    an argument rounded twice, which moves it by 2 U32 g^2 of itself; the exponential in f within 8 U32 of an argument rounded twice, g^2 U32 of it."""
+    g = torch.linspace(-12.5, 12.5, n, device="cuda")
+    x = torch.stack([g, torch.ones_like(g)], 1)
+    w_in, w_out = torch.eye(2, device="cuda"), torch.tensor([[1.0], [0.0]], device="cuda")
+    y, kept = sp.sp_ffn_fwd(x, w_in, w_out, "gelu")
+    G = host(g)
+    p, f = np.array([math.erfc(-v / math.sqrt(2)) / 2 for v in G]), np.exp(-G * G / 2) / math.sqrt(2 * math.pi)
+    within(y[:, 0], G * p, (36 + 2 * G * G) * U32 * np.abs(G) * p, "gelu")
+    dx, _, _ = sp.sp_ffn_bwd(x, w_in, w_out, kept, torch.ones_like(x), "gelu")
+    within(dx[:, 0], p + G * f, U32 * ((36 + 2 * G * G) * p + (12 + 2 * G * G) * np.abs(G) * f), "slope")
