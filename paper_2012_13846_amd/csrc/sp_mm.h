@@ -208,11 +208,14 @@ __device__ __forceinline__ void put_out(const Mm& a, int64_t row, int col, const
     }
 }
 
-// Codes 8 e .. 8 e + 7 of a lane's 32, times their scale (the word's lowest byte)
-__device__ __forceinline__ bf16x8 q8_values(const i32x8& codes, int e, int scale) {
+// 8-bit products as bf16.  A code times its scale is a bf16 value if the scale's code is 64 to 191 (3 to 246 would do, but of these exactly
+// one of the two highest bits is set).  Smaller scales would lose codes' bits and larger ones make them infinite; there a step's sum of codes
+// alone gets both scales' exponents, together, since one by itself may take the sum beyond fp32.
+constexpr uint32_t kPlain = 0x80808080u;
+__device__ __forceinline__ uint32_t q8_plain(uint32_t word) { return word ^ word << 1; }  // has all of kPlain's bits if a word's four scales are such
+// Codes 8 e .. 8 e + 7 of a lane's 32, times `times`, a power of two or what a scale of 255 stands for
+__device__ __forceinline__ bf16x8 q8_values(const i32x8& codes, int e, float times) {
     typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-    const uint32_t code = (uint32_t)scale & 255u;
-    const float times = __uint_as_float(code == 0 ? 0x00400000u : code << 23);
     bf16x8 r;
 #pragma unroll
     for (int w = 0; w < 2; ++w) {
@@ -222,6 +225,9 @@ __device__ __forceinline__ bf16x8 q8_values(const i32x8& codes, int e, int scale
     }
     return r;
 }
+__device__ __forceinline__ float q8_all(int scale) { return __uint_as_float(((uint32_t)scale & 255u) << 23); }  // a plain scale (a word's lowest byte)
+__device__ __forceinline__ float q8_none(int scale) { return __uint_as_float((scale & 255) == (int)kQ8NaN ? 0x7f800000u : 0x3f800000u); }
+__device__ __forceinline__ float q8_scaled(float sum, int first, int second) { return ldexpf(sum, (first & 255) + (second & 255) - 254); }
 
 // ---- tiles -----------------------------------------------------------------------------------------------------
 constexpr int kStepBytes = 128;
@@ -450,7 +456,7 @@ struct Room {  // LDS: [ST][tile of the first operand, of the second], [2][scale
 // a third more from LDS and nothing ahead, 214), 212 in the block, where the memory still writes what was kept.  8 bits: fragments are twice as long and
 // only registers for one set are left; 16384 x 4096 x 6144 at 2500 TFLOP/s.  fp32: about 90 % of the fp32 matrix rate in 8192 x 1024 x 2048.
 // Last steps: 8 bytes a result of the gate and 10 of its gradient are memory's, 8192 x 2048 x 8192: 493 us for 370 of products, 341 for 190.
-// EXACT (8-bit operands): codes become bf16, which holds them and their scales exactly, for the bf16 products.  The 8-bit products themselves take
+// EXACT (8-bit operands): codes and their scales become bf16, exactly (q8_plain), for the bf16 products.  The 8-bit products themselves take
 // eight neighbouring elements at a time and cut their products off at 2^-13 of the largest's power of two (found by cancelling that one); of
 // random rows 1.5e-5 of the result, whatever their length, against 1e-8: far below a bf16 result's rounding (1.7e-3), but not an fp32 one's.
 template <typename T, typename Sh, bool TA, bool TB, bool VEC, bool EXACT, Last LAST>
@@ -517,17 +523,47 @@ __device__ __forceinline__ void mm_body(const Mm& a, uint32_t block, char* room)
     auto product = [&](const Frag (&x)[MT], const Frag (&y)[NT]) { product_of(x, y, std::integral_constant<int, 0>{}, std::integral_constant<int, MT>{}); };
     // 8 bits: the scales of a row's next four steps, a byte each; step u's (opsel) is a constant of the matrix instruction
     int sa[MT], sb[NT];
+    bool plain = true;  // (EXACT) these scales, of the rows that there are
     auto take_scales = [&](int step) {
         const int* words = reinterpret_cast<const int*>(room + ST * kStage) + (step >> 2 & 1) * kWords + (l & 15);
 #pragma unroll
         for (int i = 0; i < MT; ++i) sa[i] = words[32 * wm * MP + 16 * i];
 #pragma unroll
         for (int i = 0; i < NT; ++i) sb[i] = words[Sh::BM + 32 * wn * NP + 16 * i];
+        if constexpr (EXACT) {
+            uint32_t all = kPlain;
+#pragma unroll
+            for (int i = 0; i < MT; ++i) all &= pa.first + 32 * wm * MP + 16 * i + (l & 15) >= a.m ? kPlain : q8_plain((uint32_t)sa[i]);
+#pragma unroll
+            for (int i = 0; i < NT; ++i) all &= pb.first + 32 * wn * NP + 16 * i + (l & 15) >= a.n ? kPlain : q8_plain((uint32_t)sb[i]);
+            plain = __all(all == kPlain);
+        }
     };
     auto multiply = [&](const char* stage, auto opsel) {
         constexpr int U = decltype(opsel)::value;
 #pragma unroll
         for (int s = 0; s < K::kSub; ++s) {
+            if constexpr (EXACT) if (!plain) {
+#pragma unroll
+                for (int i = 0; i < MT; ++i) {
+                    asm volatile("" ::: "memory");  // blocks are read one by one: all of them, as bf16, are more registers than two workgroups a CU have
+                    const Frag x = fa.frag(stage, i, A::template block<MT>(i, half), s);
+                    int scale[4];                   // of rows 4 (l / 16) ..: the lanes of those rows have them
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) scale[e] = __shfl(sa[i], 4 * (l >> 4) + e) >> (8 * U);
+#pragma unroll
+                    for (int j = 0; j < NT; ++j) {
+                        const Frag y = fb.frag(stage + A::kBytes, j, B::template block<NT>(j, 0), s);
+                        f32x4 t = {};
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            t = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q8_values(x, e, q8_none(sa[i] >> (8 * U))), q8_values(y, e, q8_none(sb[j] >> (8 * U))), t, 0, 0, 0);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[i][j][e] += q8_scaled(t[e], scale[e], sb[j] >> (8 * U));
+                    }
+                }
+                continue;
+            }
             Frag x[MT], y[NT];
             take(stage, s, x, y);
             if constexpr (EXACT) {
@@ -535,9 +571,9 @@ __device__ __forceinline__ void mm_body(const Mm& a, uint32_t block, char* room)
                 for (int e = 0; e < 4; ++e) {
                     bf16x8 u[MT], v[NT];
 #pragma unroll
-                    for (int i = 0; i < MT; ++i) u[i] = q8_values(x[i], e, sa[i] >> (8 * U));
+                    for (int i = 0; i < MT; ++i) u[i] = q8_values(x[i], e, q8_all(sa[i] >> (8 * U)));
 #pragma unroll
-                    for (int j = 0; j < NT; ++j) v[j] = q8_values(y[j], e, sb[j] >> (8 * U));
+                    for (int j = 0; j < NT; ++j) v[j] = q8_values(y[j], e, q8_all(sb[j] >> (8 * U)));
 #pragma unroll
                     for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -861,9 +897,9 @@ __global__ __launch_bounds__(1024) void mm_thin_kernel(Mm a) {
         if constexpr (sizeof(T) == 1) {
             static_assert(kAtOnce <= kWhole, "one word");
 #pragma unroll
-            for (int i = 0; i < kSides; ++i) sx[i] = *reinterpret_cast<const uint32_t*>(scales[i] + (s0 & ~3)) >> (8 * (s0 & 3));
+            for (int i = 0; i < kSides; ++i) sx[i] = *reinterpret_cast<const uint32_t*>(scales[i] + (s0 & ~3));
 #pragma unroll
-            for (int j = 0; j < NB; ++j) sy[j] = *reinterpret_cast<const uint32_t*>(scales[kSides + j] + (s0 & ~3)) >> (8 * (s0 & 3));
+            for (int j = 0; j < NB; ++j) sy[j] = *reinterpret_cast<const uint32_t*>(scales[kSides + j] + (s0 & ~3));
         }
 #pragma unroll
         for (int u = 0; u < kAtOnce; ++u) {
@@ -873,6 +909,21 @@ __global__ __launch_bounds__(1024) void mm_thin_kernel(Mm a) {
 #pragma unroll
             for (int j = 0; j < NB; ++j) y[u][j] = fragment(from[kSides + j], s0 + u);
         }
+        bool plain = true;
+        if constexpr (sizeof(T) == 1) {
+            if constexpr (EXACT) {
+                uint32_t all = kPlain;
+#pragma unroll
+                for (int i = 0; i < kSides; ++i) all &= q8_plain(sx[i]);
+#pragma unroll
+                for (int j = 0; j < NB; ++j) all &= q8_plain(sy[j]);
+                plain = __all(all == kPlain);
+            }
+#pragma unroll
+            for (int i = 0; i < kSides; ++i) sx[i] >>= 8 * (s0 & 3);
+#pragma unroll
+            for (int j = 0; j < NB; ++j) sy[j] >>= 8 * (s0 & 3);
+        }
 #pragma unroll
         for (int u = 0; u < kAtOnce; ++u) {
             if (u >= count) break;
@@ -881,9 +932,18 @@ __global__ __launch_bounds__(1024) void mm_thin_kernel(Mm a) {
 #pragma unroll
                 for (int j = 0; j < NB; ++j) {
                     if constexpr (EXACT) {
+                        if (plain) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q8_values(x[u][i], e, (int)(sx[i] >> (8 * u))), q8_values(y[u][j], e, (int)(sy[j] >> (8 * u))), acc[i][j], 0, 0, 0);
+                            for (int e = 0; e < 4; ++e)
+                                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q8_values(x[u][i], e, q8_all((int)(sx[i] >> (8 * u)))), q8_values(y[u][j], e, q8_all((int)(sy[j] >> (8 * u)))), acc[i][j], 0, 0, 0);
+                        } else {
+                            f32x4 t = {};
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                t = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q8_values(x[u][i], e, q8_none((int)(sx[i] >> (8 * u)))), q8_values(y[u][j], e, q8_none((int)(sy[j] >> (8 * u)))), t, 0, 0, 0);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) acc[i][j][e] += q8_scaled(t[e], __shfl((int)sx[i], 4 * h + e) >> (8 * u), (int)(sy[j] >> (8 * u)));
+                        }
                     } else if constexpr (sizeof(T) == 1) {
                         acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x[u][i], y[u][j], acc[i][j], 0, 0, 0, (int)(sx[i] >> (8 * u)), 0, (int)(sy[j] >> (8 * u)));
                     } else if constexpr (sizeof(T) == 2) {

@@ -709,3 +709,30 @@ def test_gelu_keeps_its_tail_in_fp32(sp, n):
     within(y[:, 0], G * p, (36 + 2 * G * G) * U32 * np.abs(G) * p, "gelu")
     dx, _, _ = sp.sp_ffn_bwd(x, w_in, w_out, kept, torch.ones_like(x), "gelu")
     within(dx[:, 0], p + G * f, U32 * ((36 + 2 * G * G) * p + (12 + 2 * G * G) * np.abs(G) * f), "slope")
+
+
+@pytest.mark.parametrize("out", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("n,c,m", [(9, 100, 20), (9, 1300, 40), (70, 640, 150), (300, 200, 90)])
+def test_q8_linear_of_scales_over_their_range(sp, n, c, m, out):
+    """Rows from subnormal to the largest values, codes of every scale that there is.  Compared where the products' sizes sum to less than 2^127 and, of the scaled
+    instruction (bf16), to more than 2^-100; elsewhere a result may be infinite, or below what fp32 holds.  Each step's sum may be subnormal: half of 2^-149."""
+    rng = np.random.default_rng(n + c)
+    x, w = rows(rng, F32, n, c), rows(rng, F32, m, c)
+    for t, sizes in ((x, (-145, -133, -126, -118, -100, 0, 60, 120)), (w, (-140, -127, -120, -60, -35, -10, 0, 10, 100, 120))):
+        for r in range(t.shape[0]):
+            t[r] = torch.ldexp(t[r], torch.tensor(sizes[r % len(sizes)], device="cuda"))
+    x[4] = torch.where(x[4] > 0, 3.39e38, -3.39e38)          # 256 times 2^120: beyond bf16
+    w[5, :50] = 0
+    w[6] = 0
+    qx, qw = sp.sp_q8_rows(x), sp.sp_q8_rows(w)
+    s = qx[1].view(torch.uint8)
+    s[n - 1, 0], s[n - 2, 0] = 254, 1                        # larger ones than any row's own
+    X, W = (block.q8_values(q.view(torch.uint8).cpu().numpy(), e.view(torch.uint8).cpu().numpy()) for q, e in (qx, qw))
+    size = np.abs(X) @ np.abs(W).T
+    Y = X @ W.T
+    y = sp.sp_q8_linear(qx, qw, out)
+    seen = (size < 2.0 ** 127) & ((size > 2.0 ** -100) | (size == 0) if out == BF16 else True)
+    assert seen.mean() > 0.3 and not y[:, 6].any()
+    got = host(y)
+    bound = q8_bound(X, W, Y, out) + -(-c // 128) * 2.0 ** -149
+    within_values(np.where(seen, got, 0), np.where(seen, Y, 0), bound, "y")
