@@ -741,19 +741,21 @@ _idle = {}
 _Parts = C.c_int32 * 4
 
 
+_index = operator.index
+
+
 @functools.lru_cache(maxsize=64)
 def _rope_parts(parts: tuple, dim: int):
-    """Their number, and the library's array of them."""
-    parts = [operator.index(p) for p in parts]
+    """Their number, and the library's array of them.  Of ints: the cache would take 12.0 for 12."""
     if not 1 <= len(parts) <= 4 or any(not 0 <= p <= dim for p in parts):
         raise ValueError("1 to 4 axes, each turning at most a head's elements")
     return len(parts), _Parts(*parts)
 
 
 def _rope(name, x, pos, parts, base, split, scale, out):
-    ptr, ld = _head_rows(x, x.dtype, "x")
     n, heads, dim = x.shape
-    axes, parts = _rope_parts(tuple(parts), dim)
+    axes, parts = _rope_parts(tuple(map(_index, parts)), dim)
+    ptr, ld = _head_rows(x, x.dtype, "x")
     if not pos.is_cuda or pos.dtype != torch.int32 or pos.shape != (n, axes):
         raise ValueError(f"pos must be a CUDA int32 tensor {(n, axes)}")
     step, apart = pos.stride()

@@ -204,3 +204,17 @@ def test_ffn_refusals(lib):
         assert bwd(**bad) == INVALID, bad
     assert fwd(c=2 ** 18 + 1) == UNSUPPORTED and fwd(m=2 ** 18 + 1) == UNSUPPORTED and fwd(n=2 ** 30 + 1) == UNSUPPORTED
     assert lib.sp_ffn_work_bytes(C.byref(Ffn(3, 8, 16, 0, 1)), 0) >= 3 * 16 * 2 and lib.sp_ffn_work_bytes(C.byref(Ffn(3, 8, 0, 0, 1)), 1) == -1
+
+
+def test_parts_of_a_head_are_whole_numbers_whatever_was_asked_before():
+    from paper_2012_13846_amd import binding
+    x, pos = torch.zeros((2, 1, 32)), torch.zeros((2, 3), dtype=torch.int32)
+    for call in (binding.sp_rope_fwd, binding.sp_rope_bwd):
+        with pytest.raises(ValueError, match="CUDA"):                     # these parts would do
+            call(x, pos, (12, 10, 10))
+        for bad in ((12.0, 10.0, 10.0), (12, 10, 10.0), ("12",)):
+            with pytest.raises(TypeError):
+                call(x, pos, bad)
+        for bad in ((), (2, 2, 2, 2, 2), (34,), (-2,)):
+            with pytest.raises(ValueError, match="axes"):
+                call(x, pos, bad)
