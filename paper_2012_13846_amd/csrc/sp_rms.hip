@@ -594,12 +594,12 @@ __global__ __launch_bounds__(256) void q8_rows_kernel(const T* __restrict__ x, i
 // four of them, with 32 bits an element: 14.5).
 constexpr int kTurnCols = 64;
 template <typename T, bool ALIGNED>
-__global__ __launch_bounds__(256) void q8_turned_kernel(const T* __restrict__ x, int64_t ldx, int64_t n, int c, uint8_t* q, uint8_t* qs) {
+__global__ __launch_bounds__(256) void q8_turned_kernel(const T* __restrict__ x, int64_t ldx, int64_t n, int c, int64_t first, uint8_t* q, uint8_t* qs) {
     constexpr int V = 16 / (int)sizeof(T), kPieces = kTurnCols / V, kEach = kQ8Block * kPieces / 256;
     constexpr int kPad = 4 / (int)sizeof(T);  // a column is an odd number of banks behind the last
     __shared__ __attribute__((aligned(4))) T tile[kTurnCols][kQ8Block + kPad];
     const int64_t blocks = (n + kQ8Block - 1) / kQ8Block, wide = blocks * kQ8Block, scales = (blocks + 3) / 4 * 4;
-    const int64_t block = blockIdx.x, row0 = block * kQ8Block;
+    const int64_t block = first + blockIdx.x, row0 = block * kQ8Block;
     const int col0 = blockIdx.y * kTurnCols;
     Piece<T, V> in[kEach];
 #pragma unroll
@@ -644,11 +644,13 @@ int q8_rows(const T* x, int64_t ldx, int64_t n, int c, bool transposed, uint8_t*
     constexpr int V = 16 / (int)sizeof(T);
     const bool aligned = aligned16(x) && c % V == 0 && (ldx % V == 0 || n == 1);
     if (transposed) {
-        const int64_t blocks = q8_blocks(n);
-        if (blocks > 0x7fffffff) return fail(SP_ERR_UNSUPPORTED, "too many rows");
-        const dim3 grid((unsigned)blocks, (unsigned)((c + kTurnCols - 1) / kTurnCols));
-        if (aligned) hipLaunchKernelGGL((q8_turned_kernel<T, true>), grid, dim3(256), 0, s, x, ldx, n, c, q, qs);
-        else hipLaunchKernelGGL((q8_turned_kernel<T, false>), grid, dim3(256), 0, s, x, ldx, n, c, q, qs);
+        // A launch of 2^32 threads or more is cut short without an error.
+        constexpr int64_t kMost = 1 << 22;
+        for (int64_t first = 0, blocks = q8_blocks(n); first < blocks; first += kMost) {
+            const dim3 grid((unsigned)std::min(kMost, blocks - first), (unsigned)((c + kTurnCols - 1) / kTurnCols));
+            if (aligned) hipLaunchKernelGGL((q8_turned_kernel<T, true>), grid, dim3(256), 0, s, x, ldx, n, c, first, q, qs);
+            else hipLaunchKernelGGL((q8_turned_kernel<T, false>), grid, dim3(256), 0, s, x, ldx, n, c, first, q, qs);
+        }
     } else {
         const int64_t each = 256 / (kQ8Block / V), want = (n * q8_blocks(c) + each - 1) / each;
         const dim3 grid((unsigned)std::min<int64_t>(want, 8192));

@@ -736,3 +736,30 @@ def test_q8_linear_of_scales_over_their_range(sp, n, c, m, out):
     got = host(y)
     bound = q8_bound(X, W, Y, out) + -(-c // 128) * 2.0 ** -149
     within_values(np.where(seen, got, 0), np.where(seen, Y, 0), bound, "y")
+
+
+# ---- more rows than one launch takes ---------------------------------------------------------------------------
+def test_q8_rows_transposed_of_more_rows_than_a_launch_takes(sp):
+    """2^31 + 77 rows of one element: every 2^29 of them by themselves have the same codes."""
+    n, most = (1 << 31) + 77, 1 << 29
+    x = torch.randn((most + 3, 1), device="cuda").bfloat16().repeat(5, 1)[:n]
+    codes, scales = (t.view(torch.uint8) for t in sp.sp_q8_rows(x, transposed=True))
+    for at in range(0, n, most):
+        some = x[at:at + most]
+        q, s = (t.view(torch.uint8) for t in sp.sp_q8_rows(some, transposed=True))
+        blocks = -(-some.shape[0] // 128)
+        assert torch.equal(codes[:, at:at + blocks * 128], q) and torch.equal(scales[:, at // 128:at // 128 + blocks], s[:, :blocks]), at
+    assert (scales[:, -(-n // 128):] == 127).all()
+    del x, codes, scales, some, q, s
+    torch.cuda.empty_cache()
+
+
+def test_q8_rows_transposed_of_the_widest(sp):
+    """2^22 columns: the largest grid across."""
+    x = torch.randn((3, 1 << 22), device="cuda").bfloat16()
+    codes, scales = (t.view(torch.uint8) for t in sp.sp_q8_rows(x, transposed=True))
+    for at in (0, (1 << 21) - 64, (1 << 22) - 200):
+        q, s = (t.view(torch.uint8) for t in sp.sp_q8_rows(x[:, at:at + 200].contiguous(), transposed=True))
+        assert torch.equal(codes[at:at + 200], q) and torch.equal(scales[at:at + 200], s)
+    del x, codes, scales
+    torch.cuda.empty_cache()
