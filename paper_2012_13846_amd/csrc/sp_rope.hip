@@ -119,16 +119,20 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(Rope a, const T* x, T* y
 }
 
 template <typename T, int V, bool SPLIT>
-int rope_launch(const Rope& a, const void* x, void* y, hipStream_t s) {
-    const int64_t blocks = (a.n + a.rows - 1) / a.rows;
-    if (blocks > 0x7fffffff) return fail(SP_ERR_UNSUPPORTED, "too many rows");
-    hipLaunchKernelGGL((rope_kernel<T, V, SPLIT>), dim3((unsigned)blocks), dim3(kThreads), 0, s, a, static_cast<const T*>(x), static_cast<T*>(y));
-    SP_HIP(hipGetLastError());
+int rope_launch(Rope& a, const void* x, void* y, hipStream_t s) {
+    // A launch of 2^32 threads or more is cut short without an error.
+    const int64_t n = a.n, most = (int64_t)a.rows << 22;
+    for (int64_t row = 0; row < n; row += most, a.pos += most * a.ld_pos) {
+        a.n = std::min(most, n - row);
+        hipLaunchKernelGGL((rope_kernel<T, V, SPLIT>), dim3((unsigned)((a.n + a.rows - 1) / a.rows)), dim3(kThreads), 0, s, a,
+                           static_cast<const T*>(x) + row * a.ldx, static_cast<T*>(y) + row * a.ldy);
+        SP_HIP(hipGetLastError());
+    }
     return SP_OK;
 }
 
 template <typename T>
-int rope_typed(const Rope& a, bool split, const void* x, void* y, hipStream_t s) {
+int rope_typed(Rope& a, bool split, const void* x, void* y, hipStream_t s) {
     constexpr int kN = 16 / (int)sizeof(T);
     bool pieces = aligned16(x) && aligned16(y) && a.dim % kN == 0 && (a.n == 1 || (a.ldx % kN == 0 && a.ldy % kN == 0));
     if (split)

@@ -763,3 +763,17 @@ def test_q8_rows_transposed_of_the_widest(sp):
         assert torch.equal(codes[at:at + 200], q) and torch.equal(scales[at:at + 200], s)
     del x, codes, scales
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("split", [False, True], ids=["neighbours", "halves"])
+def test_rope_of_more_rows_than_a_launch_takes(sp, split):
+    """2^27 + 1000 rows of 256, eight rows a workgroup of 256 threads, in place: rows here and there by themselves turn to the same bits."""
+    n = (1 << 27) + 1000
+    x = torch.ones((n, 1, 256), dtype=torch.bfloat16, device="cuda")
+    pos = torch.arange(n, dtype=torch.int32, device="cuda")[:, None]
+    sp.sp_rope_fwd(x, pos, (256,), split=split, out=x)
+    for at in (0, (1 << 25) - 500, (1 << 26) - 500, (1 << 27) - 500, n - 1000):
+        want = sp.sp_rope_fwd(torch.ones((1000, 1, 256), dtype=torch.bfloat16, device="cuda"), pos[at:at + 1000], (256,), split=split)
+        assert torch.equal(x[at:at + 1000], want), at
+    del x, pos
+    torch.cuda.empty_cache()
