@@ -365,7 +365,8 @@ int sp_rms_norm_bwd(const void* d_h, const void* d_dy, const void* d_dh, int64_t
  * sp_q8_rows: of x (rows ldx elements apart), to nearest even; transposed != 0: of the c rows of the transposed matrix, n elements each.
  * sp_q8_linear: y [n][m] of type dt = x w^T for x [n][c] and w [m][c] in 8 bits, sums fp32.  bf16 results come from the scaled 8-bit matrix
  * instruction, which cuts products off at 2^-13 of the largest of eight neighbouring elements (1.5e-5 of the result of random rows); for fp32 results
- * codes are multiplied as bf16, which is exact.  For gradients (dx = dy w, dw = dy^T x) it is given operands in 8 bits along the other axis.  c <= 2^22. */
+ * codes are multiplied as bf16, which is exact.  For gradients (dx = dy w, dw = dy^T x) it is given operands in 8 bits along the other axis.
+ * c <= 2^22, n, m <= 2^30; a product of 2^38 results or more may have more tiles than a launch takes (SP_ERR_UNSUPPORTED, work size -1). */
 int64_t sp_q8_codes_bytes(int64_t n, int64_t c);
 int64_t sp_q8_scales_bytes(int64_t n, int64_t c);
 int sp_q8_rows(const void* d_x, int64_t ldx, int64_t n, int32_t c, int32_t transposed, uint8_t* d_q, uint8_t* d_scales, sp_dtype dt, void* stream);
@@ -378,7 +379,7 @@ int sp_q8_linear(const uint8_t* d_q, const uint8_t* d_scales, int64_t n, int64_t
  * sp_ffn_fwd writes y [n][c] and, unless d_kept is NULL, what the backward pass reads (g, u and act(g) * u in a layout of the library's own):
  * [n][3 m] of fp32, or [n][4 m] of bf16.  sp_ffn_bwd: gradients of sum(y * dy): dx like x, dw_in and dw_out like the weights, of type dt.  Sums fp32;
  * in bf16 act(g) * u and the gradients of g and u are rounded before they are multiplied again, g and u are kept in 24 bits.  All arrays dense;
- * outputs overlap nothing.  n <= 2^30, c, m <= 2^18 (SP_ERR_UNSUPPORTED beyond). */
+ * outputs overlap nothing.  n <= 2^30, c, m <= 2^18; a product of 2^38 results or more may have more tiles than a launch takes (SP_ERR_UNSUPPORTED, work size -1). */
 typedef enum { SP_GATE_SILU = 0, SP_GATE_GELU = 1 } sp_gate;
 typedef struct {
     int64_t n;

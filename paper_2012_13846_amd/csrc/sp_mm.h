@@ -989,14 +989,22 @@ inline int thin_waves(int64_t groups, int64_t fragments) {
     return waves;
 }
 template <typename T, bool GATE, bool VEC, bool EXACT>
-int mm_thin(const Mm& a, hipStream_t s) {
-    const int64_t groups = (a.m + 15) / 16, bytes = sizeof(T) == 1 ? 128 : 64;
-    if (groups > 0x7fffffff) return fail(SP_ERR_UNSUPPORTED, "too many columns");
+int mm_thin(Mm a, hipStream_t s) {
+    const int64_t groups = ((int64_t)a.m + 15) / 16, bytes = sizeof(T) == 1 ? 128 : 64;
     const int waves = thin_waves(groups, ((int64_t)a.k * (int)sizeof(T) + bytes - 1) / bytes);
     const size_t room = (size_t)waves * (GATE ? 2 : 1) * (a.n > 16 ? 2 : 1) * 1024;
-    if (a.n <= 16) hipLaunchKernelGGL((mm_thin_kernel<T, 1, GATE, VEC, EXACT>), dim3((unsigned)groups), dim3(waves * 64), room, s, a);
-    else hipLaunchKernelGGL((mm_thin_kernel<T, 2, GATE, VEC, EXACT>), dim3((unsigned)groups), dim3(waves * 64), room, s, a);
-    SP_HIP(hipGetLastError());
+    // (of gates there are at most 2^14 groups, one launch)
+    const int64_t most = ((int64_t)1 << 26) / (waves * 64);
+    for (int64_t group = 0; group < groups; group += most) {
+        const dim3 grid((unsigned)(groups - group < most ? groups - group : most));
+        if (a.n <= 16) hipLaunchKernelGGL((mm_thin_kernel<T, 1, GATE, VEC, EXACT>), grid, dim3(waves * 64), room, s, a);
+        else hipLaunchKernelGGL((mm_thin_kernel<T, 2, GATE, VEC, EXACT>), grid, dim3(waves * 64), room, s, a);
+        SP_HIP(hipGetLastError());
+        a.m -= (int)(most * 16);
+        a.first = static_cast<const char*>(a.first) + most * 16 * a.ld_first;
+        a.first_scales += most * 16 * a.scales;
+        a.out = static_cast<char*>(a.out) + most * 16 * (sizeof(T) > 1 ? (int)sizeof(T) : a.out_f32 ? 4 : 2);
+    }
     return SP_OK;
 }
 
@@ -1007,6 +1015,9 @@ struct Plan {
     int splits, per_split, tiles_m, tiles_n;
     double time;  // us, about
 };
+constexpr double kNoPlan = 1e300;                           // (time) more tiles than a launch has threads for
+constexpr int64_t kNoWork = (int64_t)1 << 62;
+constexpr int64_t kMostThreads = ((int64_t)1 << 32) - 1;  // a launch of more is cut short without an error
 // rows: of the first operand (a gate: 2 m); k_bytes: of a row of the contraction
 enum MmType { kF32, kBf16, kQ8, kQ8Exact };
 Plan mm_plan(int64_t rows, int64_t n, int64_t k_bytes, MmType type, bool pieces);
@@ -1014,13 +1025,13 @@ Plan mm_plan(int64_t rows, int64_t n, int64_t k_bytes, MmType type, bool pieces)
 inline int64_t mm_work(int64_t rows, int64_t n, int64_t k_bytes, MmType type, bool direct, bool pieces) {
     if (direct && n <= kThinRows) return 0;
     const Plan p = mm_plan(rows, n, k_bytes, type, pieces);
+    if (p.time == kNoPlan) return kNoWork;
     return p.splits > 1 ? (int64_t)p.splits * rows * n * 4 : 0;
 }
 
 template <typename T, typename Sh, bool TA, bool TB, bool VEC, bool EXACT, Last LAST>
 int mm_launch(const Mm& a, hipStream_t s) {
     const int64_t blocks = (int64_t)a.tiles_m * a.tiles_n * a.splits;
-    if (blocks > 0x7fffffff) return fail(SP_ERR_UNSUPPORTED, "too many tiles");
     hipLaunchKernelGGL((mm_kernel<T, Sh, TA, TB, VEC, EXACT, LAST>), dim3((unsigned)blocks), dim3(Sh::kThreads), 0, s, a);
     SP_HIP(hipGetLastError());
     return SP_OK;
@@ -1050,6 +1061,7 @@ int mm(Mm a, float* part, hipStream_t s) {
         }
     const MmType type = sizeof(T) == 4 ? kF32 : sizeof(T) == 2 ? kBf16 : a.out_f32 ? kQ8Exact : kQ8;
     const Plan p = mm_plan(gate ? (int64_t)2 * a.m : a.m, a.n, k_bytes, type, pieces);
+    if (p.time == kNoPlan) return fail(SP_ERR_UNSUPPORTED, "more results than a launch has threads for");
     a.steps = (int)((k_bytes + kStepBytes - 1) / kStepBytes);
     a.per_split = p.per_split, a.splits = p.splits, a.tiles_m = p.tiles_m, a.tiles_n = p.tiles_n;
     Mm last = a;
@@ -1093,7 +1105,7 @@ int mm(Mm a, float* part, hipStream_t s) {
         auto add = [&](auto groups) -> int {
             constexpr int G = decltype(groups)::value;
             const int64_t blocks = ((int64_t)((last.m + 7) / 8) * last.n + 256 / G - 1) / (256 / G);
-            if (blocks > 0x7fffffff) return fail(SP_ERR_UNSUPPORTED, "too many results");
+            if (blocks > kMostThreads / 256) return fail(SP_ERR_UNSUPPORTED, "more results than a launch has threads for");
             hipLaunchKernelGGL((mm_join_kernel<T, G>), dim3((unsigned)blocks), dim3(256), 0, s, last);
             SP_HIP(hipGetLastError());
             return SP_OK;

@@ -12,33 +12,33 @@ namespace sp {
 namespace {
 struct Cost {
     ShapeName name;
-    int bm, bn;
+    int bm, bn, threads;
     double alone[4], shared[4];  // by type; shared 0: a CU holds one
 };
 //                                f32   bf16  8 bits, and exactly
-constexpr Cost kCosts[] = {{kLarge, 256, 256, {7.9, 1.35, 1.7, 0}, {0, 0, 0, 0}},
-                           {kMiddle, 128, 128, {2.0, 0.55, 0.68, 1.15}, {4.06, 1.0, 1.13, 1.96}},
-                           {kNarrow, 64, 128, {1.15, 0.37, 0.55, 0.85}, {2.1, 0.65, 0.81, 1.26}},
-                           {kFew, 128, 32, {0.7, 0.35, 0, 0}, {1.1, 0.55, 0, 0}}};
+constexpr Cost kCosts[] = {{kLarge, 256, 256, 512, {7.9, 1.35, 1.7, 0}, {0, 0, 0, 0}},
+                           {kMiddle, 128, 128, 256, {2.0, 0.55, 0.68, 1.15}, {4.06, 1.0, 1.13, 1.96}},
+                           {kNarrow, 64, 128, 256, {1.15, 0.37, 0.55, 0.85}, {2.1, 0.65, 0.81, 1.26}},
+                           {kFew, 128, 32, 256, {0.7, 0.35, 0, 0}, {1.1, 0.55, 0, 0}}};
 constexpr double kLaunch = 3.5, kRound = 2, kRoundAlone = 8;
 double join_time(int64_t splits, int64_t rows, int64_t n) { return 8.0 * (double)splits * (double)rows * (double)n / 4e6; }
 }  // namespace
 
 Plan mm_plan(int64_t rows, int64_t n, int64_t k_bytes, MmType type, bool pieces) {
     const int64_t steps = (k_bytes + kStepBytes - 1) / kStepBytes;
-    Plan best{kMiddle, 1, (int)steps, 1, 1, 1e300};
+    Plan best{kMiddle, 0, (int)steps, 0, 0, kNoPlan};
     for (const Cost& kind : kCosts) {
         if (kind.name == kLarge && (!pieces || type == kQ8Exact)) continue;
         if ((kind.name == kFew) != (n <= kThinRows && type < kQ8)) continue;
         const int64_t tiles_m = (rows + kind.bm - 1) / kind.bm, tiles_n = (n + kind.bn - 1) / kind.bn, tiles = tiles_m * tiles_n;
-        if (tiles > 0x7fffffff) continue;
+        const int64_t most = kMostThreads / kind.threads;
         const double alone = kind.alone[type], shared = kind.shared[type];
         int64_t last = 0;
         for (int64_t want = 1; want <= 128 && want <= std::max<int64_t>(1, steps / 2); want = want < 4 ? want + 1 : want + want / 2) {
             int64_t each = std::max<int64_t>(1, (steps + want - 1) / want);
             if (type >= kQ8 && want > 1) each = (each + 3) / 4 * 4;  // a word of scales is four steps'
             const int64_t splits = std::max<int64_t>(1, (steps + each - 1) / each);
-            if (splits == last || tiles * splits > 0x7fffffff) continue;
+            if (splits == last || tiles * splits > most) continue;
             last = splits;
             const int64_t groups = tiles * splits, slots = shared > 0 ? 512 : 256, rest = groups % slots;
             const double round = shared > 0 ? kRound : kRoundAlone;
@@ -100,7 +100,7 @@ static int64_t ffn_work(int64_t n, int c, int m, int size, bool backward) {
             if (n > 0) part = std::max(part, mm_work_three(of, type, pieces));
         }
     }
-    return up256((backward ? 2 : 1) * n * m * size) + up256(part) + 256;
+    return part == kNoWork ? -1 : up256((backward ? 2 : 1) * n * m * size) + up256(part) + 256;
 }
 
 namespace {
@@ -152,7 +152,8 @@ int sp_ffn_bwd(const sp_ffn* f, const void* d_x, const void* d_w_in, const void*
 int64_t sp_q8_linear_work(int64_t n, int64_t c, int64_t m) {
     if (n < 0 || n > kMostRows || c < 1 || c > kMostRow || m < 1 || m > kMostRows) return -1;
     const int64_t wide = q8_blocks(c) * kQ8Block;  // the results' type is not known yet
-    return up256(std::max(mm_work(m, n, wide, kQ8, true, true), mm_work(m, n, wide, kQ8Exact, true, true))) + 256;
+    const int64_t part = std::max(mm_work(m, n, wide, kQ8, true, true), mm_work(m, n, wide, kQ8Exact, true, true));
+    return part == kNoWork ? -1 : up256(part) + 256;
 }
 
 int sp_q8_linear(const uint8_t* d_q, const uint8_t* d_scales, int64_t n, int64_t c, const uint8_t* d_wq, const uint8_t* d_wscales, int64_t m,

@@ -218,3 +218,17 @@ def test_parts_of_a_head_are_whole_numbers_whatever_was_asked_before():
         for bad in ((), (2, 2, 2, 2, 2), (34,), (-2,)):
             with pytest.raises(ValueError, match="axes"):
                 call(x, pos, bad)
+
+
+def test_products_of_more_results_than_a_launch_has_threads_for_are_refused(lib):
+    linear = lambda n, m, dt: lib.sp_q8_linear(P, P, i8(n), i8(128), P, P, i8(m), P, dt, P, None)  # noqa: E731
+    for n, m in ((2 ** 30, 2 ** 30), (2 ** 30, 2 ** 12), (2 ** 12, 2 ** 30)):
+        assert lib.sp_q8_linear_work(i8(n), i8(128), i8(m)) == -1 and linear(n, m, 0) == UNSUPPORTED and linear(n, m, 1) == UNSUPPORTED
+    for dt in (0, 1):
+        f = C.byref(Ffn(2 ** 30, 64, 2 ** 18, 0, dt))
+        assert lib.sp_ffn_work_bytes(f, 0) == -1 and lib.sp_ffn_work_bytes(f, 1) == -1
+        assert lib.sp_ffn_fwd(f, P, P, P, None, P, P, None) == UNSUPPORTED
+        assert lib.sp_ffn_bwd(f, P, P, P, P, P, P, P, P, P, None) == UNSUPPORTED
+        f = C.byref(Ffn(2 ** 18, 2 ** 13, 2 ** 15, 0, dt))                # large, and taken
+        assert lib.sp_ffn_work_bytes(f, 0) > 2 ** 34 and lib.sp_ffn_work_bytes(f, 1) > 2 ** 34
+    assert lib.sp_q8_linear_work(i8(2 ** 18), i8(2 ** 15), i8(2 ** 18)) >= 256 and lib.sp_q8_linear_work(i8(2 ** 30), i8(128), i8(64)) >= 256

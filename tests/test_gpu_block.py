@@ -777,3 +777,17 @@ def test_rope_of_more_rows_than_a_launch_takes(sp, split):
         assert torch.equal(x[at:at + 1000], want), at
     del x, pos
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("out", [F32, BF16], ids=["f32", "bf16"])
+def test_q8_linear_of_more_weights_than_a_launch_of_few_rows_takes(sp, out):
+    """Few rows by 2^24 + 2^20 + 40 weights, 2^24 of them a launch: weights here and there by themselves give the same bits."""
+    m = (1 << 24) + (1 << 20) + 40
+    g = torch.Generator(device="cuda").manual_seed(5)
+    qx = sp.sp_q8_rows(torch.randn((3, 100), device="cuda", generator=g))
+    q, s = sp.sp_q8_rows(torch.randn((m, 100), device="cuda", generator=g))
+    y = sp.sp_q8_linear(qx, (q, s), out)
+    for at in (0, (1 << 23) - 100, (1 << 24) - 1000, m - 2000):
+        assert torch.equal(y[:, at:at + 2000], sp.sp_q8_linear(qx, (q[at:at + 2000], s[at:at + 2000]), out)), at
+    del q, s, y
+    torch.cuda.empty_cache()
