@@ -705,12 +705,14 @@ int sp_rms_norm_bwd(const void* d_h, const void* d_dy, const void* d_dh, int64_t
 }
 
 int64_t sp_q8_codes_bytes(int64_t n, int64_t c) {
-    if (n < 0 || c < 1 || n > (int64_t)1 << 40 || c > (int64_t)1 << 40) return -1;
-    return n * q8_blocks(c) * kQ8Block;
+    int64_t bytes;
+    if (n < 0 || c < 1 || n > (int64_t)1 << 40 || c > (int64_t)1 << 40 || __builtin_mul_overflow(n, q8_blocks(c) * kQ8Block, &bytes)) return -1;
+    return bytes;
 }
 int64_t sp_q8_scales_bytes(int64_t n, int64_t c) {
-    if (n < 0 || c < 1 || n > (int64_t)1 << 40 || c > (int64_t)1 << 40) return -1;
-    return n * q8_scales(c);
+    int64_t bytes;
+    if (n < 0 || c < 1 || n > (int64_t)1 << 40 || c > (int64_t)1 << 40 || __builtin_mul_overflow(n, q8_scales(c), &bytes)) return -1;
+    return bytes;
 }
 
 int sp_q8_rows(const void* d_x, int64_t ldx, int64_t n, int32_t c, int32_t transposed, uint8_t* d_q, uint8_t* d_scales, sp_dtype dt, void* stream) {

@@ -232,3 +232,11 @@ def test_products_of_more_results_than_a_launch_has_threads_for_are_refused(lib)
         f = C.byref(Ffn(2 ** 18, 2 ** 13, 2 ** 15, 0, dt))                # large, and taken
         assert lib.sp_ffn_work_bytes(f, 0) > 2 ** 34 and lib.sp_ffn_work_bytes(f, 1) > 2 ** 34
     assert lib.sp_q8_linear_work(i8(2 ** 18), i8(2 ** 15), i8(2 ** 18)) >= 256 and lib.sp_q8_linear_work(i8(2 ** 30), i8(128), i8(64)) >= 256
+
+
+def test_sizes_in_8_bits_beyond_64_bits_are_refused(lib):
+    far = 2 ** 40
+    assert lib.sp_q8_codes_bytes(i8(far), i8(far)) == -1 and lib.sp_q8_codes_bytes(i8(2 ** 24), i8(far)) == -1
+    assert lib.sp_q8_scales_bytes(i8(far), i8(far)) == -1
+    assert lib.sp_q8_codes_bytes(i8(2 ** 22), i8(far)) == 2 ** 62 and lib.sp_q8_scales_bytes(i8(2 ** 22), i8(far)) == 2 ** 55
+    assert lib.sp_q8_codes_bytes(i8(0), i8(far)) == 0
