@@ -791,3 +791,30 @@ def test_q8_linear_of_more_weights_than_a_launch_of_few_rows_takes(sp, out):
         assert torch.equal(y[:, at:at + 2000], sp.sp_q8_linear(qx, (q[at:at + 2000], s[at:at + 2000]), out)), at
     del q, s, y
     torch.cuda.empty_cache()
+
+
+@TYPES
+@pytest.mark.parametrize("n,c", [(1428, 128), (60, 77), (5000, 64), (9, 4096), (5, 8191), (3, 16392), (4, 40001)])
+def test_rms_norm_forward_in_place(sp, n, c, dt):
+    """The sum in x's or the residual's memory, y in either that the sum is not in (or in x, without a residual): the same bits."""
+    rng = np.random.default_rng(n + c)
+    x, res = rows(rng, dt, n, c), rows(rng, dt, n, c)
+    gamma = 1 + rows(rng, F32, c, scale=0.2)
+    l, t, stream = sp._block_argtypes(), sp._dt(x), sp._stream()
+    h, y, rstd = sp.sp_rms_norm_fwd(x, gamma, res)
+    _, (q, s) = sp.sp_rms_norm_q8(x, gamma, res)
+    for sum_in, out_in in ((0, None), (1, None), (0, 1), (1, 0), (None, 0), (None, 1)):
+        own = [x.clone(), res.clone()]
+        to_h, to_y = own[sum_in] if sum_in is not None else torch.empty_like(x), own[out_in] if out_in is not None else torch.empty_like(x)
+        r = torch.empty_like(rstd)
+        assert l.sp_rms_norm_fwd(own[0].data_ptr(), own[1].data_ptr(), n, c, gamma.data_ptr(), 1e-5, to_h.data_ptr(), to_y.data_ptr(), r.data_ptr(), t, stream) == 0
+        assert torch.equal(to_h, h) and torch.equal(to_y, y) and torch.equal(r, rstd), (sum_in, out_in)
+        if out_in is None:
+            own = [x.clone(), res.clone()]
+            q2, s2 = sp._q8_new(n, c, x.device)
+            assert l.sp_rms_norm_q8(own[0].data_ptr(), own[1].data_ptr(), n, c, gamma.data_ptr(), 1e-5, own[sum_in].data_ptr(), q2.data_ptr(), s2.data_ptr(), t, stream) == 0
+            assert torch.equal(own[sum_in], h) and torch.equal(q2.view(torch.uint8), q.view(torch.uint8)) and torch.equal(s2.view(torch.uint8), s.view(torch.uint8))
+    _, y, rstd = sp.sp_rms_norm_fwd(x, gamma)
+    own, r = x.clone(), torch.empty_like(rstd)
+    assert l.sp_rms_norm_fwd(own.data_ptr(), None, n, c, gamma.data_ptr(), 1e-5, None, own.data_ptr(), r.data_ptr(), t, stream) == 0
+    assert torch.equal(own, y) and torch.equal(r, rstd)
