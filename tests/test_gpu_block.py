@@ -818,3 +818,85 @@ def test_rms_norm_forward_in_place(sp, n, c, dt):
     own, r = x.clone(), torch.empty_like(rstd)
     assert l.sp_rms_norm_fwd(own.data_ptr(), None, n, c, gamma.data_ptr(), 1e-5, None, own.data_ptr(), r.data_ptr(), t, stream) == 0
     assert torch.equal(own, y) and torch.equal(r, rstd)
+
+
+# ---- memory beyond 32 bits of bytes, and off 16-byte borders -----------------------------------------------------
+def off_border(t):
+    """The same values one element behind a 16-byte border."""
+    flat = torch.empty(t.numel() + 1, dtype=t.dtype, device="cuda")
+    flat[1:] = t.reshape(-1)
+    return flat[1:].view(t.shape)
+
+
+@TYPES
+@pytest.mark.parametrize("which", ["x", "w_in", "w_out", "dy", "kept", "all"])
+@pytest.mark.parametrize("n,c,m", [(20, 64, 128), (500, 72, 136), (2000, 256, 512)])
+def test_ffn_of_unaligned_memory(sp, n, c, m, which, dt):
+    """Each array by itself off a border: its products alone go through registers."""
+    rng = np.random.default_rng(n)
+    t = {"x": rows(rng, dt, n, c), "dy": rows(rng, dt, n, c), "w_in": rows(rng, dt, 2 * m, c, scale=1.5 / math.sqrt(c)), "w_out": rows(rng, dt, c, m, scale=1 / math.sqrt(m))}
+    t = {k: off_border(v) if which in (k, "all") else v for k, v in t.items()}
+    u = half_step(dt) if dt == BF16 else U32
+    X, DY, WI, WO = (host(t[k]) for k in ("x", "dy", "w_in", "w_out"))
+    (Y, _, _, _), (_, _, e_y) = ffn_forward_bounds(X, WI, WO, "silu", u)
+    y, kept = sp.sp_ffn_fwd(t["x"], t["w_in"], t["w_out"])
+    within(y, Y, e_y, "y")
+    if which in ("kept", "all"):
+        kept = off_border(kept)
+    want, bounds = ffn_backward_bounds(X, WI, WO, kept_values(kept, m), DY, "silu", u)
+    for got, ref, bound, name in zip(sp.sp_ffn_bwd(t["x"], t["w_in"], t["w_out"], kept, t["dy"]), want, bounds, ("dx", "dw_in", "dw_out")):
+        within(got, ref, bound, name)
+
+
+def test_ffn_of_more_than_32_bits_of_bytes(sp):
+    """What is kept of 300007 rows of 2048 gates is 4.9 GB: rows at both ends, and the weights' gradients of a few hidden channels."""
+    n, c, m, u = 300007, 64, 2048, half_step(BF16)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    normal = lambda *s: torch.randn(s, device="cuda", generator=g)  # noqa: E731
+    x, dy = normal(n, c).bfloat16(), normal(n, c).bfloat16()
+    w_in, w_out = (normal(2 * m, c) / 8).bfloat16(), (normal(c, m) / math.sqrt(m)).bfloat16()
+    y, kept = sp.sp_ffn_fwd(x, w_in, w_out)
+    dx, dw_in, dw_out = sp.sp_ffn_bwd(x, w_in, w_out, kept, dy)
+    r = torch.tensor([0, 1, 131071, 262143, 262144, n - 130, n - 2, n - 1], device="cuda")
+    WI, WO = host(w_in), host(w_out)
+    (Y, _, _, _), (_, _, e_y) = ffn_forward_bounds(host(x[r]), WI, WO, "silu", u)
+    within(y[r], Y, e_y, "y")
+    (DX, _, _), (e_dx, _, _) = ffn_backward_bounds(host(x[r]), WI, WO, kept_values(kept[r], m), host(dy[r]), "silu", u)
+    within(dx[r], DX, e_dx, "dx")
+    j = torch.tensor([0, 777, m - 1], device="cuda")
+    k = kept_values(kept[:, torch.cat([j, m + j, 2 * m + j, 3 * m + j])], 3)
+    (_, DWI, DWO), (_, e_wi, e_wo) = ffn_backward_bounds(host(x), host(torch.cat([w_in[j], w_in[m + j]])), host(w_out[:, j]), k, host(dy), "silu", u)
+    within(torch.cat([dw_in[j], dw_in[m + j]]), DWI, e_wi, "dw_in")
+    within(dw_out[:, j], DWO, e_wo, "dw_out")
+    del x, y, dx, dy, kept
+    torch.cuda.empty_cache()
+
+
+def test_norm_and_rows_in_8_bits_of_more_than_32_bits_of_bytes(sp):
+    """4.9 GB of rows, 2.5 GB of codes: the last rows by themselves give the same bits, and the product of the codes is the definition's."""
+    n, c = 300007, 8192
+    gamma = 1 + 0.1 * torch.randn(c, device="cuda")
+    x = torch.empty((n, c), dtype=BF16, device="cuda").normal_()
+    dy = x.flip(0)
+    _, y, rstd = sp.sp_rms_norm_fwd(x, gamma)
+    dx, _ = sp.sp_rms_norm_bwd(x, dy, gamma, rstd)
+    _, (q, s) = sp.sp_rms_norm_q8(x, gamma)
+    for at in (0, 262140, n - 300):
+        some = x[at:at + 300].contiguous()
+        _, ys, rs = sp.sp_rms_norm_fwd(some, gamma)
+        assert torch.equal(ys, y[at:at + 300]) and torch.equal(rs, rstd[at:at + 300])
+        assert torch.equal(sp.sp_rms_norm_bwd(some, dy[at:at + 300].contiguous(), gamma, rs)[0], dx[at:at + 300])
+        qs, ss = sp.sp_rms_norm_q8(some, gamma)[1]
+        assert torch.equal(qs.view(torch.uint8), q[at:at + 300].view(torch.uint8)) and torch.equal(ss.view(torch.uint8), s[at:at + 300].view(torch.uint8))
+        assert all(torch.equal(a.view(torch.uint8), b[at:at + 300].view(torch.uint8)) for a, b in zip(sp.sp_q8_rows(ys), sp.sp_q8_rows(y)))
+    del x, y, dx, dy
+    torch.cuda.empty_cache()
+    wq = sp.sp_q8_rows(torch.randn((24, c), device="cuda"))
+    r = torch.tensor([0, 262143, 262144, n - 1], device="cuda")
+    X, W = (block.q8_values(a.view(torch.uint8).cpu().numpy(), b.view(torch.uint8).cpu().numpy())
+            for a, b in ((q.view(torch.uint8)[r], s.view(torch.uint8)[r]), wq))
+    for out in (F32, BF16):
+        Y = X @ W.T
+        within(sp.sp_q8_linear((q, s), wq, out)[r], Y, q8_bound(X, W, Y, out), "z")
+    del q, s
+    torch.cuda.empty_cache()
