@@ -985,7 +985,7 @@ constexpr int kThinRows = 32;
 // Wavefronts of a workgroup: 16 a CU, while each has two fragments to read; enough threads for the last step.
 inline int thin_waves(int64_t groups, int64_t fragments) {
     int waves = 16;
-    while (waves > 1 && (groups * waves > 4096 && waves > 4 || 2 * (waves - 1) >= fragments)) waves /= 2;
+    while (waves > 1 && ((groups * waves > 4096 && waves > 4) || 2 * (waves - 1) >= fragments)) waves /= 2;
     return waves;
 }
 template <typename T, bool GATE, bool VEC, bool EXACT>

@@ -6,7 +6,7 @@
 // the next row is asked for before this one is reduced.  Pieces that are not aligned (odd widths, views) are loaded and stored as wide by
 // unaligned instructions, but for the piece that holds a row's end.  What is normalised is the sum as it is stored, so that the backward
 // pass finds the same.  In 8 bits the 16 (fp32: 32) neighbouring lanes that hold 128 elements share their largest size.  The weight's gradient is
-// summed in the lanes that own the columns, then over a workgroup's row groups through LDS, and the workgroups' sums are added in fp64 in X16384 x 4096 in bf16: 93 us forward (5.7 TB/s), 115 + 5 back (4.7).  Rows to 8 bits: 8192 x 2048 10.5 us, transposed 14.
+// summed in the lanes that own the columns, then over a workgroup's row groups through LDS, and the workgroups' sums are added in fp64 in X16384 x 4096 in bf16: 93 us forward (5.7 TB/s), 115 + 5 back (4.7).  Rows to 8 bits: 8192 x 2048 10.5 us, transposed 11.5.
 #include <algorithm>
 #include <type_traits>
 
