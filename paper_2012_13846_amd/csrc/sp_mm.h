@@ -454,11 +454,13 @@ struct Room {  // LDS: [ST][tile of the first operand, of the second], [2][scale
 // multiplied, an LDS read for every two products; one barrier a step, between them, behind which this step's tiles are free and the next one's are
 // there.  Large has 8 wavefronts of 128 x 64 results: 2048 x 8192 of 8192 in bf16 takes 184 us alone (1500 TFLOP/s; 16 wavefronts of 64 x 64, which read
 // a third more from LDS and nothing ahead, 214), 212 in the block, where the memory still writes what was kept.  8 bits: fragments are twice as long and
-// only registers for one set are left; 16384 x 4096 x 6144 at 2500 TFLOP/s.  fp32: about 90 % of the fp32 matrix rate in 8192 x 1024 x 2048.
-// Last steps: 8 bytes a result of the gate and 10 of its gradient are memory's, 8192 x 2048 x 8192: 493 us for 370 of products, 341 for 190.
+// only registers for one set are left; 16384 x 4096 x 6144 at 2500 TFLOP/s.  fp32: 134 TFLOP/s in 8192 x 1024 x 2048, of 152.
+// Last steps: 8 bytes a result of the gate and 10 of its gradient are memory's, 8192 x 2048 x 8192: 493 us for 370 of products, 331 for 190
+// (what is kept and read ahead leaves its last step six registers short: 28 bytes of scratch a lane).
 // EXACT (8-bit operands): codes and their scales become bf16, exactly (q8_plain), for the bf16 products.  The 8-bit products themselves take
 // eight neighbouring elements at a time and cut their products off at 2^-13 of the largest's power of two (found by cancelling that one); of
 // random rows 1.5e-5 of the result, whatever their length, against 1e-8: far below a bf16 result's rounding (1.7e-3), but not an fp32 one's.
+// 16384 x 4096 x 6144: 706 us, 1170 TFLOP/s (686 without a way for scales that bf16 does not take).
 template <typename T, typename Sh, bool TA, bool TB, bool VEC, bool EXACT, Last LAST>
 __device__ __forceinline__ void mm_body(const Mm& a, uint32_t block, char* room) {
     using K = Kind<T>;
